@@ -9,7 +9,7 @@
 
 #include "../../include/sk.h"
 #include "../../include/sk_debug.h"
-#include "sk_launch.h"
+#include "sk_block_launch.h"
 
 // Scratch of sk_linear_bwd_weight_noalloc (SK_NOALLOC_SCRATCH_BYTES, include/sk.h): device
 // memory that belongs to the loaded code object (one copy per GPU, held until the process
@@ -112,6 +112,7 @@ sk_status check_shape(int64_t tokens, int64_t in, int64_t out, int32_t l, int32_
 
 namespace sk {
 LaunchHooks* launch_hooks() { return g_hooks; }
+void note_hip_error(hipError_t e, const char* what) { (void)hip_fail(e, what); }
 }  // namespace sk
 
 namespace {

@@ -1,0 +1,119 @@
+// What the attention kernels share: MFMA operands of either type, the rows and keys of a work-group, masks.
+//
+// Every product of these kernels has its C operand as [32 x 32] with the column in the lane (lane % 32) and rows
+// 8 (r / 4) + 4 (lane / 32) + r % 4 in register r.  The probabilities come out of one product with the reduced
+// dimension of the next along the registers, and a contraction may run in any order, so they go into the next one as
+// they lie, only rounded: register r is element r % 8 of k step r / 8, for which the other operand's rows are read in
+// the same order.  No probability passes through LDS or another lane.
+#pragma once
+#include "sk_bf16_tile.h"
+#include "sk_block_launch.h"
+
+namespace sk {
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
+
+template <typename T>
+struct Mma;
+
+template <>
+struct Mma<bf16> {
+  typedef bf16x8 Frag;                 // of a lane: 16 bytes
+  static constexpr int E = 8;          // values in them
+  static constexpr int STEP = 16;      // of the contraction, covered by a fragment
+  static __device__ __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  // Rows row0 .. + 31 of a row-major tile, contraction along its rows' elements
+  static __device__ __forceinline__ Frag along(const bf16* tile, int ld, int row0, int ks, int lane) {
+    return *reinterpret_cast<const Frag*>(tile + (row0 + (lane & 31)) * ld + ks * 16 + (lane >> 5) * 8);
+  }
+  // Columns col0 .. + 31 of it, contraction along rows row0 .. + 31 in the order of of_acc
+  static __device__ __forceinline__ Frag across(const bf16* tile, int ld, int row0, int s, int col0, int lane) {
+    const bf16* p = tile + (row0 + s * 16 + (lane >> 5) * 4 + ((lane & 15) >> 2)) * ld + col0 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * ld));
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_bit_cast(Frag, both);
+  }
+  static __device__ __forceinline__ Frag of_acc(const f32x16& p, int s) {
+    uint4 u;
+    u.x = pack_bf16x2(p[8 * s + 0], p[8 * s + 1]);
+    u.y = pack_bf16x2(p[8 * s + 2], p[8 * s + 3]);
+    u.z = pack_bf16x2(p[8 * s + 4], p[8 * s + 5]);
+    u.w = pack_bf16x2(p[8 * s + 6], p[8 * s + 7]);
+    return __builtin_bit_cast(Frag, u);
+  }
+  static __device__ __forceinline__ float dot(Frag a, Frag b) {
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s += (float)a[j] * (float)b[j];
+    return s;
+  }
+  static __device__ __forceinline__ void store4(void* base, int64_t at, float a, float b, float c, float d) {
+    *reinterpret_cast<uint2*>(static_cast<bf16*>(base) + at) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
+  }
+};
+
+template <>
+struct Mma<float> {
+  typedef f32x4 Frag;
+  static constexpr int E = 4;
+  static constexpr int STEP = 8;
+  static __device__ __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ Frag along(const float* tile, int ld, int row0, int ks, int lane) {
+    return *reinterpret_cast<const Frag*>(tile + (row0 + (lane & 31)) * ld + ks * 8 + (lane >> 5) * 4);
+  }
+  static __device__ __forceinline__ Frag across(const float* tile, int ld, int row0, int s, int col0, int lane) {
+    const float* p = tile + (row0 + s * 8 + (lane >> 5) * 4) * ld + col0 + (lane & 31);
+    return Frag{p[0], p[ld], p[2 * ld], p[3 * ld]};
+  }
+  static __device__ __forceinline__ Frag of_acc(const f32x16& p, int s) { return Frag{p[4 * s], p[4 * s + 1], p[4 * s + 2], p[4 * s + 3]}; }
+  static __device__ __forceinline__ float dot(Frag a, Frag b) { return a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3]; }
+  static __device__ __forceinline__ void store4(void* base, int64_t at, float a, float b, float c, float d) {
+    *reinterpret_cast<f32x4*>(static_cast<float*>(base) + at) = f32x4{a, b, c, d};
+  }
+};
+
+__device__ __forceinline__ f32x16 zeros() {
+  f32x16 z;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = 0.f;
+  return z;
+}
+
+// Row of register r in the C operand's lane layout.
+__device__ __forceinline__ int acc_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
+
+// The other half of the wave's value.
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+// What a sequence has: n queries, m keys, and by how much the keys that query i sees end past i (limit(i) keys).
+struct Sequence {
+  int n, m, shift;
+  bool causal;
+  __device__ __forceinline__ Sequence(const AttentionArgs& p, int b) {
+    n = p.q_len; m = p.k_len;
+    if (p.q_lengths != nullptr) n = p.q_lengths[b];
+    if (p.k_lengths != nullptr) m = p.k_lengths[b];
+    n = n < 0 ? 0 : n > p.q_len ? p.q_len : n;
+    m = m < 0 ? 0 : m > p.k_len ? p.k_len : m;
+    causal = p.causal != 0;
+    shift = m - n + 1;
+  }
+  // Keys 0 .. limit(i) - 1 are those that query i sees (none where it is not positive).
+  __device__ __forceinline__ int limit(int i) const {
+    if (i >= n) return 0;
+    return !causal ? m : i + shift < m ? i + shift : m;
+  }
+  // ... that any of queries first .. last sees: the last one's
+  __device__ __forceinline__ int seen(int first, int last) const {
+    return first >= n ? 0 : limit(last < n ? last : n - 1);
+  }
+};
+
+}  // namespace sk

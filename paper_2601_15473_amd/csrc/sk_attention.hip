@@ -1,0 +1,324 @@
+// Attention and its gradients (see sk_attention.h for the operands' layouts).
+//
+// Forward, a wave to 32 rows (query, head of the group): s^T = K q^T has a row's scores in its own lane (and the lane 32
+// further), so the running maximum and sum of the softmax are registers; o^T += V^T p^T.  Backward, no
+// atomics: dq by the same walk over the keys with p from lse, dk and dv by a walk over the queries for 32 keys a wave.
+#include "sk_attention.h"
+
+namespace sk {
+namespace {
+
+constexpr int ROWS = 32;   // rows of a staged tile
+
+// Rows row0 .. + 31 of `base` (rows `stride` elements apart, D values each) into LDS, zeros at and past row `rows` and past D.
+template <typename T, int DP>
+__device__ __forceinline__ void stage(T* tile, const T* base, int64_t stride, int row0, int rows, int D, int tid) {
+  typedef Mma<T> M;
+  constexpr int PIECES = DP / M::E, LD = DP + M::E;
+#pragma unroll
+  for (int i = 0; i < ROWS * PIECES / 256; ++i) {
+    const int piece = i * 256 + tid, row = piece / PIECES, c = piece % PIECES * M::E;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (row0 + row < rows && c < D) v = *reinterpret_cast<const uint4*>(base + (row0 + row) * stride + c);
+    *reinterpret_cast<uint4*>(tile + row * LD + c) = v;
+  }
+}
+
+// A lane's row as fragments of a product's second operand: zeros past D and where the row is not there.
+template <typename T, int DP>
+__device__ __forceinline__ void load_row(typename Mma<T>::Frag (&f)[DP / Mma<T>::STEP], const T* row, bool there, int D, int lane) {
+  typedef Mma<T> M;
+#pragma unroll
+  for (int ks = 0; ks < DP / M::STEP; ++ks) {
+    const int c = ks * M::STEP + (lane >> 5) * M::E;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (there && c < D) v = *reinterpret_cast<const uint4*>(row + c);
+    f[ks] = __builtin_bit_cast(typename M::Frag, v);
+  }
+}
+
+// [DP x 32] with a row of the result to a lane, as rows of D values; nothing where `row` is null
+template <typename T, int DP>
+__device__ __forceinline__ void store_row(T* row, const f32x16 (&acc)[DP / 32], float scale, int D, int lane) {
+  if (row == nullptr) return;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int c = d * 32 + 8 * g + 4 * (lane >> 5);
+      if (c < D) Mma<T>::store4(row, c, acc[d][4 * g] * scale, acc[d][4 * g + 1] * scale, acc[d][4 * g + 2] * scale, acc[d][4 * g + 3] * scale);
+    }
+}
+
+// Work-group -> (sequence, key head, tile); neighbours on one XCD share keys and values.
+__device__ __forceinline__ void locate(const AttentionArgs& p, int tiles, int& b, int& hk, int& tile) {
+  const int id = xcd_remap(blockIdx.x, gridDim.x);
+  tile = id % tiles;
+  hk = id / tiles % p.kv_heads;
+  b = id / tiles / p.kv_heads;
+}
+
+// A lane's row of the packed rows (query, head of the group) of a key head.
+struct Row {
+  int i, h;
+  bool there;
+  __device__ __forceinline__ Row(const AttentionArgs& p, int r, int hk) {
+    i = r / p.group;
+    h = hk * p.group + (r - i * p.group);
+    there = i < p.q_len;
+  }
+};
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void attention_fwd_simple_kernel(const AttentionArgs p, int tiles) {
+  typedef Mma<T> M;
+  constexpr int KS = DP / M::STEP, LD = DP + M::E;
+  __shared__ __align__(16) T k_tile[ROWS * LD];
+  __shared__ __align__(16) T v_tile[ROWS * LD];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int b, hk, tile;
+  locate(p, tiles, b, hk, tile);
+  const Sequence q(p, b);
+  const int r0 = tile * 128;
+  const Row row(p, r0 + wave * 32 + (lane & 31), hk);
+  const int limit = row.there ? q.limit(row.i) : 0;
+  const int keys = q.seen(r0 / p.group, (r0 + 127) / p.group);
+
+  typename M::Frag qf[KS];
+  load_row<T, DP>(qf, static_cast<const T*>(p.q) + b * p.qs[0] + row.i * p.qs[1] + row.h * p.qs[2], row.there && row.i < q.n, p.D, lane);
+  f32x16 o[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) o[d] = zeros();
+  float top = -INFINITY, sum = 0.f;
+  const float c = p.scale * LOG2E;
+  const T* const kb = static_cast<const T*>(p.k) + b * p.ks[0] + hk * p.ks[2];
+  const T* const vb = static_cast<const T*>(p.v) + b * p.vs[0] + hk * p.vs[2];
+  for (int j0 = 0; j0 < keys; j0 += ROWS) {
+    __syncthreads();
+    stage<T, DP>(k_tile, kb, p.ks[1], j0, q.m, p.D, tid);
+    stage<T, DP>(v_tile, vb, p.vs[1], j0, q.m, p.D, tid);
+    __syncthreads();
+    f32x16 s = zeros();
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) s = M::mma(M::along(k_tile, LD, 0, ks, lane), qf[ks], s);
+    float m = top;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = j0 + acc_row(r, lane) < limit ? s[r] * c : -INFINITY;
+      m = fmaxf(m, s[r]);
+    }
+    m = fmaxf(m, other_half(m));
+    const float base = m == -INFINITY ? 0.f : m;   // (a row that has seen nothing: exp2(-inf) are its weights)
+    const float keep = __builtin_amdgcn_exp2f(top - base);
+    top = m;
+    sum *= keep;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = __builtin_amdgcn_exp2f(s[r] - base);
+      sum += s[r];
+    }
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] *= keep;
+#pragma unroll
+      for (int t = 0; t < 32 / M::STEP; ++t) o[d] = M::mma(M::across(v_tile, LD, 0, t, d * 32, lane), M::of_acc(s, t), o[d]);
+    }
+  }
+  sum += other_half(sum);
+  if (row.there) {
+    store_row<T, DP>(static_cast<T*>(p.o) + (((int64_t)b * p.q_len + row.i) * p.heads + row.h) * p.D, o, sum == 0.f ? 0.f : 1.f / sum, p.D, lane);
+    if (p.lse != nullptr && lane < 32)
+      p.lse[((int64_t)b * p.heads + row.h) * p.q_len + row.i] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
+  }
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void attention_dq_simple_kernel(const AttentionArgs p, int tiles) {
+  typedef Mma<T> M;
+  constexpr int KS = DP / M::STEP, LD = DP + M::E;
+  __shared__ __align__(16) T k_tile[ROWS * LD];
+  __shared__ __align__(16) T v_tile[ROWS * LD];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int b, hk, tile;
+  locate(p, tiles, b, hk, tile);
+  const Sequence q(p, b);
+  const int r0 = tile * 128;
+  const Row row(p, r0 + wave * 32 + (lane & 31), hk);
+  const int limit = row.there ? q.limit(row.i) : 0;
+  const int keys = q.seen(r0 / p.group, (r0 + 127) / p.group);
+  const bool counts = row.there && row.i < q.n;
+
+  typename M::Frag qf[KS], gf[KS];
+  const int64_t at = (((int64_t)b * p.q_len + row.i) * p.heads + row.h) * p.D;
+  const int64_t stat = ((int64_t)b * p.heads + row.h) * p.q_len + row.i;
+  load_row<T, DP>(qf, static_cast<const T*>(p.q) + b * p.qs[0] + row.i * p.qs[1] + row.h * p.qs[2], counts, p.D, lane);
+  load_row<T, DP>(gf, static_cast<const T*>(p.d_o) + at, counts, p.D, lane);
+  float delta = 0.f;
+  {
+    typename M::Frag of[KS];
+    load_row<T, DP>(of, static_cast<const T*>(p.o_in) + at, counts, p.D, lane);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) delta += M::dot(of[ks], gf[ks]);
+  }
+  delta += other_half(delta);
+  if (row.there && lane < 32) p.delta[stat] = delta;
+  // (a row that sees nothing has no probabilities, whatever its lse says)
+  const float lse = limit > 0 ? p.lse[stat] * LOG2E : INFINITY;
+  f32x16 dq[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) dq[d] = zeros();
+  const float c = p.scale * LOG2E;
+  const T* const kb = static_cast<const T*>(p.k) + b * p.ks[0] + hk * p.ks[2];
+  const T* const vb = static_cast<const T*>(p.v) + b * p.vs[0] + hk * p.vs[2];
+  for (int j0 = 0; j0 < keys; j0 += ROWS) {
+    __syncthreads();
+    stage<T, DP>(k_tile, kb, p.ks[1], j0, q.m, p.D, tid);
+    stage<T, DP>(v_tile, vb, p.vs[1], j0, q.m, p.D, tid);
+    __syncthreads();
+    f32x16 s = zeros(), g = zeros();
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      s = M::mma(M::along(k_tile, LD, 0, ks, lane), qf[ks], s);
+      g = M::mma(M::along(v_tile, LD, 0, ks, lane), gf[ks], g);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float w = j0 + acc_row(r, lane) < limit ? __builtin_amdgcn_exp2f(s[r] * c - lse) : 0.f;
+      s[r] = w * (g[r] - delta);
+    }
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int t = 0; t < 32 / M::STEP; ++t) dq[d] = M::mma(M::across(k_tile, LD, 0, t, d * 32, lane), M::of_acc(s, t), dq[d]);
+  }
+  store_row<T, DP>(row.there ? static_cast<T*>(p.dq) + at : nullptr, dq, p.scale, p.D, lane);
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void attention_dkv_simple_kernel(const AttentionArgs p, int tiles) {
+  typedef Mma<T> M;
+  constexpr int KS = DP / M::STEP, LD = DP + M::E;
+  __shared__ __align__(16) T q_tile[ROWS * LD];
+  __shared__ __align__(16) T g_tile[ROWS * LD];
+  __shared__ float lse_tile[ROWS], delta_tile[ROWS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int b, hk, tile;
+  locate(p, tiles, b, hk, tile);
+  const Sequence q(p, b);
+  const int j0 = tile * 128, j = j0 + wave * 32 + (lane & 31);
+  const bool there = j < q.m;
+  // the first query that sees key j, and the work-group's first
+  const int first = q.causal ? j - q.shift + 1 : 0;
+  const int i_begin = j0 >= q.m ? q.n : q.causal && j0 - q.shift + 1 > 0 ? (j0 - q.shift + 1) / ROWS * ROWS : 0;
+
+  typename M::Frag kf[KS], vf[KS];
+  load_row<T, DP>(kf, static_cast<const T*>(p.k) + b * p.ks[0] + j * p.ks[1] + hk * p.ks[2], there, p.D, lane);
+  load_row<T, DP>(vf, static_cast<const T*>(p.v) + b * p.vs[0] + j * p.vs[1] + hk * p.vs[2], there, p.D, lane);
+  f32x16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = zeros();
+  const float c = p.scale * LOG2E;
+  for (int gh = 0; gh < p.group; ++gh) {
+    const int h = hk * p.group + gh;
+    const T* const qb = static_cast<const T*>(p.q) + b * p.qs[0] + h * p.qs[2];
+    const T* const gb = static_cast<const T*>(p.d_o) + ((int64_t)b * p.q_len * p.heads + h) * p.D;
+    const float* const lse = p.lse + ((int64_t)b * p.heads + h) * p.q_len;
+    const float* const delta = p.delta + ((int64_t)b * p.heads + h) * p.q_len;
+    for (int i0 = i_begin; i0 < q.n; i0 += ROWS) {
+      __syncthreads();
+      stage<T, DP>(q_tile, qb, p.qs[1], i0, q.n, p.D, tid);
+      stage<T, DP>(g_tile, gb, (int64_t)p.heads * p.D, i0, q.n, p.D, tid);
+      if (tid < ROWS) {
+        lse_tile[tid] = i0 + tid < q.n ? lse[i0 + tid] * LOG2E : INFINITY;
+        delta_tile[tid] = i0 + tid < q.n ? delta[i0 + tid] : 0.f;
+      }
+      __syncthreads();
+      f32x16 s = zeros(), g = zeros();
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        s = M::mma(M::along(q_tile, LD, 0, ks, lane), kf[ks], s);
+        g = M::mma(M::along(g_tile, LD, 0, ks, lane), vf[ks], g);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int i = acc_row(r, lane);
+        s[r] = there && i0 + i >= first && i0 + i < q.n ? __builtin_amdgcn_exp2f(s[r] * c - lse_tile[i]) : 0.f;
+        g[r] = s[r] * (g[r] - delta_tile[i]);
+      }
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int t = 0; t < 32 / M::STEP; ++t) {
+          dv[d] = M::mma(M::across(g_tile, LD, 0, t, d * 32, lane), M::of_acc(s, t), dv[d]);
+          dk[d] = M::mma(M::across(q_tile, LD, 0, t, d * 32, lane), M::of_acc(g, t), dk[d]);
+        }
+    }
+  }
+  const int64_t at = (((int64_t)b * p.k_len + j) * p.kv_heads + hk) * p.D;
+  store_row<T, DP>(j < p.k_len ? static_cast<T*>(p.dk) + at : nullptr, dk, p.scale, p.D, lane);
+  store_row<T, DP>(j < p.k_len ? static_cast<T*>(p.dv) + at : nullptr, dv, 1.f, p.D, lane);
+}
+
+// The trace's view of a strided [batch, tokens, heads, D] array.
+void note_strided(const void* base, int esize, int64_t batch, int64_t tokens, int64_t heads, int64_t D, const int64_t (&st)[3]) {
+  note_matrix(base, 1, (batch - 1) * st[0] + (tokens - 1) * st[1] + (heads - 1) * st[2] + D, 0, esize, false);
+}
+void note_inputs(const AttentionArgs& a, int esize) {
+  if (!tracing()) return;
+  note_strided(a.q, esize, a.batch, a.q_len, a.heads, a.D, a.qs);
+  note_strided(a.k, esize, a.batch, a.k_len, a.kv_heads, a.D, a.ks);
+  note_strided(a.v, esize, a.batch, a.k_len, a.kv_heads, a.D, a.vs);
+  note_matrix(a.q_lengths, 1, a.batch, a.batch, 4, false);
+  note_matrix(a.k_lengths, 1, a.batch, a.batch, 4, false);
+}
+
+int64_t rows_of(const AttentionArgs& a) { return (int64_t)a.batch * a.q_len * a.heads; }
+double pairs(const AttentionArgs& a) { return (double)rows_of(a) * a.k_len * a.D; }
+
+template <typename T, int DP>
+hipError_t fwd(const AttentionArgs& a, hipStream_t s) {
+  const int esize = sizeof(T), tiles = ((int64_t)a.q_len * a.group + 127) / 128;
+  note_inputs(a, esize);
+  note_matrix(a.o, rows_of(a), a.D, a.D, esize, true);
+  if (a.lse != nullptr) note_matrix(a.lse, 1, rows_of(a), rows_of(a), 4, true);
+  return launch_kernel(kernel_label("attention_fwd_simple_kernel", {esize == 2 ? "bf16" : "float", lbl(DP)}).c_str(),
+                       Work{4 * pairs(a), 0.0}, attention_fwd_simple_kernel<T, DP>, dim3(a.batch * a.kv_heads * tiles), dim3(256), s, a, tiles);
+}
+
+template <typename T, int DP>
+hipError_t bwd(const AttentionArgs& a, hipStream_t s) {
+  const int esize = sizeof(T), tiles = ((int64_t)a.q_len * a.group + 127) / 128, k_tiles = (a.k_len + 127) / 128;
+  const char* type = esize == 2 ? "bf16" : "float";
+  note_inputs(a, esize);
+  note_matrix(a.d_o, rows_of(a), a.D, a.D, esize, false);
+  note_matrix(a.o_in, rows_of(a), a.D, a.D, esize, false);
+  note_matrix(a.lse, 1, rows_of(a), rows_of(a), 4, false);
+  note_matrix(a.delta, 1, rows_of(a), rows_of(a), 4, true);
+  note_matrix(a.dq, rows_of(a), a.D, a.D, esize, true);
+  hipError_t e = launch_kernel(kernel_label("attention_dq_simple_kernel", {type, lbl(DP)}).c_str(), Work{6 * pairs(a), 0.0},
+                               attention_dq_simple_kernel<T, DP>, dim3(a.batch * a.kv_heads * tiles), dim3(256), s, a, tiles);
+  if (e != hipSuccess) return e;
+  note_inputs(a, esize);
+  note_matrix(a.d_o, rows_of(a), a.D, a.D, esize, false);
+  note_matrix(a.lse, 1, rows_of(a), rows_of(a), 4, false);
+  note_matrix(a.delta, 1, rows_of(a), rows_of(a), 4, false);
+  note_matrix(a.dk, (int64_t)a.batch * a.k_len * a.kv_heads, a.D, a.D, esize, true);
+  note_matrix(a.dv, (int64_t)a.batch * a.k_len * a.kv_heads, a.D, a.D, esize, true);
+  return launch_kernel(kernel_label("attention_dkv_simple_kernel", {type, lbl(DP)}).c_str(), Work{8 * pairs(a), 0.0},
+                       attention_dkv_simple_kernel<T, DP>, dim3(a.batch * a.kv_heads * k_tiles), dim3(256), s, a, k_tiles);
+}
+
+}  // namespace
+
+hipError_t launch_attention_fwd(const AttentionArgs& a, bool f32, hipStream_t s) {
+  if (f32) return a.D <= 64 ? fwd<float, 64>(a, s) : fwd<float, 128>(a, s);
+  return a.D <= 64 ? fwd<bf16, 64>(a, s) : fwd<bf16, 128>(a, s);
+}
+
+hipError_t launch_attention_bwd(const AttentionArgs& a, bool f32, hipStream_t s) {
+  if (f32) return a.D <= 64 ? bwd<float, 64>(a, s) : bwd<float, 128>(a, s);
+  return a.D <= 64 ? bwd<bf16, 64>(a, s) : bwd<bf16, 128>(a, s);
+}
+
+}  // namespace sk

@@ -1,0 +1,73 @@
+// Host-side launchers of the block operators' kernels (internal; the public ABI is include/sk_block.h).
+#pragma once
+#include "sk_launch.h"
+
+namespace sk {
+
+// A HIP error under the calling thread's sk_last_hip_error (sk_api.hip).
+void note_hip_error(hipError_t e, const char* what);
+
+// Arguments of the attention kernels.  Rows of o, dO and dq are dense [batch, q_len, heads, D], lse and delta
+// [batch, heads, q_len], dk and dv dense [batch, k_len, kv_heads, D].
+struct AttentionArgs {
+  const void *q, *k, *v, *d_o;
+  const void* o_in;             // backward: the forward pass's result
+  void *o, *dq, *dk, *dv;
+  float* lse;                   // forward: written unless null; backward: read
+  float* delta;                 // backward: sum_d dO o of every row
+  const int32_t *q_lengths, *k_lengths;
+  int64_t qs[3], ks[3], vs[3];  // batch, token, head strides in elements
+  int batch, q_len, k_len, heads, kv_heads, group, D;
+  int causal;
+  float scale;
+};
+
+hipError_t launch_attention_fwd(const AttentionArgs& a, bool f32, hipStream_t s);
+// dq and delta, then dk and dv
+hipError_t launch_attention_bwd(const AttentionArgs& a, bool f32, hipStream_t s);
+
+struct NormRopeArgs {
+  const void *q, *k, *wq, *wk;
+  const float *cos, *sin;
+  const void* positions;
+  void *q_out, *k_out;                    // forward: the results; backward: dq, dk
+  const void *dq_out, *dk_out;            // backward
+  float* partial;                         // backward: [groups][2][D] sums of dwq, dwk
+  void *dwq, *dwk;
+  int64_t qs[2], ks[2], qos[2], kos[2];
+  int64_t tokens, table_rows;
+  int heads, kv_heads, D, rotary, interleaved, pos64;
+  float eps;
+};
+constexpr int NORM_ROPE_MAX_GROUPS = 1024;
+hipError_t launch_norm_rope_fwd(const NormRopeArgs& a, bool f32, hipStream_t s);
+hipError_t launch_norm_rope_bwd(const NormRopeArgs& a, bool f32, hipStream_t s);
+
+struct EmbeddingArgs {
+  const void* ids;
+  const void* table;     // forward
+  const void* dy;        // backward
+  void* out;             // y, or dtable
+  int64_t tokens, rows;
+  int width, ids64;
+  float scale;
+  // backward: the tokens sorted by id (stable), and the fp32 sums of runs that are cut
+  unsigned *keys, *order, *keys_runs, *order_runs;
+  float* partial;        // [chunks][2][width]
+};
+constexpr int EMBEDDING_RUN = 16384;   // tokens one work-group sorts
+constexpr int EMBEDDING_CHUNK = 32;    // sorted tokens one work-group sums
+hipError_t launch_embedding_fwd(const EmbeddingArgs& a, bool f32, hipStream_t s);
+hipError_t launch_embedding_bwd(const EmbeddingArgs& a, bool f32, hipStream_t s);
+
+struct DropoutArgs {
+  const void *x, *residual;
+  void* y;
+  int64_t n;
+  unsigned drop;         // of 65536 words, those below it
+  float scale;           // 65536 / (65536 - drop), 0 if that has no value
+  unsigned key[2], offset[2];
+};
+hipError_t launch_dropout(const DropoutArgs& a, bool f32, hipStream_t s);
+
+}  // namespace sk

@@ -1,4 +1,4 @@
-"""ctypes binding of libsk.so: the entry points of include/sk.h under the same
+"""ctypes binding of libsk.so: the entry points of include/sk.h and include/sk_block.h under the same
 names.  Argument marshalling only -- every step of the computation runs in the
 library's HIP kernels.  There is no CPU fallback: if the library has not been
 built (``python -m paper_2601_15473_amd.build``) importing this module fails.
@@ -69,6 +69,44 @@ _lib.sk_last_hip_error.restype = ctypes.c_char_p
 _lib.sk_last_hip_error.argtypes = []
 _lib.sk_set_plan.restype = ctypes.c_int
 _lib.sk_set_plan.argtypes = [ctypes.c_int]
+
+# ---- the operators of a transformer block (include/sk_block.h) ----
+
+class AttentionShape(ctypes.Structure):
+    """sk_attention_shape; the lengths are device addresses or None"""
+    _fields_ = [("batch", _i64), ("q_len", _i64), ("k_len", _i64),
+                ("heads", _i32), ("kv_heads", _i32), ("head_dim", _i32), ("causal", _i32),
+                ("scale", ctypes.c_float), ("dtype", ctypes.c_int),
+                ("q_strides", _i64 * 3), ("k_strides", _i64 * 3), ("v_strides", _i64 * 3),
+                ("q_lengths", _vp), ("k_lengths", _vp)]
+
+
+class NormRopeShape(ctypes.Structure):
+    """sk_norm_rope_shape"""
+    _fields_ = [("tokens", _i64), ("heads", _i32), ("kv_heads", _i32), ("head_dim", _i32), ("rotary_dim", _i32),
+                ("interleaved", _i32), ("position_bytes", _i32), ("table_rows", _i64), ("eps", ctypes.c_float),
+                ("dtype", ctypes.c_int), ("q_strides", _i64 * 2), ("k_strides", _i64 * 2),
+                ("q_out_strides", _i64 * 2), ("k_out_strides", _i64 * 2)]
+
+
+_shape, _f32, _u64 = ctypes.POINTER(AttentionShape), ctypes.c_float, ctypes.c_uint64
+_norm_shape = ctypes.POINTER(NormRopeShape)
+for _name, _restype, _argtypes in (
+        ("sk_attention_workspace_bytes", _sz, [_shape, _i32]),
+        ("sk_attention_fwd", ctypes.c_int, [_shape] + [_vp] * 6 + [_sz, _vp]),
+        ("sk_attention_bwd", ctypes.c_int, [_shape] + [_vp] * 10 + [_sz, _vp]),
+        ("sk_norm_rope_fwd", ctypes.c_int, [_norm_shape] + [_vp] * 10),
+        ("sk_norm_rope_workspace_bytes", _sz, [_norm_shape]),
+        ("sk_norm_rope_bwd", ctypes.c_int, [_norm_shape] + [_vp] * 14 + [_sz, _vp]),
+        ("sk_embedding_fwd", ctypes.c_int, [_vp, _i32, _vp, _vp, _i64, _i64, _i64, _f32, ctypes.c_int, _vp]),
+        ("sk_embedding_workspace_bytes", _sz, [_i64, _i64, _i64, ctypes.c_int]),
+        ("sk_embedding_bwd", ctypes.c_int, [_vp, _i32, _vp, _vp, _i64, _i64, _i64, _f32, ctypes.c_int, _vp, _sz, _vp]),
+        ("sk_dropout", ctypes.c_int, [_vp, _vp, _vp, _i64, _f32, _u64, _u64, ctypes.c_int, _vp])):
+    getattr(_lib, _name).restype = _restype
+    getattr(_lib, _name).argtypes = _argtypes
+
+BLOCK_EXPORTS = ("sk_attention_workspace_bytes", "sk_attention_fwd", "sk_attention_bwd", "sk_norm_rope_fwd", "sk_norm_rope_bwd",
+                 "sk_norm_rope_workspace_bytes", "sk_embedding_fwd", "sk_embedding_bwd", "sk_embedding_workspace_bytes", "sk_dropout")
 
 # ---- testing / tuning / measurement aids (include/sk_debug.h) ----
 (SK_TUNE_TILE, SK_TUNE_WTILE, SK_TUNE_WSPLITS, SK_TUNE_BM, SK_TUNE_SLICES, SK_TUNE_STILE, SK_TUNE_SSPLITS,
@@ -191,6 +229,52 @@ def sk_round_gradients(sources, targets, counts, stream=None):
 
 def sk_linear_workspace_bytes(op, tokens, d_in, d_out, l, k, dtype):
     return _lib.sk_linear_workspace_bytes(op, tokens, d_in, d_out, l, k, dtype)
+
+
+def sk_attention_workspace_bytes(shape, backward):
+    return _lib.sk_attention_workspace_bytes(shape, backward)
+
+
+def sk_attention_fwd(shape, q, k, v, o, lse, workspace, workspace_bytes, stream=None):
+    return _lib.sk_attention_fwd(shape, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(workspace), workspace_bytes, _stream(stream))
+
+
+def sk_attention_bwd(shape, q, k, v, o, lse, d_o, dq, dk, dv, workspace, workspace_bytes, stream=None):
+    return _lib.sk_attention_bwd(shape, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(d_o), _ptr(dq), _ptr(dk), _ptr(dv),
+                                 _ptr(workspace), workspace_bytes, _stream(stream))
+
+
+def sk_norm_rope_fwd(shape, q, k, q_weight, k_weight, cos, sin, positions, q_out, k_out, stream=None):
+    return _lib.sk_norm_rope_fwd(shape, _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(cos), _ptr(sin), _ptr(positions),
+                                 _ptr(q_out), _ptr(k_out), _stream(stream))
+
+
+def sk_norm_rope_workspace_bytes(shape):
+    return _lib.sk_norm_rope_workspace_bytes(shape)
+
+
+def sk_norm_rope_bwd(shape, q, k, q_weight, k_weight, cos, sin, positions, dq_out, dk_out, dq, dk, dq_weight, dk_weight,
+                     workspace, workspace_bytes, stream=None):
+    return _lib.sk_norm_rope_bwd(shape, _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(cos), _ptr(sin), _ptr(positions),
+                                 _ptr(dq_out), _ptr(dk_out), _ptr(dq), _ptr(dk), _ptr(dq_weight), _ptr(dk_weight),
+                                 _ptr(workspace), workspace_bytes, _stream(stream))
+
+
+def sk_embedding_fwd(ids, id_bytes, table, y, tokens, rows, width, scale, dtype, stream=None):
+    return _lib.sk_embedding_fwd(_ptr(ids), id_bytes, _ptr(table), _ptr(y), tokens, rows, width, scale, dtype, _stream(stream))
+
+
+def sk_embedding_workspace_bytes(tokens, rows, width, dtype):
+    return _lib.sk_embedding_workspace_bytes(tokens, rows, width, dtype)
+
+
+def sk_embedding_bwd(ids, id_bytes, dy, dtable, tokens, rows, width, scale, dtype, workspace, workspace_bytes, stream=None):
+    return _lib.sk_embedding_bwd(_ptr(ids), id_bytes, _ptr(dy), _ptr(dtable), tokens, rows, width, scale, dtype, _ptr(workspace),
+                                 workspace_bytes, _stream(stream))
+
+
+def sk_dropout(x, residual, y, n, p, seed, offset, dtype, stream=None):
+    return _lib.sk_dropout(_ptr(x), _ptr(residual), _ptr(y), n, p, seed, offset, dtype, _stream(stream))
 
 
 def sk_status_string(status):

@@ -1,0 +1,105 @@
+"""The scaled embedding and its gradient by sorted tokens, against the plain form in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import block_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def block():
+    from paper_2601_15473_amd import block
+    return block
+
+
+def _normal(seed, shape, dtype, std=1.0):
+    g = torch.Generator(device="cpu").manual_seed(seed)
+    return (torch.randn(shape, generator=g) * std).to(dtype).cuda()
+
+
+def _ids(kind, T, V, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    if kind == "same":
+        return torch.full((T,), V - 1)
+    if kind == "distinct":
+        return torch.randperm(max(T, V), generator=g)[:T] % V
+    if kind == "outside":
+        return torch.randint(-3, V + 4, (T,), generator=g)
+    if kind == "sorted":
+        return torch.arange(T) * V // T
+    return (torch.exp(torch.rand(T, generator=g, dtype=torch.float64) * math.log(V + 1)) - 1).long().clamp(0, V - 1)   # by rank
+
+
+CASES = [  # tokens, rows, width, ids
+    (1, 1, 8, "same"), (1, 300, 64, "by rank"), (31, 7, 8, "by rank"), (32, 40, 16, "same"), (33, 40, 16, "same"), (64, 64, 24, "distinct"),
+    (65, 5, 40, "outside"), (1000, 300, 768, "by rank"), (1025, 70000, 72, "distinct"), (4001, 256, 136, "by rank"), (4096, 255, 8, "outside"),
+    (5000, 1, 2056, "same"), (16384, 1000, 8, "by rank"), (16385, 1000, 8, "by rank"), (50000, 513, 16, "outside"), (40000, 3, 24, "sorted"),
+    (200, 1 << 17, 8, "by rank"), (300, 9, 4104, "by rank"),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c)))
+def test_against_the_plain_form(block, case, dtype):
+    T, V, W, kind = case
+    ids = _ids(kind, T, V).cuda()
+    table, dy, scale = _normal(1, (V, W), dtype).requires_grad_(), _normal(2, (T, W), dtype), 2.7
+    there = ((ids >= 0) & (ids < V)).cpu()
+    at = ids.cpu()[there]
+    want = torch.zeros(T, W, dtype=torch.float64)
+    want[there] = O.wide(table)[at] * scale
+    sums, sizes, counts = (torch.zeros(V, n, dtype=torch.float64) for n in (W, W, 1))
+    sums.index_add_(0, at, O.wide(dy)[there])
+    sizes.index_add_(0, at, O.wide(dy)[there].abs())
+    counts.index_add_(0, at, torch.ones(len(at), 1, dtype=torch.float64))
+    bound = scale * (O.U[dtype] * sums.abs() + (counts + 4) * O.F * sizes)
+    first = None
+    for i in (ids, ids.int()):
+        torch.full((V, W), math.nan, dtype=dtype, device="cuda")     # (what the gradient's memory held)
+        y = block.embedding(i, table, scale)
+        g, = torch.autograd.grad(y, table, dy)
+        O.assert_within(y, want, (O.U[dtype] + 2 * O.F) * want.abs(), "y")
+        O.assert_within(g, scale * sums, bound, "dtable")
+        first = g if first is None else first
+        assert torch.equal(first, g)
+
+
+def test_shapes_strides_and_no_gradient(block):
+    table = _normal(0, (50, 32), torch.bfloat16)
+    ids = torch.arange(24, device="cuda").view(2, 3, 4)
+    y = block.embedding(ids.transpose(0, 2), table.t().contiguous().t())
+    assert torch.equal(y, table[ids.transpose(0, 2)])
+    table.requires_grad_()
+    g, = torch.autograd.grad(block.embedding(ids[:, :1], table).sum(), table)     # (an expanded gradient)
+    want = torch.zeros(50, 32, dtype=torch.bfloat16, device="cuda")
+    want[ids[:, :1].reshape(-1)] = 1
+    assert torch.equal(g, want)
+    assert block.embedding(ids[:0], table).shape == (0, 3, 4, 32)
+    assert not torch.autograd.grad(block.embedding(ids[:0], table).sum(), table)[0].any()
+
+
+def test_not_a_number_stays_in_its_row(block):
+    table = torch.zeros(9, 8, device="cuda").requires_grad_()
+    ids = torch.tensor([4, 2, 4, 7], device="cuda")
+    dy = torch.ones(4, 8, device="cuda")
+    dy[1] = math.nan
+    g, = torch.autograd.grad(block.embedding(ids, table), table, dy)
+    assert torch.isnan(g[2]).all() and torch.isfinite(g[[0, 1, 3, 4, 5, 6, 7, 8]]).all() and (g[4] == 2).all()
+
+
+def test_refusals(block):
+    from paper_2601_15473_amd import libsk as sk
+    table, ids = torch.zeros(5, 16, device="cuda"), torch.zeros(3, dtype=torch.long, device="cuda")
+    with pytest.raises(TypeError):
+        block.embedding(ids.float(), table)
+    with pytest.raises(TypeError):
+        block.embedding(ids, table.half())
+    with pytest.raises(RuntimeError):
+        block.embedding(ids.cpu(), table)
+    with pytest.raises(ValueError):
+        block.embedding(ids, table[:0])
+    with pytest.raises(sk.SkError):
+        block.embedding(ids, torch.zeros(5, 12, device="cuda"))
