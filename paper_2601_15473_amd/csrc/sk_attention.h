@@ -116,4 +116,42 @@ struct Sequence {
   }
 };
 
+// The trace's view of a strided [batch, tokens, heads, D] array.
+inline void note_strided(const void* base, int esize, int64_t batch, int64_t tokens, int64_t heads, int64_t D, const int64_t (&st)[3]) {
+  note_matrix(base, 1, (batch - 1) * st[0] + (tokens - 1) * st[1] + (heads - 1) * st[2] + D, 0, esize, false);
+}
+inline void note_attention_inputs(const AttentionArgs& a, int esize) {
+  if (!tracing()) return;
+  note_strided(a.q, esize, a.batch, a.q_len, a.heads, a.D, a.qs);
+  note_strided(a.k, esize, a.batch, a.k_len, a.kv_heads, a.D, a.ks);
+  note_strided(a.v, esize, a.batch, a.k_len, a.kv_heads, a.D, a.vs);
+  note_matrix(a.q_lengths, 1, a.batch, a.batch, 4, false);
+  note_matrix(a.k_lengths, 1, a.batch, a.batch, 4, false);
+}
+
+inline int64_t rows_of(const AttentionArgs& a) { return (int64_t)a.batch * a.q_len * a.heads; }
+
+inline void note_attention_fwd(const AttentionArgs& a, int esize) {
+  note_attention_inputs(a, esize);
+  note_matrix(a.o, rows_of(a), a.D, a.D, esize, true);
+  note_matrix(a.lse, 1, rows_of(a), rows_of(a), 4, true);
+}
+inline void note_attention_dq(const AttentionArgs& a, int esize) {
+  note_attention_inputs(a, esize);
+  note_matrix(a.d_o, rows_of(a), a.D, a.D, esize, false);
+  note_matrix(a.o_in, rows_of(a), a.D, a.D, esize, false);
+  note_matrix(a.lse, 1, rows_of(a), rows_of(a), 4, false);
+  note_matrix(a.lse2, 1, rows_of(a), rows_of(a), 4, true);
+  note_matrix(a.delta, 1, rows_of(a), rows_of(a), 4, true);
+  note_matrix(a.dq, rows_of(a), a.D, a.D, esize, true);
+}
+inline void note_attention_dkv(const AttentionArgs& a, int esize) {
+  note_attention_inputs(a, esize);
+  note_matrix(a.d_o, rows_of(a), a.D, a.D, esize, false);
+  note_matrix(a.lse2, 1, rows_of(a), rows_of(a), 4, false);
+  note_matrix(a.delta, 1, rows_of(a), rows_of(a), 4, false);
+  note_matrix(a.dk, (int64_t)a.batch * a.k_len * a.kv_heads, a.D, a.D, esize, true);
+  note_matrix(a.dv, (int64_t)a.batch * a.k_len * a.kv_heads, a.D, a.D, esize, true);
+}
+
 }  // namespace sk

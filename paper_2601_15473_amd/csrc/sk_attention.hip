@@ -159,12 +159,15 @@ __global__ __launch_bounds__(256) void attention_dq_simple_kernel(const Attentio
     typename M::Frag of[KS];
     load_row<T, DP>(of, static_cast<const T*>(p.o_in) + at, counts, p.D, lane);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) delta += M::dot(of[ks], gf[ks]);
+    for (int ks = 0; ks < KS; ++ks) delta -= M::dot(of[ks], gf[ks]);
   }
   delta += other_half(delta);
-  if (row.there && lane < 32) p.delta[stat] = delta;
   // (a row that sees nothing has no probabilities, whatever its lse says)
   const float lse = limit > 0 ? p.lse[stat] * LOG2E : INFINITY;
+  if (row.there && lane < 32) {
+    p.lse2[stat] = lse;
+    p.delta[stat] = delta;
+  }
   f32x16 dq[DP / 32];
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) dq[d] = zeros();
@@ -185,7 +188,7 @@ __global__ __launch_bounds__(256) void attention_dq_simple_kernel(const Attentio
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const float w = j0 + acc_row(r, lane) < limit ? __builtin_amdgcn_exp2f(s[r] * c - lse) : 0.f;
-      s[r] = w * (g[r] - delta);
+      s[r] = w * (g[r] + delta);
     }
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
@@ -223,14 +226,14 @@ __global__ __launch_bounds__(256) void attention_dkv_simple_kernel(const Attenti
     const int h = hk * p.group + gh;
     const T* const qb = static_cast<const T*>(p.q) + b * p.qs[0] + h * p.qs[2];
     const T* const gb = static_cast<const T*>(p.d_o) + ((int64_t)b * p.q_len * p.heads + h) * p.D;
-    const float* const lse = p.lse + ((int64_t)b * p.heads + h) * p.q_len;
+    const float* const lse = p.lse2 + ((int64_t)b * p.heads + h) * p.q_len;
     const float* const delta = p.delta + ((int64_t)b * p.heads + h) * p.q_len;
     for (int i0 = i_begin; i0 < q.n; i0 += ROWS) {
       __syncthreads();
       stage<T, DP>(q_tile, qb, p.qs[1], i0, q.n, p.D, tid);
       stage<T, DP>(g_tile, gb, (int64_t)p.heads * p.D, i0, q.n, p.D, tid);
       if (tid < ROWS) {
-        lse_tile[tid] = i0 + tid < q.n ? lse[i0 + tid] * LOG2E : INFINITY;
+        lse_tile[tid] = i0 + tid < q.n ? lse[i0 + tid] : INFINITY;
         delta_tile[tid] = i0 + tid < q.n ? delta[i0 + tid] : 0.f;
       }
       __syncthreads();
@@ -244,7 +247,7 @@ __global__ __launch_bounds__(256) void attention_dkv_simple_kernel(const Attenti
       for (int r = 0; r < 16; ++r) {
         const int i = acc_row(r, lane);
         s[r] = there && i0 + i >= first && i0 + i < q.n ? __builtin_amdgcn_exp2f(s[r] * c - lse_tile[i]) : 0.f;
-        g[r] = s[r] * (g[r] - delta_tile[i]);
+        g[r] = s[r] * (g[r] + delta_tile[i]);
       }
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d)
@@ -260,65 +263,38 @@ __global__ __launch_bounds__(256) void attention_dkv_simple_kernel(const Attenti
   store_row<T, DP>(j < p.k_len ? static_cast<T*>(p.dv) + at : nullptr, dv, 1.f, p.D, lane);
 }
 
-// The trace's view of a strided [batch, tokens, heads, D] array.
-void note_strided(const void* base, int esize, int64_t batch, int64_t tokens, int64_t heads, int64_t D, const int64_t (&st)[3]) {
-  note_matrix(base, 1, (batch - 1) * st[0] + (tokens - 1) * st[1] + (heads - 1) * st[2] + D, 0, esize, false);
-}
-void note_inputs(const AttentionArgs& a, int esize) {
-  if (!tracing()) return;
-  note_strided(a.q, esize, a.batch, a.q_len, a.heads, a.D, a.qs);
-  note_strided(a.k, esize, a.batch, a.k_len, a.kv_heads, a.D, a.ks);
-  note_strided(a.v, esize, a.batch, a.k_len, a.kv_heads, a.D, a.vs);
-  note_matrix(a.q_lengths, 1, a.batch, a.batch, 4, false);
-  note_matrix(a.k_lengths, 1, a.batch, a.batch, 4, false);
-}
-
-int64_t rows_of(const AttentionArgs& a) { return (int64_t)a.batch * a.q_len * a.heads; }
-double pairs(const AttentionArgs& a) { return (double)rows_of(a) * a.k_len * a.D; }
+double pairs(const AttentionArgs& a) { return (double)a.batch * a.q_len * a.heads * a.k_len * a.D; }
 
 template <typename T, int DP>
 hipError_t fwd(const AttentionArgs& a, hipStream_t s) {
-  const int esize = sizeof(T), tiles = ((int64_t)a.q_len * a.group + 127) / 128;
-  note_inputs(a, esize);
-  note_matrix(a.o, rows_of(a), a.D, a.D, esize, true);
-  if (a.lse != nullptr) note_matrix(a.lse, 1, rows_of(a), rows_of(a), 4, true);
-  return launch_kernel(kernel_label("attention_fwd_simple_kernel", {esize == 2 ? "bf16" : "float", lbl(DP)}).c_str(),
+  const int tiles = ((int64_t)a.q_len * a.group + 127) / 128;
+  note_attention_fwd(a, sizeof(T));
+  return launch_kernel(kernel_label("attention_fwd_simple_kernel", {"float", lbl(DP)}).c_str(),
                        Work{4 * pairs(a), 0.0}, attention_fwd_simple_kernel<T, DP>, dim3(a.batch * a.kv_heads * tiles), dim3(256), s, a, tiles);
 }
 
 template <typename T, int DP>
 hipError_t bwd(const AttentionArgs& a, hipStream_t s) {
-  const int esize = sizeof(T), tiles = ((int64_t)a.q_len * a.group + 127) / 128, k_tiles = (a.k_len + 127) / 128;
-  const char* type = esize == 2 ? "bf16" : "float";
-  note_inputs(a, esize);
-  note_matrix(a.d_o, rows_of(a), a.D, a.D, esize, false);
-  note_matrix(a.o_in, rows_of(a), a.D, a.D, esize, false);
-  note_matrix(a.lse, 1, rows_of(a), rows_of(a), 4, false);
-  note_matrix(a.delta, 1, rows_of(a), rows_of(a), 4, true);
-  note_matrix(a.dq, rows_of(a), a.D, a.D, esize, true);
-  hipError_t e = launch_kernel(kernel_label("attention_dq_simple_kernel", {type, lbl(DP)}).c_str(), Work{6 * pairs(a), 0.0},
+  const int tiles = ((int64_t)a.q_len * a.group + 127) / 128, k_tiles = (a.k_len + 127) / 128;
+  note_attention_dq(a, sizeof(T));
+  hipError_t e = launch_kernel(kernel_label("attention_dq_simple_kernel", {"float", lbl(DP)}).c_str(), Work{6 * pairs(a), 0.0},
                                attention_dq_simple_kernel<T, DP>, dim3(a.batch * a.kv_heads * tiles), dim3(256), s, a, tiles);
   if (e != hipSuccess) return e;
-  note_inputs(a, esize);
-  note_matrix(a.d_o, rows_of(a), a.D, a.D, esize, false);
-  note_matrix(a.lse, 1, rows_of(a), rows_of(a), 4, false);
-  note_matrix(a.delta, 1, rows_of(a), rows_of(a), 4, false);
-  note_matrix(a.dk, (int64_t)a.batch * a.k_len * a.kv_heads, a.D, a.D, esize, true);
-  note_matrix(a.dv, (int64_t)a.batch * a.k_len * a.kv_heads, a.D, a.D, esize, true);
-  return launch_kernel(kernel_label("attention_dkv_simple_kernel", {type, lbl(DP)}).c_str(), Work{8 * pairs(a), 0.0},
+  note_attention_dkv(a, sizeof(T));
+  return launch_kernel(kernel_label("attention_dkv_simple_kernel", {"float", lbl(DP)}).c_str(), Work{8 * pairs(a), 0.0},
                        attention_dkv_simple_kernel<T, DP>, dim3(a.batch * a.kv_heads * k_tiles), dim3(256), s, a, k_tiles);
 }
 
 }  // namespace
 
 hipError_t launch_attention_fwd(const AttentionArgs& a, bool f32, hipStream_t s) {
-  if (f32) return a.D <= 64 ? fwd<float, 64>(a, s) : fwd<float, 128>(a, s);
-  return a.D <= 64 ? fwd<bf16, 64>(a, s) : fwd<bf16, 128>(a, s);
+  if (!f32) return launch_attention_fwd_bf16(a, s);
+  return a.D <= 64 ? fwd<float, 64>(a, s) : fwd<float, 128>(a, s);
 }
 
 hipError_t launch_attention_bwd(const AttentionArgs& a, bool f32, hipStream_t s) {
-  if (f32) return a.D <= 64 ? bwd<float, 64>(a, s) : bwd<float, 128>(a, s);
-  return a.D <= 64 ? bwd<bf16, 64>(a, s) : bwd<bf16, 128>(a, s);
+  if (!f32) return launch_attention_bwd_bf16(a, s);
+  return a.D <= 64 ? bwd<float, 64>(a, s) : bwd<float, 128>(a, s);
 }
 
 }  // namespace sk

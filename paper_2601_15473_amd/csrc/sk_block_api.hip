@@ -61,7 +61,7 @@ sk_status attention_args(const sk_attention_shape* s, AttentionArgs& a) {
 }
 bool lengths_aligned(const AttentionArgs& a) { return ((reinterpret_cast<uintptr_t>(a.q_lengths) | reinterpret_cast<uintptr_t>(a.k_lengths)) & 3u) == 0; }
 size_t attention_bytes(const AttentionArgs& a, bool backward) {
-  return backward ? align_up((size_t)a.batch * a.heads * a.q_len * 4) : 0;
+  return backward ? 2 * align_up((size_t)a.batch * a.heads * a.q_len * 4) : 0;
 }
 
 sk_status norm_rope_args(const sk_norm_rope_shape* s, NormRopeArgs& a, bool back) {
@@ -148,7 +148,8 @@ sk_status sk_attention_bwd(const sk_attention_shape* shape, const void* q, const
   if (!lengths_aligned(a)) return SK_ERR_INVALID_ARG;
   if (!workspace || workspace_bytes < attention_bytes(a, true)) return SK_ERR_WORKSPACE;
   a.q = q; a.k = k; a.v = v; a.o_in = o; a.lse = const_cast<float*>(lse); a.d_o = d_o;
-  a.dq = dq; a.dk = dk; a.dv = dv; a.delta = static_cast<float*>(workspace);
+  a.dq = dq; a.dk = dk; a.dv = dv; a.lse2 = static_cast<float*>(workspace);
+  a.delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + attention_bytes(a, true) / 2);
   return launched(launch_attention_bwd(a, shape->dtype == SK_F32, static_cast<hipStream_t>(stream)), "sk_attention_bwd");
 }
 

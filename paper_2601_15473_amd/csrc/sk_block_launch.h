@@ -7,14 +7,14 @@ namespace sk {
 // A HIP error under the calling thread's sk_last_hip_error (sk_api.hip).
 void note_hip_error(hipError_t e, const char* what);
 
-// Arguments of the attention kernels.  Rows of o, dO and dq are dense [batch, q_len, heads, D], lse and delta
+// Arguments of the attention kernels.  Rows of o, dO and dq are dense [batch, q_len, heads, D], lse and the like
 // [batch, heads, q_len], dk and dv dense [batch, k_len, kv_heads, D].
 struct AttentionArgs {
   const void *q, *k, *v, *d_o;
   const void* o_in;             // backward: the forward pass's result
   void *o, *dq, *dk, *dv;
   float* lse;                   // forward: written unless null; backward: read
-  float* delta;                 // backward: sum_d dO o of every row
+  float *lse2, *delta;          // backward: lse log2(e) and -sum_d dO o of every row, left by dq's kernel for dk's and dv's
   const int32_t *q_lengths, *k_lengths;
   int64_t qs[3], ks[3], vs[3];  // batch, token, head strides in elements
   int batch, q_len, k_len, heads, kv_heads, group, D;
@@ -25,6 +25,9 @@ struct AttentionArgs {
 hipError_t launch_attention_fwd(const AttentionArgs& a, bool f32, hipStream_t s);
 // dq and delta, then dk and dv
 hipError_t launch_attention_bwd(const AttentionArgs& a, bool f32, hipStream_t s);
+
+hipError_t launch_attention_fwd_bf16(const AttentionArgs& a, hipStream_t s);
+hipError_t launch_attention_bwd_bf16(const AttentionArgs& a, hipStream_t s);
 
 struct NormRopeArgs {
   const void *q, *k, *wq, *wk;
