@@ -1,8 +1,15 @@
 // Attention and its gradients in bf16 (see sk_attention.h and sk_attention_tiles.h for the operands' layouts).
 #include "sk_attention_tiles.h"
+#include "sk_rows.h"
 
 namespace sk {
 namespace {
+
+// Few rows: how the keys are cut, and where the ranges' results are.
+struct FewPlan {
+  int row_tiles, splits, chunk;   // tiles of 32 rows; ranges of `chunk` keys
+  float *sums, *stats;            // [heads][splits][rows][D], [heads][splits][rows][2]
+};
 
 // Work-group -> (sequence and key head, tile): consecutive work-groups go to the eight XCDs in turn, so with a multiple of
 // eight heads each one's tiles, which share keys and values, stay on one XCD's L2; and the tiles with most keys come first.
@@ -25,15 +32,28 @@ struct Row {
   }
 };
 
-// A lane's row as fragments of a product's second operand: zeros past D and where the row is not there.
+// A lane's row as fragments of a product's second operand: zeros past D and where the row is not there (`array`, any row that is, is read
+// instead: no branch keeps a load waiting for another).
 template <int DP>
-__device__ __forceinline__ void load_row(bf16x8 (&f)[DP / 16], const bf16* row, bool there, int D, int lane) {
+__device__ __forceinline__ void load_row(bf16x8 (&f)[DP / 16], const void* array, int64_t row, bool there, int D, int lane) {
 #pragma unroll
   for (int ks = 0; ks < DP / 16; ++ks) {
     const int c = ks * 16 + (lane >> 5) * 8;
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (there && c < D) v = *reinterpret_cast<const uint4*>(row + c);
-    f[ks] = __builtin_bit_cast(bf16x8, v);
+    const bool ok = there && c < D;
+    uint4 v = *reinterpret_cast<const uint4*>(static_cast<const bf16*>(array) + (ok ? row + c : 0));
+    f[ks] = __builtin_bit_cast(bf16x8, ok ? v : make_uint4(0, 0, 0, 0));
+  }
+}
+
+// Waits for what has been loaded into them here, ahead of a loop whose own loads go on meanwhile: the compiler, which does not see
+// those, would wait for all that is on its way wherever the loop first uses a fragment.
+template <int N>
+__device__ __forceinline__ void settle(bf16x8 (&f)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    u32x4 u = __builtin_bit_cast(u32x4, f[i]);
+    asm volatile("" : "+v"(u));
+    f[i] = __builtin_bit_cast(bf16x8, u);
   }
 }
 
@@ -131,8 +151,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const Atte
   const int common = __builtin_amdgcn_readfirstlane(last_i < q.n ? q.limit(first_i) : 0);
 
   bf16x8 qf[KS];
-  load_row<DP>(qf, static_cast<const bf16*>(p.q) + b * p.qs[0] + row.i * p.qs[1] + row.h * p.qs[2], row.there && row.i < q.n, p.D, lane);
+  load_row<DP>(qf, p.q, b * p.qs[0] + row.i * p.qs[1] + row.h * p.qs[2], row.there && row.i < q.n, p.D, lane);
   take_sign(qf, p.scale);
+  settle(qf);
   f32x16 o[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = zeros();
@@ -178,6 +199,156 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const Atte
     p.lse[((int64_t)b * p.heads + row.h) * p.q_len + row.i] = sum == 0.f ? -INFINITY : (sm.top + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
+// Forward for few rows: 32 rows a work-group, a range of the keys, of which every wave takes every fourth tile of 32
+// by itself (no barrier; 64 KB of LDS, so that eight waves a CU have 8 to 16 KB each on their way), joined through LDS.  With several
+// ranges the sums, their maxima and the weights' sums go to the workspace and attention_join_kernel puts them together.
+template <int DP>
+__global__ __launch_bounds__(256, 2) void attention_few_kernel(const AttentionArgs p, FewPlan plan) {
+  typedef Tile<DP, 32> L;
+  typedef Mma<bf16> M;
+  constexpr int KS = DP / 16, ND = DP / 32, LD = DP + 4, EACH = L::INSTRUCTIONS;
+  constexpr int ROOM = 2 * L::BYTES > 32 * LD * 4 ? 2 * L::BYTES : 32 * LD * 4;   // of a wave: K and V, at the end its sums
+  __shared__ __align__(1024) unsigned char smem[4 * ROOM + 4 * 32 * 8];
+  asm volatile("" ::"v"((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem) : "memory");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int heads = p.batch * p.kv_heads;
+  const int id = blockIdx.x / heads, bh = blockIdx.x - id * heads, split = id / plan.row_tiles, tile = id - split * plan.row_tiles;
+  const int b = bh / p.kv_heads, hk = bh - b * p.kv_heads;
+  const Sequence q(p, b);
+  const int r0 = tile * 32, rows = p.q_len * p.group - r0 < 32 ? p.q_len * p.group - r0 : 32;
+  const Row row(p, r0 + (lane & 31), hk);
+  const int limit = row.there ? q.limit(row.i) : 0;
+  const int keys = q.seen(r0 / p.group, (r0 + rows - 1) / p.group);
+  const int begin = split * plan.chunk, end = begin + plan.chunk < keys ? begin + plan.chunk : keys;
+  if (begin >= end && split > 0) return;   // (the join knows; without keys at all the first range writes zeros)
+  const int common = __builtin_amdgcn_readfirstlane((r0 + rows - 1) / p.group < q.n ? q.limit(r0 / p.group) : 0);
+
+  const bf16* const kb = static_cast<const bf16*>(p.k) + b * p.ks[0] + hk * p.ks[2];
+  const bf16* const vb = static_cast<const bf16*>(p.v) + b * p.vs[0] + hk * p.vs[2];
+  const typename L::template Loader<1> load_k(0, lane, p.ks[1], p.D), load_v(0, lane, p.vs[1], p.D);
+  const unsigned room = wave * ROOM, k_at = room + L::along_address(lane), v_at = room + L::BYTES + L::across_address(lane);
+  int j0 = begin + wave * 32;
+  if (j0 < end) {
+    load_k.load(rows_from(kb, p.ks[1], j0, q.m, p.D), room, 0);
+    load_v.load(rows_from(vb, p.vs[1], j0, q.m, p.D), room + L::BYTES, 0);
+  }
+  bf16x8 qf[KS];
+  load_row<DP>(qf, p.q, b * p.qs[0] + row.i * p.qs[1] + row.h * p.qs[2], row.there && row.i < q.n, p.D, lane);
+  take_sign(qf, p.scale);
+  settle(qf);
+  f32x16 o[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d) o[d] = zeros();
+  Softmax sm;
+  const float factor = score_factor(p.scale);
+  for (; j0 < end; j0 += 128) {
+    f32x16 s[1] = {zeros()};
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(EACH) : "memory");   // all but V's loads, the youngest: K is there
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) s[0] = M::mma(L::along(k_at, 0, ks), qf[ks], s[0]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");            // K has been read
+    const int next = j0 + 128 < end ? j0 + 128 : q.m;             // (past the last: nothing is fetched)
+    load_k.load(rows_from(kb, p.ks[1], next, j0 + 128 < end ? q.m : 0, p.D), room, 0);
+    if (j0 + 32 > common)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (j0 + acc_row(r, lane) >= limit) s[0][r] = -INFINITY;
+    sm.update(s, o, factor);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(EACH) : "memory");   // V is there
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const bf16x8 w = M::of_acc(s[0], t);
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] = M::mma(L::across(v_at, d, t), w, o[d]);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    load_v.load(rows_from(vb, p.vs[1], next, j0 + 128 < end ? q.m : 0, p.D), room + L::BYTES, 0);
+  }
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");     // (no load may land on what follows)
+  const float sum = sm.sum + other_half(sm.sum);
+  float* const sums = reinterpret_cast<float*>(smem + wave * ROOM);
+  float* const stats = reinterpret_cast<float*>(smem + 4 * ROOM);   // [wave][row]: maximum, sum
+  if (lane < 32) {
+    stats[(wave * 32 + lane) * 2] = sm.top;
+    stats[(wave * 32 + lane) * 2 + 1] = sum;
+  }
+  if ((lane & 31) < rows)
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4*>(sums + (lane & 31) * LD + d * 32 + 8 * g + 4 * (lane >> 5)) = f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+  __syncthreads();
+  // eight features a thread, rows in turn
+  constexpr int PER = DP / 8;
+  for (int at = threadIdx.x; at < rows * PER; at += 256) {
+    const int r = at / PER, c = (at - r * PER) * 8;
+    if (c >= p.D) continue;
+    float top = -INFINITY, total = 0.f, v[8];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, stats[(w * 32 + r) * 2]);
+    const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float keep = __builtin_amdgcn_exp2f(stats[(w * 32 + r) * 2] - base);
+      total += stats[(w * 32 + r) * 2 + 1] * keep;
+      const float* const from = reinterpret_cast<const float*>(smem + w * ROOM) + r * LD + c;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += from[i] * keep;
+    }
+    if (plan.splits > 1) {
+      const int64_t slot = ((int64_t)bh * plan.splits + split) * p.q_len * p.group + r0 + r;
+      store_values<float, 8>(plan.sums + slot * p.D + c, v);
+      if (c == 0) { plan.stats[slot * 2] = top; plan.stats[slot * 2 + 1] = total; }
+    } else {
+      const Row out(p, r0 + r, hk);
+      const float scale = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] *= scale;
+      store_values<bf16, 8>(static_cast<bf16*>(p.o) + (((int64_t)b * p.q_len + out.i) * p.heads + out.h) * p.D + c, v);
+      if (p.lse != nullptr && c == 0) p.lse[((int64_t)b * p.heads + out.h) * p.q_len + out.i] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * LN2;
+    }
+  }
+}
+
+// A wave to a row: the ranges' sums in order, each brought to the largest maximum.
+__global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs p, FewPlan plan) {
+  const int lane = threadIdx.x & 63, rows = p.q_len * p.group, bh = blockIdx.y;
+  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= rows) return;
+  const int b = bh / p.kv_heads, hk = bh - b * p.kv_heads;
+  const Sequence q(p, b);
+  const int r0 = r / 32 * 32, last = r0 + 31 < rows ? r0 + 31 : rows - 1;
+  const int keys = q.seen(r0 / p.group, last / p.group);
+  const int splits = keys > 0 ? (keys + plan.chunk - 1) / plan.chunk : 1;
+  const float* const stats = plan.stats + ((int64_t)bh * plan.splits * rows + r) * 2;
+  float top = -INFINITY;
+  for (int s = lane; s < splits; s += 64) top = fmaxf(top, stats[(int64_t)s * rows * 2]);
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+  const float base = top == -INFINITY ? 0.f : top;
+  const int c = lane * 2;
+  float total = 0.f, x = 0.f, y = 0.f;
+  const float* const sums = plan.sums + ((int64_t)bh * plan.splits * rows + r) * p.D + c;
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s) {
+    const float keep = __builtin_amdgcn_exp2f(stats[(int64_t)s * rows * 2] - base);
+    total += stats[(int64_t)s * rows * 2 + 1] * keep;
+    if (c < p.D) {
+      const float2 v = *reinterpret_cast<const float2*>(sums + (int64_t)s * rows * p.D);
+      x += v.x * keep;
+      y += v.y * keep;
+    }
+  }
+  const Row out(p, r, hk);
+  const float scale = total == 0.f ? 0.f : 1.f / total;
+  if (c < p.D)
+    *reinterpret_cast<unsigned*>(static_cast<bf16*>(p.o) + (((int64_t)b * p.q_len + out.i) * p.heads + out.h) * p.D + c) = pack_bf16x2(x * scale, y * scale);
+  if (p.lse != nullptr && lane == 0) p.lse[((int64_t)b * p.heads + out.h) * p.q_len + out.i] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * LN2;
+}
+
 // dq: the forward pass's walk over the keys, with the probabilities from lse.  Leaves lse log2(e) and minus sum_d dO o of every row for dk and dv.
 template <int DP, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const AttentionArgs p) {
@@ -213,19 +384,22 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
   bf16x8 qf[KS], gf[KS];
   const int64_t at = (((int64_t)b * p.q_len + row.i) * p.heads + row.h) * p.D;
   const int64_t stat = ((int64_t)b * p.heads + row.h) * p.q_len + row.i;
-  load_row<DP>(qf, static_cast<const bf16*>(p.q) + b * p.qs[0] + row.i * p.qs[1] + row.h * p.qs[2], counts, p.D, lane);
+  load_row<DP>(qf, p.q, b * p.qs[0] + row.i * p.qs[1] + row.h * p.qs[2], counts, p.D, lane);
   take_sign(qf, p.scale);
-  load_row<DP>(gf, static_cast<const bf16*>(p.d_o) + at, counts, p.D, lane);
+  load_row<DP>(gf, p.d_o, at, counts, p.D, lane);
   float delta = 0.f;
   {
     bf16x8 of[KS];
-    load_row<DP>(of, static_cast<const bf16*>(p.o_in) + at, counts, p.D, lane);
+    load_row<DP>(of, p.o_in, at, counts, p.D, lane);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) delta -= M::dot(of[ks], gf[ks]);
   }
   delta += other_half(delta);
+  settle(qf);
+  settle(gf);
   // (a row that sees nothing has no probabilities, whatever its lse says)
-  const float lse = limit > 0 ? p.lse[stat] * LOG2E : INFINITY;
+  float lse = limit > 0 ? p.lse[stat] * LOG2E : INFINITY;
+  asm volatile("" : "+v"(lse), "+v"(delta));
   if (row.there && lane < 32) {
     p.lse2[stat] = lse;
     p.delta[stat] = delta;
@@ -311,9 +485,11 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dkv_kernel(const Atte
   if (steps > 0) load(0, i_begin, 0u);
 
   bf16x8 kf[KS], vf[KS];
-  load_row<DP>(kf, static_cast<const bf16*>(p.k) + b * p.ks[0] + j * p.ks[1] + hk * p.ks[2], there, p.D, lane);
+  load_row<DP>(kf, p.k, b * p.ks[0] + j * p.ks[1] + hk * p.ks[2], there, p.D, lane);
   take_sign(kf, p.scale);
-  load_row<DP>(vf, static_cast<const bf16*>(p.v) + b * p.vs[0] + j * p.vs[1] + hk * p.vs[2], there, p.D, lane);
+  load_row<DP>(vf, p.v, b * p.vs[0] + j * p.vs[1] + hk * p.vs[2], there, p.D, lane);
+  settle(kf);
+  settle(vf);
   f32x16 dk[ND], dv[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) dk[d] = dv[d] = zeros();
@@ -371,8 +547,46 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dkv_kernel(const Atte
 double pairs(const AttentionArgs& a) { return (double)a.batch * a.q_len * a.heads * a.k_len * a.D; }
 unsigned groups_of(const AttentionArgs& a, int64_t rows, int per) { return (unsigned)((int64_t)a.batch * a.kv_heads * ((rows + per - 1) / per)); }
 
+// Whether the forward pass goes by attention_few_kernel, and how: rows that fill one wave's tile at most, or too few work-groups of 128 rows
+// to give half the CUs one with a long way through the keys.
+bool few_rows(const AttentionArgs& a, FewPlan& plan) {
+  const int64_t heads = (int64_t)a.batch * a.kv_heads, rows = (int64_t)a.q_len * a.group;
+  if (rows > 32 && (heads * ((rows + 127) / 128) >= NUM_CUS / 2 || a.k_len < 1024)) return false;
+  plan.row_tiles = (int)((rows + 31) / 32);
+  // ranges for two rounds of two work-groups a CU, of 512 keys at least: less than four tiles a wave cost less than the join's launch
+  const int64_t wanted = (4 * NUM_CUS + heads * plan.row_tiles - 1) / (heads * plan.row_tiles);
+  int64_t chunk = (a.k_len + wanted - 1) / wanted;
+  chunk = chunk < 512 ? 512 : (chunk + 127) / 128 * 128;
+  plan.splits = (int)((a.k_len + chunk - 1) / chunk);
+  plan.chunk = (int)chunk;
+  return true;
+}
+size_t few_sums(const AttentionArgs& a, const FewPlan& plan) {
+  return plan.splits > 1 ? (size_t)a.batch * a.kv_heads * plan.splits * a.q_len * a.group * a.D * 4 : 0;
+}
+size_t few_bytes(const AttentionArgs& a, const FewPlan& plan) { return few_sums(a, plan) + few_sums(a, plan) / a.D * 2; }
+
+template <int DP>
+hipError_t few(const AttentionArgs& a, FewPlan plan, hipStream_t s) {
+  const size_t sums = few_sums(a, plan), bytes = few_bytes(a, plan);
+  const int heads = a.batch * a.kv_heads, rows = a.q_len * a.group;
+  plan.sums = static_cast<float*>(a.workspace);
+  plan.stats = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + sums);
+  note_attention_inputs(a, 2);
+  if (plan.splits == 1) note_attention_fwd(a, 2);
+  else note_matrix(a.workspace, 1, bytes, bytes, 1, true);
+  hipError_t e = launch_kernel(kernel_label("attention_few_kernel", {lbl(DP)}).c_str(), Work{4 * pairs(a), 0.0}, attention_few_kernel<DP>,
+                               dim3((unsigned)heads * plan.row_tiles * plan.splits), dim3(256), s, a, plan);
+  if (e != hipSuccess || plan.splits == 1) return e;
+  note_matrix(a.workspace, 1, bytes, bytes, 1, false);
+  note_attention_fwd(a, 2);
+  return launch_kernel("attention_join_kernel", Work{0.0, (double)bytes}, attention_join_kernel, dim3((rows + 3) / 4, heads), dim3(256), s, a, plan);
+}
+
 template <int DP>
 hipError_t fwd(const AttentionArgs& a, hipStream_t s) {
+  FewPlan plan;
+  if (few_rows(a, plan)) return few<DP>(a, plan, s);
   constexpr int WAVES = 4;
   note_attention_fwd(a, 2);
   return launch_kernel(kernel_label("attention_fwd_kernel", {lbl(DP), lbl(WAVES)}).c_str(), Work{4 * pairs(a), 0.0}, attention_fwd_kernel<DP, WAVES>,
@@ -393,6 +607,10 @@ hipError_t bwd(const AttentionArgs& a, hipStream_t s) {
 
 }  // namespace
 
+size_t attention_fwd_bytes_bf16(const AttentionArgs& a) {
+  FewPlan plan;
+  return few_rows(a, plan) ? few_bytes(a, plan) : 0;
+}
 hipError_t launch_attention_fwd_bf16(const AttentionArgs& a, hipStream_t s) { return a.D <= 64 ? fwd<64>(a, s) : fwd<128>(a, s); }
 hipError_t launch_attention_bwd_bf16(const AttentionArgs& a, hipStream_t s) { return a.D <= 64 ? bwd<64>(a, s) : bwd<128>(a, s); }
 

@@ -1,4 +1,4 @@
-// Tiles of 64 rows (keys, or queries) in LDS that both kinds of MFMA operand are read from: along the features
+// Tiles of 64 rows (keys, or queries; 32 where a wave has one to itself) in LDS that both kinds of MFMA operand are read from: along the features
 // (scores) and across the rows (what is summed over them).
 //
 // A tile of DP features is DP / 64 panels of [64 rows][64 features], 128 bytes a row.  It goes from global memory straight
@@ -14,9 +14,9 @@ namespace sk {
 
 constexpr int TILE_ROWS = 64;
 
-template <int DP>
+template <int DP, int ROWS = TILE_ROWS>
 struct Tile {
-  static constexpr int PANELS = DP / 64, PANEL_BYTES = TILE_ROWS * 128, BYTES = PANELS * PANEL_BYTES;
+  static constexpr int PANELS = DP / 64, PANEL_BYTES = ROWS * 128, BYTES = PANELS * PANEL_BYTES;
   static constexpr int INSTRUCTIONS = BYTES / 1024;   // a wave's load fills eight rows of a panel
   static __device__ __forceinline__ int swizzle(int row) {
     const int t = (row >> 1) & 7;
@@ -26,19 +26,21 @@ struct Tile {
   // A wave's share of a tile's loads: instruction i of WAVES * i + wave.
   template <int WAVES>
   struct Loader {
-    static_assert(WAVES == 4 || WAVES == 8, "a wave's instructions in a panel are a multiple of 16 rows apart");
-    static constexpr int EACH = INSTRUCTIONS / WAVES, PER_PANEL = 8 / WAVES;
-    unsigned at[PANELS];   // byte offset of this lane's piece in its first rows, by panel; out of bounds past D
-    unsigned step;         // bytes between a wave's instructions in a panel
+    static constexpr int EACH = INSTRUCTIONS / WAVES, PER_PANEL = ROWS / 8 / WAVES;
+    // (the swizzle has a period of 16 rows: a lone wave's odd instructions have another piece of it)
+    static constexpr int KINDS = WAVES == 1 ? 2 : 1;
+    static_assert(WAVES == 1 || WAVES == 4 || WAVES == 8, "a wave's instructions in a panel are a multiple of 16 rows apart, or turn by turn");
+    unsigned at[PANELS][KINDS];   // byte offset of this lane's piece in its first rows; out of bounds past D
+    unsigned step;                // bytes between instructions of a kind in a panel
     __device__ __forceinline__ Loader(int wave, int lane, int64_t stride, int D) {
-      const int row = wave * 8 + (lane >> 3);
-      step = (unsigned)stride * 2u * (WAVES * 8);
+      step = (unsigned)stride * 2u * (WAVES * KINDS * 8);
 #pragma unroll
-      for (int p = 0; p < PANELS; ++p) {
-        // (rows 32 or 64 further down have the same swizzle; an offset out of bounds stays so, a tile being at most 1 GB)
-        const int piece = p * 8 + ((lane & 7) ^ swizzle(row));
-        at[p] = piece * 8 < D ? (unsigned)row * (unsigned)stride * 2u + (unsigned)piece * 16u : OOB_OFFSET;
-      }
+      for (int p = 0; p < PANELS; ++p)
+#pragma unroll
+        for (int k = 0; k < KINDS; ++k) {   // (an offset out of bounds stays so, a tile being at most 1 GB)
+          const int row = (wave + k) * 8 + (lane >> 3), piece = p * 8 + ((lane & 7) ^ swizzle(row));
+          at[p][k] = piece * 8 < D ? (unsigned)row * (unsigned)stride * 2u + (unsigned)piece * 16u : OOB_OFFSET;
+        }
     }
     // Rows from the descriptor's start on to LDS byte `lds` on.
     __device__ __forceinline__ void load(u32x4 rows, unsigned lds, int wave) const {
@@ -46,7 +48,7 @@ struct Tile {
       for (int p = 0; p < PANELS; ++p)
 #pragma unroll
         for (int i = 0; i < PER_PANEL; ++i)
-          load_to_lds(lds + p * PANEL_BYTES + (i * WAVES + wave) * 1024, at[p] + i * step, rows, 0u);
+          load_to_lds(lds + p * PANEL_BYTES + (i * WAVES + wave) * 1024, at[p][i % KINDS] + i / KINDS * step, rows, 0u);
     }
   };
 

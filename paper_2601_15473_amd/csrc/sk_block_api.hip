@@ -60,8 +60,9 @@ sk_status attention_args(const sk_attention_shape* s, AttentionArgs& a) {
   return SK_OK;
 }
 bool lengths_aligned(const AttentionArgs& a) { return ((reinterpret_cast<uintptr_t>(a.q_lengths) | reinterpret_cast<uintptr_t>(a.k_lengths)) & 3u) == 0; }
-size_t attention_bytes(const AttentionArgs& a, bool backward) {
-  return backward ? 2 * align_up((size_t)a.batch * a.heads * a.q_len * 4) : 0;
+size_t attention_bytes(const AttentionArgs& a, bool f32, bool backward) {
+  if (!backward) return f32 ? 0 : align_up(attention_fwd_bytes_bf16(a));
+  return 2 * align_up((size_t)a.batch * a.heads * a.q_len * 4);
 }
 
 sk_status norm_rope_args(const sk_norm_rope_shape* s, NormRopeArgs& a, bool back) {
@@ -122,7 +123,7 @@ extern "C" {
 size_t sk_attention_workspace_bytes(const sk_attention_shape* shape, int32_t backward) {
   AttentionArgs a{};
   if (attention_args(shape, a) != SK_OK) return (size_t)-1;
-  return attention_bytes(a, backward != 0);
+  return attention_bytes(a, shape->dtype == SK_F32, backward != 0);
 }
 
 sk_status sk_attention_fwd(const sk_attention_shape* shape, const void* q, const void* k, const void* v, void* o, float* lse,
@@ -132,9 +133,9 @@ sk_status sk_attention_fwd(const sk_attention_shape* shape, const void* q, const
   const sk_status st = attention_args(shape, a);
   if (st != SK_OK) return st;
   if (!lengths_aligned(a)) return SK_ERR_INVALID_ARG;
-  const size_t need = attention_bytes(a, false);
+  const size_t need = attention_bytes(a, shape->dtype == SK_F32, false);
   if (need > 0 && (!workspace || workspace_bytes < need)) return SK_ERR_WORKSPACE;
-  a.q = q; a.k = k; a.v = v; a.o = o; a.lse = lse;
+  a.q = q; a.k = k; a.v = v; a.o = o; a.lse = lse; a.workspace = workspace;
   return launched(launch_attention_fwd(a, shape->dtype == SK_F32, static_cast<hipStream_t>(stream)), "sk_attention_fwd");
 }
 
@@ -146,10 +147,10 @@ sk_status sk_attention_bwd(const sk_attention_shape* shape, const void* q, const
   const sk_status st = attention_args(shape, a);
   if (st != SK_OK) return st;
   if (!lengths_aligned(a)) return SK_ERR_INVALID_ARG;
-  if (!workspace || workspace_bytes < attention_bytes(a, true)) return SK_ERR_WORKSPACE;
+  if (!workspace || workspace_bytes < attention_bytes(a, shape->dtype == SK_F32, true)) return SK_ERR_WORKSPACE;
   a.q = q; a.k = k; a.v = v; a.o_in = o; a.lse = const_cast<float*>(lse); a.d_o = d_o;
   a.dq = dq; a.dk = dk; a.dv = dv; a.lse2 = static_cast<float*>(workspace);
-  a.delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + attention_bytes(a, true) / 2);
+  a.delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + attention_bytes(a, shape->dtype == SK_F32, true) / 2);
   return launched(launch_attention_bwd(a, shape->dtype == SK_F32, static_cast<hipStream_t>(stream)), "sk_attention_bwd");
 }
 

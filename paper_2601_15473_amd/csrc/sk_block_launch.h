@@ -20,8 +20,10 @@ struct AttentionArgs {
   int batch, q_len, k_len, heads, kv_heads, group, D;
   int causal;
   float scale;
+  void* workspace;              // forward
 };
 
+size_t attention_fwd_bytes_bf16(const AttentionArgs& a);
 hipError_t launch_attention_fwd(const AttentionArgs& a, bool f32, hipStream_t s);
 // dq and delta, then dk and dv
 hipError_t launch_attention_bwd(const AttentionArgs& a, bool f32, hipStream_t s);
