@@ -448,13 +448,16 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
 }
 
 // dk and dv: 32 keys a wave, their sums in registers over all queries of all heads that share them; tiles of 64 queries and their
-// dO through the ring, with what dq's kernel left of their rows.
+// dO through the ring, with what dq's kernel left of their rows.  Two waves a SIMD, so that one's exponentials run under the other's
+// products, is what the registers are kept to: one wave of 330 took 1572 us where two take 1098 (16384 tokens in sequences of 4096, 32 heads on 8 of 128,
+// causal).  256 keys a work-group instead of 128 load half as much for 1 % there, and cost 17 to 25 % at 128 to 512 keys of 64.
 template <int DP, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, 1) void attention_dkv_kernel(const AttentionArgs p) {
+__global__ __launch_bounds__(WAVES * 64, 2) void attention_dkv_kernel(const AttentionArgs p) {
   typedef Tile<DP> L;
   typedef Mma<bf16> M;
   constexpr int KS = DP / 16, ND = DP / 32, STATS = 2 * L::BYTES, SLOT = STATS + 1024;
-  __shared__ __align__(1024) unsigned char smem[2 * SLOT];
+  constexpr int APART = DP > 64 ? 1 : 0;   // fragments of v that lie in LDS, a lane's own to read: all of them in registers are four too many
+  __shared__ __align__(1024) unsigned char smem[2 * SLOT + WAVES * APART * 1024];
   asm volatile("" ::"v"((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem) : "memory");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int b, hk, tile;
@@ -462,17 +465,16 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dkv_kernel(const Atte
   const Sequence q(p, b);
   const int j0 = tile * WAVES * 32, jw = j0 + wave * 32, j = jw + (lane & 31);
   const bool there = j < q.m;
-  // the first query that sees key j (past the end: none does), and the first tile that the work-group and the wave look at
-  const int first = there ? (q.causal ? j - q.shift + 1 : 0) : INT32_MAX;
+  // the first tile that the work-group and the wave look at (the first query that sees a key; past the end none does)
   const int i_begin = q.causal && j0 - q.shift + 1 > 0 ? (j0 - q.shift + 1) / TILE_ROWS * TILE_ROWS : 0;
   const int i_wave = jw < q.m ? (q.causal ? jw - q.shift + 1 : 0) : INT32_MAX;
   const int i_whole = jw + 31 < q.m ? (q.causal ? jw + 31 - q.shift + 1 : 0) : INT32_MAX;   // from here on queries see all the wave's keys
   const int per_head = j0 < q.m && q.n > i_begin ? (q.n - i_begin + TILE_ROWS - 1) / TILE_ROWS : 0, steps = per_head * p.group;
 
-  const typename L::template Loader<WAVES> load_q(wave, lane, p.qs[1], p.D), load_g(wave, lane, (int64_t)p.heads * p.D, p.D);
-  const unsigned at_along = L::along_address(lane), at_across = L::across_address(lane);
+  // (sums, keys and values take 192 registers of 256, scores 32: a lane's offsets are computed where they are used)
   auto load = [&](int h, int i0, unsigned slot) {
-    const int head = hk * p.group + h;
+    const int head = hk * p.group + h, lane = lane_again();
+    const typename L::template Loader<WAVES> load_q(wave, lane, p.qs[1], p.D), load_g(wave, lane, (int64_t)p.heads * p.D, p.D);
     load_q.load(rows_from(static_cast<const bf16*>(p.q) + b * p.qs[0] + head * p.qs[2], p.qs[1], i0, q.n, p.D), slot, wave);
     load_g.load(rows_from(static_cast<const bf16*>(p.d_o) + ((int64_t)b * p.q_len * p.heads + head) * p.D, (int64_t)p.heads * p.D, i0, q.n, p.D), slot + L::BYTES, wave);
     if (wave < 2) {   // 64 rows' statistics: zeros behind the last, where q and dO are zeros too and nothing comes of them
@@ -490,6 +492,9 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dkv_kernel(const Atte
   load_row<DP>(vf, p.v, b * p.vs[0] + j * p.vs[1] + hk * p.vs[2], there, p.D, lane);
   settle(kf);
   settle(vf);
+  const unsigned apart = 2 * SLOT + wave * APART * 1024;
+#pragma unroll
+  for (int i = 0; i < APART; ++i) *reinterpret_cast<bf16x8*>(smem + apart + i * 1024 + lane * 16) = vf[KS - APART + i];
   f32x16 dk[ND], dv[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) dk[d] = dv[d] = zeros();
@@ -503,45 +508,55 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dkv_kernel(const Atte
     if (i0 >= q.n) { i0 = i_begin; ++h; }
     if (step + 1 < steps) load(h, i0, SLOT - slot);
     if (i_now + TILE_ROWS <= i_wave) continue;
-#pragma unroll
+#pragma unroll 1
     for (int t = 0; t < 2; ++t) {
+      typedef __attribute__((address_space(3))) const f32x4 lds_f32x4;
+      const int lane = lane_again();
+      const unsigned q_at = slot + t * 4096 + L::along_address(lane), g_at = q_at + L::BYTES, stat_at = slot + STATS + t * 128 + (lane >> 5) * 16;
       f32x16 s = zeros(), g;
-      float lse[16];
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
-        typedef __attribute__((address_space(3))) const f32x4 lds_f32x4;
-        const unsigned at = slot + STATS + (t * 32 + acc_row(r, lane)) * 4;
-        const f32x4 a = *(lds_f32x4*)(uintptr_t)at, d = *(lds_f32x4*)(uintptr_t)(at + 256);
+        const f32x4 d = *(lds_f32x4*)(uintptr_t)(stat_at + 256 + r * 8);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) { lse[r + u] = a[u]; g[r + u] = d[u]; }
+        for (int u = 0; u < 4; ++u) g[r + u] = d[u];
       }
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        s = M::mma(L::along(slot + at_along, t, ks), kf[ks], s);
-        g = M::mma(L::along(slot + L::BYTES + at_along, t, ks), vf[ks], g);
+        s = M::mma(L::along(q_at, 0, ks), kf[ks], s);
+        typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+        g = M::mma(L::along(g_at, 0, ks), ks < KS - APART ? vf[ks] : *(lds_bf16x8*)(uintptr_t)(apart + (ks - KS + APART) * 1024 + lane * 16), g);
       }
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] * factor - lse[r]);
-      if (i_now < i_whole)
+      for (int r = 0; r < 16; r += 4) {
+        const f32x4 lse = *(lds_f32x4*)(uintptr_t)(stat_at + r * 8);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s[r + u] = __builtin_amdgcn_exp2f(s[r + u] * factor - lse[u]);
+      }
+      if (i_now < i_whole) {
+        const int j = jw + (lane & 31), first = j < q.m ? (q.causal ? j - q.shift + 1 : 0) : INT32_MAX;   // the first query that sees key j
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (i_now + t * 32 + acc_row(r, lane) < first) s[r] = 0.f;
+      }
 #pragma unroll
       for (int r = 0; r < 16; ++r) g[r] *= s[r];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const bf16x8 w = M::of_acc(s, u), e = M::of_acc(g, u);
+        const unsigned qt_at = slot + L::across_address(lane) + (t * 2 + u) * 2048;
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
-          dv[d] = M::mma(L::across(slot + L::BYTES + at_across, d, t * 2 + u), w, dv[d]);
-          dk[d] = M::mma(L::across(slot + at_across, d, t * 2 + u), e, dk[d]);
+          dv[d] = M::mma(L::across(qt_at + L::BYTES, d, 0), w, dv[d]);
+          dk[d] = M::mma(L::across(qt_at, d, 0), e, dk[d]);
         }
       }
     }
   }
-  const int64_t at = (((int64_t)b * p.k_len + j) * p.kv_heads + hk) * p.D;
-  store_row<DP>(static_cast<bf16*>(p.dk) + at, j < p.k_len, dk, p.scale, p.D, lane);
-  store_row<DP>(static_cast<bf16*>(p.dv) + at, j < p.k_len, dv, 1.f, p.D, lane);
+  const int j_out = jw + (lane_again() & 31);
+  const int64_t at = (((int64_t)b * p.k_len + j_out) * p.kv_heads + hk) * p.D;
+  store_row<DP>(static_cast<bf16*>(p.dk) + at, j_out < p.k_len, dk, p.scale, p.D, lane_again());
+  store_row<DP>(static_cast<bf16*>(p.dv) + at, j_out < p.k_len, dv, 1.f, p.D, lane_again());
 }
 
 double pairs(const AttentionArgs& a) { return (double)a.batch * a.q_len * a.heads * a.k_len * a.D; }
