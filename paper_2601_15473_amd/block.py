@@ -11,12 +11,37 @@ Tensors are float32 or bfloat16, all floating ones of a call alike; sums are fp3
 """
 from __future__ import annotations
 
+import functools
+
 import torch
 
 from . import libsk as sk
-from .nn import _DTYPES, _on, _stream, _workspace
+from .nn import _DTYPES, _native, _on, _stream, _workspace
 
 _REFUSED = 2 ** 64 - 1
+
+
+def _natively() -> bool:
+    """Whether a call may try its native function (csrc/sk_torch_block.cpp), which computes the same for plain tensors outside of
+    compilation, tracing and torch's modes and transforms, and gives None for anything else."""
+    return _native is not None and not torch.compiler.is_compiling()
+
+
+def _once(backward):
+    """A backward pass whose gradients cannot be differentiated again, and say so where that is tried, whatever the gradients it was
+    given depend on (they themselves do on what it has saved)."""
+    @functools.wraps(backward)
+    def wrapper(ctx, *grads):
+        with torch.no_grad():
+            out = backward(ctx, *grads)
+        if not torch.is_grad_enabled():
+            return out
+        there = [g.detach().requires_grad_() for g in out if g is not None]
+        fail = torch._C._functions.DelayedError(b"trying to differentiate twice a function that was marked with @once_differentiable", len(there))
+        marked = fail(*there)
+        left = iter(marked if isinstance(marked, tuple) else (marked,))
+        return tuple(None if g is None else next(left) for g in out)
+    return wrapper
 
 
 def _checked(what: str, first: torch.Tensor, **tensors):
@@ -108,7 +133,7 @@ class AttentionFunction(torch.autograd.Function):
         return o
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, do):
         q, k, v, o, lse, q_lengths, k_lengths = ctx.saved_tensors
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
@@ -135,6 +160,10 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lengths: torc
 
     Strided views (slices of a projection's output, of a cache) are read in place.  head_dim: a multiple of 8 up to 128.
     """
+    if _natively():
+        o = _native.attention(q, k, v, q_lengths, k_lengths, causal, scale)
+        if o is not None:
+            return o
     _checked("attention", q, q=q, k=k, v=v)
     if q.dim() != 4 or k.dim() != 4 or k.shape != v.shape or q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3]:
         raise ValueError("attention: shapes do not match (q [batch, q_len, heads, head_dim], k and v [batch, k_len, kv_heads, head_dim])")
@@ -189,7 +218,7 @@ class NormRopeFunction(torch.autograd.Function):
         return _norm_rope_forward(q, k, wq, wk, cos, sin, positions, eps, interleaved)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, dq_out, dk_out):
         q, k, wq, wk, cos, sin, positions = ctx.saved_tensors
         dq, dk, dwq, dwk = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, wq, wk))
@@ -216,6 +245,10 @@ def head_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: torch.Tensor, k_w
 
     Strided views are read in place.  head_dim: a multiple of 8 up to 256; the number of rotated features is a multiple of 8.
     """
+    if out is None and _natively():
+        both = _native.head_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
+        if both is not None:
+            return both
     _checked("head_norm_rope", q, q=q, k=k, q_weight=q_weight, k_weight=k_weight)
     D = q.shape[-1]
     if q.dim() < 3 or q.dim() != k.dim() or q.shape[:-2] != k.shape[:-2] or k.shape[-1] != D or q_weight.shape != (D,) or k_weight.shape != (D,):
@@ -275,7 +308,7 @@ class EmbeddingFunction(torch.autograd.Function):
         return _embedding_forward(ids, _dense(table), scale)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, dy):
         ids, = ctx.saved_tensors
         rows, width = ctx.shape
@@ -298,6 +331,10 @@ def embedding(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0) -> tor
     """``scale * table[ids]``: ids int32 or int64 of any shape, table ``[rows, width]``, width a multiple of 8.  An id
     outside the table (a padding token's, say) gives zeros and no gradient.  The table's gradient is dense, added up in fp32 by
     sorted tokens, the same from run to run."""
+    if _natively():
+        y = _native.embedding(ids, table, scale)
+        if y is not None:
+            return y
     _checked("embedding", table, table=table)
     _integers("embedding", "ids", ids, table.device)
     if table.dim() != 2 or table.shape[0] == 0 or table.shape[1] == 0:
@@ -341,6 +378,10 @@ def dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, residual: tor
 
     What is dropped is a function of (seed, offset) and a value's place in x alone: the gradient draws it again.  Calls that are to
     differ take other offsets (or seeds), 64-bit unsigned numbers both; a graph that replays a call replays its numbers."""
+    if _natively():
+        y = _native.dropout(x, p, seed, offset, residual)
+        if y is not None:
+            return y
     _checked("dropout", x, x=x, residual=residual)
     if not 0.0 <= p <= 1.0:
         raise ValueError(f"dropout: a rate of {p} is not between 0 and 1")

@@ -55,11 +55,11 @@ def build_torch(verbose: bool = True) -> str:
            "-DUSE_ROCM=1", "-D__HIP_PLATFORM_AMD__=1", f'-DSK_TORCH_VERSION="{torch.__version__}"', f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
            "-isystem", include, "-isystem", os.path.join(include, "torch", "csrc", "api", "include"),
            "-isystem", "/opt/rocm/include", "-isystem", sysconfig.get_paths()["include"],
-           os.path.join(CSRC, "sk_torch.cpp"), OUT, "-L" + os.path.join(root, "lib"),
+           os.path.join(CSRC, "sk_torch.cpp"), os.path.join(CSRC, "sk_torch_block.cpp"), OUT, "-L" + os.path.join(root, "lib"),
            "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch", "-ltorch_python", "-Wl,-rpath,$ORIGIN", "-o", OUT_TORCH]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
-        raise RuntimeError("g++ failed on sk_torch.cpp:\n" + r.stderr)
+        raise RuntimeError("g++ failed on sk_torch*.cpp:\n" + r.stderr)
     if r.stderr.strip():
         sys.stderr.write(r.stderr)
     if verbose:

@@ -7,93 +7,12 @@
 // from Python and a backward pass none.  `linear` and `linear_two_sided` return None for whatever they
 // do not take -- subclasses of Tensor, functorch transforms, dispatch and function modes, tracing,
 // forward-mode gradients, arguments that are to be refused -- and the Python functions go on from there.
-#include <Python.h>
-
-#include <dlfcn.h>
-#include <stdlib.h>
-
-#include <list>
-#include <mutex>
-#include <string>
-
-#include <ATen/ATen.h>
-#include <ATen/PythonTorchFunctionTLS.h>
-#include <c10/core/DeviceGuard.h>
-#include <c10/core/impl/LocalDispatchKeySet.h>
-#include <c10/core/impl/TorchDispatchModeTLS.h>
-#include <torch/csrc/Exceptions.h>
-#include <torch/csrc/autograd/custom_function.h>
-#include <torch/csrc/autograd/python_variable.h>
-#include <torch/csrc/utils/pybind.h>
-
-#define __HIP_PLATFORM_AMD__ 1
-#include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
-
-#include "../../include/sk.h"
+#include "sk_torch.h"
+#include "sk_torch_block.h"
 
 namespace {
 
-using at::Tensor;
-using torch::autograd::AutogradContext;
-using torch::autograd::variable_list;
-
-// One scratch buffer per (device, stream), grown to the largest request; the least recently used of more
-// than MAX_STREAMS goes back to the allocator, which keeps it until the work queued on it is done.
-// Calls queue their kernels under the lock: two threads that share a stream share its buffer.
-struct Workspaces {
-  static constexpr size_t MAX_STREAMS = 8;
-  // Most that a pass keeps here beside its workspace: an allocation a pass is 1 us of host, 1 to 2 % of a small two-sided layer's step, and the sums
-  // of a large one (4096 -> 11008, 2048 columns: 107 MB) would stay on every stream.
-  static constexpr size_t MAX_SUMS = 4 << 20;
-  struct Entry {
-    c10::DeviceIndex device;
-    void* stream;
-    Tensor buffer;
-  };
-  std::mutex mutex;
-  std::list<Entry> entries;   // most recently used first
-
-  const Tensor& get(const at::Device& device, void* stream, size_t bytes) {   // (with the lock held)
-    auto it = entries.begin();
-    while (it != entries.end() && !(it->device == device.index() && it->stream == stream)) ++it;
-    if (it == entries.end()) entries.push_front(Entry{device.index(), stream, Tensor()});
-    else if (it != entries.begin()) entries.splice(entries.begin(), entries, it);
-    Entry& e = entries.front();
-    if (!e.buffer.defined() || (size_t)e.buffer.numel() < bytes)
-      e.buffer = at::empty({(int64_t)(bytes < 256 ? 256 : bytes)}, at::TensorOptions().dtype(at::kByte).device(device));
-    if (entries.size() > MAX_STREAMS) entries.pop_back();
-    return e.buffer;
-  }
-};
-// (never destroyed: the allocator may be gone before this library's own destructors run)
-Workspaces& workspaces() {
-  static Workspaces* w = new Workspaces;
-  return *w;
-}
-
-sk_dtype dtype_of(const Tensor& t) { return t.scalar_type() == at::kFloat ? SK_F32 : SK_BF16; }
-
-void* stream_of(const at::Device& device) {
-  return static_cast<hipStream_t>(c10::hip::getCurrentHIPStreamMasqueradingAsCUDA(device.index()).stream());
-}
-
-PyObject* g_error = nullptr;   // libsk.SkError, which nn.py hands over
-
-// As libsk.check: raises SkError with its status.  (Not under the workspaces' lock: it takes the GIL and runs Python.)
-void check(sk_status s) {
-  if (s == SK_OK) return;
-  pybind11::gil_scoped_acquire gil;
-  PyObject* const e = g_error != nullptr ? PyObject_CallFunction(g_error, "i", (int)s) : nullptr;
-  if (e != nullptr) {
-    PyErr_SetObject(g_error, e);
-    Py_DECREF(e);
-  } else if (!PyErr_Occurred()) {
-    PyErr_SetString(PyExc_RuntimeError, sk_status_string(s));
-  }
-  python_error error;
-  error.persist();   // (a backward pass is on another thread than its caller)
-  throw error;
-}
+using namespace sk_torch;
 
 Tensor rows(const Tensor& x, int64_t width) {
   if (x.dim() == 2 && x.is_contiguous()) return x;
@@ -284,25 +203,6 @@ struct LinearTwoSided : torch::autograd::Function<LinearTwoSided> {
   }
 };
 
-PyTypeObject* g_parameter = nullptr;   // torch.nn.Parameter
-
-// A plain tensor or parameter on `device` (any, if null) with the given type and dense rows
-const Tensor* plain(PyObject* o) {
-  PyTypeObject* const type = Py_TYPE(o);
-  if (type != reinterpret_cast<PyTypeObject*>(THPVariableClass) && type != g_parameter) return nullptr;
-  const Tensor& t = THPVariable_Unpack(o);
-  return t.defined() && t.is_cuda() && t.layout() == at::kStrided && !t.is_conj() && !t.is_neg() ? &t : nullptr;
-}
-
-// Nothing is watching that the native functions would pass by.
-bool unwatched() {
-  using at::DispatchKey;
-  for (DispatchKey k : {DispatchKey::FuncTorchDynamicLayerFrontMode, DispatchKey::FuncTorchDynamicLayerBackMode, DispatchKey::Tracer, DispatchKey::Functionalize})
-    if (c10::impl::tls_is_dispatch_key_included(k)) return false;
-  return !c10::impl::TorchDispatchModeTLS::any_modes_set() && !at::impl::torch_function_mode_enabled();
-}
-bool no_tangent(const Tensor& t) { return !t._fw_grad(0).defined(); }
-
 // Tensors of one layer: of x's type and device, without forward-mode gradients
 bool same(const Tensor& x, const Tensor& t) { return t.scalar_type() == x.scalar_type() && t.device() == x.device() && no_tangent(t); }
 bool takes(const Tensor& x, int64_t in, int64_t out, int64_t l, int64_t k) {
@@ -310,7 +210,6 @@ bool takes(const Tensor& x, int64_t in, int64_t out, int64_t l, int64_t k) {
   if (l < 1 || k < 1 || l > INT32_MAX / 2 || k > INT32_MAX) return false;
   return sk_linear_workspace_bytes(SK_OP_FWD, x.numel() / in, in, out, (int32_t)l, (int32_t)k, dtype_of(x)) != (size_t)-1;
 }
-bool aligned(const Tensor& t) { return (reinterpret_cast<uintptr_t>(t.data_ptr()) & 15) == 0; }
 
 PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {   // x, S, U, bias or None, l, k
   HANDLE_TH_ERRORS
@@ -385,6 +284,10 @@ PyObject* raise_as(PyObject*, PyObject* type) {
 PyMethodDef methods[] = {
     {"linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(linear)), METH_FASTCALL, "y, or None for a call it does not take"},
     {"linear_two_sided", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(linear_two_sided)), METH_FASTCALL, "y, or None for a call it does not take"},
+    {"attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(sk_torch::attention)), METH_FASTCALL, "o, or None for a call it does not take"},
+    {"head_norm_rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(sk_torch::head_norm_rope)), METH_FASTCALL, "(q, k), or None for a call it does not take"},
+    {"embedding", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(sk_torch::embedding)), METH_FASTCALL, "y, or None for a call it does not take"},
+    {"dropout", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(sk_torch::dropout)), METH_FASTCALL, "y, or None for a call it does not take"},
     {"raise_as", raise_as, METH_O, "the exception type of a refused call, made from its status"},
     {"release_workspaces", release_workspaces, METH_NOARGS, "gives the scratch buffers back to the allocator"},
     {nullptr, nullptr, 0, nullptr}};

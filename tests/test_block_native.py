@@ -1,0 +1,165 @@
+"""The block operators' native functions against the Python ones: the same bits, the same refusals, what they leave to Python, and
+what happens to gradients of gradients."""
+import threading
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def block():
+    from paper_2601_15473_amd import block
+    assert block._native is not None
+    return block
+
+
+def _normal(seed, shape, dtype=torch.bfloat16):
+    g = torch.Generator(device="cpu").manual_seed(seed)
+    return torch.randn(shape, generator=g).to(dtype).cuda()
+
+
+def _calls(block, dtype):
+    """name -> (inputs with gradients, call)"""
+    fused = _normal(0, (2, 37, 8, 64), dtype)
+    lengths = torch.tensor([37, 20], dtype=torch.int32, device="cuda")
+    flat = fused.view(-1, 8, 64)
+    w = _normal(1, (64,), dtype), _normal(2, (64,), dtype)
+    cos, sin = torch.rand(80, 32, device="cuda"), torch.rand(80, 32, device="cuda")
+    pos = torch.arange(74, device="cuda")
+    ids = torch.randint(0, 50, (3, 25), generator=torch.Generator().manual_seed(3)).cuda()
+    x = _normal(4, (9, 33), dtype)
+    return {
+        "attention": ([fused[:, :, :4], fused[:, :, 4:6], fused[:, :, 6:]], lambda q, k, v: block.attention(q, k, v, causal=True)),
+        "attention of lengths": ([fused[:, :, :4], fused[:, :, 4:6], fused[:, :, 6:]], lambda q, k, v: block.attention(q, k, v, lengths, lengths, scale=0.2)),
+        "head_norm_rope": ([flat[:, :4], flat[:, 4:6], *w], lambda q, k, a, b: block.head_norm_rope(q, k, a, b, cos, sin, pos, interleaved=True)),
+        "embedding": ([_normal(5, (50, 72), dtype)], lambda t: block.embedding(ids, t, 1.5)),
+        "dropout": ([x], lambda t: block.dropout(t, 0.3, 1 << 63, 5)),
+        "dropout and residual": ([x, x + 1], lambda t, r: block.dropout(t, 0.3, 7, residual=r)),
+    }
+
+
+NAMES = ["attention", "attention of lengths", "head_norm_rope", "embedding", "dropout", "dropout and residual"]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("name", NAMES)
+def test_same_as_the_python_functions(block, monkeypatch, name, dtype):
+    inputs, call = _calls(block, dtype)[name]
+
+    def both():
+        with torch.no_grad():
+            alone = call(*inputs)
+        leaves = [t.detach().requires_grad_() for t in inputs]
+        out = call(*leaves)
+        outs, alone = (out, alone) if isinstance(out, tuple) else ((out,), (alone,))
+        grads = torch.autograd.grad(outs, leaves, [torch.sin(torch.arange(o.numel(), device="cuda")).view(o.shape).to(o.dtype) for o in outs])
+        return [*outs, *alone, *grads], [type(o.grad_fn).__name__ for o in outs]
+
+    got, nodes = both()
+    monkeypatch.setattr(block, "_native", None)
+    want, python_nodes = both()
+    assert nodes != python_nodes                       # (the native function did take the call)
+    for a, b in zip(got, want):
+        assert a.dtype == b.dtype and a.shape == b.shape and a.stride() == b.stride() and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("native", [True, False], ids=["native", "python"])
+@pytest.mark.parametrize("name", NAMES[:4])
+def test_gradients_of_gradients_are_refused(block, monkeypatch, name, native):
+    if not native:
+        monkeypatch.setattr(block, "_native", None)
+    inputs, call = _calls(block, torch.float32)[name]
+    leaves = [t.detach().requires_grad_() for t in inputs]
+    out = call(*leaves)
+    out = out if isinstance(out, tuple) else (out,)
+    grads = torch.autograd.grad(sum(o.sum() for o in out), leaves, create_graph=True)
+    assert torch.isfinite(grads[0]).all()
+    with pytest.raises(RuntimeError, match="twice"):
+        grads[0].square().sum().backward()
+
+
+@pytest.mark.parametrize("native", [True, False], ids=["native", "python"])
+def test_a_result_nobody_uses(block, monkeypatch, native):
+    if not native:
+        monkeypatch.setattr(block, "_native", None)
+    inputs, call = _calls(block, torch.float32)["head_norm_rope"]
+    leaves = [t.detach().requires_grad_() for t in inputs]
+    q, _ = call(*leaves)
+    dq, dk, dwq, dwk = torch.autograd.grad(q.sum(), leaves)
+    assert dq.any() and dwq.any() and not dk.any() and not dwk.any()
+    only = [leaves[0].detach(), leaves[1].detach(), leaves[2], leaves[3].detach()]     # the gradient of one weight alone
+    assert torch.equal(torch.autograd.grad(call(*only)[0].sum(), only[2])[0], dwq)
+
+
+def test_calls_left_to_python(block):
+    """Copies to make, other types of integers, subclasses, dispatch modes: the same results."""
+    from torch.utils._python_dispatch import TorchDispatchMode
+    q, k, v = (_normal(i, (1, 16, 2, 64)) for i in range(3))
+    want = block.attention(q, k, v)
+    n = block._native
+    assert torch.equal(n.attention(q, k, v, None, None, False, None), want)
+    odd = torch.cat([q, q[..., :4]], -1)[..., :64]
+    assert n.attention(odd, k, v, None, None, False, None) is None and torch.equal(block.attention(odd, k, v), want)
+    long = torch.tensor([16], device="cuda")
+    assert n.attention(q, k, v, None, long, False, None) is None and torch.equal(block.attention(q, k, v, k_lengths=long), want)
+    assert n.attention(q[..., :60], k[..., :60], v[..., :60], None, None, False, None) is None
+    assert n.dropout(q, 2.0, 1, 0, None) is None and n.dropout(q, 0.5, -1, 0, None) is None and n.dropout(q, 0.5, 1 << 64, 0, None) is None
+    assert n.embedding(torch.zeros(2, dtype=torch.long), q[0, 0], 1.0) is None
+
+    class Mode(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            return func(*args, **(kwargs or {}))
+
+    with Mode():
+        assert n.attention(q, k, v, None, None, False, None) is None
+        assert torch.equal(block.attention(q, k, v), want)
+    assert n.attention(torch.nn.Parameter(q), k, v, None, None, False, None) is not None
+
+
+def test_parameters_hooks_and_accumulation(block):
+    table = torch.nn.Parameter(_normal(0, (20, 16), torch.float32))
+    ids = torch.tensor([3, 3, 19], device="cuda")
+    for _ in range(2):
+        block.embedding(ids, table).sum().backward()
+    assert (table.grad[3] == 4).all() and (table.grad[19] == 2).all() and table.grad.sum() == 6 * 16
+
+
+def test_inputs_changed_in_place_are_noticed(block):
+    q, k, v = (_normal(i, (1, 16, 2, 64)).requires_grad_() for i in range(3))
+    k2 = k * 1
+    o = block.attention(q, k2, v)
+    with torch.no_grad():
+        k2.zero_()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        o.sum().backward()
+
+
+def test_threads_and_streams(block):
+    """Threads on streams of their own, and on one they share."""
+    inputs, call = _calls(block, torch.bfloat16)["attention"]
+    big = [_normal(i, (2, 300, 4, 128)) for i in range(3)]
+
+    def work(stream, out, i):
+        with torch.cuda.stream(stream):
+            for _ in range(10):
+                leaves = [t.detach().requires_grad_() for t in (inputs if i % 2 else big)]
+                o = call(*leaves)
+                got = torch.autograd.grad(o, leaves, o.detach())
+            out[i] = [o.detach(), *got]
+        stream.synchronize()
+
+    want = {}
+    for i in (0, 1):
+        work(torch.cuda.current_stream(), want, i)
+    for streams in ([torch.cuda.Stream() for _ in range(4)], [torch.cuda.Stream()] * 4):
+        got = {}
+        torch.cuda.synchronize()
+        threads = [threading.Thread(target=work, args=(streams[i], got, i)) for i in range(4)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        for i in range(4):
+            assert all(torch.equal(a, b) for a, b in zip(got[i], want[i % 2])), i

@@ -56,6 +56,7 @@ SHAPES = [  # batch, q_len, k_len, heads, kv_heads, head_dim
     (1, 1, 1, 1, 1, 8), (2, 1, 7, 4, 2, 64), (1, 5, 3, 2, 1, 16), (2, 33, 33, 3, 1, 72), (1, 129, 257, 2, 2, 128),
     (3, 64, 64, 4, 4, 64), (1, 31, 300, 7, 1, 96), (1, 260, 131, 6, 2, 32), (2, 128, 128, 2, 1, 120), (1, 1, 1030, 16, 2, 128),
     (2, 3, 515, 8, 2, 80), (1, 515, 640, 2, 2, 64), (1, 300, 300, 5, 1, 40),
+    (1, 70, 1500, 4, 2, 128), (2, 9, 2100, 12, 1, 64),   # ranges of the keys, over one tile of rows
 ]
 
 
