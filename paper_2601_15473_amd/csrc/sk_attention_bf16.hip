@@ -8,6 +8,7 @@ namespace {
 // Few rows: how the keys are cut, and where the ranges' results are.
 struct FewPlan {
   int row_tiles, splits, chunk;   // tiles of 32 rows; ranges of `chunk` keys
+  int xcds;                       // that sequences' ranges are dealt over
   float *sums, *stats;            // [heads][splits][rows][D], [heads][splits][rows][2]
 };
 
@@ -95,12 +96,12 @@ __device__ __forceinline__ void store_row(bf16* row, bool there, const f32x16 (&
 
 // Running softmax of a lane's row (the lane 32 further has the row's other keys): the maximum and its own keys' sum.
 struct Softmax {
-  float top = -INFINITY, sum = 0.f;
-  // s: a block's scores before the factor, on return its weights; o: what the weights so far have summed up.  What is summed is
-  // brought down only when a row's maximum has risen by more than 2^8 since it last was: until then the weights are up to
-  // 2^8 instead of 1, which neither an fp32 sum nor a bf16's relative rounding minds.
+  float top = -INFINITY, sum = 0.f, base = 0.f;
+  // Takes in a block's scores (before the factor).  What is summed so far, o, is brought down only when a row's maximum has
+  // risen by more than 2^8 since it last was: until then the weights are up to 2^8 instead of 1, which neither an fp32 sum nor a
+  // bf16's relative rounding minds.
   template <int NB, int ND>
-  __device__ __forceinline__ void update(f32x16 (&s)[NB], f32x16 (&o)[ND], float factor) {
+  __device__ __forceinline__ void raise(const f32x16 (&s)[NB], f32x16 (&o)[ND], float factor) {
     float m = s[0][0];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -116,16 +117,34 @@ struct Softmax {
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] *= keep;
     }
-    const float base = top == -INFINITY ? 0.f : top;   // (nothing seen yet: weights of exp2(-inf))
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[b][r] = __builtin_amdgcn_exp2f(s[b][r] * factor - base);
-        sum += s[b][r];
-      }
+    base = top == -INFINITY ? 0.f : top;   // (nothing seen yet: weights of exp2(-inf))
+  }
+  // A score's weight
+  __device__ __forceinline__ float weigh(float s, float factor) {
+    const float w = __builtin_amdgcn_exp2f(s * factor - base);
+    sum += w;
+    return w;
   }
 };
+
+// N products whose first operands are read AHEAD of them: read(i) gives operand i, mma(i, operand) multiplies it, beside(i) is what
+// else goes under product i.  In that order: left to itself the compiler reads an operand right before it is used, and waits.
+template <int N, int AHEAD, typename Read, typename Multiply, typename Beside>
+__device__ __forceinline__ void pipelined(bf16x8 (&f)[AHEAD], Read&& read, Multiply&& mma, Beside&& beside) {
+  __builtin_amdgcn_sched_barrier(0);
+  static_for<0, N>([&](auto ic) {
+    constexpr int i = decltype(ic)::value;
+    mma(ic, f[i % AHEAD]);
+    if constexpr (i + AHEAD < N) f[i % AHEAD] = read(IntC<i + AHEAD>{});
+    beside(ic);
+    __builtin_amdgcn_sched_barrier(0);
+  });
+}
+template <int AHEAD, typename Read>
+__device__ __forceinline__ void read_first(bf16x8 (&f)[AHEAD], Read&& read) {
+  static_for<0, AHEAD>([&](auto ic) { f[decltype(ic)::value] = read(ic); });
+  __builtin_amdgcn_sched_barrier(0);
+}
 
 // Forward: WAVES x 32 rows a work-group, tiles of 64 keys and values through a ring of two slots in LDS, asked for a tile
 // ahead; one barrier a tile.
@@ -133,7 +152,7 @@ template <int DP, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const AttentionArgs p) {
   typedef Tile<DP> L;
   typedef Mma<bf16> M;
-  constexpr int KS = DP / 16, ND = DP / 32, SLOT = 2 * L::BYTES;
+  constexpr int KS = DP / 16, ND = DP / 32, SLOT = 2 * L::BYTES, K_AHEAD = 6, V_AHEAD = 4;
   __shared__ __align__(1024) unsigned char smem[2 * SLOT];
   asm volatile("" ::"v"((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem) : "memory");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -164,34 +183,53 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const Atte
   const bf16* const vb = static_cast<const bf16*>(p.v) + b * p.vs[0] + hk * p.vs[2];
   const typename L::template Loader<WAVES> load_k(wave, lane, p.ks[1], p.D), load_v(wave, lane, p.vs[1], p.D);
   const unsigned k_at = L::along_address(lane), v_at = L::across_address(lane);
-  auto load = [&](int j0, unsigned slot) {
-    load_k.load(rows_from(kb, p.ks[1], j0, q.m, p.D), slot, wave);
-    load_v.load(rows_from(vb, p.vs[1], j0, q.m, p.D), slot + L::BYTES, wave);
+  Walk<TILE_ROWS> walk_k(kb, p.ks[1], 0, p.D), walk_v(vb, p.vs[1], 0, p.D);
+  int left = q.m;
+  auto load = [&](unsigned slot) {
+    load_k.load(walk_k.window(left), slot, wave);
+    load_v.load(walk_v.window(left), slot + L::BYTES, wave);
+    left -= TILE_ROWS;
+    walk_k.skip(TILE_ROWS);
+    walk_v.skip(TILE_ROWS);
   };
-  if (keys > 0) load(0, 0u);
+  if (keys > 0) load(0u);
+
   unsigned slot = 0;
   for (int j0 = 0; j0 < keys; j0 += TILE_ROWS, slot ^= SLOT) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // this tile is there, and nobody reads the other slot
-    if (j0 + TILE_ROWS < keys) load(j0 + TILE_ROWS, slot ^ SLOT);
+    if (j0 + TILE_ROWS < keys) load(slot ^ SLOT);
     if (j0 >= most) continue;
     f32x16 s[2] = {zeros(), zeros()};
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-      for (int t = 0; t < 2; ++t) s[t] = M::mma(L::along(slot + k_at, t, ks), qf[ks], s[t]);
+    {
+      bf16x8 f[K_AHEAD];
+      auto read = [&](auto ic) { return L::along(slot + k_at, decltype(ic)::value & 1, decltype(ic)::value >> 1); };
+      read_first(f, read);
+      pipelined<2 * KS>(f, read, [&](auto ic, bf16x8 a) { constexpr int i = decltype(ic)::value; s[i & 1] = M::mma(a, qf[i >> 1], s[i & 1]); }, [](auto) {});
+    }
+    // values 16 step .. + 15 (step i / ND), features 32 (i % ND) .. + 31; the first on their way under the softmax
+    bf16x8 f[V_AHEAD];
+    auto read = [&](auto ic) { return L::across(slot + L::BYTES + v_at, decltype(ic)::value % ND, decltype(ic)::value / ND); };
+    read_first(f, read);
     if (j0 + TILE_ROWS > common)
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (j0 + t * 32 + acc_row(r, lane) >= limit) s[t][r] = -INFINITY;
-    sm.update(s, o, factor);
+    sm.raise(s, o, factor);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const bf16x8 w = M::of_acc(s[t >> 1], t & 1);
+    for (int r = 0; r < 16; ++r) s[0][r] = sm.weigh(s[0][r], factor);
+    bf16x8 w[4] = {M::of_acc(s[0], 0), M::of_acc(s[0], 1)};
+    pipelined<4 * ND>(f, read, [&](auto ic, bf16x8 a) { constexpr int i = decltype(ic)::value; o[i % ND] = M::mma(a, w[i / ND], o[i % ND]); },
+                      [&](auto ic) {   // the second block's weights under the first one's products
+                        constexpr int i = decltype(ic)::value, EACH = 16 / (2 * ND);
+                        if constexpr (i < 2 * ND) {
 #pragma unroll
-      for (int d = 0; d < ND; ++d) o[d] = M::mma(L::across(slot + L::BYTES + v_at, d, t), w, o[d]);
-    }
+                          for (int r = i * EACH; r < (i + 1) * EACH; ++r) s[1][r] = sm.weigh(s[1][r], factor);
+                          if constexpr (i == ND - 1) w[2] = M::of_acc(s[1], 0);
+                          if constexpr (i == 2 * ND - 1) w[3] = M::of_acc(s[1], 1);
+                        }
+                      });
   }
   const float sum = sm.sum + other_half(sm.sum);
   store_row<DP>(static_cast<bf16*>(p.o) + (((int64_t)b * p.q_len + row.i) * p.heads + row.h) * p.D, row.there, o, sum == 0.f ? 0.f : 1.f / sum, p.D, lane);
@@ -211,9 +249,12 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(const AttentionAr
   __shared__ __align__(1024) unsigned char smem[4 * ROOM + 4 * 32 * 8];
   asm volatile("" ::"v"((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem) : "memory");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int heads = p.batch * p.kv_heads;
-  const int id = blockIdx.x / heads, bh = blockIdx.x - id * heads, split = id / plan.row_tiles, tile = id - split * plan.row_tiles;
-  const int b = bh / p.kv_heads, hk = bh - b * p.kv_heads;
+  // A range's heads, whose keys lie in the same stretch of memory, go to one XCD, the sequences' ranges to the XCDs in turn (another turn each
+  // range, so that no XCD has one sequence): 68 us where heads dealt over the XCDs took 71, as above.
+  const int local = blockIdx.x / plan.xcds, turn = local / p.kv_heads, hk = local - turn * p.kv_heads, unit = turn * plan.xcds + blockIdx.x - local * plan.xcds;
+  const int id = unit / p.batch;
+  if (id >= plan.row_tiles * plan.splits) return;
+  const int b = (unit + id) % p.batch, bh = b * p.kv_heads + hk, split = id / plan.row_tiles, tile = id - split * plan.row_tiles;
   const Sequence q(p, b);
   const int r0 = tile * 32, rows = p.q_len * p.group - r0 < 32 ? p.q_len * p.group - r0 : 32;
   const Row row(p, r0 + (lane & 31), hk);
@@ -228,9 +269,10 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(const AttentionAr
   const typename L::template Loader<1> load_k(0, lane, p.ks[1], p.D), load_v(0, lane, p.vs[1], p.D);
   const unsigned room = wave * ROOM, k_at = room + L::along_address(lane), v_at = room + L::BYTES + L::across_address(lane);
   int j0 = begin + wave * 32;
+  Walk<32> walk_k(kb, p.ks[1], j0, p.D), walk_v(vb, p.vs[1], j0, p.D);
   if (j0 < end) {
-    load_k.load(rows_from(kb, p.ks[1], j0, q.m, p.D), room, 0);
-    load_v.load(rows_from(vb, p.vs[1], j0, q.m, p.D), room + L::BYTES, 0);
+    load_k.load(walk_k.window(q.m - j0), room, 0);
+    load_v.load(walk_v.window(q.m - j0), room + L::BYTES, 0);
   }
   bf16x8 qf[KS];
   load_row<DP>(qf, p.q, b * p.qs[0] + row.i * p.qs[1] + row.h * p.qs[2], row.there && row.i < q.n, p.D, lane);
@@ -247,13 +289,17 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(const AttentionAr
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) s[0] = M::mma(L::along(k_at, 0, ks), qf[ks], s[0]);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");            // K has been read
-    const int next = j0 + 128 < end ? j0 + 128 : q.m;             // (past the last: nothing is fetched)
-    load_k.load(rows_from(kb, p.ks[1], next, j0 + 128 < end ? q.m : 0, p.D), room, 0);
+    const int left = j0 + 128 < end ? q.m - j0 - 128 : 0;         // (past the last: nothing is fetched)
+    walk_k.skip(128);
+    walk_v.skip(128);
+    load_k.load(walk_k.window(left), room, 0);
     if (j0 + 32 > common)
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         if (j0 + acc_row(r, lane) >= limit) s[0][r] = -INFINITY;
-    sm.update(s, o, factor);
+    sm.raise(s, o, factor);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[0][r] = sm.weigh(s[0][r], factor);
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(EACH) : "memory");   // V is there
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -262,7 +308,7 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(const AttentionAr
       for (int d = 0; d < ND; ++d) o[d] = M::mma(L::across(v_at, d, t), w, o[d]);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    load_v.load(rows_from(vb, p.vs[1], next, j0 + 128 < end ? q.m : 0, p.D), room + L::BYTES, 0);
+    load_v.load(walk_v.window(left), room + L::BYTES, 0);
   }
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");     // (no load may land on what follows)
   const float sum = sm.sum + other_half(sm.sum);
@@ -313,7 +359,8 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(const AttentionAr
   }
 }
 
-// A wave to a row: the ranges' sums in order, each brought to the largest maximum.
+// A wave to a row: the ranges' sums in order, each brought to the largest maximum.  64 ranges at a time: a lane to a range's maximum and
+// sum, then a lane to two features with eight ranges on their way.
 __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs p, FewPlan plan) {
   const int lane = threadIdx.x & 63, rows = p.q_len * p.group, bh = blockIdx.y;
   const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -323,23 +370,35 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs
   const int r0 = r / 32 * 32, last = r0 + 31 < rows ? r0 + 31 : rows - 1;
   const int keys = q.seen(r0 / p.group, last / p.group);
   const int splits = keys > 0 ? (keys + plan.chunk - 1) / plan.chunk : 1;
-  const float* const stats = plan.stats + ((int64_t)bh * plan.splits * rows + r) * 2;
-  float top = -INFINITY;
-  for (int s = lane; s < splits; s += 64) top = fmaxf(top, stats[(int64_t)s * rows * 2]);
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
-  const float base = top == -INFINITY ? 0.f : top;
   const int c = lane * 2;
-  float total = 0.f, x = 0.f, y = 0.f;
-  const float* const sums = plan.sums + ((int64_t)bh * plan.splits * rows + r) * p.D + c;
-#pragma unroll 4
-  for (int s = 0; s < splits; ++s) {
-    const float keep = __builtin_amdgcn_exp2f(stats[(int64_t)s * rows * 2] - base);
-    total += stats[(int64_t)s * rows * 2 + 1] * keep;
-    if (c < p.D) {
-      const float2 v = *reinterpret_cast<const float2*>(sums + (int64_t)s * rows * p.D);
-      x += v.x * keep;
-      y += v.y * keep;
+  float top = -INFINITY, total = 0.f, x = 0.f, y = 0.f;
+  for (int s0 = 0; s0 < splits; s0 += 64) {
+    const int n = splits - s0 < 64 ? splits - s0 : 64;
+    const int64_t slot = ((int64_t)bh * plan.splits + s0) * rows + r;
+    const float2 stat = lane < n ? *reinterpret_cast<const float2*>(plan.stats + (slot + (int64_t)lane * rows) * 2) : make_float2(-INFINITY, 0.f);
+    float m = fmaxf(top, stat.x);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+    const float base = m == -INFINITY ? 0.f : m, before = __builtin_amdgcn_exp2f(top - base);
+    const float keep = __builtin_amdgcn_exp2f(stat.x - base);
+    float sum = stat.y * keep;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+    total = total * before + sum;
+    x *= before;
+    y *= before;
+    top = m;
+    const float* const sums = plan.sums + slot * p.D + (c < p.D ? c : 0);
+    for (int s = 0; s < n; s += 8) {
+      float2 v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const float2*>(sums + (int64_t)(s + u < n ? s + u : s) * rows * p.D);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float k = s + u < n ? __shfl(keep, s + u) : 0.f;
+        x += v[u].x * k;
+        y += v[u].y * k;
+      }
     }
   }
   const Row out(p, r, hk);
@@ -375,11 +434,16 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
   const bf16* const vb = static_cast<const bf16*>(p.v) + b * p.vs[0] + hk * p.vs[2];
   const typename L::template Loader<WAVES> load_k(wave, lane, p.ks[1], p.D), load_v(wave, lane, p.vs[1], p.D);
   const unsigned k_at = L::along_address(lane), kt_at = L::across_address(lane);
-  auto load = [&](int j0, unsigned slot) {
-    load_k.load(rows_from(kb, p.ks[1], j0, q.m, p.D), slot, wave);
-    load_v.load(rows_from(vb, p.vs[1], j0, q.m, p.D), slot + L::BYTES, wave);
+  Walk<TILE_ROWS> walk_k(kb, p.ks[1], 0, p.D), walk_v(vb, p.vs[1], 0, p.D);
+  int left = q.m;
+  auto load = [&](unsigned slot) {
+    load_k.load(walk_k.window(left), slot, wave);
+    load_v.load(walk_v.window(left), slot + L::BYTES, wave);
+    left -= TILE_ROWS;
+    walk_k.skip(TILE_ROWS);
+    walk_v.skip(TILE_ROWS);
   };
-  if (keys > 0) load(0, 0u);
+  if (keys > 0) load(0u);
 
   bf16x8 qf[KS], gf[KS];
   const int64_t at = (((int64_t)b * p.q_len + row.i) * p.heads + row.h) * p.D;
@@ -411,7 +475,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
   unsigned slot = 0;
   for (int j0 = 0; j0 < keys; j0 += TILE_ROWS, slot ^= SLOT) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (j0 + TILE_ROWS < keys) load(j0 + TILE_ROWS, slot ^ SLOT);
+    if (j0 + TILE_ROWS < keys) load(slot ^ SLOT);
     if (j0 >= most) continue;
     f32x16 s[2], g[2];
 #pragma unroll
@@ -472,19 +536,35 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dkv_kernel(const Atte
   const int per_head = j0 < q.m && q.n > i_begin ? (q.n - i_begin + TILE_ROWS - 1) / TILE_ROWS : 0, steps = per_head * p.group;
 
   // (sums, keys and values take 192 registers of 256, scores 32: a lane's offsets are computed where they are used)
-  auto load = [&](int h, int i0, unsigned slot) {
-    const int head = hk * p.group + h, lane = lane_again();
+  Walk<TILE_ROWS> walk_q(static_cast<const bf16*>(p.q) + b * p.qs[0] + hk * p.group * p.qs[2], p.qs[1], i_begin, p.D);
+  Walk<TILE_ROWS> walk_g(static_cast<const bf16*>(p.d_o) + ((int64_t)b * p.q_len * p.heads + hk * p.group) * p.D, (int64_t)p.heads * p.D, i_begin, p.D);
+  const float* stat = (wave == 0 ? p.lse2 : p.delta) + ((int64_t)b * p.heads + hk * p.group) * p.q_len + i_begin;
+  const int per_tile = per_head * TILE_ROWS;
+  int left = q.n - i_begin;
+  auto load = [&](unsigned slot) {
+    const int lane = lane_again();
     const typename L::template Loader<WAVES> load_q(wave, lane, p.qs[1], p.D), load_g(wave, lane, (int64_t)p.heads * p.D, p.D);
-    load_q.load(rows_from(static_cast<const bf16*>(p.q) + b * p.qs[0] + head * p.qs[2], p.qs[1], i0, q.n, p.D), slot, wave);
-    load_g.load(rows_from(static_cast<const bf16*>(p.d_o) + ((int64_t)b * p.q_len * p.heads + head) * p.D, (int64_t)p.heads * p.D, i0, q.n, p.D), slot + L::BYTES, wave);
+    load_q.load(walk_q.window(left), slot, wave);
+    load_g.load(walk_g.window(left), slot + L::BYTES, wave);
     if (wave < 2) {   // 64 rows' statistics: zeros behind the last, where q and dO are zeros too and nothing comes of them
-      const float* const stat = (wave == 0 ? p.lse2 : p.delta) + ((int64_t)b * p.heads + head) * p.q_len + i0;
       const uint64_t at = (uint64_t)stat;
-      const u32x4 left = scalar(u32x4{(unsigned)at, (unsigned)(at >> 32), (unsigned)(q.n - i0) * 4u, 0x00020000u});
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(slot + STATS + wave * 256), "v"((unsigned)lane * 4u), "s"(left), "s"(0u) : "m0");
+      const u32x4 rows = scalar(u32x4{(unsigned)at, (unsigned)(at >> 32), (unsigned)left * 4u, 0x00020000u});
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(slot + STATS + wave * 256), "v"((unsigned)lane * 4u), "s"(rows), "s"(0u) : "m0");
+    }
+    left -= TILE_ROWS;
+    if (left > 0) {
+      walk_q.skip(TILE_ROWS);
+      walk_g.skip(TILE_ROWS);
+      stat += TILE_ROWS;
+    } else {   // the group's next head from the first tile on
+      const int back = per_tile - TILE_ROWS;
+      left = q.n - i_begin;
+      walk_q.at += (uint64_t)(p.qs[2] * 2) - (uint64_t)back * walk_q.stride;
+      walk_g.at += (uint64_t)(p.D * 2) - (uint64_t)back * walk_g.stride;
+      stat += p.q_len - back;
     }
   };
-  if (steps > 0) load(0, i_begin, 0u);
+  if (steps > 0) load(0u);
 
   bf16x8 kf[KS], vf[KS];
   load_row<DP>(kf, p.k, b * p.ks[0] + j * p.ks[1] + hk * p.ks[2], there, p.D, lane);
@@ -500,13 +580,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dkv_kernel(const Atte
   for (int d = 0; d < ND; ++d) dk[d] = dv[d] = zeros();
   const float factor = score_factor(p.scale);
   unsigned slot = 0;
-  int h = 0, i0 = i_begin;
+  int i0 = i_begin;
   for (int step = 0; step < steps; ++step, slot = SLOT - slot) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     const int i_now = i0;
     i0 += TILE_ROWS;
-    if (i0 >= q.n) { i0 = i_begin; ++h; }
-    if (step + 1 < steps) load(h, i0, SLOT - slot);
+    if (i0 >= q.n) i0 = i_begin;
+    if (step + 1 < steps) load(SLOT - slot);
     if (i_now + TILE_ROWS <= i_wave) continue;
 #pragma unroll 1
     for (int t = 0; t < 2; ++t) {
@@ -585,13 +665,16 @@ template <int DP>
 hipError_t few(const AttentionArgs& a, FewPlan plan, hipStream_t s) {
   const size_t sums = few_sums(a, plan), bytes = few_bytes(a, plan);
   const int heads = a.batch * a.kv_heads, rows = a.q_len * a.group;
+  const int64_t units = (int64_t)a.batch * plan.row_tiles * plan.splits;
+  plan.xcds = units < 8 ? (int)units : 8;
   plan.sums = static_cast<float*>(a.workspace);
   plan.stats = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + sums);
   note_attention_inputs(a, 2);
   if (plan.splits == 1) note_attention_fwd(a, 2);
   else note_matrix(a.workspace, 1, bytes, bytes, 1, true);
   hipError_t e = launch_kernel(kernel_label("attention_few_kernel", {lbl(DP)}).c_str(), Work{4 * pairs(a), 0.0}, attention_few_kernel<DP>,
-                               dim3((unsigned)heads * plan.row_tiles * plan.splits), dim3(256), s, a, plan);
+                               
+                               dim3((unsigned)((units + plan.xcds - 1) / plan.xcds * plan.xcds * a.kv_heads)), dim3(256), s, a, plan);
   if (e != hipSuccess || plan.splits == 1) return e;
   note_matrix(a.workspace, 1, bytes, bytes, 1, false);
   note_attention_fwd(a, 2);

@@ -78,13 +78,26 @@ struct Tile {
   }
 };
 
-// What is left of `rows` rows (D values each, `stride` apart) from row `first` on, as a buffer that reads as zeros behind the last.
-__device__ __forceinline__ u32x4 rows_from(const bf16* base, int64_t stride, int first, int rows, int D) {
-  const int64_t left = rows > first ? (int64_t)(rows - 1 - first) * stride + D : 0;
-  const int64_t bytes = left * 2 < 0x7fffffff ? left * 2 : 0x7fffffff;
-  const uint64_t at = (uint64_t)(base + (rows > first ? first : 0) * stride);
-  return scalar(u32x4{(unsigned)at, (unsigned)(at >> 32), (unsigned)bytes, 0x00020000u});
-}
+// A walk over an array's rows (D values each, `stride` elements apart), ROWS at a time, as buffers that read as zeros behind the last: a
+// scalar's few additions a tile.
+template <int ROWS>
+struct Walk {
+  uint64_t at;                     // of the tile's first row
+  unsigned stride, row, whole;     // bytes from row to row, of a row, and of ROWS of them
+  __device__ __forceinline__ Walk(const bf16* base, int64_t stride_, int first, int D) {
+    const uint64_t a = (uint64_t)(base + first * stride_);
+    at = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(a >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)a);
+    stride = __builtin_amdgcn_readfirstlane((int)stride_ * 2);
+    row = D * 2;
+    whole = (ROWS - 1) * stride + row;
+  }
+  // The tile's rows, `left` of which there are from its first on (none where that is not positive)
+  __device__ __forceinline__ u32x4 window(int left) const {
+    const unsigned bytes = left >= ROWS ? whole : left > 0 ? (unsigned)(left - 1) * stride + row : 0u;
+    return u32x4{(unsigned)at, (unsigned)(at >> 32), (unsigned)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
+  }
+  __device__ __forceinline__ void skip(int rows) { at += (uint64_t)rows * stride; }
+};
 
 // The larger of a value and the other half-wave's.
 __device__ __forceinline__ float max_halves(float x) {
