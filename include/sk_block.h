@@ -114,7 +114,7 @@ size_t sk_norm_rope_workspace_bytes(const sk_norm_rope_shape* shape);
 /*
  * y[t] = scale * table[ids[t]]: ids int32 or int64 (id_bytes 4 or 8) [tokens], table [rows, width], y [tokens, width].
  * An id outside 0 .. rows - 1 gives a row of zeros, and no gradient.  width a multiple of 8 up to 2^20, rows < 2^31, tokens up
- * to 2^27 and tokens * width below 2^37.
+ * to 2^27 and tokens * width below 2^36.
  */
 sk_status sk_embedding_fwd(const void* ids, int32_t id_bytes, const void* table, void* y, int64_t tokens, int64_t rows,
                            int64_t width, float scale, sk_dtype dtype, void* stream);

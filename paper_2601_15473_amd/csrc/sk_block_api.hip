@@ -100,7 +100,7 @@ size_t norm_rope_bytes(const NormRopeArgs& a) {
 sk_status embedding_args(const void* ids, int32_t id_bytes, int64_t tokens, int64_t rows, int64_t width, float scale, sk_dtype dtype, EmbeddingArgs& a) {
   if (tokens < 1 || rows < 1 || width < 1 || !std::isfinite(scale)) return SK_ERR_INVALID_ARG;
   if (!known(dtype) || (id_bytes != 4 && id_bytes != 8) || width % 8 != 0 || width > (1 << 20) || rows > INT32_MAX || tokens > MOST_ROWS) return SK_ERR_UNSUPPORTED;
-  if ((double)((tokens + EMBEDDING_CHUNK - 1) / EMBEDDING_CHUNK) * ((width + 255) / 256) > MOST_GROUPS) return SK_ERR_UNSUPPORTED;
+  if ((double)((tokens + 15) / 16) * ((width + 255) / 256) > MOST_GROUPS) return SK_ERR_UNSUPPORTED;
   a = EmbeddingArgs{};
   a.ids = ids; a.ids64 = id_bytes == 8;
   a.tokens = tokens; a.rows = rows; a.width = (int)width; a.scale = scale;
@@ -108,11 +108,12 @@ sk_status embedding_args(const void* ids, int32_t id_bytes, int64_t tokens, int6
 }
 struct EmbeddingRoom {
   size_t keys, order, keys_runs, order_runs, partial, total;
-  EmbeddingRoom(int64_t tokens, int64_t width) {
+  EmbeddingRoom(int64_t tokens, int64_t width, sk_dtype dtype) {
+    const int chunk = embedding_chunk(tokens, width, esize(dtype));
     const size_t list = align_up((size_t)tokens * 4), runs = tokens > EMBEDDING_RUN ? list : 0;
     keys = 0; order = keys + list; keys_runs = order + list; order_runs = keys_runs + runs;
     partial = order_runs + runs;
-    total = partial + align_up((size_t)((tokens + EMBEDDING_CHUNK - 1) / EMBEDDING_CHUNK) * 2 * width * 4);
+    total = partial + align_up((size_t)((tokens + chunk - 1) / chunk) * 2 * width * 4);
   }
 };
 
@@ -204,7 +205,7 @@ sk_status sk_embedding_fwd(const void* ids, int32_t id_bytes, const void* table,
 size_t sk_embedding_workspace_bytes(int64_t tokens, int64_t rows, int64_t width, sk_dtype dtype) {
   EmbeddingArgs a;
   if (embedding_args(nullptr, 8, tokens, rows, width, 1.f, dtype, a) != SK_OK) return (size_t)-1;
-  return EmbeddingRoom(tokens, width).total;
+  return EmbeddingRoom(tokens, width, dtype).total;
 }
 
 sk_status sk_embedding_bwd(const void* ids, int32_t id_bytes, const void* dy, void* dtable, int64_t tokens, int64_t rows,
@@ -213,7 +214,7 @@ sk_status sk_embedding_bwd(const void* ids, int32_t id_bytes, const void* dy, vo
   EmbeddingArgs a;
   const sk_status st = embedding_args(ids, id_bytes, tokens, rows, width, scale, dtype, a);
   if (st != SK_OK) return st;
-  const EmbeddingRoom room(tokens, width);
+  const EmbeddingRoom room(tokens, width, dtype);
   if (!workspace || workspace_bytes < room.total) return SK_ERR_WORKSPACE;
   char* const w = static_cast<char*>(workspace);
   a.dy = dy; a.out = dtable;

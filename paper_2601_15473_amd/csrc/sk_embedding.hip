@@ -1,7 +1,7 @@
 // Token embedding with scaling, and its gradient by sorted tokens.
 //
 // The gradient in three launches: (1) a work-group sorts up to 16384 tokens by id in LDS, while the others fill the
-// gradient with zeros; (more tokens: sorted runs, put into one order by a second launch); (2) every run of 32 sorted tokens is
+// gradient with zeros; (more tokens: sorted runs, put into one order by a second launch); (2) every run of 16 or 32 sorted tokens is
 // summed by id, ids wholly inside written, the others' sums left in the workspace; (3) those are added up in order.
 #include "sk_block_launch.h"
 #include "sk_rows.h"
@@ -9,28 +9,34 @@
 namespace sk {
 namespace {
 
-constexpr int RUN = EMBEDDING_RUN, CHUNK = EMBEDDING_CHUNK;
-constexpr int SORT_THREADS = 1024, SORT_WAVES = SORT_THREADS / 64, SORT_STEPS = RUN / SORT_THREADS;
+constexpr int RUN = EMBEDDING_RUN;
+constexpr int SORT_THREADS = 1024, SORT_WAVES = SORT_THREADS / 64, SORT_STEPS = RUN / SORT_THREADS, FILL_PIECES = 4 * SORT_THREADS;
 
 __device__ __forceinline__ int64_t id_at(const EmbeddingArgs& p, int64_t t) {
   return p.ids64 ? static_cast<const int64_t*>(p.ids)[t] : static_cast<const int32_t*>(p.ids)[t];
 }
 
+// `threads` of a work-group to a row, 16 bytes a thread and step; all of a row's steps (up to four) are on their way at once.
 template <typename T>
-__global__ __launch_bounds__(256) void embedding_fwd_kernel(const EmbeddingArgs p) {
-  const int per_row = p.width / 8;
-  const int64_t pieces = p.tokens * per_row, stride = (int64_t)gridDim.x * 256;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += stride) {
-    const int64_t t = i / per_row, c = (i - t * per_row) * 8, id = id_at(p, t);
-    float v[8];
+__global__ __launch_bounds__(256) void embedding_fwd_kernel(const EmbeddingArgs p, int threads) {
+  constexpr int V = 16 / sizeof(T), STEPS = 4;
+  const int sub = threadIdx.x / threads, first = (threadIdx.x - sub * threads) * V, step = threads * V;
+  const int64_t t = (int64_t)blockIdx.x * (256 / threads) + sub;
+  if (t >= p.tokens) return;
+  const int64_t id = id_at(p, t);
+  const bool there = id >= 0 && id < p.rows;
+  const T* const from = static_cast<const T*>(p.table) + (there ? id : 0) * p.width;
+  T* const to = static_cast<T*>(p.out) + t * p.width;
+  for (int c0 = first; c0 < p.width; c0 += STEPS * step) {
+    float v[STEPS][V];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = 0.f;
-    if (id >= 0 && id < p.rows) {
-      load_values<T, 8>(v, static_cast<const T*>(p.table) + id * p.width + c);
+    for (int k = 0; k < STEPS; ++k) load_values<T, V>(v[k], from + (c0 + k * step < p.width ? c0 + k * step : c0));
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] *= p.scale;
+    for (int k = 0; k < STEPS; ++k) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[k][j] = there ? v[k][j] * p.scale : 0.f;
+      if (c0 + k * step < p.width) store_values<T, V>(to + c0 + k * step, v[k]);
     }
-    store_values<T, 8>(static_cast<T*>(p.out) + t * p.width + c, v);
   }
 }
 
@@ -127,9 +133,12 @@ __global__ __launch_bounds__(SORT_THREADS) void embedding_sort_kernel(const Embe
   if ((int)blockIdx.x < runs) {
     sort_run(p, room, blockIdx.x, digits, runs > 1 ? p.keys_runs : p.keys, runs > 1 ? p.order_runs : p.order);
   } else {
-    const int64_t stride = (int64_t)(gridDim.x - runs) * SORT_THREADS;
-    for (int64_t i = (int64_t)(blockIdx.x - runs) * SORT_THREADS + threadIdx.x; i < bytes / 16; i += stride)
-      static_cast<uint4*>(p.out)[i] = make_uint4(0, 0, 0, 0);
+    // 64 KB at a time
+    const int64_t pieces = bytes / 16, stride = (int64_t)(gridDim.x - runs) * FILL_PIECES;
+    for (int64_t i0 = (int64_t)(blockIdx.x - runs) * FILL_PIECES; i0 < pieces; i0 += stride)
+#pragma unroll
+      for (int k = 0; k < FILL_PIECES; k += SORT_THREADS)
+        if (i0 + k + threadIdx.x < pieces) static_cast<uint4*>(p.out)[i0 + k + threadIdx.x] = make_uint4(0, 0, 0, 0);
   }
 }
 
@@ -160,66 +169,70 @@ __global__ __launch_bounds__(256) void embedding_merge_kernel(const EmbeddingArg
   p.order[to] = p.order_runs[i];
 }
 
-// Eight columns a thread, `threads` of them to a chunk.
-template <typename T>
-__global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbeddingArgs p, int threads, int blocks, int64_t chunks) {
-  const int per = 256 / threads, sub = threadIdx.x / threads;
-  const int64_t id = blockIdx.x / blocks;
-  const int64_t chunk = id * per + sub;
-  const int column = ((int)(blockIdx.x - id * blocks) * threads + threadIdx.x - sub * threads) * 8;
-  if (sub >= per || chunk >= chunks || column >= p.width) return;
-  const int64_t first = chunk * CHUNK;
+// G lanes of a wave, 16 bytes each, sum a chunk's columns: its tokens and their order in one load, then 16 rows on their way at a time.
+template <typename T, int G, int CHUNK>
+__global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbeddingArgs p, int blocks, int64_t chunks) {
+  constexpr int V = 16 / sizeof(T), AT_ONCE = 16, HELD = (CHUNK + G - 1) / G;
+  const int lane = threadIdx.x & 63, l = lane % G;
+  const int64_t unit = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * (64 / G) + lane / G;   // (all of a chunk's column blocks in a row)
+  const int64_t chunk = unit / blocks;
+  const int column = ((int)(unit - chunk * blocks) * G + l) * V;
+  const bool there = chunk < chunks && column < p.width;
+  const int64_t first = (chunk < chunks ? chunk : 0) * CHUNK;
   const int n = p.tokens - first < CHUNK ? (int)(p.tokens - first) : CHUNK;
-  const unsigned* const keys = p.keys + first;
-  const unsigned* const order = p.order + first;
-  bool head = first > 0 && keys[-1] == keys[0];   // of an id that began before
-  const bool open = first + n < p.tokens && keys[n] == keys[n - 1];
-  float acc[8];
+  unsigned key[HELD], from[HELD];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-  constexpr int AT_ONCE = 8;
-  for (int i0 = 0; i0 < n; i0 += AT_ONCE) {
-    float v[AT_ONCE][8];
-    unsigned key[AT_ONCE];
+  for (int h = 0; h < HELD; ++h) {   // (past the chunk: its last token again)
+    const int i = h * G + l < n ? h * G + l : n - 1;
+    key[h] = p.keys[first + i];
+    from[h] = p.order[first + i];
+  }
+  const unsigned before = first > 0 ? p.keys[first - 1] : ~0u, behind = first + n < p.tokens ? p.keys[first + n] : ~0u;   // (no key: ids are below 2^31)
+  auto held = [&](const unsigned (&v)[HELD], int i) { return (unsigned)__shfl((int)v[i / G], i % G, G); };
+  const T* const dy = static_cast<const T*>(p.dy) + (there ? column : 0);
+  bool head = before == held(key, 0);   // of an id that began before
+  float acc[V];
 #pragma unroll
-    for (int k = 0; k < AT_ONCE; ++k) {   // (past the chunk: its last token again)
-      const int i = i0 + k < n ? i0 + k : n - 1;
-      key[k] = keys[i];
-      load_values<T, 8>(v[k], static_cast<const T*>(p.dy) + (int64_t)order[i] * p.width + column);
-    }
+  for (int j = 0; j < V; ++j) acc[j] = 0.f;
+#pragma unroll
+  for (int i0 = 0; i0 < CHUNK; i0 += AT_ONCE) {
+    if (i0 > 0 && i0 >= n) break;
+    float v[AT_ONCE][V];
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) load_values<T, V>(v[k], dy + (int64_t)held(from, i0 + k) * p.width);
 #pragma unroll
     for (int k = 0; k < AT_ONCE; ++k) {
       const int i = i0 + k;
       if (i >= n) break;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] += v[k][j];
-      const bool last = i == n - 1;
-      if (!last && (k + 1 < AT_ONCE ? key[k + 1 < AT_ONCE ? k + 1 : 0] : keys[i + 1]) == key[k]) continue;
-      if (head || (last && open)) {
-        store_values<float, 8>(p.partial + (chunk * 2 + (head ? 0 : 1)) * p.width + column, acc);
-      } else if (key[k] < p.rows) {
+      for (int j = 0; j < V; ++j) acc[j] += v[k][j];
+      const unsigned now = held(key, i), next = i == n - 1 ? behind : held(key, i + 1 < CHUNK ? i + 1 : i);
+      if (next == now && i < n - 1) continue;
+      if (head || next == now) {
+        if (there) store_values<float, V>(p.partial + (chunk * 2 + (head ? 0 : 1)) * p.width + column, acc);
+      } else if (now < p.rows && there) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] *= p.scale;
-        store_values<T, 8>(static_cast<T*>(p.out) + (int64_t)key[k] * p.width + column, acc);
+        for (int j = 0; j < V; ++j) acc[j] *= p.scale;
+        store_values<T, V>(static_cast<T*>(p.out) + (int64_t)now * p.width + column, acc);
       }
       head = false;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+      for (int j = 0; j < V; ++j) acc[j] = 0.f;
     }
   }
 }
 
 // The id that begins in a chunk and goes on behind it: its chunks' sums, dealt over four waves and joined in their order.
 template <typename T>
-__global__ __launch_bounds__(256) void embedding_join_kernel(const EmbeddingArgs p, int blocks) {
+__global__ __launch_bounds__(256) void embedding_join_kernel(const EmbeddingArgs p, int blocks, int run) {
   __shared__ float4 sums[4][64];
-  const int64_t chunk = blockIdx.x / blocks, first = chunk * CHUNK, next = first + CHUNK;
+  const int64_t chunk = blockIdx.x / blocks, first = chunk * run, next = first + run;
   const unsigned key = p.keys[next - 1];
   if (p.keys[next] != key || key >= p.rows || (first > 0 && p.keys[first] == key && p.keys[first - 1] == key)) return;   // (uniform)
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int column = ((int)(blockIdx.x - chunk * blocks) * 64 + lane) * 4;
   const bool there = column < p.width;
-  const int64_t last = (next + keys_below(p.keys + next, p.tokens - next, key, true) - 1) / CHUNK;
+  const int64_t last = (next + keys_below(p.keys + next, p.tokens - next, key, true) - 1) / run;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   if (there) {
 #pragma unroll 4
@@ -243,12 +256,13 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(const EmbeddingArgs
 
 template <typename T>
 hipError_t fwd(const EmbeddingArgs& a, hipStream_t s) {
-  const int64_t pieces = a.tokens * (a.width / 8), groups = (pieces + 255) / 256;
+  int threads = 8;
+  while (threads < 256 && threads * 16 < a.width * (int)sizeof(T)) threads *= 2;
   note_matrix(a.ids, 1, a.tokens, a.tokens, a.ids64 ? 8 : 4, false);
   note_matrix(a.table, a.rows, a.width, a.width, sizeof(T), false);
   note_matrix(a.out, a.tokens, a.width, a.width, sizeof(T), true);
   return launch_kernel("embedding_fwd_kernel", Work{0.0, 2.0 * a.tokens * a.width * sizeof(T)}, embedding_fwd_kernel<T>,
-                       dim3((unsigned)(groups < 16 * NUM_CUS ? groups : 16 * NUM_CUS)), dim3(256), s, a);
+                       dim3((unsigned)((a.tokens + 256 / threads - 1) / (256 / threads))), dim3(256), s, a, threads);
 }
 
 template <typename T>
@@ -257,14 +271,15 @@ hipError_t bwd(const EmbeddingArgs& a, hipStream_t s) {
   int digits = 1;
   while (digits < 4 && (uint64_t)a.rows >> (8 * digits) != 0) ++digits;
   const int64_t bytes = a.rows * a.width * (int64_t)sizeof(T);
-  const int64_t chunks = (a.tokens + CHUNK - 1) / CHUNK;
+  const int chunk = embedding_chunk(a.tokens, a.width, sizeof(T));
+  const int64_t chunks = (a.tokens + chunk - 1) / chunk;
   unsigned* const keys = runs > 1 ? a.keys_runs : a.keys;
   unsigned* const order = runs > 1 ? a.order_runs : a.order;
   note_matrix(a.ids, 1, a.tokens, a.tokens, a.ids64 ? 8 : 4, false);
   note_matrix(keys, 1, a.tokens, a.tokens, 4, true);
   note_matrix(order, 1, a.tokens, a.tokens, 4, true);
   note_matrix(a.out, a.rows, a.width, a.width, sizeof(T), true);
-  const int64_t fill = (bytes / 16 + SORT_THREADS * 8 - 1) / (SORT_THREADS * 8);
+  const int64_t fill = (bytes / 16 + FILL_PIECES - 1) / FILL_PIECES;
   hipError_t e = launch_kernel("embedding_sort_kernel", Work{0.0, (double)bytes}, embedding_sort_kernel,
                                dim3((unsigned)(runs + (fill < NUM_CUS * 4 ? fill : NUM_CUS * 4))), dim3(SORT_THREADS), s, a, runs, digits, bytes);
   if (e != hipSuccess) return e;
@@ -281,15 +296,20 @@ hipError_t bwd(const EmbeddingArgs& a, hipStream_t s) {
   note_matrix(a.dy, a.tokens, a.width, a.width, sizeof(T), false);
   note_matrix(a.out, a.rows, a.width, a.width, sizeof(T), true);
   note_matrix(a.partial, chunks * 2, a.width, a.width, 4, true);
-  const int columns = a.width / 8, threads = columns < 256 ? columns : 256, blocks = (columns + threads - 1) / threads, per = 256 / threads;
-  e = launch_kernel("embedding_sum_kernel", Work{0.0, 2.0 * a.tokens * a.width * sizeof(T)}, embedding_sum_kernel<T>,
-                    dim3((unsigned)((chunks + per - 1) / per * blocks)), dim3(256), s, a, threads, blocks, chunks);
+  auto sum = [&](auto g) {
+    constexpr int G = decltype(g)::value;
+    const int blocks = (a.width * (int)sizeof(T) / 16 + G - 1) / G;
+    return launch_kernel("embedding_sum_kernel", Work{0.0, 2.0 * a.tokens * a.width * sizeof(T)}, chunk == 32 ? embedding_sum_kernel<T, G, 32> : embedding_sum_kernel<T, G, 16>,
+                         dim3((unsigned)((chunks * blocks + 4 * (64 / G) - 1) / (4 * (64 / G)))), dim3(256), s, a, blocks, chunks);
+  };
+  const int lanes = a.width * (int)sizeof(T) / 16;
+  e = lanes <= 8 ? sum(IntC<8>{}) : lanes <= 16 ? sum(IntC<16>{}) : lanes <= 32 ? sum(IntC<32>{}) : sum(IntC<64>{});
   if (e != hipSuccess || chunks == 1) return e;
   note_matrix(a.keys, 1, a.tokens, a.tokens, 4, false);
   note_matrix(a.partial, chunks * 2, a.width, a.width, 4, false);
   note_matrix(a.out, a.rows, a.width, a.width, sizeof(T), true);
   const int join_blocks = (a.width + 255) / 256;
-  return launch_kernel("embedding_join_kernel", Work{0.0, 0.0}, embedding_join_kernel<T>, dim3((unsigned)((chunks - 1) * join_blocks)), dim3(256), s, a, join_blocks);
+  return launch_kernel("embedding_join_kernel", Work{0.0, 0.0}, embedding_join_kernel<T>, dim3((unsigned)((chunks - 1) * join_blocks)), dim3(256), s, a, join_blocks, chunk);
 }
 
 }  // namespace
