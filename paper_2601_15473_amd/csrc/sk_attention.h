@@ -150,8 +150,13 @@ inline void note_attention_dkv(const AttentionArgs& a, int esize) {
   note_matrix(a.d_o, rows_of(a), a.D, a.D, esize, false);
   note_matrix(a.lse2, 1, rows_of(a), rows_of(a), 4, false);
   note_matrix(a.delta, 1, rows_of(a), rows_of(a), 4, false);
-  note_matrix(a.dk, (int64_t)a.batch * a.k_len * a.kv_heads, a.D, a.D, esize, true);
-  note_matrix(a.dv, (int64_t)a.batch * a.k_len * a.kv_heads, a.D, a.D, esize, true);
+  const int64_t keys = (int64_t)a.batch * a.k_len * a.kv_heads;
+  if (a.parts > 1) {
+    note_matrix(a.partial, 2 * a.parts * keys, a.D, a.D, 4, true);
+  } else {
+    note_matrix(a.dk, keys, a.D, a.D, esize, true);
+    note_matrix(a.dv, keys, a.D, a.D, esize, true);
+  }
 }
 
 }  // namespace sk

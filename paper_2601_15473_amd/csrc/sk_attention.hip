@@ -207,7 +207,9 @@ __global__ __launch_bounds__(256) void attention_dkv_simple_kernel(const Attenti
   __shared__ float lse_tile[ROWS], delta_tile[ROWS];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int b, hk, tile;
-  locate(p, tiles, b, hk, tile);
+  locate(p, tiles * p.parts, b, hk, tile);
+  const int part = tile / tiles;
+  tile -= part * tiles;
   const Sequence q(p, b);
   const int j0 = tile * 128, j = j0 + wave * 32 + (lane & 31);
   const bool there = j < q.m;
@@ -222,13 +224,18 @@ __global__ __launch_bounds__(256) void attention_dkv_simple_kernel(const Attenti
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = zeros();
   const float c = p.scale * LOG2E;
+  // this part's tiles of all heads' (one head's behind the other's)
+  const int per_head = q.n > i_begin ? (q.n - i_begin + ROWS - 1) / ROWS : 0, all = per_head * p.group;
+  const int begin = (int)((int64_t)all * part / p.parts), end = (int)((int64_t)all * (part + 1) / p.parts);
   for (int gh = 0; gh < p.group; ++gh) {
     const int h = hk * p.group + gh;
     const T* const qb = static_cast<const T*>(p.q) + b * p.qs[0] + h * p.qs[2];
     const T* const gb = static_cast<const T*>(p.d_o) + ((int64_t)b * p.q_len * p.heads + h) * p.D;
     const float* const lse = p.lse2 + ((int64_t)b * p.heads + h) * p.q_len;
     const float* const delta = p.delta + ((int64_t)b * p.heads + h) * p.q_len;
-    for (int i0 = i_begin; i0 < q.n; i0 += ROWS) {
+    const int from = begin - gh * per_head > 0 ? begin - gh * per_head : 0, to = end - gh * per_head < per_head ? end - gh * per_head : per_head;
+    for (int step = from; step < to; ++step) {
+      const int i0 = i_begin + step * ROWS;
       __syncthreads();
       stage<T, DP>(q_tile, qb, p.qs[1], i0, q.n, p.D, tid);
       stage<T, DP>(g_tile, gb, (int64_t)p.heads * p.D, i0, q.n, p.D, tid);
@@ -259,6 +266,13 @@ __global__ __launch_bounds__(256) void attention_dkv_simple_kernel(const Attenti
     }
   }
   const int64_t at = (((int64_t)b * p.k_len + j) * p.kv_heads + hk) * p.D;
+  if (p.parts > 1) {
+    const int64_t values = (int64_t)p.batch * p.k_len * p.kv_heads * p.D;
+    float* const to = p.partial + part * 2 * values + at;
+    store_row<float, DP>(j < p.k_len ? to : nullptr, dk, 1.f, p.D, lane);
+    store_row<float, DP>(j < p.k_len ? to + values : nullptr, dv, 1.f, p.D, lane);
+    return;
+  }
   store_row<T, DP>(j < p.k_len ? static_cast<T*>(p.dk) + at : nullptr, dk, p.scale, p.D, lane);
   store_row<T, DP>(j < p.k_len ? static_cast<T*>(p.dv) + at : nullptr, dv, 1.f, p.D, lane);
 }
@@ -281,8 +295,9 @@ hipError_t bwd(const AttentionArgs& a, hipStream_t s) {
                                attention_dq_simple_kernel<T, DP>, dim3(a.batch * a.kv_heads * tiles), dim3(256), s, a, tiles);
   if (e != hipSuccess) return e;
   note_attention_dkv(a, sizeof(T));
-  return launch_kernel(kernel_label("attention_dkv_simple_kernel", {"float", lbl(DP)}).c_str(), Work{8 * pairs(a), 0.0},
-                       attention_dkv_simple_kernel<T, DP>, dim3(a.batch * a.kv_heads * k_tiles), dim3(256), s, a, k_tiles);
+  e = launch_kernel(kernel_label("attention_dkv_simple_kernel", {"float", lbl(DP)}).c_str(), Work{8 * pairs(a), 0.0},
+                       attention_dkv_simple_kernel<T, DP>, dim3(a.batch * a.kv_heads * k_tiles * a.parts), dim3(256), s, a, k_tiles);
+  return e != hipSuccess || a.parts == 1 ? e : launch_attention_sum_parts(a, true, s);
 }
 
 }  // namespace

@@ -184,27 +184,38 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const Atte
   const typename L::template Loader<WAVES> load_k(wave, lane, p.ks[1], p.D), load_v(wave, lane, p.vs[1], p.D);
   const unsigned k_at = L::along_address(lane), v_at = L::across_address(lane);
   Walk<TILE_ROWS> walk_k(kb, p.ks[1], 0, p.D), walk_v(vb, p.vs[1], 0, p.D);
-  int left = q.m;
-  auto load = [&](unsigned slot) {
-    load_k.load(walk_k.window(left), slot, wave);
-    load_v.load(walk_v.window(left), slot + L::BYTES, wave);
-    left -= TILE_ROWS;
-    walk_k.skip(TILE_ROWS);
-    walk_v.skip(TILE_ROWS);
-  };
-  if (keys > 0) load(0u);
+  if (keys > 0) {
+    load_k.load(walk_k.window(q.m), 0u, wave);
+    load_v.load(walk_v.window(q.m), L::BYTES, wave);
+  }
 
   unsigned slot = 0;
   for (int j0 = 0; j0 < keys; j0 += TILE_ROWS, slot ^= SLOT) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // this tile is there, and nobody reads the other slot
-    if (j0 + TILE_ROWS < keys) load(slot ^ SLOT);
-    if (j0 >= most) continue;
+    walk_k.skip(TILE_ROWS);
+    walk_v.skip(TILE_ROWS);
+    const int left = j0 + TILE_ROWS < keys ? q.m - j0 - TILE_ROWS : 0;   // (behind the last tile nothing is fetched)
+    const u32x4 next_k = walk_k.window(left), next_v = walk_v.window(left);
+    // The next tile is asked for an instruction at a time under the scores' products: its 32 KB are half a thousand cycles of the CU's path
+    // from memory, in which a wave that asked for all of its own at once would do nothing else.
+    constexpr int EACH = L::template Loader<WAVES>::EACH;
+    auto ask = [&](auto ic) {
+      constexpr int i = decltype(ic)::value, n = 2 * EACH * (i + 1) / (2 * KS) - 1;   // (of K's and V's EACH, at most one a product)
+      if constexpr (2 * EACH * i / (2 * KS) <= n) {
+        if constexpr (n < EACH) load_k.template load_one<n>(next_k, slot ^ SLOT, wave);
+        else load_v.template load_one<n - EACH>(next_v, (slot ^ SLOT) + L::BYTES, wave);
+      }
+    };
+    if (j0 >= most) {
+      static_for<0, 2 * KS>(ask);
+      continue;
+    }
     f32x16 s[2] = {zeros(), zeros()};
     {
       bf16x8 f[K_AHEAD];
       auto read = [&](auto ic) { return L::along(slot + k_at, decltype(ic)::value & 1, decltype(ic)::value >> 1); };
       read_first(f, read);
-      pipelined<2 * KS>(f, read, [&](auto ic, bf16x8 a) { constexpr int i = decltype(ic)::value; s[i & 1] = M::mma(a, qf[i >> 1], s[i & 1]); }, [](auto) {});
+      pipelined<2 * KS>(f, read, [&](auto ic, bf16x8 a) { constexpr int i = decltype(ic)::value; s[i & 1] = M::mma(a, qf[i >> 1], s[i & 1]); }, ask);
     }
     // values 16 step .. + 15 (step i / ND), features 32 (i % ND) .. + 31; the first on their way under the softmax
     bf16x8 f[V_AHEAD];
@@ -231,6 +242,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const Atte
                         }
                       });
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing may land in LDS any more)
   const float sum = sm.sum + other_half(sm.sum);
   store_row<DP>(static_cast<bf16*>(p.o) + (((int64_t)b * p.q_len + row.i) * p.heads + row.h) * p.D, row.there, o, sum == 0.f ? 0.f : 1.f / sum, p.D, lane);
   if (p.lse != nullptr && row.there && lane < 32)
@@ -413,7 +425,7 @@ template <int DP, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const AttentionArgs p) {
   typedef Tile<DP> L;
   typedef Mma<bf16> M;
-  constexpr int KS = DP / 16, ND = DP / 32, SLOT = 2 * L::BYTES;
+  constexpr int KS = DP / 16, ND = DP / 32, SLOT = 2 * L::BYTES, AHEAD = 4;
   __shared__ __align__(1024) unsigned char smem[2 * SLOT];
   asm volatile("" ::"v"((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem) : "memory");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -435,15 +447,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
   const typename L::template Loader<WAVES> load_k(wave, lane, p.ks[1], p.D), load_v(wave, lane, p.vs[1], p.D);
   const unsigned k_at = L::along_address(lane), kt_at = L::across_address(lane);
   Walk<TILE_ROWS> walk_k(kb, p.ks[1], 0, p.D), walk_v(vb, p.vs[1], 0, p.D);
-  int left = q.m;
-  auto load = [&](unsigned slot) {
-    load_k.load(walk_k.window(left), slot, wave);
-    load_v.load(walk_v.window(left), slot + L::BYTES, wave);
-    left -= TILE_ROWS;
-    walk_k.skip(TILE_ROWS);
-    walk_v.skip(TILE_ROWS);
-  };
-  if (keys > 0) load(0u);
+  if (keys > 0) {
+    load_k.load(walk_k.window(q.m), 0u, wave);
+    load_v.load(walk_v.window(q.m), L::BYTES, wave);
+  }
 
   bf16x8 qf[KS], gf[KS];
   const int64_t at = (((int64_t)b * p.q_len + row.i) * p.heads + row.h) * p.D;
@@ -475,8 +482,22 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
   unsigned slot = 0;
   for (int j0 = 0; j0 < keys; j0 += TILE_ROWS, slot ^= SLOT) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (j0 + TILE_ROWS < keys) load(slot ^ SLOT);
-    if (j0 >= most) continue;
+    walk_k.skip(TILE_ROWS);
+    walk_v.skip(TILE_ROWS);
+    const int left = j0 + TILE_ROWS < keys ? q.m - j0 - TILE_ROWS : 0;
+    const u32x4 next_k = walk_k.window(left), next_v = walk_v.window(left);
+    constexpr int EACH = L::template Loader<WAVES>::EACH;
+    auto ask = [&](auto ic) {   // (as the forward pass's, one to two products)
+      constexpr int i = decltype(ic)::value, n = 2 * EACH * (i + 1) / (4 * KS) - 1;
+      if constexpr (2 * EACH * i / (4 * KS) <= n) {
+        if constexpr (n < EACH) load_k.template load_one<n>(next_k, slot ^ SLOT, wave);
+        else load_v.template load_one<n - EACH>(next_v, (slot ^ SLOT) + L::BYTES, wave);
+      }
+    };
+    if (j0 >= most) {
+      static_for<0, 4 * KS>(ask);
+      continue;
+    }
     f32x16 s[2], g[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -484,13 +505,28 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
 #pragma unroll
       for (int r = 0; r < 16; ++r) g[t][r] = delta;
     }
+    if constexpr (DP > 64) {   // operand i: of k and v in turn, two blocks each, 16 features after 16
+      bf16x8 f[AHEAD];
+      auto read = [&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        return L::along(slot + (i & 2 ? L::BYTES : 0) + k_at, i & 1, i >> 2);
+      };
+      read_first(f, read);
+      pipelined<4 * KS>(f, read, [&](auto ic, bf16x8 a) {
+        constexpr int i = decltype(ic)::value;
+        if constexpr (i & 2) g[i & 1] = M::mma(a, gf[i >> 2], g[i & 1]);
+        else s[i & 1] = M::mma(a, qf[i >> 2], s[i & 1]);
+      }, ask);
+    } else {   // (the compiler's order keeps within the registers of three waves a SIMD, which at 64 features are worth more)
+      static_for<0, 4 * KS>(ask);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+      for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        s[t] = M::mma(L::along(slot + k_at, t, ks), qf[ks], s[t]);
-        g[t] = M::mma(L::along(slot + L::BYTES + k_at, t, ks), gf[ks], g[t]);
-      }
+        for (int t = 0; t < 2; ++t) {
+          s[t] = M::mma(L::along(slot + k_at, t, ks), qf[ks], s[t]);
+          g[t] = M::mma(L::along(slot + L::BYTES + k_at, t, ks), gf[ks], g[t]);
+        }
+    }
     if (j0 + TILE_ROWS > common)
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -508,6 +544,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
       for (int d = 0; d < ND; ++d) dq[d] = M::mma(L::across(slot + kt_at, d, t), w, dq[d]);
     }
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   store_row<DP>(static_cast<bf16*>(p.dq) + at, row.there, dq, p.scale, p.D, lane);
 }
 
@@ -526,6 +563,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dkv_kernel(const Atte
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int b, hk, tile;
   locate(p, b, hk, tile);
+  const int part = tile % p.parts;
+  tile /= p.parts;
   const Sequence q(p, b);
   const int j0 = tile * WAVES * 32, jw = j0 + wave * 32, j = jw + (lane & 31);
   const bool there = j < q.m;
@@ -533,14 +572,17 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dkv_kernel(const Atte
   const int i_begin = q.causal && j0 - q.shift + 1 > 0 ? (j0 - q.shift + 1) / TILE_ROWS * TILE_ROWS : 0;
   const int i_wave = jw < q.m ? (q.causal ? jw - q.shift + 1 : 0) : INT32_MAX;
   const int i_whole = jw + 31 < q.m ? (q.causal ? jw + 31 - q.shift + 1 : 0) : INT32_MAX;   // from here on queries see all the wave's keys
-  const int per_head = j0 < q.m && q.n > i_begin ? (q.n - i_begin + TILE_ROWS - 1) / TILE_ROWS : 0, steps = per_head * p.group;
+  const int per_head = j0 < q.m && q.n > i_begin ? (q.n - i_begin + TILE_ROWS - 1) / TILE_ROWS : 0;
+  // this part's tiles of all heads' (one head's behind the other's): `first_head`'s from i_first on
+  const int all = per_head * p.group, begin = (int)((int64_t)all * part / p.parts), steps = (int)((int64_t)all * (part + 1) / p.parts) - begin;
+  const int first_head = hk * p.group + (steps > 0 ? begin / per_head : 0), i_first = i_begin + (steps > 0 ? begin % per_head : 0) * TILE_ROWS;
 
   // (sums, keys and values take 192 registers of 256, scores 32: a lane's offsets are computed where they are used)
-  Walk<TILE_ROWS> walk_q(static_cast<const bf16*>(p.q) + b * p.qs[0] + hk * p.group * p.qs[2], p.qs[1], i_begin, p.D);
-  Walk<TILE_ROWS> walk_g(static_cast<const bf16*>(p.d_o) + ((int64_t)b * p.q_len * p.heads + hk * p.group) * p.D, (int64_t)p.heads * p.D, i_begin, p.D);
-  const float* stat = (wave == 0 ? p.lse2 : p.delta) + ((int64_t)b * p.heads + hk * p.group) * p.q_len + i_begin;
+  Walk<TILE_ROWS> walk_q(static_cast<const bf16*>(p.q) + b * p.qs[0] + first_head * p.qs[2], p.qs[1], i_first, p.D);
+  Walk<TILE_ROWS> walk_g(static_cast<const bf16*>(p.d_o) + ((int64_t)b * p.q_len * p.heads + first_head) * p.D, (int64_t)p.heads * p.D, i_first, p.D);
+  const float* stat = (wave == 0 ? p.lse2 : p.delta) + ((int64_t)b * p.heads + first_head) * p.q_len + i_first;
   const int per_tile = per_head * TILE_ROWS;
-  int left = q.n - i_begin;
+  int left = q.n - i_first;
   auto load = [&](unsigned slot) {
     const int lane = lane_again();
     const typename L::template Loader<WAVES> load_q(wave, lane, p.qs[1], p.D), load_g(wave, lane, (int64_t)p.heads * p.D, p.D);
@@ -580,7 +622,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dkv_kernel(const Atte
   for (int d = 0; d < ND; ++d) dk[d] = dv[d] = zeros();
   const float factor = score_factor(p.scale);
   unsigned slot = 0;
-  int i0 = i_begin;
+  int i0 = i_first;
   for (int step = 0; step < steps; ++step, slot = SLOT - slot) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     const int i_now = i0;
@@ -634,9 +676,23 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dkv_kernel(const Atte
     }
   }
   const int j_out = jw + (lane_again() & 31);
-  const int64_t at = (((int64_t)b * p.k_len + j_out) * p.kv_heads + hk) * p.D;
-  store_row<DP>(static_cast<bf16*>(p.dk) + at, j_out < p.k_len, dk, p.scale, p.D, lane_again());
-  store_row<DP>(static_cast<bf16*>(p.dv) + at, j_out < p.k_len, dv, 1.f, p.D, lane_again());
+  const int64_t row = ((int64_t)b * p.k_len + j_out) * p.kv_heads + hk;
+  if (p.parts == 1) {
+    store_row<DP>(static_cast<bf16*>(p.dk) + row * p.D, j_out < p.k_len, dk, p.scale, p.D, lane_again());
+    store_row<DP>(static_cast<bf16*>(p.dv) + row * p.D, j_out < p.k_len, dv, 1.f, p.D, lane_again());
+  } else if (j_out < p.k_len) {
+    const int64_t values = (int64_t)p.batch * p.k_len * p.kv_heads * p.D;
+    float* const to = p.partial + part * 2 * values + row * p.D;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int c = d * 32 + 8 * g + 4 * (lane_again() >> 5);
+        if (c >= p.D) continue;
+        *reinterpret_cast<f32x4*>(to + c) = f32x4{dk[d][4 * g], dk[d][4 * g + 1], dk[d][4 * g + 2], dk[d][4 * g + 3]};
+        *reinterpret_cast<f32x4*>(to + values + c) = f32x4{dv[d][4 * g], dv[d][4 * g + 1], dv[d][4 * g + 2], dv[d][4 * g + 3]};
+      }
+  }
 }
 
 double pairs(const AttentionArgs& a) { return (double)a.batch * a.q_len * a.heads * a.k_len * a.D; }
@@ -699,17 +755,58 @@ hipError_t bwd(const AttentionArgs& a, hipStream_t s) {
                                dim3(groups_of(a, (int64_t)a.q_len * a.group, WAVES * 32)), dim3(WAVES * 64), s, a);
   if (e != hipSuccess) return e;
   note_attention_dkv(a, 2);
-  return launch_kernel(kernel_label("attention_dkv_kernel", {lbl(DP), lbl(WAVES)}).c_str(), Work{8 * pairs(a), 0.0}, attention_dkv_kernel<DP, WAVES>,
-                       dim3(groups_of(a, a.k_len, WAVES * 32)), dim3(WAVES * 64), s, a);
+  e = launch_kernel(kernel_label("attention_dkv_kernel", {lbl(DP), lbl(WAVES)}).c_str(), Work{8 * pairs(a), 0.0}, attention_dkv_kernel<DP, WAVES>,
+                       dim3(groups_of(a, a.k_len, WAVES * 32) * a.parts), dim3(WAVES * 64), s, a);
+  return e != hipSuccess || a.parts == 1 ? e : launch_attention_sum_parts(a, false, s);
 }
 
 }  // namespace
+
+template <typename T>
+__global__ __launch_bounds__(256) void attention_sum_parts_kernel(const AttentionArgs p, int64_t values) {
+  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  const bool v = blockIdx.y == 1;
+  if (at >= values) return;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  const float* const from = p.partial + (v ? values : 0) + at;
+#pragma unroll 4
+  for (int part = 0; part < p.parts; ++part) {
+    const float4 x = *reinterpret_cast<const float4*>(from + part * 2 * values);
+    s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+  }
+  const float scale = v ? 1.f : p.scale, out[4] = {s.x * scale, s.y * scale, s.z * scale, s.w * scale};
+  store_values<T, 4>(static_cast<T*>(v ? p.dv : p.dk) + at, out);
+}
 
 size_t attention_fwd_bytes_bf16(const AttentionArgs& a) {
   FewPlan plan;
   return few_rows(a, plan) ? few_bytes(a, plan) : 0;
 }
 hipError_t launch_attention_fwd_bf16(const AttentionArgs& a, hipStream_t s) { return a.D <= 64 ? fwd<64>(a, s) : fwd<128>(a, s); }
+hipError_t launch_attention_sum_parts(const AttentionArgs& a, bool f32, hipStream_t s) {
+  const int64_t values = (int64_t)a.batch * a.k_len * a.kv_heads * a.D;
+  note_matrix(a.partial, 2 * a.parts, values, values, 4, false);
+  note_matrix(a.dk, 1, values, values, f32 ? 4 : 2, true);
+  note_matrix(a.dv, 1, values, values, f32 ? 4 : 2, true);
+  const dim3 grid((unsigned)((values / 4 + 255) / 256), 2);
+  const Work work{0.0, (8.0 * a.parts + (f32 ? 8 : 4)) * values};
+  if (f32) return launch_kernel("attention_sum_parts_kernel", work, attention_sum_parts_kernel<float>, grid, dim3(256), s, a, values);
+  return launch_kernel("attention_sum_parts_kernel", work, attention_sum_parts_kernel<bf16>, grid, dim3(256), s, a, values);
+}
+
+// dk and dv's kernel gets as many work-groups as there are tiles of 128 keys, which with few key heads leaves CUs without one while
+// each walks over the queries of a whole group: below two a CU the walk is cut into parts of eight tiles at least (what the sum's launch
+// costs), whose fp32 results a second kernel adds up in order: for two a CU, or under a causal mask, whose tiles differ in length,
+// three.  One sequence of 2048 tokens, 32 heads on 8 of 128, causal: 317 us in one part, 106 + 14 at two a CU, 92 + 19 at three; of 4096 on 4,
+// not causal: 1250, 549 + 15, 583 + 19.
+int attention_parts(const AttentionArgs& a, bool f32) {
+  const int64_t groups = (int64_t)a.batch * a.kv_heads * ((a.k_len + 127) / 128), tiles = (int64_t)a.group * ((a.q_len + (f32 ? 31 : 63)) / (f32 ? 32 : 64));
+  if (groups >= 2 * NUM_CUS) return 1;
+  int64_t parts = ((a.causal ? 3 : 2) * NUM_CUS + groups - 1) / groups;
+  if (parts > tiles / 8) parts = tiles / 8;
+  return parts < 1 ? 1 : parts > 16 ? 16 : (int)parts;
+}
+
 hipError_t launch_attention_bwd_bf16(const AttentionArgs& a, hipStream_t s) { return a.D <= 64 ? bwd<64>(a, s) : bwd<128>(a, s); }
 
 }  // namespace sk

@@ -42,13 +42,14 @@ struct Tile {
           at[p][k] = piece * 8 < D ? (unsigned)row * (unsigned)stride * 2u + (unsigned)piece * 16u : OOB_OFFSET;
         }
     }
-    // Rows from the descriptor's start on to LDS byte `lds` on.
+    // Rows from the descriptor's start on to LDS byte `lds` on: instruction i of EACH, or all of them.
+    template <int I>
+    __device__ __forceinline__ void load_one(u32x4 rows, unsigned lds, int wave) const {
+      constexpr int P = I / PER_PANEL, K = I % PER_PANEL;
+      load_to_lds(lds + P * PANEL_BYTES + (K * WAVES + wave) * 1024, at[P][K % KINDS] + K / KINDS * step, rows, 0u);
+    }
     __device__ __forceinline__ void load(u32x4 rows, unsigned lds, int wave) const {
-#pragma unroll
-      for (int p = 0; p < PANELS; ++p)
-#pragma unroll
-        for (int i = 0; i < PER_PANEL; ++i)
-          load_to_lds(lds + p * PANEL_BYTES + (i * WAVES + wave) * 1024, at[p][i % KINDS] + i / KINDS * step, rows, 0u);
+      static_for<0, EACH>([&](auto ic) { load_one<decltype(ic)::value>(rows, lds, wave); });
     }
   };
 

@@ -60,9 +60,11 @@ sk_status attention_args(const sk_attention_shape* s, AttentionArgs& a) {
   return SK_OK;
 }
 bool lengths_aligned(const AttentionArgs& a) { return ((reinterpret_cast<uintptr_t>(a.q_lengths) | reinterpret_cast<uintptr_t>(a.k_lengths)) & 3u) == 0; }
+size_t stat_bytes(const AttentionArgs& a) { return align_up((size_t)a.batch * a.heads * a.q_len * 4); }
 size_t attention_bytes(const AttentionArgs& a, bool f32, bool backward) {
   if (!backward) return f32 ? 0 : align_up(attention_fwd_bytes_bf16(a));
-  return 2 * align_up((size_t)a.batch * a.heads * a.q_len * 4);
+  const int parts = attention_parts(a, f32);
+  return 2 * stat_bytes(a) + (parts > 1 ? align_up((size_t)parts * 2 * a.batch * a.k_len * a.kv_heads * a.D * 4) : 0);
 }
 
 sk_status norm_rope_args(const sk_norm_rope_shape* s, NormRopeArgs& a, bool back) {
@@ -150,8 +152,12 @@ sk_status sk_attention_bwd(const sk_attention_shape* shape, const void* q, const
   if (!lengths_aligned(a)) return SK_ERR_INVALID_ARG;
   if (!workspace || workspace_bytes < attention_bytes(a, shape->dtype == SK_F32, true)) return SK_ERR_WORKSPACE;
   a.q = q; a.k = k; a.v = v; a.o_in = o; a.lse = const_cast<float*>(lse); a.d_o = d_o;
-  a.dq = dq; a.dk = dk; a.dv = dv; a.lse2 = static_cast<float*>(workspace);
-  a.delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + attention_bytes(a, shape->dtype == SK_F32, true) / 2);
+  a.dq = dq; a.dk = dk; a.dv = dv;
+  char* const w = static_cast<char*>(workspace);
+  a.lse2 = reinterpret_cast<float*>(w);
+  a.delta = reinterpret_cast<float*>(w + stat_bytes(a));
+  a.parts = attention_parts(a, shape->dtype == SK_F32);
+  a.partial = reinterpret_cast<float*>(w + 2 * stat_bytes(a));
   return launched(launch_attention_bwd(a, shape->dtype == SK_F32, static_cast<hipStream_t>(stream)), "sk_attention_bwd");
 }
 

@@ -21,7 +21,12 @@ struct AttentionArgs {
   int causal;
   float scale;
   void* workspace;              // forward
+  // backward: parts that dk and dv are summed in, and room for [parts][dk, dv] in fp32 where there are several
+  int parts;
+  float* partial;
 };
+int attention_parts(const AttentionArgs& a, bool f32);
+hipError_t launch_attention_sum_parts(const AttentionArgs& a, bool f32, hipStream_t s);
 
 size_t attention_fwd_bytes_bf16(const AttentionArgs& a);
 hipError_t launch_attention_fwd(const AttentionArgs& a, bool f32, hipStream_t s);

@@ -57,6 +57,7 @@ SHAPES = [  # batch, q_len, k_len, heads, kv_heads, head_dim
     (3, 64, 64, 4, 4, 64), (1, 31, 300, 7, 1, 96), (1, 260, 131, 6, 2, 32), (2, 128, 128, 2, 1, 120), (1, 1, 1030, 16, 2, 128),
     (2, 3, 515, 8, 2, 80), (1, 515, 640, 2, 2, 64), (1, 300, 300, 5, 1, 40),
     (1, 70, 1500, 4, 2, 128), (2, 9, 2100, 12, 1, 64),   # ranges of the keys, over one tile of rows
+    (1, 600, 330, 8, 1, 64), (2, 333, 260, 6, 2, 128),   # parts of the queries for few key heads
 ]
 
 
@@ -76,6 +77,7 @@ RAGGED = [  # shape, queries', keys' lengths
     ((2, 150, 90, 2, 1, 48), [150, 20], [90, 64]),
     ((3, 130, 260, 3, 3, 64), [130, 128, -4], [260, 1000, 17]),   # out of range: clamped
     ((2, 257, 257, 2, 1, 128), [129, 257], [129, 256]),
+    ((3, 520, 300, 8, 1, 64), [0, 520, 65], [300, 200, 3]),
 ]
 
 
