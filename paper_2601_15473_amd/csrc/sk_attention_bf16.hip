@@ -698,11 +698,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dkv_kernel(const Atte
 double pairs(const AttentionArgs& a) { return (double)a.batch * a.q_len * a.heads * a.k_len * a.D; }
 unsigned groups_of(const AttentionArgs& a, int64_t rows, int per) { return (unsigned)((int64_t)a.batch * a.kv_heads * ((rows + per - 1) / per)); }
 
-// Whether the forward pass goes by attention_few_kernel, and how: rows that fill one wave's tile at most, or too few work-groups of 128 rows
-// to give half the CUs one with a long way through the keys.
+// Whether the forward pass goes by attention_few_kernel, and how: rows that fill one wave's tile at most, or so few that tiles of 32, whose four
+// waves share the way through the keys, leave no CU with two (two sequences of 355, eight heads of 64: 8.7 us where tiles of 128 took
+// 11.7; 640 queries of 16 heads, 320 tiles of 32: 24.8 and 13.7).
 bool few_rows(const AttentionArgs& a, FewPlan& plan) {
   const int64_t heads = (int64_t)a.batch * a.kv_heads, rows = (int64_t)a.q_len * a.group;
-  if (rows > 32 && (heads * ((rows + 127) / 128) >= NUM_CUS / 2 || a.k_len < 1024)) return false;
+  if (rows > 32 && (heads * ((rows + 31) / 32) > NUM_CUS || a.k_len < 128)) return false;
   plan.row_tiles = (int)((rows + 31) / 32);
   // ranges for two rounds of two work-groups a CU, of 512 keys at least: less than four tiles a wave cost less than the join's launch
   const int64_t wanted = (4 * NUM_CUS + heads * plan.row_tiles - 1) / (heads * plan.row_tiles);

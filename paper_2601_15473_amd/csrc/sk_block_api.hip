@@ -110,9 +110,9 @@ sk_status embedding_args(const void* ids, int32_t id_bytes, int64_t tokens, int6
 }
 struct EmbeddingRoom {
   size_t keys, order, keys_runs, order_runs, partial, total;
-  EmbeddingRoom(int64_t tokens, int64_t width, sk_dtype dtype) {
+  EmbeddingRoom(int64_t tokens, int64_t rows, int64_t width, sk_dtype dtype) {
     const int chunk = embedding_chunk(tokens, width, esize(dtype));
-    const size_t list = align_up((size_t)tokens * 4), runs = tokens > EMBEDDING_RUN ? list : 0;
+    const size_t list = align_up((size_t)tokens * 4), runs = tokens > embedding_run(tokens, rows, width, esize(dtype)) ? list : 0;
     keys = 0; order = keys + list; keys_runs = order + list; order_runs = keys_runs + runs;
     partial = order_runs + runs;
     total = partial + align_up((size_t)((tokens + chunk - 1) / chunk) * 2 * width * 4);
@@ -211,7 +211,7 @@ sk_status sk_embedding_fwd(const void* ids, int32_t id_bytes, const void* table,
 size_t sk_embedding_workspace_bytes(int64_t tokens, int64_t rows, int64_t width, sk_dtype dtype) {
   EmbeddingArgs a;
   if (embedding_args(nullptr, 8, tokens, rows, width, 1.f, dtype, a) != SK_OK) return (size_t)-1;
-  return EmbeddingRoom(tokens, width, dtype).total;
+  return EmbeddingRoom(tokens, rows, width, dtype).total;
 }
 
 sk_status sk_embedding_bwd(const void* ids, int32_t id_bytes, const void* dy, void* dtable, int64_t tokens, int64_t rows,
@@ -220,7 +220,8 @@ sk_status sk_embedding_bwd(const void* ids, int32_t id_bytes, const void* dy, vo
   EmbeddingArgs a;
   const sk_status st = embedding_args(ids, id_bytes, tokens, rows, width, scale, dtype, a);
   if (st != SK_OK) return st;
-  const EmbeddingRoom room(tokens, width, dtype);
+  const EmbeddingRoom room(tokens, rows, width, dtype);
+  a.run = embedding_run(tokens, rows, width, esize(dtype));
   if (!workspace || workspace_bytes < room.total) return SK_ERR_WORKSPACE;
   char* const w = static_cast<char*>(workspace);
   a.dy = dy; a.out = dtable;

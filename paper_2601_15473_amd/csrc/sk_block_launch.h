@@ -60,16 +60,22 @@ struct EmbeddingArgs {
   void* out;             // y, or dtable
   int64_t tokens, rows;
   int width, ids64;
+  int run;               // backward: tokens of a sorted run
   float scale;
   // backward: the tokens sorted by id (stable), and the fp32 sums of runs that are cut
   unsigned *keys, *order, *keys_runs, *order_runs;
   float* partial;        // [chunks][2][width]
 };
-constexpr int EMBEDDING_RUN = 16384;   // tokens one work-group sorts
+constexpr int EMBEDDING_RUN = 16384;   // tokens one work-group sorts at most
 // Sorted tokens summed at a stretch (backward): 32 where that gives two waves a SIMD, else 16.  Sums in f32 of 4001 tokens of 768 features 14.3 us
 // with 32, 10.6 with 16; 16384 of 4096 in bf16 70.9 and 72.6, and the joins behind them 13.8 and 18.5.
 inline int embedding_chunk(int64_t tokens, int64_t width, int esize) {
   return (tokens + 31) / 32 * ((width * esize / 16 + 63) / 64) >= 8 * NUM_CUS ? 32 : 16;
+}
+// Tokens of a sorted run: all that fit one work-group's LDS where the gradient's fill, in the same launch, takes longer than their sort (16384 take 30
+// us, at 6.7 TB/s as long as 200 MB), or there are many runs to put in order, else 4096 (10 us) and a launch that orders up to eight runs (8 us).
+inline int embedding_run(int64_t tokens, int64_t rows, int64_t width, int esize) {
+  return tokens <= 8192 || tokens > 8 * 4096 || rows * width * esize >= (int64_t)128 << 20 ? EMBEDDING_RUN : 4096;
 }
 hipError_t launch_embedding_fwd(const EmbeddingArgs& a, bool f32, hipStream_t s);
 hipError_t launch_embedding_bwd(const EmbeddingArgs& a, bool f32, hipStream_t s);

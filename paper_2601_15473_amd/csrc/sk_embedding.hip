@@ -16,27 +16,36 @@ __device__ __forceinline__ int64_t id_at(const EmbeddingArgs& p, int64_t t) {
   return p.ids64 ? static_cast<const int64_t*>(p.ids)[t] : static_cast<const int32_t*>(p.ids)[t];
 }
 
-// `threads` of a work-group to a row, 16 bytes a thread and step; all of a row's steps (up to four) are on their way at once.
-template <typename T>
+// `threads` of a work-group to a row, 16 bytes a thread and step; four steps are on their way at once, of ROWS rows (narrow ones, whose ids are
+// the first trip to memory of two).
+template <typename T, int ROWS>
 __global__ __launch_bounds__(256) void embedding_fwd_kernel(const EmbeddingArgs p, int threads) {
-  constexpr int V = 16 / sizeof(T), STEPS = 4;
-  const int sub = threadIdx.x / threads, first = (threadIdx.x - sub * threads) * V, step = threads * V;
-  const int64_t t = (int64_t)blockIdx.x * (256 / threads) + sub;
-  if (t >= p.tokens) return;
-  const int64_t id = id_at(p, t);
-  const bool there = id >= 0 && id < p.rows;
-  const T* const from = static_cast<const T*>(p.table) + (there ? id : 0) * p.width;
-  T* const to = static_cast<T*>(p.out) + t * p.width;
+  constexpr int V = 16 / sizeof(T), STEPS = 4 / ROWS;
+  const int subs = 256 / threads, sub = threadIdx.x / threads, first = (threadIdx.x - sub * threads) * V, step = threads * V;
+  const int64_t t0 = (int64_t)blockIdx.x * subs * ROWS + sub;
+  const T* from[ROWS];
+  bool there[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    const int64_t t = t0 + r * subs, id = id_at(p, t < p.tokens ? t : p.tokens - 1);
+    there[r] = id >= 0 && id < p.rows;
+    from[r] = static_cast<const T*>(p.table) + (there[r] ? id : 0) * p.width;
+  }
   for (int c0 = first; c0 < p.width; c0 += STEPS * step) {
-    float v[STEPS][V];
+    float v[ROWS][STEPS][V];
 #pragma unroll
-    for (int k = 0; k < STEPS; ++k) load_values<T, V>(v[k], from + (c0 + k * step < p.width ? c0 + k * step : c0));
+    for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-    for (int k = 0; k < STEPS; ++k) {
+      for (int k = 0; k < STEPS; ++k) load_values<T, V>(v[r][k], from[r] + (c0 + k * step < p.width ? c0 + k * step : c0));
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[k][j] = there ? v[k][j] * p.scale : 0.f;
-      if (c0 + k * step < p.width) store_values<T, V>(to + c0 + k * step, v[k]);
-    }
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+      for (int k = 0; k < STEPS; ++k) {
+        const int64_t t = t0 + r * subs;
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[r][k][j] = there[r] ? v[r][k][j] * p.scale : 0.f;
+        if (t < p.tokens && c0 + k * step < p.width) store_values<T, V>(static_cast<T*>(p.out) + t * p.width + c0 + k * step, v[r][k]);
+      }
   }
 }
 
@@ -52,8 +61,8 @@ struct SortRoom {
 
 __device__ __forceinline__ void sort_run(const EmbeddingArgs& p, SortRoom& m, int run, int digits, unsigned* keys, unsigned* order) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t first = (int64_t)run * RUN;
-  const int n = p.tokens - first < RUN ? (int)(p.tokens - first) : RUN;
+  const int64_t first = (int64_t)run * p.run;
+  const int n = p.tokens - first < p.run ? (int)(p.tokens - first) : p.run;
   const int steps = (n + SORT_THREADS - 1) / SORT_THREADS, begin = wave * steps * 64;
   for (int i = tid; i < n; i += SORT_THREADS) {
     const int64_t id = id_at(p, first + i);
@@ -157,12 +166,12 @@ __device__ __forceinline__ int64_t keys_below(const unsigned* keys, int64_t n, u
 __global__ __launch_bounds__(256) void embedding_merge_kernel(const EmbeddingArgs p, int runs) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= p.tokens) return;
-  const int run = (int)(i / RUN);
+  const int run = (int)(i / p.run);
   const unsigned key = p.keys_runs[i];
-  int64_t to = i - (int64_t)run * RUN;
+  int64_t to = i - (int64_t)run * p.run;
   for (int r = 0; r < runs; ++r) {
     if (r == run) continue;
-    const int64_t first = (int64_t)r * RUN, n = p.tokens - first < RUN ? p.tokens - first : RUN;
+    const int64_t first = (int64_t)r * p.run, n = p.tokens - first < p.run ? p.tokens - first : p.run;
     to += keys_below(p.keys_runs + first, n, key, r < run);
   }
   p.keys[to] = key;
@@ -261,13 +270,17 @@ hipError_t fwd(const EmbeddingArgs& a, hipStream_t s) {
   note_matrix(a.ids, 1, a.tokens, a.tokens, a.ids64 ? 8 : 4, false);
   note_matrix(a.table, a.rows, a.width, a.width, sizeof(T), false);
   note_matrix(a.out, a.tokens, a.width, a.width, sizeof(T), true);
-  return launch_kernel("embedding_fwd_kernel", Work{0.0, 2.0 * a.tokens * a.width * sizeof(T)}, embedding_fwd_kernel<T>,
-                       dim3((unsigned)((a.tokens + 256 / threads - 1) / (256 / threads))), dim3(256), s, a, threads);
+  // rows to a thread: as many as leave it four steps, and every CU eight work-groups
+  const int steps = (a.width * (int)sizeof(T) / 16 + threads - 1) / threads, subs = 256 / threads;
+  const int most = (int)(a.tokens / (8 * NUM_CUS * subs)), rows = steps == 1 && most >= 4 ? 4 : steps <= 2 && most >= 2 ? 2 : 1;
+  return launch_kernel("embedding_fwd_kernel", Work{0.0, 2.0 * a.tokens * a.width * sizeof(T)},
+                       rows == 4 ? embedding_fwd_kernel<T, 4> : rows == 2 ? embedding_fwd_kernel<T, 2> : embedding_fwd_kernel<T, 1>,
+                       dim3((unsigned)((a.tokens + subs * rows - 1) / (subs * rows))), dim3(256), s, a, threads);
 }
 
 template <typename T>
 hipError_t bwd(const EmbeddingArgs& a, hipStream_t s) {
-  const int runs = (int)((a.tokens + RUN - 1) / RUN);
+  const int runs = (int)((a.tokens + a.run - 1) / a.run);
   int digits = 1;
   while (digits < 4 && (uint64_t)a.rows >> (8 * digits) != 0) ++digits;
   const int64_t bytes = a.rows * a.width * (int64_t)sizeof(T);
