@@ -58,20 +58,23 @@ typedef struct {
 /* Bytes of workspace of the forward pass, and of the backward pass ((size_t)-1 for a shape that would be refused). */
 size_t sk_attention_workspace_bytes(const sk_attention_shape* shape, int32_t backward);
 
-/* o [batch, q_len, heads, head_dim] dense; lse [batch, heads, q_len] dense or NULL (wanted for a backward pass). */
+/*
+ * o [batch, q_len, heads, head_dim] dense.  For a backward pass: lse [batch, heads, q_len] dense or NULL, and in bf16 o_rest, as o, or
+ * NULL: what rounding leaves off o, in bf16 (looked at in bf16 only).
+ */
 sk_status sk_attention_fwd(const sk_attention_shape* shape, const void* q, const void* k, const void* v, void* o, float* lse,
-                           void* workspace, size_t workspace_bytes, void* stream);
+                           void* o_rest, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * The exact derivative of the above, probabilities recomputed from q, k and lse:
  *     dv_j = sum_i p_ij do_i,  ds_ij = scale * p_ij (do_i . v_j - do_i . o_i),  dq_i = sum_j ds_ij k_j,  dk_j = sum_i ds_ij q_i
- * (dk and dv summed over the query heads that share them, too).  o and lse are the forward pass's,
- * d_o as o; dq, dk and dv dense, [batch, tokens, heads, head_dim] of their own.  Zeros for queries and
+ * (dk and dv summed over the query heads that share them, too).  o, lse and o_rest are the forward pass's
+ * (without o_rest, NULL, do_i . o_i is taken of the rounded o alone: in bf16 dq and dk are then off by a tenth more), d_o as o; dq, dk and dv dense, [batch, tokens, heads, head_dim] of their own.  Zeros for queries and
  * keys past their lengths.
  */
 sk_status sk_attention_bwd(const sk_attention_shape* shape, const void* q, const void* k, const void* v, const void* o,
-                           const float* lse, const void* d_o, void* dq, void* dk, void* dv, void* workspace,
-                           size_t workspace_bytes, void* stream);
+                           const float* lse, const void* o_rest, const void* d_o, void* dq, void* dk, void* dv,
+                           void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * RMS norm of every query and key head, then the rotation of its first `rotary_dim` features by the

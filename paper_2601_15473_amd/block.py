@@ -108,34 +108,37 @@ def _attention_workspace(shape, backward, device, stream):
     return _workspace(device, stream, need)
 
 
-def _attention_forward(q, k, v, q_lengths, k_lengths, causal, scale, want_lse):
+def _attention_forward(q, k, v, q_lengths, k_lengths, causal, scale, training):
+    """o, and for a backward pass the rows' log of their sums and (bf16) what o's rounding left off."""
     o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device) if want_lse else None
+    lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device) if training else None
+    rest = torch.empty_like(o) if training and q.dtype == torch.bfloat16 else None
     if q.numel() == 0 or k.numel() == 0:
-        return o.zero_(), lse
+        return o.zero_(), lse, rest
     shape = _attention_shape(q, k, v, q_lengths, k_lengths, causal, scale)
     with _on(q.device):
         stream = _stream(q.device)
         ws = _attention_workspace(shape, 0, q.device, stream)
-        sk.check(sk.sk_attention_fwd(shape, q, k, v, o, lse, ws, ws.numel(), stream))
-    return o, lse
+        sk.check(sk.sk_attention_fwd(shape, q, k, v, o, lse, rest, ws, ws.numel(), stream))
+    return o, lse, rest
 
 
 class AttentionFunction(torch.autograd.Function):
-    """See ``attention``; keeps q, k, v, o and a row's log of its sum of exponentials, and recomputes the probabilities."""
+    """See ``attention``; keeps q, k, v, o (in bf16 with what its rounding left off) and a row's log of its sum of exponentials, and
+    recomputes the probabilities."""
 
     @staticmethod
     def forward(ctx, q, k, v, q_lengths, k_lengths, causal, scale):
         qs, ks, vs = (_strided(t, 1) for t in (q, k, v))
-        o, lse = _attention_forward(qs, ks, vs, q_lengths, k_lengths, causal, scale, True)
-        ctx.save_for_backward(qs, ks, vs, o, lse, q_lengths, k_lengths)
+        o, lse, rest = _attention_forward(qs, ks, vs, q_lengths, k_lengths, causal, scale, True)
+        ctx.save_for_backward(qs, ks, vs, o, lse, rest, q_lengths, k_lengths)
         ctx.causal, ctx.scale = causal, scale
         return o
 
     @staticmethod
     @_once
     def backward(ctx, do):
-        q, k, v, o, lse, q_lengths, k_lengths = ctx.saved_tensors
+        q, k, v, o, lse, rest, q_lengths, k_lengths = ctx.saved_tensors
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
         if q.numel() == 0 or k.numel() == 0:
             return dq.zero_(), dk.zero_(), dv.zero_(), None, None, None, None
@@ -144,7 +147,7 @@ class AttentionFunction(torch.autograd.Function):
         with _on(q.device):
             stream = _stream(q.device)
             ws = _attention_workspace(shape, 1, q.device, stream)
-            sk.check(sk.sk_attention_bwd(shape, q, k, v, o, lse, do, dq, dk, dv, ws, ws.numel(), stream))
+            sk.check(sk.sk_attention_bwd(shape, q, k, v, o, lse, rest, do, dq, dk, dv, ws, ws.numel(), stream))
         return dq, dk, dv, None, None, None, None
 
 

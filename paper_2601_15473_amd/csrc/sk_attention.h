@@ -135,11 +135,13 @@ inline void note_attention_fwd(const AttentionArgs& a, int esize) {
   note_attention_inputs(a, esize);
   note_matrix(a.o, rows_of(a), a.D, a.D, esize, true);
   note_matrix(a.lse, 1, rows_of(a), rows_of(a), 4, true);
+  note_matrix(a.o_rest, rows_of(a), a.D, a.D, esize, true);
 }
 inline void note_attention_dq(const AttentionArgs& a, int esize) {
   note_attention_inputs(a, esize);
   note_matrix(a.d_o, rows_of(a), a.D, a.D, esize, false);
   note_matrix(a.o_in, rows_of(a), a.D, a.D, esize, false);
+  note_matrix(a.o_rest, rows_of(a), a.D, a.D, esize, false);
   note_matrix(a.lse, 1, rows_of(a), rows_of(a), 4, false);
   note_matrix(a.lse2, 1, rows_of(a), rows_of(a), 4, true);
   note_matrix(a.delta, 1, rows_of(a), rows_of(a), 4, true);

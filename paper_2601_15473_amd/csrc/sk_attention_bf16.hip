@@ -94,6 +94,20 @@ __device__ __forceinline__ void store_row(bf16* row, bool there, const f32x16 (&
     }
 }
 
+// The same, and in `rest` what rounding leaves off (rounded itself): the backward pass's sum of dO o takes both, since o's rounding alone
+// is a third as large an error in dq and dk as their own.
+template <int DP>
+__device__ __forceinline__ void store_row_and_rest(bf16* row, bf16* rest, bool there, const f32x16 (&acc)[DP / 32], float scale, int D, int lane) {
+  store_row<DP>(row, there, acc, scale, D, lane);
+  if (rest == nullptr) return;
+  f32x16 left[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) left[d][r] = acc[d][r] * scale - (float)(bf16)(acc[d][r] * scale);
+  store_row<DP>(rest, there, left, 1.f, D, lane);
+}
+
 // Running softmax of a lane's row (the lane 32 further has the row's other keys): the maximum and its own keys' sum.
 struct Softmax {
   float top = -INFINITY, sum = 0.f, base = 0.f;
@@ -244,7 +258,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const Atte
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing may land in LDS any more)
   const float sum = sm.sum + other_half(sm.sum);
-  store_row<DP>(static_cast<bf16*>(p.o) + (((int64_t)b * p.q_len + row.i) * p.heads + row.h) * p.D, row.there, o, sum == 0.f ? 0.f : 1.f / sum, p.D, lane);
+  const int64_t at = (((int64_t)b * p.q_len + row.i) * p.heads + row.h) * p.D;
+  store_row_and_rest<DP>(static_cast<bf16*>(p.o) + at, p.o_rest != nullptr ? static_cast<bf16*>(p.o_rest) + at : nullptr, row.there, o, sum == 0.f ? 0.f : 1.f / sum, p.D,
+                         lane);
   if (p.lse != nullptr && row.there && lane < 32)
     p.lse[((int64_t)b * p.heads + row.h) * p.q_len + row.i] = sum == 0.f ? -INFINITY : (sm.top + __builtin_amdgcn_logf(sum)) * LN2;
 }
@@ -365,7 +381,13 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(const AttentionAr
       const float scale = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] *= scale;
-      store_values<bf16, 8>(static_cast<bf16*>(p.o) + (((int64_t)b * p.q_len + out.i) * p.heads + out.h) * p.D + c, v);
+      const int64_t to = (((int64_t)b * p.q_len + out.i) * p.heads + out.h) * p.D + c;
+      store_values<bf16, 8>(static_cast<bf16*>(p.o) + to, v);
+      if (p.o_rest != nullptr) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] -= (float)(bf16)v[i];
+        store_values<bf16, 8>(static_cast<bf16*>(p.o_rest) + to, v);
+      }
       if (p.lse != nullptr && c == 0) p.lse[((int64_t)b * p.heads + out.h) * p.q_len + out.i] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * LN2;
     }
   }
@@ -415,8 +437,13 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs
   }
   const Row out(p, r, hk);
   const float scale = total == 0.f ? 0.f : 1.f / total;
-  if (c < p.D)
-    *reinterpret_cast<unsigned*>(static_cast<bf16*>(p.o) + (((int64_t)b * p.q_len + out.i) * p.heads + out.h) * p.D + c) = pack_bf16x2(x * scale, y * scale);
+  if (c < p.D) {
+    const int64_t to = (((int64_t)b * p.q_len + out.i) * p.heads + out.h) * p.D + c;
+    x *= scale;
+    y *= scale;
+    *reinterpret_cast<unsigned*>(static_cast<bf16*>(p.o) + to) = pack_bf16x2(x, y);
+    if (p.o_rest != nullptr) *reinterpret_cast<unsigned*>(static_cast<bf16*>(p.o_rest) + to) = pack_bf16x2(x - (float)(bf16)x, y - (float)(bf16)y);
+  }
   if (p.lse != nullptr && lane == 0) p.lse[((int64_t)b * p.heads + out.h) * p.q_len + out.i] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * LN2;
 }
 
@@ -464,6 +491,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
     load_row<DP>(of, p.o_in, at, counts, p.D, lane);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) delta -= M::dot(of[ks], gf[ks]);
+    if (p.o_rest != nullptr) {
+      load_row<DP>(of, p.o_rest, at, counts, p.D, lane);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) delta -= M::dot(of[ks], gf[ks]);
+    }
   }
   delta += other_half(delta);
   settle(qf);

@@ -130,8 +130,8 @@ size_t sk_attention_workspace_bytes(const sk_attention_shape* shape, int32_t bac
 }
 
 sk_status sk_attention_fwd(const sk_attention_shape* shape, const void* q, const void* k, const void* v, void* o, float* lse,
-                           void* workspace, size_t workspace_bytes, void* stream) {
-  if (!q || !k || !v || !o || !aligned16(q, k, v, o, lse, workspace)) return SK_ERR_INVALID_ARG;
+                           void* o_rest, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q || !k || !v || !o || !aligned16(q, k, v, o, lse, o_rest, workspace)) return SK_ERR_INVALID_ARG;
   AttentionArgs a{};
   const sk_status st = attention_args(shape, a);
   if (st != SK_OK) return st;
@@ -139,19 +139,21 @@ sk_status sk_attention_fwd(const sk_attention_shape* shape, const void* q, const
   const size_t need = attention_bytes(a, shape->dtype == SK_F32, false);
   if (need > 0 && (!workspace || workspace_bytes < need)) return SK_ERR_WORKSPACE;
   a.q = q; a.k = k; a.v = v; a.o = o; a.lse = lse; a.workspace = workspace;
+  a.o_rest = shape->dtype == SK_F32 ? nullptr : o_rest;
   return launched(launch_attention_fwd(a, shape->dtype == SK_F32, static_cast<hipStream_t>(stream)), "sk_attention_fwd");
 }
 
 sk_status sk_attention_bwd(const sk_attention_shape* shape, const void* q, const void* k, const void* v, const void* o,
-                           const float* lse, const void* d_o, void* dq, void* dk, void* dv, void* workspace,
+                           const float* lse, const void* o_rest, const void* d_o, void* dq, void* dk, void* dv, void* workspace,
                            size_t workspace_bytes, void* stream) {
-  if (!q || !k || !v || !o || !lse || !d_o || !dq || !dk || !dv || !aligned16(q, k, v, o, lse, d_o, dq, dk, dv, workspace)) return SK_ERR_INVALID_ARG;
+  if (!q || !k || !v || !o || !lse || !d_o || !dq || !dk || !dv || !aligned16(q, k, v, o, lse, o_rest, d_o, dq, dk, dv, workspace)) return SK_ERR_INVALID_ARG;
   AttentionArgs a{};
   const sk_status st = attention_args(shape, a);
   if (st != SK_OK) return st;
   if (!lengths_aligned(a)) return SK_ERR_INVALID_ARG;
   if (!workspace || workspace_bytes < attention_bytes(a, shape->dtype == SK_F32, true)) return SK_ERR_WORKSPACE;
   a.q = q; a.k = k; a.v = v; a.o_in = o; a.lse = const_cast<float*>(lse); a.d_o = d_o;
+  a.o_rest = shape->dtype == SK_F32 ? nullptr : const_cast<void*>(o_rest);
   a.dq = dq; a.dk = dk; a.dv = dv;
   char* const w = static_cast<char*>(workspace);
   a.lse2 = reinterpret_cast<float*>(w);

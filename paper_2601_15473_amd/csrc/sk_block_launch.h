@@ -14,6 +14,7 @@ struct AttentionArgs {
   const void* o_in;             // backward: the forward pass's result
   void *o, *dq, *dk, *dv;
   float* lse;                   // forward: written unless null; backward: read
+  void* o_rest;                 // bf16: what o's rounding left off, or null; as lse
   float *lse2, *delta;          // backward: lse log2(e) and -sum_d dO o of every row, left by dq's kernel for dk's and dv's
   const int32_t *q_lengths, *k_lengths;
   int64_t qs[3], ks[3], vs[3];  // batch, token, head strides in elements

@@ -72,10 +72,11 @@ struct AttentionCall {
   }
 };
 
-Tensor attention_forward(const Tensor& q, const Tensor& k, const Tensor& v, const AttentionCall& c, Tensor* lse) {
+Tensor attention_forward(const Tensor& q, const Tensor& k, const Tensor& v, const AttentionCall& c, Tensor* lse, Tensor* rest) {
   const c10::DeviceGuard guard(q.device());
   Tensor o = at::empty(q.sizes(), q.options());
   if (lse) *lse = at::empty({q.size(0), q.size(2), q.size(1)}, q.options().dtype(at::kFloat));
+  if (rest && c.s.dtype == SK_BF16) *rest = at::empty(q.sizes(), q.options());
   void* const stream = stream_of(q.device());
   const size_t need = sk_attention_workspace_bytes(&c.s, 0);
   Workspaces& w = workspaces();
@@ -83,7 +84,8 @@ Tensor attention_forward(const Tensor& q, const Tensor& k, const Tensor& v, cons
   {
     const std::lock_guard<std::mutex> lock(w.mutex);
     const Tensor& ws = w.get(q.device(), stream, need);
-    st = sk_attention_fwd(&c.s, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse ? lse->data_ptr<float>() : nullptr, ws.data_ptr(), (size_t)ws.numel(), stream);
+    st = sk_attention_fwd(&c.s, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse ? lse->data_ptr<float>() : nullptr,
+                          rest && rest->defined() ? rest->data_ptr() : nullptr, ws.data_ptr(), (size_t)ws.numel(), stream);
   }
   check(st);
   return o;
@@ -92,10 +94,10 @@ Tensor attention_forward(const Tensor& q, const Tensor& k, const Tensor& v, cons
 struct Attention : torch::autograd::Function<Attention> {
   static Tensor forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& v, const std::optional<Tensor>& ql, const std::optional<Tensor>& kl, bool causal,
                         double scale) {
-    Tensor lse;
+    Tensor lse, rest;
     const Tensor n = ql.value_or(Tensor()), m = kl.value_or(Tensor());
-    const Tensor o = attention_forward(q, k, v, AttentionCall(q, k, v, n, m, causal, scale), &lse);
-    ctx->save_for_backward({q, k, v, o, lse, n, m});
+    const Tensor o = attention_forward(q, k, v, AttentionCall(q, k, v, n, m, causal, scale), &lse, &rest);
+    ctx->save_for_backward({q, k, v, o, lse, rest, n, m});
     ctx->saved_data["causal"] = causal;
     ctx->saved_data["scale"] = scale;
     return o;
@@ -106,7 +108,7 @@ struct Attention : torch::autograd::Function<Attention> {
     const Tensor &q = saved[0], &k = saved[1], &v = saved[2];
     const c10::DeviceGuard guard(q.device());
     const Tensor dO = made_dense(grads[0]);
-    const AttentionCall c(q, k, v, saved[5], saved[6], ctx->saved_data["causal"].toBool(), ctx->saved_data["scale"].toDouble());
+    const AttentionCall c(q, k, v, saved[6], saved[7], ctx->saved_data["causal"].toBool(), ctx->saved_data["scale"].toDouble());
     const Tensor dq = at::empty(q.sizes(), q.options()), dk = at::empty(k.sizes(), q.options()), dv = at::empty(k.sizes(), q.options());
     void* const stream = stream_of(q.device());
     const size_t need = sk_attention_workspace_bytes(&c.s, 1);
@@ -115,7 +117,7 @@ struct Attention : torch::autograd::Function<Attention> {
     {
       const std::lock_guard<std::mutex> lock(w.mutex);
       const Tensor& ws = w.get(q.device(), stream, need);
-      st = sk_attention_bwd(&c.s, q.data_ptr(), k.data_ptr(), v.data_ptr(), saved[3].data_ptr(), saved[4].data_ptr<float>(), dO.data_ptr(), dq.data_ptr(), dk.data_ptr(),
+      st = sk_attention_bwd(&c.s, q.data_ptr(), k.data_ptr(), v.data_ptr(), saved[3].data_ptr(), saved[4].data_ptr<float>(), saved[5].defined() ? saved[5].data_ptr() : nullptr, dO.data_ptr(), dq.data_ptr(), dk.data_ptr(),
                             dv.data_ptr(), ws.data_ptr(), (size_t)ws.numel(), stream);
     }
     check(st);
@@ -280,7 +282,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (at::GradMode::is_enabled() && (q->requires_grad() || k->requires_grad() || v->requires_grad()))
       o = Attention::apply(*q, *k, *v, given(lengths[0]), given(lengths[1]), causal, scale);
     else
-      o = attention_forward(*q, *k, *v, c, nullptr);
+      o = attention_forward(*q, *k, *v, c, nullptr, nullptr);
   }
   return THPVariable_Wrap(std::move(o));
   END_HANDLE_TH_ERRORS

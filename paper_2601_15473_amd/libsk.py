@@ -93,8 +93,8 @@ _shape, _f32, _u64 = ctypes.POINTER(AttentionShape), ctypes.c_float, ctypes.c_ui
 _norm_shape = ctypes.POINTER(NormRopeShape)
 for _name, _restype, _argtypes in (
         ("sk_attention_workspace_bytes", _sz, [_shape, _i32]),
-        ("sk_attention_fwd", ctypes.c_int, [_shape] + [_vp] * 6 + [_sz, _vp]),
-        ("sk_attention_bwd", ctypes.c_int, [_shape] + [_vp] * 10 + [_sz, _vp]),
+        ("sk_attention_fwd", ctypes.c_int, [_shape] + [_vp] * 7 + [_sz, _vp]),
+        ("sk_attention_bwd", ctypes.c_int, [_shape] + [_vp] * 11 + [_sz, _vp]),
         ("sk_norm_rope_fwd", ctypes.c_int, [_norm_shape] + [_vp] * 10),
         ("sk_norm_rope_workspace_bytes", _sz, [_norm_shape]),
         ("sk_norm_rope_bwd", ctypes.c_int, [_norm_shape] + [_vp] * 14 + [_sz, _vp]),
@@ -235,13 +235,14 @@ def sk_attention_workspace_bytes(shape, backward):
     return _lib.sk_attention_workspace_bytes(shape, backward)
 
 
-def sk_attention_fwd(shape, q, k, v, o, lse, workspace, workspace_bytes, stream=None):
-    return _lib.sk_attention_fwd(shape, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(workspace), workspace_bytes, _stream(stream))
+def sk_attention_fwd(shape, q, k, v, o, lse, o_rest, workspace, workspace_bytes, stream=None):
+    return _lib.sk_attention_fwd(shape, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(o_rest), _ptr(workspace), workspace_bytes,
+                                 _stream(stream))
 
 
-def sk_attention_bwd(shape, q, k, v, o, lse, d_o, dq, dk, dv, workspace, workspace_bytes, stream=None):
-    return _lib.sk_attention_bwd(shape, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(d_o), _ptr(dq), _ptr(dk), _ptr(dv),
-                                 _ptr(workspace), workspace_bytes, _stream(stream))
+def sk_attention_bwd(shape, q, k, v, o, lse, o_rest, d_o, dq, dk, dv, workspace, workspace_bytes, stream=None):
+    return _lib.sk_attention_bwd(shape, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(o_rest), _ptr(d_o), _ptr(dq), _ptr(dk),
+                                 _ptr(dv), _ptr(workspace), workspace_bytes, _stream(stream))
 
 
 def sk_norm_rope_fwd(shape, q, k, q_weight, k_weight, cos, sin, positions, q_out, k_out, stream=None):

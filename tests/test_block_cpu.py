@@ -36,12 +36,13 @@ def norm_shape(tokens=5, heads=4, kv_heads=2, head_dim=64, rotary_dim=64, interl
     return s
 
 
-def fwd(s, q=P, k=P, v=P, o=P, lse=P, ws=P, n=BIG):
-    return sk.sk_attention_fwd(s, q, k, v, o, lse, ws, n)
+def fwd(s, q=P, k=P, v=P, o=P, lse=P, rest=P, ws=P, n=BIG):
+    return sk.sk_attention_fwd(s, q, k, v, o, lse, rest, ws, n)
 
 
 def bwd(s, *ptrs, ws=P, n=BIG):
-    return sk.sk_attention_bwd(s, *(ptrs or (P,) * 9), ws, n)
+    ptrs = ptrs or (P,) * 9
+    return sk.sk_attention_bwd(s, *ptrs[:5], P, *ptrs[5:], ws, n)
 
 
 def test_every_declared_symbol_is_exported():
@@ -73,7 +74,7 @@ def test_attention_pointers_and_workspace():
             args = [P] * 4
             args[i] = bad
             assert fwd(s, *args) == sk.SK_ERR_INVALID_ARG, i
-    assert fwd(s, lse=P + 4) == sk.SK_ERR_INVALID_ARG and sk.sk_attention_fwd(None, P, P, P, P, P, P, BIG) == sk.SK_ERR_INVALID_ARG
+    assert fwd(s, lse=P + 4) == fwd(s, rest=P + 8) == sk.SK_ERR_INVALID_ARG and sk.sk_attention_fwd(None, P, P, P, P, P, P, P, BIG) == sk.SK_ERR_INVALID_ARG
     for i in range(9):
         args = [P] * 9
         args[i] = None
@@ -161,14 +162,14 @@ def test_attention_accesses(shape, dtype, e):
     s = attention_shape(*shape, dtype=dtype, q_lengths=buf.new(4 * B), k_lengths=buf.new(4 * B))
     rows, keys = B * Tq * H, B * Tk * Hkv * D * e
     q, k, v = buf.new(rows * D * e), buf.new(keys), buf.new(keys)
-    o, lse = buf.new(rows * D * e, both=True), buf.new(rows * 4, both=True)
+    o, lse, rest = buf.new(rows * D * e, both=True), buf.new(rows * 4, both=True), buf.new(rows * D * e, both=True)
     need = sk.sk_attention_workspace_bytes(s, 0)
-    accesses, launches = traced(lambda: sk.sk_attention_fwd(s, q, k, v, o, lse, buf.new(need, both=True), need))
+    accesses, launches = traced(lambda: sk.sk_attention_fwd(s, q, k, v, o, lse, rest, buf.new(need, both=True), need))
     buf.check(accesses)
     assert 1 <= launches <= 2
     need = sk.sk_attention_workspace_bytes(s, 1)
     grads = buf.new(rows * D * e), buf.new(rows * D * e, write=True), buf.new(keys, write=True), buf.new(keys, write=True)
-    accesses, launches = traced(lambda: sk.sk_attention_bwd(s, q, k, v, o, lse, *grads, buf.new(need, both=True), need))
+    accesses, launches = traced(lambda: sk.sk_attention_bwd(s, q, k, v, o, lse, rest, *grads, buf.new(need, both=True), need))
     buf.check(accesses)
 
 
