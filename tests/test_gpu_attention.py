@@ -248,3 +248,25 @@ def test_replays_from_a_graph(block):
         torch.cuda.synchronize()
         for a, b in zip(out, eager):
             assert torch.equal(a, b), rep
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_offsets_past_32_bits(block, dtype):
+    """A cache whose last keys lie more than 4 GB behind its first, and sequences that far apart, against dense copies of the same numbers."""
+    tokens, apart = 700, 1 << 22 if dtype == torch.float32 else (1 << 22) - 8
+    room = torch.zeros(tokens * apart, dtype=dtype, device="cuda")
+    far = room.view(tokens, apart)[:, :2 * 64].view(1, tokens, 2, 64)
+    far.copy_(_normal(0, (1, tokens, 2, 64), dtype))
+    q, do = _normal(1, (1, 130, 4, 64), dtype), _normal(2, (1, 130, 4, 64), dtype)
+
+    def both(k, v, q):
+        a, b, c = (t.detach().requires_grad_() for t in (q, k, v))
+        o = block.attention(a, b, c, causal=True)
+        return (block.attention(q[:, :1], k, v), o.detach(), *torch.autograd.grad(o, (a, b, c), do))
+
+    assert far.stride(1) * (tokens - 1) * far.element_size() > 1 << 32
+    for x, y in zip(both(far, far, q), both(far.contiguous(), far.contiguous(), q)):
+        assert torch.equal(x, y)
+    batch = room[:(tokens * apart) // 64 // 256 * 64 * 256].view(2, -1)[:, :700 * 128].view(2, 700, 2, 64)      # two sequences half the room apart
+    want = block.attention(q.expand(2, -1, -1, -1), batch.contiguous(), batch.contiguous())
+    assert torch.equal(block.attention(q.expand(2, -1, -1, -1), batch, batch), want)

@@ -103,3 +103,19 @@ def test_refusals(block):
         block.embedding(ids, table[:0])
     with pytest.raises(sk.SkError):
         block.embedding(ids, torch.zeros(5, 12, device="cuda"))
+
+
+def test_tables_past_32_bits(block):
+    """A table of more than 2^32 bytes: its last rows, forward and back."""
+    rows, width = 70000, 32768
+    table = torch.zeros(rows, width, dtype=torch.bfloat16, device="cuda")
+    ids = torch.tensor([rows - 1, 5, rows - 2, rows - 1], device="cuda")
+    table[ids] = _normal(0, (4, width), torch.bfloat16)[[0, 1, 2, 0]]
+    table.requires_grad_()
+    y = block.embedding(ids, table)
+    assert torch.equal(y, table[ids])
+    dy = _normal(1, (4, width), torch.bfloat16)
+    g, = torch.autograd.grad(y, table, dy)
+    assert torch.equal(g[5], dy[1]) and torch.equal(g[rows - 2], dy[2]) and torch.equal(g[rows - 1], (dy[0].float() + dy[3].float()).bfloat16())
+    g[ids] = 0
+    assert not g.any()
