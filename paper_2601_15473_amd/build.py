@@ -19,7 +19,7 @@ OUT_TORCH = os.path.join(HERE, "lib", "_sktorch.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 SOURCES = ["sk_api.hip", "sk_bf16_gemm.hip", "sk_bf16_gemm256.hip", "sk_bf16_few_rows.hip",
            "sk_f32_gemm.hip", "sk_chain.hip", "sk_bwd_narrow.hip",
-           "sk_block_api.hip", "sk_attention.hip", "sk_attention_bf16.hip", "sk_norm_rope.hip", "sk_embedding.hip", "sk_dropout.hip"]
+           "sk_block_api.hip", "sk_attention_f32.hip", "sk_attention_bf16.hip", "sk_norm_rope.hip", "sk_embedding.hip", "sk_dropout.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # packed fp32 VALU forms are kept off on the test machines

@@ -23,19 +23,6 @@ struct Mma<bf16> {
   static constexpr int E = 8;          // values in them
   static constexpr int STEP = 16;      // of the contraction, covered by a fragment
   static __device__ __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-  // Rows row0 .. + 31 of a row-major tile, contraction along its rows' elements
-  static __device__ __forceinline__ Frag along(const bf16* tile, int ld, int row0, int ks, int lane) {
-    return *reinterpret_cast<const Frag*>(tile + (row0 + (lane & 31)) * ld + ks * 16 + (lane >> 5) * 8);
-  }
-  // Columns col0 .. + 31 of it, contraction along rows row0 .. + 31 in the order of of_acc
-  static __device__ __forceinline__ Frag across(const bf16* tile, int ld, int row0, int s, int col0, int lane) {
-    const bf16* p = tile + (row0 + s * 16 + (lane >> 5) * 4 + ((lane & 15) >> 2)) * ld + col0 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * ld));
-    typedef short s16x8 __attribute__((ext_vector_type(8)));
-    const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    return __builtin_bit_cast(Frag, both);
-  }
   static __device__ __forceinline__ Frag of_acc(const f32x16& p, int s) {
     uint4 u;
     u.x = pack_bf16x2(p[8 * s + 0], p[8 * s + 1]);
@@ -50,9 +37,6 @@ struct Mma<bf16> {
     for (int j = 0; j < 8; ++j) s += (float)a[j] * (float)b[j];
     return s;
   }
-  static __device__ __forceinline__ void store4(void* base, int64_t at, float a, float b, float c, float d) {
-    *reinterpret_cast<uint2*>(static_cast<bf16*>(base) + at) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
-  }
 };
 
 template <>
@@ -65,18 +49,17 @@ struct Mma<float> {
     for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
     return c;
   }
+  // Rows row0 .. + 31 of a row-major tile, contraction along its rows' elements
   static __device__ __forceinline__ Frag along(const float* tile, int ld, int row0, int ks, int lane) {
     return *reinterpret_cast<const Frag*>(tile + (row0 + (lane & 31)) * ld + ks * 8 + (lane >> 5) * 4);
   }
+  // Columns col0 .. + 31 of it, contraction along rows row0 .. + 31 in the order of of_acc
   static __device__ __forceinline__ Frag across(const float* tile, int ld, int row0, int s, int col0, int lane) {
     const float* p = tile + (row0 + s * 8 + (lane >> 5) * 4) * ld + col0 + (lane & 31);
     return Frag{p[0], p[ld], p[2 * ld], p[3 * ld]};
   }
   static __device__ __forceinline__ Frag of_acc(const f32x16& p, int s) { return Frag{p[4 * s], p[4 * s + 1], p[4 * s + 2], p[4 * s + 3]}; }
   static __device__ __forceinline__ float dot(Frag a, Frag b) { return a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3]; }
-  static __device__ __forceinline__ void store4(void* base, int64_t at, float a, float b, float c, float d) {
-    *reinterpret_cast<f32x4*>(static_cast<float*>(base) + at) = f32x4{a, b, c, d};
-  }
 };
 
 __device__ __forceinline__ f32x16 zeros() {

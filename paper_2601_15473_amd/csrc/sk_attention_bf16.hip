@@ -761,7 +761,7 @@ hipError_t few(const AttentionArgs& a, FewPlan plan, hipStream_t s) {
   note_attention_inputs(a, 2);
   if (plan.splits == 1) note_attention_fwd(a, 2);
   else note_matrix(a.workspace, 1, bytes, bytes, 1, true);
-  hipError_t e = launch_kernel(kernel_label("attention_few_kernel", {lbl(DP)}).c_str(), Work{4 * pairs(a), 0.0}, attention_few_kernel<DP>,
+  hipError_t e = launch_kernel(DP == 64 ? "attention_few_kernel<64>" : "attention_few_kernel<128>", Work{4 * pairs(a), 0.0}, attention_few_kernel<DP>,
                                
                                dim3((unsigned)((units + plan.xcds - 1) / plan.xcds * plan.xcds * a.kv_heads)), dim3(256), s, a, plan);
   if (e != hipSuccess || plan.splits == 1) return e;
@@ -776,7 +776,7 @@ hipError_t fwd(const AttentionArgs& a, hipStream_t s) {
   if (few_rows(a, plan)) return few<DP>(a, plan, s);
   constexpr int WAVES = 4;
   note_attention_fwd(a, 2);
-  return launch_kernel(kernel_label("attention_fwd_kernel", {lbl(DP), lbl(WAVES)}).c_str(), Work{4 * pairs(a), 0.0}, attention_fwd_kernel<DP, WAVES>,
+  return launch_kernel(DP == 64 ? "attention_fwd_kernel<64, 4>" : "attention_fwd_kernel<128, 4>", Work{4 * pairs(a), 0.0}, attention_fwd_kernel<DP, WAVES>,
                        dim3(groups_of(a, (int64_t)a.q_len * a.group, WAVES * 32)), dim3(WAVES * 64), s, a);
 }
 
@@ -784,11 +784,11 @@ template <int DP>
 hipError_t bwd(const AttentionArgs& a, hipStream_t s) {
   constexpr int WAVES = 4;
   note_attention_dq(a, 2);
-  hipError_t e = launch_kernel(kernel_label("attention_dq_kernel", {lbl(DP), lbl(WAVES)}).c_str(), Work{6 * pairs(a), 0.0}, attention_dq_kernel<DP, WAVES>,
+  hipError_t e = launch_kernel(DP == 64 ? "attention_dq_kernel<64, 4>" : "attention_dq_kernel<128, 4>", Work{6 * pairs(a), 0.0}, attention_dq_kernel<DP, WAVES>,
                                dim3(groups_of(a, (int64_t)a.q_len * a.group, WAVES * 32)), dim3(WAVES * 64), s, a);
   if (e != hipSuccess) return e;
   note_attention_dkv(a, 2);
-  e = launch_kernel(kernel_label("attention_dkv_kernel", {lbl(DP), lbl(WAVES)}).c_str(), Work{8 * pairs(a), 0.0}, attention_dkv_kernel<DP, WAVES>,
+  e = launch_kernel(DP == 64 ? "attention_dkv_kernel<64, 4>" : "attention_dkv_kernel<128, 4>", Work{8 * pairs(a), 0.0}, attention_dkv_kernel<DP, WAVES>,
                        dim3(groups_of(a, a.k_len, WAVES * 32) * a.parts), dim3(WAVES * 64), s, a);
   return e != hipSuccess || a.parts == 1 ? e : launch_attention_sum_parts(a, false, s);
 }

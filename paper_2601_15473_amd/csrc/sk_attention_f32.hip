@@ -1,8 +1,12 @@
-// Attention and its gradients (see sk_attention.h for the operands' layouts).
+// Attention and its gradients in fp32, the accuracy path, and which type's kernels a call goes to (see sk_attention.h for the
+// operands' layouts).
 //
 // Forward, a wave to 32 rows (query, head of the group): s^T = K q^T has a row's scores in its own lane (and the lane 32
-// further), so the running maximum and sum of the softmax are registers; o^T += V^T p^T.  Backward, no
-// atomics: dq by the same walk over the keys with p from lse, dk and dv by a walk over the queries for 32 keys a wave.
+// further), so the running maximum and sum of the softmax are registers; o^T += V^T p^T.  Backward, no atomics: dq by the same walk
+// over the keys with p from lse, dk and dv by a walk over the queries for 32 keys a wave.  Tiles of 32 keys (queries) go through
+// registers into LDS, one at a time: with fp32 products at a sixteenth of the bf16 ones' rate a wave has 4096 cycles of them a tile at 64 features,
+// and the matrix unit is the bound (16 sequences of 512, eight heads of 64: 103 + 137 + 189 us, 70 TFLOP/s of the 14 flops a pair and feature,
+// 90 of what is executed, where the library's product reaches 146).
 #include "sk_attention.h"
 
 namespace sk {
@@ -11,9 +15,9 @@ namespace {
 constexpr int ROWS = 32;   // rows of a staged tile
 
 // Rows row0 .. + 31 of `base` (rows `stride` elements apart, D values each) into LDS, zeros at and past row `rows` and past D.
-template <typename T, int DP>
-__device__ __forceinline__ void stage(T* tile, const T* base, int64_t stride, int row0, int rows, int D, int tid) {
-  typedef Mma<T> M;
+template <int DP>
+__device__ __forceinline__ void stage(float* tile, const float* base, int64_t stride, int row0, int rows, int D, int tid) {
+  typedef Mma<float> M;
   constexpr int PIECES = DP / M::E, LD = DP + M::E;
 #pragma unroll
   for (int i = 0; i < ROWS * PIECES / 256; ++i) {
@@ -25,9 +29,9 @@ __device__ __forceinline__ void stage(T* tile, const T* base, int64_t stride, in
 }
 
 // A lane's row as fragments of a product's second operand: zeros past D and where the row is not there.
-template <typename T, int DP>
-__device__ __forceinline__ void load_row(typename Mma<T>::Frag (&f)[DP / Mma<T>::STEP], const T* row, bool there, int D, int lane) {
-  typedef Mma<T> M;
+template <int DP>
+__device__ __forceinline__ void load_row(typename Mma<float>::Frag (&f)[DP / Mma<float>::STEP], const float* row, bool there, int D, int lane) {
+  typedef Mma<float> M;
 #pragma unroll
   for (int ks = 0; ks < DP / M::STEP; ++ks) {
     const int c = ks * M::STEP + (lane >> 5) * M::E;
@@ -38,15 +42,15 @@ __device__ __forceinline__ void load_row(typename Mma<T>::Frag (&f)[DP / Mma<T>:
 }
 
 // [DP x 32] with a row of the result to a lane, as rows of D values; nothing where `row` is null
-template <typename T, int DP>
-__device__ __forceinline__ void store_row(T* row, const f32x16 (&acc)[DP / 32], float scale, int D, int lane) {
+template <int DP>
+__device__ __forceinline__ void store_row(float* row, const f32x16 (&acc)[DP / 32], float scale, int D, int lane) {
   if (row == nullptr) return;
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const int c = d * 32 + 8 * g + 4 * (lane >> 5);
-      if (c < D) Mma<T>::store4(row, c, acc[d][4 * g] * scale, acc[d][4 * g + 1] * scale, acc[d][4 * g + 2] * scale, acc[d][4 * g + 3] * scale);
+      if (c < D) *reinterpret_cast<f32x4*>(row + c) = f32x4{acc[d][4 * g] * scale, acc[d][4 * g + 1] * scale, acc[d][4 * g + 2] * scale, acc[d][4 * g + 3] * scale};
     }
 }
 
@@ -69,12 +73,12 @@ struct Row {
   }
 };
 
-template <typename T, int DP>
-__global__ __launch_bounds__(256) void attention_fwd_simple_kernel(const AttentionArgs p, int tiles) {
-  typedef Mma<T> M;
+template <int DP>
+__global__ __launch_bounds__(256) void attention_fwd_f32_kernel(const AttentionArgs p, int tiles) {
+  typedef Mma<float> M;
   constexpr int KS = DP / M::STEP, LD = DP + M::E;
-  __shared__ __align__(16) T k_tile[ROWS * LD];
-  __shared__ __align__(16) T v_tile[ROWS * LD];
+  __shared__ __align__(16) float k_tile[ROWS * LD];
+  __shared__ __align__(16) float v_tile[ROWS * LD];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int b, hk, tile;
   locate(p, tiles, b, hk, tile);
@@ -85,18 +89,18 @@ __global__ __launch_bounds__(256) void attention_fwd_simple_kernel(const Attenti
   const int keys = q.seen(r0 / p.group, (r0 + 127) / p.group);
 
   typename M::Frag qf[KS];
-  load_row<T, DP>(qf, static_cast<const T*>(p.q) + b * p.qs[0] + row.i * p.qs[1] + row.h * p.qs[2], row.there && row.i < q.n, p.D, lane);
+  load_row<DP>(qf, static_cast<const float*>(p.q) + b * p.qs[0] + row.i * p.qs[1] + row.h * p.qs[2], row.there && row.i < q.n, p.D, lane);
   f32x16 o[DP / 32];
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) o[d] = zeros();
   float top = -INFINITY, sum = 0.f;
   const float c = p.scale * LOG2E;
-  const T* const kb = static_cast<const T*>(p.k) + b * p.ks[0] + hk * p.ks[2];
-  const T* const vb = static_cast<const T*>(p.v) + b * p.vs[0] + hk * p.vs[2];
+  const float* const kb = static_cast<const float*>(p.k) + b * p.ks[0] + hk * p.ks[2];
+  const float* const vb = static_cast<const float*>(p.v) + b * p.vs[0] + hk * p.vs[2];
   for (int j0 = 0; j0 < keys; j0 += ROWS) {
     __syncthreads();
-    stage<T, DP>(k_tile, kb, p.ks[1], j0, q.m, p.D, tid);
-    stage<T, DP>(v_tile, vb, p.vs[1], j0, q.m, p.D, tid);
+    stage<DP>(k_tile, kb, p.ks[1], j0, q.m, p.D, tid);
+    stage<DP>(v_tile, vb, p.vs[1], j0, q.m, p.D, tid);
     __syncthreads();
     f32x16 s = zeros();
 #pragma unroll
@@ -127,18 +131,18 @@ __global__ __launch_bounds__(256) void attention_fwd_simple_kernel(const Attenti
   }
   sum += other_half(sum);
   if (row.there) {
-    store_row<T, DP>(static_cast<T*>(p.o) + (((int64_t)b * p.q_len + row.i) * p.heads + row.h) * p.D, o, sum == 0.f ? 0.f : 1.f / sum, p.D, lane);
+    store_row<DP>(static_cast<float*>(p.o) + (((int64_t)b * p.q_len + row.i) * p.heads + row.h) * p.D, o, sum == 0.f ? 0.f : 1.f / sum, p.D, lane);
     if (p.lse != nullptr && lane < 32)
       p.lse[((int64_t)b * p.heads + row.h) * p.q_len + row.i] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
   }
 }
 
-template <typename T, int DP>
-__global__ __launch_bounds__(256) void attention_dq_simple_kernel(const AttentionArgs p, int tiles) {
-  typedef Mma<T> M;
+template <int DP>
+__global__ __launch_bounds__(256) void attention_dq_f32_kernel(const AttentionArgs p, int tiles) {
+  typedef Mma<float> M;
   constexpr int KS = DP / M::STEP, LD = DP + M::E;
-  __shared__ __align__(16) T k_tile[ROWS * LD];
-  __shared__ __align__(16) T v_tile[ROWS * LD];
+  __shared__ __align__(16) float k_tile[ROWS * LD];
+  __shared__ __align__(16) float v_tile[ROWS * LD];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int b, hk, tile;
   locate(p, tiles, b, hk, tile);
@@ -152,12 +156,12 @@ __global__ __launch_bounds__(256) void attention_dq_simple_kernel(const Attentio
   typename M::Frag qf[KS], gf[KS];
   const int64_t at = (((int64_t)b * p.q_len + row.i) * p.heads + row.h) * p.D;
   const int64_t stat = ((int64_t)b * p.heads + row.h) * p.q_len + row.i;
-  load_row<T, DP>(qf, static_cast<const T*>(p.q) + b * p.qs[0] + row.i * p.qs[1] + row.h * p.qs[2], counts, p.D, lane);
-  load_row<T, DP>(gf, static_cast<const T*>(p.d_o) + at, counts, p.D, lane);
+  load_row<DP>(qf, static_cast<const float*>(p.q) + b * p.qs[0] + row.i * p.qs[1] + row.h * p.qs[2], counts, p.D, lane);
+  load_row<DP>(gf, static_cast<const float*>(p.d_o) + at, counts, p.D, lane);
   float delta = 0.f;
   {
     typename M::Frag of[KS];
-    load_row<T, DP>(of, static_cast<const T*>(p.o_in) + at, counts, p.D, lane);
+    load_row<DP>(of, static_cast<const float*>(p.o_in) + at, counts, p.D, lane);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) delta -= M::dot(of[ks], gf[ks]);
   }
@@ -172,12 +176,12 @@ __global__ __launch_bounds__(256) void attention_dq_simple_kernel(const Attentio
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) dq[d] = zeros();
   const float c = p.scale * LOG2E;
-  const T* const kb = static_cast<const T*>(p.k) + b * p.ks[0] + hk * p.ks[2];
-  const T* const vb = static_cast<const T*>(p.v) + b * p.vs[0] + hk * p.vs[2];
+  const float* const kb = static_cast<const float*>(p.k) + b * p.ks[0] + hk * p.ks[2];
+  const float* const vb = static_cast<const float*>(p.v) + b * p.vs[0] + hk * p.vs[2];
   for (int j0 = 0; j0 < keys; j0 += ROWS) {
     __syncthreads();
-    stage<T, DP>(k_tile, kb, p.ks[1], j0, q.m, p.D, tid);
-    stage<T, DP>(v_tile, vb, p.vs[1], j0, q.m, p.D, tid);
+    stage<DP>(k_tile, kb, p.ks[1], j0, q.m, p.D, tid);
+    stage<DP>(v_tile, vb, p.vs[1], j0, q.m, p.D, tid);
     __syncthreads();
     f32x16 s = zeros(), g = zeros();
 #pragma unroll
@@ -195,15 +199,15 @@ __global__ __launch_bounds__(256) void attention_dq_simple_kernel(const Attentio
 #pragma unroll
       for (int t = 0; t < 32 / M::STEP; ++t) dq[d] = M::mma(M::across(k_tile, LD, 0, t, d * 32, lane), M::of_acc(s, t), dq[d]);
   }
-  store_row<T, DP>(row.there ? static_cast<T*>(p.dq) + at : nullptr, dq, p.scale, p.D, lane);
+  store_row<DP>(row.there ? static_cast<float*>(p.dq) + at : nullptr, dq, p.scale, p.D, lane);
 }
 
-template <typename T, int DP>
-__global__ __launch_bounds__(256) void attention_dkv_simple_kernel(const AttentionArgs p, int tiles) {
-  typedef Mma<T> M;
+template <int DP>
+__global__ __launch_bounds__(256) void attention_dkv_f32_kernel(const AttentionArgs p, int tiles) {
+  typedef Mma<float> M;
   constexpr int KS = DP / M::STEP, LD = DP + M::E;
-  __shared__ __align__(16) T q_tile[ROWS * LD];
-  __shared__ __align__(16) T g_tile[ROWS * LD];
+  __shared__ __align__(16) float q_tile[ROWS * LD];
+  __shared__ __align__(16) float g_tile[ROWS * LD];
   __shared__ float lse_tile[ROWS], delta_tile[ROWS];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int b, hk, tile;
@@ -218,8 +222,8 @@ __global__ __launch_bounds__(256) void attention_dkv_simple_kernel(const Attenti
   const int i_begin = j0 >= q.m ? q.n : q.causal && j0 - q.shift + 1 > 0 ? (j0 - q.shift + 1) / ROWS * ROWS : 0;
 
   typename M::Frag kf[KS], vf[KS];
-  load_row<T, DP>(kf, static_cast<const T*>(p.k) + b * p.ks[0] + j * p.ks[1] + hk * p.ks[2], there, p.D, lane);
-  load_row<T, DP>(vf, static_cast<const T*>(p.v) + b * p.vs[0] + j * p.vs[1] + hk * p.vs[2], there, p.D, lane);
+  load_row<DP>(kf, static_cast<const float*>(p.k) + b * p.ks[0] + j * p.ks[1] + hk * p.ks[2], there, p.D, lane);
+  load_row<DP>(vf, static_cast<const float*>(p.v) + b * p.vs[0] + j * p.vs[1] + hk * p.vs[2], there, p.D, lane);
   f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = zeros();
@@ -229,16 +233,16 @@ __global__ __launch_bounds__(256) void attention_dkv_simple_kernel(const Attenti
   const int begin = (int)((int64_t)all * part / p.parts), end = (int)((int64_t)all * (part + 1) / p.parts);
   for (int gh = 0; gh < p.group; ++gh) {
     const int h = hk * p.group + gh;
-    const T* const qb = static_cast<const T*>(p.q) + b * p.qs[0] + h * p.qs[2];
-    const T* const gb = static_cast<const T*>(p.d_o) + ((int64_t)b * p.q_len * p.heads + h) * p.D;
+    const float* const qb = static_cast<const float*>(p.q) + b * p.qs[0] + h * p.qs[2];
+    const float* const gb = static_cast<const float*>(p.d_o) + ((int64_t)b * p.q_len * p.heads + h) * p.D;
     const float* const lse = p.lse2 + ((int64_t)b * p.heads + h) * p.q_len;
     const float* const delta = p.delta + ((int64_t)b * p.heads + h) * p.q_len;
     const int from = begin - gh * per_head > 0 ? begin - gh * per_head : 0, to = end - gh * per_head < per_head ? end - gh * per_head : per_head;
     for (int step = from; step < to; ++step) {
       const int i0 = i_begin + step * ROWS;
       __syncthreads();
-      stage<T, DP>(q_tile, qb, p.qs[1], i0, q.n, p.D, tid);
-      stage<T, DP>(g_tile, gb, (int64_t)p.heads * p.D, i0, q.n, p.D, tid);
+      stage<DP>(q_tile, qb, p.qs[1], i0, q.n, p.D, tid);
+      stage<DP>(g_tile, gb, (int64_t)p.heads * p.D, i0, q.n, p.D, tid);
       if (tid < ROWS) {
         lse_tile[tid] = i0 + tid < q.n ? lse[i0 + tid] : INFINITY;
         delta_tile[tid] = i0 + tid < q.n ? delta[i0 + tid] : 0.f;
@@ -269,34 +273,34 @@ __global__ __launch_bounds__(256) void attention_dkv_simple_kernel(const Attenti
   if (p.parts > 1) {
     const int64_t values = (int64_t)p.batch * p.k_len * p.kv_heads * p.D;
     float* const to = p.partial + part * 2 * values + at;
-    store_row<float, DP>(j < p.k_len ? to : nullptr, dk, 1.f, p.D, lane);
-    store_row<float, DP>(j < p.k_len ? to + values : nullptr, dv, 1.f, p.D, lane);
+    store_row<DP>(j < p.k_len ? to : nullptr, dk, 1.f, p.D, lane);
+    store_row<DP>(j < p.k_len ? to + values : nullptr, dv, 1.f, p.D, lane);
     return;
   }
-  store_row<T, DP>(j < p.k_len ? static_cast<T*>(p.dk) + at : nullptr, dk, p.scale, p.D, lane);
-  store_row<T, DP>(j < p.k_len ? static_cast<T*>(p.dv) + at : nullptr, dv, 1.f, p.D, lane);
+  store_row<DP>(j < p.k_len ? static_cast<float*>(p.dk) + at : nullptr, dk, p.scale, p.D, lane);
+  store_row<DP>(j < p.k_len ? static_cast<float*>(p.dv) + at : nullptr, dv, 1.f, p.D, lane);
 }
 
 double pairs(const AttentionArgs& a) { return (double)a.batch * a.q_len * a.heads * a.k_len * a.D; }
 
-template <typename T, int DP>
+template <int DP>
 hipError_t fwd(const AttentionArgs& a, hipStream_t s) {
   const int tiles = ((int64_t)a.q_len * a.group + 127) / 128;
-  note_attention_fwd(a, sizeof(T));
-  return launch_kernel(kernel_label("attention_fwd_simple_kernel", {"float", lbl(DP)}).c_str(),
-                       Work{4 * pairs(a), 0.0}, attention_fwd_simple_kernel<T, DP>, dim3(a.batch * a.kv_heads * tiles), dim3(256), s, a, tiles);
+  note_attention_fwd(a, 4);
+  return launch_kernel(DP == 64 ? "attention_fwd_f32_kernel<64>" : "attention_fwd_f32_kernel<128>",
+                       Work{4 * pairs(a), 0.0}, attention_fwd_f32_kernel<DP>, dim3(a.batch * a.kv_heads * tiles), dim3(256), s, a, tiles);
 }
 
-template <typename T, int DP>
+template <int DP>
 hipError_t bwd(const AttentionArgs& a, hipStream_t s) {
   const int tiles = ((int64_t)a.q_len * a.group + 127) / 128, k_tiles = (a.k_len + 127) / 128;
-  note_attention_dq(a, sizeof(T));
-  hipError_t e = launch_kernel(kernel_label("attention_dq_simple_kernel", {"float", lbl(DP)}).c_str(), Work{6 * pairs(a), 0.0},
-                               attention_dq_simple_kernel<T, DP>, dim3(a.batch * a.kv_heads * tiles), dim3(256), s, a, tiles);
+  note_attention_dq(a, 4);
+  hipError_t e = launch_kernel(DP == 64 ? "attention_dq_f32_kernel<64>" : "attention_dq_f32_kernel<128>", Work{6 * pairs(a), 0.0},
+                               attention_dq_f32_kernel<DP>, dim3(a.batch * a.kv_heads * tiles), dim3(256), s, a, tiles);
   if (e != hipSuccess) return e;
-  note_attention_dkv(a, sizeof(T));
-  e = launch_kernel(kernel_label("attention_dkv_simple_kernel", {"float", lbl(DP)}).c_str(), Work{8 * pairs(a), 0.0},
-                       attention_dkv_simple_kernel<T, DP>, dim3(a.batch * a.kv_heads * k_tiles * a.parts), dim3(256), s, a, k_tiles);
+  note_attention_dkv(a, 4);
+  e = launch_kernel(DP == 64 ? "attention_dkv_f32_kernel<64>" : "attention_dkv_f32_kernel<128>", Work{8 * pairs(a), 0.0},
+                       attention_dkv_f32_kernel<DP>, dim3(a.batch * a.kv_heads * k_tiles * a.parts), dim3(256), s, a, k_tiles);
   return e != hipSuccess || a.parts == 1 ? e : launch_attention_sum_parts(a, true, s);
 }
 
@@ -304,12 +308,12 @@ hipError_t bwd(const AttentionArgs& a, hipStream_t s) {
 
 hipError_t launch_attention_fwd(const AttentionArgs& a, bool f32, hipStream_t s) {
   if (!f32) return launch_attention_fwd_bf16(a, s);
-  return a.D <= 64 ? fwd<float, 64>(a, s) : fwd<float, 128>(a, s);
+  return a.D <= 64 ? fwd<64>(a, s) : fwd<128>(a, s);
 }
 
 hipError_t launch_attention_bwd(const AttentionArgs& a, bool f32, hipStream_t s) {
   if (!f32) return launch_attention_bwd_bf16(a, s);
-  return a.D <= 64 ? bwd<float, 64>(a, s) : bwd<float, 128>(a, s);
+  return a.D <= 64 ? bwd<64>(a, s) : bwd<128>(a, s);
 }
 
 }  // namespace sk
