@@ -39,7 +39,7 @@ extern "C" {
  * and values past m and in queries past n is not used, whatever it is.
  *
  * Limits (else SK_ERR_UNSUPPORTED): head_dim a multiple of 8 up to 128, heads a multiple of
- * kv_heads, token strides up to 2^22, q_len * heads / kv_heads and k_len up to 2^27, and batch * kv_heads times the tiles of 128 rows of
+ * kv_heads, token strides and heads * head_dim up to 2^22, q_len * heads / kv_heads and k_len up to 2^27, and batch * kv_heads times the tiles of 128 rows of
  * either below 2^24.
  */
 typedef struct {

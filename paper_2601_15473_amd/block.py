@@ -249,9 +249,14 @@ def head_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: torch.Tensor, k_w
     Strided views are read in place.  head_dim: a multiple of 8 up to 256; the number of rotated features is a multiple of 8.
     """
     if out is None and _natively():
-        both = _native.head_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
-        if both is not None:
-            return both
+        if q.dim() == 3:
+            both = _native.head_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
+            if both is not None:
+                return both
+        elif q.dim() > 3 and positions.shape == q.shape[:-2] == k.shape[:-2]:
+            both = _native.head_norm_rope(q.flatten(0, -3), k.flatten(0, -3), q_weight, k_weight, cos, sin, positions.reshape(-1), eps, interleaved)
+            if both is not None:
+                return both[0].view(q.shape), both[1].view(k.shape)
     _checked("head_norm_rope", q, q=q, k=k, q_weight=q_weight, k_weight=k_weight)
     D = q.shape[-1]
     if q.dim() < 3 or q.dim() != k.dim() or q.shape[:-2] != k.shape[:-2] or k.shape[-1] != D or q_weight.shape != (D,) or k_weight.shape != (D,):

@@ -43,7 +43,7 @@ sk_status attention_args(const sk_attention_shape* s, AttentionArgs& a) {
     return SK_ERR_INVALID_ARG;
   if (!known(s->dtype) || s->head_dim % 8 != 0 || s->head_dim > 128 || s->heads % s->kv_heads != 0) return SK_ERR_UNSUPPORTED;
   const int group = s->heads / s->kv_heads;
-  if (s->q_len > MOST_ROWS / group || s->k_len > MOST_ROWS || s->batch > MOST_ROWS) return SK_ERR_UNSUPPORTED;
+  if (s->q_len > MOST_ROWS / group || s->k_len > MOST_ROWS || s->batch > MOST_ROWS || (int64_t)s->heads * s->head_dim > MOST_TOKEN_STRIDE) return SK_ERR_UNSUPPORTED;
   const int64_t tiles = (s->q_len * group + 127) / 128 + (s->k_len + 127) / 128;
   if ((double)s->batch * s->kv_heads * tiles > MOST_GROUPS) return SK_ERR_UNSUPPORTED;
   sk_status st = SK_OK;

@@ -163,9 +163,7 @@ struct NormRope : torch::autograd::Function<NormRope> {
     const Tensor &q = t[0], &k = t[1], &wq = t[2], &wk = t[3];
     const c10::DeviceGuard guard(q.device());
     const NormRopeCall c(q, k, t[4], t[6], ctx->saved_data["eps"].toDouble(), ctx->saved_data["interleaved"].toBool());
-    // (a result that nobody used has no gradient: zeros)
-    const Tensor dqo = grads[0].defined() ? made_dense(grads[0]) : at::zeros(q.sizes(), q.options());
-    const Tensor dko = grads[1].defined() ? made_dense(grads[1]) : at::zeros(k.sizes(), q.options());
+    const Tensor dqo = made_dense(grads[0]), dko = made_dense(grads[1]);   // (zeros for a result that nobody used)
     const Tensor dq = at::empty(q.sizes(), q.options()), dk = at::empty(k.sizes(), q.options()), dwq = at::empty(wq.sizes(), q.options()), dwk = at::empty(wk.sizes(), q.options());
     void* const stream = stream_of(q.device());
     const size_t need = sk_norm_rope_workspace_bytes(&c.s);

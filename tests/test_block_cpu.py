@@ -57,7 +57,7 @@ def test_every_declared_symbol_is_exported():
     (dict(batch=0), 1), (dict(q_len=0), 1), (dict(k_len=-1), 1), (dict(kv_heads=0), 1), (dict(head_dim=0), 1), (dict(scale=math.inf), 1), (dict(scale=math.nan), 1),
     (dict(causal=2), 1), (dict(q_strides=(-640, 256, 64)), 1), (dict(k_lengths=P + 2), 1),
     (dict(dtype=7), 2), (dict(head_dim=60), 2), (dict(head_dim=136), 2), (dict(heads=5), 2), (dict(q_strides=(2560, 256, 60)), 2),
-    (dict(k_strides=(1 << 30, 1 << 23, 64)), 2), (dict(v_strides=(1 << 41, 128, 64)), 2), (dict(q_len=1 << 27), 2), (dict(k_len=(1 << 27) + 1), 2),
+    (dict(k_strides=(1 << 30, 1 << 23, 64)), 2), (dict(heads=1 << 17, kv_heads=1 << 17), 2), (dict(v_strides=(1 << 41, 128, 64)), 2), (dict(q_len=1 << 27), 2), (dict(k_len=(1 << 27) + 1), 2),
     (dict(batch=1 << 22, k_strides=(0, 0, 0), v_strides=(0, 0, 0), q_strides=(0, 0, 0)), 2),
 ])
 def test_attention_refusals(change, want):

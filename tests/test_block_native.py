@@ -163,3 +163,55 @@ def test_threads_and_streams(block):
             t.join()
         for i in range(4):
             assert all(torch.equal(a, b) for a, b in zip(got[i], want[i % 2])), i
+
+
+def test_all_of_them_replay_from_a_graph(block):
+    """A training pass of every operator, recorded once: each replay is what the same pass gives eagerly on what the inputs hold then."""
+    T, H, Hkv, D, W = 150, 4, 2, 64, 256
+    ids = torch.randint(0, 300, (T,), generator=torch.Generator().manual_seed(0)).cuda()
+    table, dy = _normal(1, (300, (H + 2 * Hkv) * D)), _normal(2, (T, H * D))
+    w = _normal(3, (D,)), _normal(4, (D,))
+    cos, sin = torch.rand(200, D // 2, device="cuda"), torch.rand(200, D // 2, device="cuda")
+    pos = torch.arange(T, device="cuda")
+    lengths = torch.tensor([T], dtype=torch.int32, device="cuda")
+
+    def step():
+        leaves = [t.detach().requires_grad_() for t in (table, *w)]
+        x = block.embedding(ids, leaves[0], 3.0).view(T, -1, D)
+        q, k = block.head_norm_rope(x[:, :H], x[:, H:H + Hkv], leaves[1], leaves[2], cos, sin, pos)
+        o = block.attention(q[None], k[None], x[None, :, H + Hkv:], lengths, lengths, causal=True)
+        y = block.dropout(o.view(T, -1), 0.2, 9, 1, residual=dy)
+        return (y.detach(), *torch.autograd.grad(y, leaves, dy))
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        out = step()
+    for rep in range(3):
+        ids.copy_(torch.randint(-5, 305, (T,), generator=torch.Generator().manual_seed(10 + rep)))
+        table.copy_(_normal(20 + rep, tuple(table.shape)))
+        lengths.fill_(T - 40 * rep)
+        want = step()
+        for t in out:
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b), rep
+
+
+def test_batches_of_heads_go_natively(block):
+    """[batch, tokens, heads, head_dim]: the native function on its rows, strided slices read in place."""
+    fused = _normal(0, (2, 9, 8, 64))
+    w, pos = _normal(1, (64,)), torch.arange(18, device="cuda").view(2, 9)
+    cos, sin = torch.rand(20, 32, device="cuda"), torch.rand(20, 32, device="cuda")
+    q, k = (t.detach().requires_grad_() for t in (fused[:, :, :4], fused[:, :, 4:6]))
+    a, b = block.head_norm_rope(q, k, w, w, cos, sin, pos)
+    c, d = block.head_norm_rope(fused.view(18, 8, 64)[:, :4], fused.view(18, 8, 64)[:, 4:6], w, w, cos, sin, pos.view(-1))
+    assert torch.equal(a.view(18, 4, 64), c) and torch.equal(b.view(18, 2, 64), d)
+    assert torch.autograd.grad((a, b), (q, k), (a.detach(), b.detach()))[0].shape == q.shape

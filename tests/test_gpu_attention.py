@@ -125,19 +125,22 @@ def test_strided_views(block, dtype):
     _check(block, odd, odd[:, :, :2], odd[:, :, 2:], do)
 
 
-def test_scores_of_all_sizes(block):
-    """Scores that would overflow without the running maximum, rows with one key that takes all, equal scores."""
-    q, k, v, do = _inputs(1, 100, 200, 2, 1, 64, torch.float32)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("heads", [2, 40], ids=["few rows", "many"])
+def test_scores_of_all_sizes(block, heads, dtype):
+    """Scores that would overflow without the running maximum, rows with one key that takes all, equal scores, scales of either sign."""
+    q, k, v, do = _inputs(1, 100, 200, heads, heads // 2, 64, dtype)
     _check(block, q * 40, k * 4, v, do)
     _check(block, q * 0, k, v, do, causal=True)
     _check(block, q, k, v, do, scale=-0.3)
     _check(block, q, k, v, do, scale=0.0)
-    rising = torch.linspace(0, 30, 200, device="cuda")[None, :, None, None] * torch.ones_like(k)   # (every tile raises the maximum)
+    rising = (torch.linspace(0, 30, 200, device="cuda")[None, :, None, None] * torch.ones_like(k)).to(dtype)   # (every tile raises the maximum)
     _check(block, torch.ones_like(q), rising, v, do)
 
 
-def test_not_a_number_where_it_counts(block):
-    q, k, v, _ = _inputs(1, 40, 40, 1, 1, 64, torch.bfloat16)
+@pytest.mark.parametrize("heads", [1, 160], ids=["few rows", "many"])
+def test_not_a_number_where_it_counts(block, heads):
+    q, k, v, _ = _inputs(1, 40, 40, heads, heads, 64, torch.bfloat16)
     k[0, 17] = math.nan
     o = block.attention(q, k, v, causal=True)
     assert torch.isfinite(o[:, :17]).all() and torch.isnan(o[:, 17:]).all()
