@@ -144,4 +144,16 @@ inline void note_attention_dkv(const AttentionArgs& a, int esize) {
   }
 }
 
+// Kernels are built for 32, 64, 96 and 128 features; those behind a head's own are zeros.  Forward and backward passes of 16 sequences of 512, 16 heads
+// of 32 take 91 us on 32 and 108 on 64, of 80 188 on 96 and 203 on 128; four of 2048, 16 heads on 8 of 96, causal: 308 and 362; in fp32, eight
+// of 256, eight heads of 32: 76 and 120, of 80: 178 and 220.
+template <typename Run>
+hipError_t by_width(int D, Run&& run) {
+  if (D <= 32) return run(IntC<32>{});
+  if (D <= 64) return run(IntC<64>{});
+  if (D <= 96) return run(IntC<96>{});
+  return run(IntC<128>{});
+}
+#define SK_LABEL_BY_WIDTH(name, DP) (DP == 32 ? name "<32>" : DP == 64 ? name "<64>" : DP == 96 ? name "<96>" : name "<128>")
+
 }  // namespace sk

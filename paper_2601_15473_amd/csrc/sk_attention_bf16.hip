@@ -166,7 +166,7 @@ template <int DP, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const AttentionArgs p) {
   typedef Tile<DP> L;
   typedef Mma<bf16> M;
-  constexpr int KS = DP / 16, ND = DP / 32, SLOT = 2 * L::BYTES, K_AHEAD = 6, V_AHEAD = 4;
+  constexpr int KS = DP / 16, ND = DP / 32, SLOT = 2 * L::BYTES, K_AHEAD = 2 * KS < 6 ? 2 * KS : 6, V_AHEAD = 4;
   __shared__ __align__(1024) unsigned char smem[2 * SLOT];
   asm volatile("" ::"v"((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem) : "memory");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -247,10 +247,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const Atte
     bf16x8 w[4] = {M::of_acc(s[0], 0), M::of_acc(s[0], 1)};
     pipelined<4 * ND>(f, read, [&](auto ic, bf16x8 a) { constexpr int i = decltype(ic)::value; o[i % ND] = M::mma(a, w[i / ND], o[i % ND]); },
                       [&](auto ic) {   // the second block's weights under the first one's products
-                        constexpr int i = decltype(ic)::value, EACH = 16 / (2 * ND);
+                        constexpr int i = decltype(ic)::value;
                         if constexpr (i < 2 * ND) {
 #pragma unroll
-                          for (int r = i * EACH; r < (i + 1) * EACH; ++r) s[1][r] = sm.weigh(s[1][r], factor);
+                          for (int r = 16 * i / (2 * ND); r < 16 * (i + 1) / (2 * ND); ++r) s[1][r] = sm.weigh(s[1][r], factor);
                           if constexpr (i == ND - 1) w[2] = M::of_acc(s[1], 0);
                           if constexpr (i == 2 * ND - 1) w[3] = M::of_acc(s[1], 1);
                         }
@@ -589,7 +589,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dkv_kernel(const Atte
   typedef Tile<DP> L;
   typedef Mma<bf16> M;
   constexpr int KS = DP / 16, ND = DP / 32, STATS = 2 * L::BYTES, SLOT = STATS + 1024;
-  constexpr int APART = DP > 64 ? 1 : 0;   // fragments of v that lie in LDS, a lane's own to read: all of them in registers are four too many
+  constexpr int APART = DP > 96 ? 1 : 0;   // fragments of v that lie in LDS, a lane's own to read: all of them in registers are four too many
   __shared__ __align__(1024) unsigned char smem[2 * SLOT + WAVES * APART * 1024];
   asm volatile("" ::"v"((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem) : "memory");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -761,8 +761,7 @@ hipError_t few(const AttentionArgs& a, FewPlan plan, hipStream_t s) {
   note_attention_inputs(a, 2);
   if (plan.splits == 1) note_attention_fwd(a, 2);
   else note_matrix(a.workspace, 1, bytes, bytes, 1, true);
-  hipError_t e = launch_kernel(DP == 64 ? "attention_few_kernel<64>" : "attention_few_kernel<128>", Work{4 * pairs(a), 0.0}, attention_few_kernel<DP>,
-                               
+  hipError_t e = launch_kernel(SK_LABEL_BY_WIDTH("attention_few_kernel", DP), Work{4 * pairs(a), 0.0}, attention_few_kernel<DP>,
                                dim3((unsigned)((units + plan.xcds - 1) / plan.xcds * plan.xcds * a.kv_heads)), dim3(256), s, a, plan);
   if (e != hipSuccess || plan.splits == 1) return e;
   note_matrix(a.workspace, 1, bytes, bytes, 1, false);
@@ -776,7 +775,7 @@ hipError_t fwd(const AttentionArgs& a, hipStream_t s) {
   if (few_rows(a, plan)) return few<DP>(a, plan, s);
   constexpr int WAVES = 4;
   note_attention_fwd(a, 2);
-  return launch_kernel(DP == 64 ? "attention_fwd_kernel<64, 4>" : "attention_fwd_kernel<128, 4>", Work{4 * pairs(a), 0.0}, attention_fwd_kernel<DP, WAVES>,
+  return launch_kernel(SK_LABEL_BY_WIDTH("attention_fwd_kernel", DP), Work{4 * pairs(a), 0.0}, attention_fwd_kernel<DP, WAVES>,
                        dim3(groups_of(a, (int64_t)a.q_len * a.group, WAVES * 32)), dim3(WAVES * 64), s, a);
 }
 
@@ -784,11 +783,11 @@ template <int DP>
 hipError_t bwd(const AttentionArgs& a, hipStream_t s) {
   constexpr int WAVES = 4;
   note_attention_dq(a, 2);
-  hipError_t e = launch_kernel(DP == 64 ? "attention_dq_kernel<64, 4>" : "attention_dq_kernel<128, 4>", Work{6 * pairs(a), 0.0}, attention_dq_kernel<DP, WAVES>,
+  hipError_t e = launch_kernel(SK_LABEL_BY_WIDTH("attention_dq_kernel", DP), Work{6 * pairs(a), 0.0}, attention_dq_kernel<DP, WAVES>,
                                dim3(groups_of(a, (int64_t)a.q_len * a.group, WAVES * 32)), dim3(WAVES * 64), s, a);
   if (e != hipSuccess) return e;
   note_attention_dkv(a, 2);
-  e = launch_kernel(DP == 64 ? "attention_dkv_kernel<64, 4>" : "attention_dkv_kernel<128, 4>", Work{8 * pairs(a), 0.0}, attention_dkv_kernel<DP, WAVES>,
+  e = launch_kernel(SK_LABEL_BY_WIDTH("attention_dkv_kernel", DP), Work{8 * pairs(a), 0.0}, attention_dkv_kernel<DP, WAVES>,
                        dim3(groups_of(a, a.k_len, WAVES * 32) * a.parts), dim3(WAVES * 64), s, a);
   return e != hipSuccess || a.parts == 1 ? e : launch_attention_sum_parts(a, false, s);
 }
@@ -815,7 +814,7 @@ size_t attention_fwd_bytes_bf16(const AttentionArgs& a) {
   FewPlan plan;
   return few_rows(a, plan) ? few_bytes(a, plan) : 0;
 }
-hipError_t launch_attention_fwd_bf16(const AttentionArgs& a, hipStream_t s) { return a.D <= 64 ? fwd<64>(a, s) : fwd<128>(a, s); }
+hipError_t launch_attention_fwd_bf16(const AttentionArgs& a, hipStream_t s) { return by_width(a.D, [&](auto dp) { return fwd<decltype(dp)::value>(a, s); }); }
 hipError_t launch_attention_sum_parts(const AttentionArgs& a, bool f32, hipStream_t s) {
   const int64_t values = (int64_t)a.batch * a.k_len * a.kv_heads * a.D;
   note_matrix(a.partial, 2 * a.parts, values, values, 4, false);
@@ -840,6 +839,6 @@ int attention_parts(const AttentionArgs& a, bool f32) {
   return parts < 1 ? 1 : parts > 16 ? 16 : (int)parts;
 }
 
-hipError_t launch_attention_bwd_bf16(const AttentionArgs& a, hipStream_t s) { return a.D <= 64 ? bwd<64>(a, s) : bwd<128>(a, s); }
+hipError_t launch_attention_bwd_bf16(const AttentionArgs& a, hipStream_t s) { return by_width(a.D, [&](auto dp) { return bwd<decltype(dp)::value>(a, s); }); }
 
 }  // namespace sk

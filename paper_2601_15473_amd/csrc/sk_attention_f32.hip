@@ -287,7 +287,7 @@ template <int DP>
 hipError_t fwd(const AttentionArgs& a, hipStream_t s) {
   const int tiles = ((int64_t)a.q_len * a.group + 127) / 128;
   note_attention_fwd(a, 4);
-  return launch_kernel(DP == 64 ? "attention_fwd_f32_kernel<64>" : "attention_fwd_f32_kernel<128>",
+  return launch_kernel(SK_LABEL_BY_WIDTH("attention_fwd_f32_kernel", DP),
                        Work{4 * pairs(a), 0.0}, attention_fwd_f32_kernel<DP>, dim3(a.batch * a.kv_heads * tiles), dim3(256), s, a, tiles);
 }
 
@@ -295,11 +295,11 @@ template <int DP>
 hipError_t bwd(const AttentionArgs& a, hipStream_t s) {
   const int tiles = ((int64_t)a.q_len * a.group + 127) / 128, k_tiles = (a.k_len + 127) / 128;
   note_attention_dq(a, 4);
-  hipError_t e = launch_kernel(DP == 64 ? "attention_dq_f32_kernel<64>" : "attention_dq_f32_kernel<128>", Work{6 * pairs(a), 0.0},
+  hipError_t e = launch_kernel(SK_LABEL_BY_WIDTH("attention_dq_f32_kernel", DP), Work{6 * pairs(a), 0.0},
                                attention_dq_f32_kernel<DP>, dim3(a.batch * a.kv_heads * tiles), dim3(256), s, a, tiles);
   if (e != hipSuccess) return e;
   note_attention_dkv(a, 4);
-  e = launch_kernel(DP == 64 ? "attention_dkv_f32_kernel<64>" : "attention_dkv_f32_kernel<128>", Work{8 * pairs(a), 0.0},
+  e = launch_kernel(SK_LABEL_BY_WIDTH("attention_dkv_f32_kernel", DP), Work{8 * pairs(a), 0.0},
                        attention_dkv_f32_kernel<DP>, dim3(a.batch * a.kv_heads * k_tiles * a.parts), dim3(256), s, a, k_tiles);
   return e != hipSuccess || a.parts == 1 ? e : launch_attention_sum_parts(a, true, s);
 }
@@ -308,12 +308,12 @@ hipError_t bwd(const AttentionArgs& a, hipStream_t s) {
 
 hipError_t launch_attention_fwd(const AttentionArgs& a, bool f32, hipStream_t s) {
   if (!f32) return launch_attention_fwd_bf16(a, s);
-  return a.D <= 64 ? fwd<64>(a, s) : fwd<128>(a, s);
+  return by_width(a.D, [&](auto dp) { return fwd<decltype(dp)::value>(a, s); });
 }
 
 hipError_t launch_attention_bwd(const AttentionArgs& a, bool f32, hipStream_t s) {
   if (!f32) return launch_attention_bwd_bf16(a, s);
-  return a.D <= 64 ? bwd<64>(a, s) : bwd<128>(a, s);
+  return by_width(a.D, [&](auto dp) { return bwd<decltype(dp)::value>(a, s); });
 }
 
 }  // namespace sk

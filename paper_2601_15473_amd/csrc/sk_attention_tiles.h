@@ -1,7 +1,7 @@
 // Tiles of 64 rows (keys, or queries; 32 where a wave has one to itself) in LDS that both kinds of MFMA operand are read from: along the features
 // (scores) and across the rows (what is summed over them).
 //
-// A tile of DP features is DP / 64 panels of [64 rows][64 features], 128 bytes a row.  It goes from global memory straight
+// A tile of DP features is DP / 64 panels (rounded up) of [64 rows][64 features], 128 bytes a row.  It goes from global memory straight
 // into LDS, eight rows an instruction, and its 16-byte pieces are XOR-swizzled by row so that neither read conflicts: along the
 // features 16 lanes read one piece of 16 consecutive rows (rows 2 i and 2 i + 1 share the 64 banks: the eight pairs
 // need eight different pieces), across them 32 lanes read four pieces of four consecutive rows (rows i and i + 2
@@ -16,7 +16,7 @@ constexpr int TILE_ROWS = 64;
 
 template <int DP, int ROWS = TILE_ROWS>
 struct Tile {
-  static constexpr int PANELS = DP / 64, PANEL_BYTES = ROWS * 128, BYTES = PANELS * PANEL_BYTES;
+  static constexpr int PANELS = (DP + 63) / 64, PANEL_BYTES = ROWS * 128, BYTES = PANELS * PANEL_BYTES;
   static constexpr int INSTRUCTIONS = BYTES / 1024;   // a wave's load fills eight rows of a panel
   static __device__ __forceinline__ int swizzle(int row) {
     const int t = (row >> 1) & 7;
