@@ -1,4 +1,7 @@
-// Token embedding with scaling, and its gradient by sorted tokens.
+// Token embedding with scaling, and its gradient by sorted tokens: y_t = scale table[id_t], dtable_v = scale sum of dY_t over the t with
+// id_t = v, in the order of t (no atomics: the same bits every run).  Both are bound by memory: 16384 tokens of 4096 features in bf16 forward 40 us
+// (268 MB moved, fewer read where tokens repeat), on 65536 rows the gradient 77 + 69 + 7 us, 537 of whose 730 MB are its zeros: they leave at 6.9 TB/s, but
+// half of them only as far as the Infinity Cache, which the rows of dY then push them out of.
 //
 // The gradient in three launches: (1) a work-group sorts up to 16384 tokens by id in LDS, while the others fill the
 // gradient with zeros; (more tokens: sorted runs, put into one order by a second launch); (2) every run of 16 or 32 sorted tokens is
@@ -231,7 +234,8 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbeddingArgs 
   }
 }
 
-// The id that begins in a chunk and goes on behind it: its chunks' sums, dealt over four waves and joined in their order.
+// The id that begins in a chunk and goes on behind it: its chunks' sums, dealt over four waves and joined in their order.  Most chunks have
+// none: the launch's own time and two trips to memory (16384 tokens of 4096 features 7 us, 11 with the id's end looked for by halves).
 template <typename T>
 __global__ __launch_bounds__(256) void embedding_join_kernel(const EmbeddingArgs p, int blocks, int run) {
   __shared__ float4 sums[4][64];
@@ -241,7 +245,12 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(const EmbeddingArgs
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int column = ((int)(blockIdx.x - chunk * blocks) * 64 + lane) * 4;
   const bool there = column < p.width;
-  const int64_t last = (next + keys_below(p.keys + next, p.tokens - next, key, true) - 1) / run;
+  int64_t last = chunk;   // the id's last chunk: those that begin with it, a lane to each
+  for (uint64_t same = ~0ull; same == ~0ull;) {
+    const int64_t at = (last + 1 + lane) * run;
+    same = __ballot(at < p.tokens && p.keys[at < p.tokens ? at : 0] == key);
+    last += same == ~0ull ? 64 : __builtin_ctzll(~same);
+  }
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   if (there) {
 #pragma unroll 4
