@@ -161,7 +161,12 @@ __device__ __forceinline__ void read_first(bf16x8 (&f)[AHEAD], Read&& read) {
 }
 
 // Forward: WAVES x 32 rows a work-group, tiles of 64 keys and values through a ring of two slots in LDS, asked for a tile
-// ahead; one barrier a tile.
+// ahead; one barrier a tile.  s^T = K q^T, p = exp2(s c - m), o^T = o^T exp2(m' - m) + V^T p^T, in the end o / sum p; a key tile is read by all
+// four waves.  At 128 features two waves a SIMD, one's exponentials under the other's products: 16384 tokens in sequences of 4096, 32 heads on 8,
+// causal, 543 us = 1010 TFLOP/s of the 4 flops a pair that is seen and feature, the matrix unit 58 % busy at the clock that the power limit
+// leaves (zeros for inputs take two thirds as long).  At 64 features four waves a SIMD and the vector unit is the bound (65 % busy, the matrix unit 32 %:
+// a score costs it a maximum, a multiplication, an exponential at a quarter of the rate, an addition and half a rounding, and only two products of 64):
+// 16 sequences of 512, 16 heads, 29 us, of which the rows' way out, 33 MB behind one round of work-groups, is about 7.
 template <int DP, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const AttentionArgs p) {
   typedef Tile<DP> L;
@@ -266,7 +271,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const Atte
 }
 
 // Forward for few rows: 32 rows a work-group, a range of the keys, of which every wave takes every fourth tile of 32
-// by itself (no barrier; 64 KB of LDS, so that eight waves a CU have 8 to 16 KB each on their way), joined through LDS.  With several
+// by itself (no barrier; 64 KB of LDS, so that eight waves a CU have 8 to 16 KB each on their way), joined through LDS.  Bound by reading: eight
+// sequences of 0 to 16384 keys, one query, 64 heads on 8 of 128, 268 MB: 67 us = 4.0 TB/s, what a sum over 2 GB reaches here too (51 where the Infinity Cache
+// has half of it), and 5 of the join.  Ranges twice and half as long, and grids of three and four work-groups a CU, were level or slower.  With several
 // ranges the sums, their maxima and the weights' sums go to the workspace and attention_join_kernel puts them together.
 template <int DP>
 __global__ __launch_bounds__(256, 2) void attention_few_kernel(const AttentionArgs p, FewPlan plan) {
@@ -278,7 +285,7 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(const AttentionAr
   asm volatile("" ::"v"((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem) : "memory");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // A range's heads, whose keys lie in the same stretch of memory, go to one XCD, the sequences' ranges to the XCDs in turn (another turn each
-  // range, so that no XCD has one sequence): 68 us where heads dealt over the XCDs took 71, as above.
+  // range, so that no XCD has one sequence): 68 us where heads dealt over the XCDs took 71, on the keys above.
   const int local = blockIdx.x / plan.xcds, turn = local / p.kv_heads, hk = local - turn * p.kv_heads, unit = turn * plan.xcds + blockIdx.x - local * plan.xcds;
   const int id = unit / p.batch;
   if (id >= plan.row_tiles * plan.splits) return;
@@ -447,7 +454,10 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs
   if (p.lse != nullptr && lane == 0) p.lse[((int64_t)b * p.heads + out.h) * p.q_len + out.i] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * LN2;
 }
 
-// dq: the forward pass's walk over the keys, with the probabilities from lse.  Leaves lse log2(e) and minus sum_d dO o of every row for dk and dv.
+// dq: the forward pass's walk over the keys, with the probabilities from lse: p = exp2(s c - lse2), dp = dO v, ds = p (dp - D), dq = scale ds k, where
+// -D = -sum dO o is what dp's accumulators begin with, so the subtraction is the product's.  726 us on the forward pass's 16384 tokens (1140
+// TFLOP/s of what is executed and seen, the matrix unit 67 % busy), 41 on its 16 sequences of 512 (a third of it the 117 MB that go in and out; 32 keys at a time
+// within the registers of four waves a SIMD were level there and 10 % slower at 32 features).  Leaves lse log2(e) and minus sum_d dO o of every row for dk and dv.
 template <int DP, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const AttentionArgs p) {
   typedef Tile<DP> L;
@@ -582,8 +592,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
 
 // dk and dv: 32 keys a wave, their sums in registers over all queries of all heads that share them; tiles of 64 queries and their
 // dO through the ring, with what dq's kernel left of their rows.  Two waves a SIMD, so that one's exponentials run under the other's
-// products, is what the registers are kept to: one wave of 330 took 1572 us where two take 1098 (16384 tokens in sequences of 4096, 32 heads on 8 of 128,
-// causal).  256 keys a work-group instead of 128 load half as much for 1 % there, and cost 17 to 25 % at 128 to 512 keys of 64.
+// products, is what the registers are kept to: one wave of 330 took 1572 us where two take 1081 (16384 tokens in sequences of 4096, 32 heads on 8 of 128,
+// causal; the matrix unit 59 % busy).  256 keys a work-group instead of 128 load half as much for 1 % there, and cost 17 to 25 % at 128 to 512 keys of 64.
 template <int DP, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void attention_dkv_kernel(const AttentionArgs p) {
   typedef Tile<DP> L;

@@ -1,4 +1,8 @@
-// Dropout by a counter-based generator, with a residual added in the same pass.
+// Dropout by a counter-based generator, with a residual added in the same pass: y = residual + x keep / (1 - p'), where p' = drop / 65536 and keep
+// is whether the value's 16 bits are not below drop.  Nothing is stored for the gradient, which is the same call on dY without a residual.
+//
+// Bound by memory: 16383 tokens of 4096 in bf16, 403 MB, 77 us = 5.2 TB/s, without a residual 44 us = 6.1 (what was just written is read
+// out of the Infinity Cache in part).
 //
 // Eight values a lane, one counter: Philox 4x32 with ten rounds (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as
 // 1, 2, 3, 2011) makes four 32-bit words of (counter, key), used as eight of 16 bits, since a drop rate needs no more than that and the generator's
