@@ -128,7 +128,8 @@ inline void note_attention_dq(const AttentionArgs& a, int esize) {
   note_matrix(a.lse, 1, rows_of(a), rows_of(a), 4, false);
   note_matrix(a.lse2, 1, rows_of(a), rows_of(a), 4, true);
   note_matrix(a.delta, 1, rows_of(a), rows_of(a), 4, true);
-  note_matrix(a.dq, rows_of(a), a.D, a.D, esize, true);
+  if (a.q_shares > 1) note_matrix(a.q_partial, a.q_shares * rows_of(a), a.D, a.D, 4, true);
+  else note_matrix(a.dq, rows_of(a), a.D, a.D, esize, true);
 }
 inline void note_attention_dkv(const AttentionArgs& a, int esize) {
   note_attention_inputs(a, esize);

@@ -5,10 +5,10 @@
 namespace sk {
 namespace {
 
-// Few rows: how the keys are cut, and where the ranges' results are.
-struct FewPlan {
-  int row_tiles, splits, chunk;   // tiles of 32 rows; ranges of `chunk` keys
-  int xcds;                       // that sequences' ranges are dealt over
+// How the keys are cut where rows alone do not fill the chip, and where the ranges' results are.
+struct RangePlan {
+  int row_tiles, splits, chunk;   // few rows: tiles of 32 rows, ranges of `chunk` keys; 0: each tile of rows has its keys in `splits` even shares
+  int xcds;                       // few rows: that sequences' ranges are dealt over
   float *sums, *stats;            // [heads][splits][rows][D], [heads][splits][rows][2]
 };
 
@@ -30,6 +30,17 @@ struct Row {
     i = r / p.group;
     h = hk * p.group + (r - i * p.group);
     there = i < p.q_len;
+  }
+};
+
+// Share `share` of `shares` of a tile of rows' keys, by whole tiles (none where there are fewer tiles than shares).
+struct Keys {
+  int begin, end;
+  __device__ __forceinline__ Keys(int keys, int share, int shares) {
+    const int tiles = (keys + TILE_ROWS - 1) / TILE_ROWS;
+    begin = tiles * share / shares * TILE_ROWS;
+    end = tiles * (share + 1) / shares * TILE_ROWS;
+    end = end < keys ? end : keys;
   }
 };
 
@@ -108,6 +119,18 @@ __device__ __forceinline__ void store_row_and_rest(bf16* row, bf16* rest, bool t
   store_row<DP>(rest, there, left, 1.f, D, lane);
 }
 
+// The same as fp32 sums, not scaled.
+template <int DP>
+__device__ __forceinline__ void store_sums(float* row, const f32x16 (&acc)[DP / 32], int D, int lane) {
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int c = d * 32 + 8 * g + 4 * (lane >> 5);
+      if (c < D) *reinterpret_cast<f32x4*>(row + c) = f32x4{acc[d][4 * g], acc[d][4 * g + 1], acc[d][4 * g + 2], acc[d][4 * g + 3]};
+    }
+}
+
 // Running softmax of a lane's row (the lane 32 further has the row's other keys): the maximum and its own keys' sum.
 struct Softmax {
   float top = -INFINITY, sum = 0.f, base = 0.f;
@@ -160,15 +183,15 @@ __device__ __forceinline__ void read_first(bf16x8 (&f)[AHEAD], Read&& read) {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// Forward: WAVES x 32 rows a work-group, tiles of 64 keys and values through a ring of two slots in LDS, asked for a tile
+// Forward: WAVES x 32 rows a work-group (with SHARES a share of their keys, whose sums attention_join_kernel puts together), tiles of 64 keys and values through a ring of two slots in LDS, asked for a tile
 // ahead; one barrier a tile.  s^T = K q^T, p = exp2(s c - m), o^T = o^T exp2(m' - m) + V^T p^T, in the end o / sum p; a key tile is read by all
 // four waves.  At 128 features two waves a SIMD, one's exponentials under the other's products: 16384 tokens in sequences of 4096, 32 heads on 8,
 // causal, 543 us = 1010 TFLOP/s of the 4 flops a pair that is seen and feature, the matrix unit 58 % busy at the clock that the power limit
 // leaves (zeros for inputs take two thirds as long).  At 64 features four waves a SIMD and the vector unit is the bound (65 % busy, the matrix unit 32 %:
 // a score costs it a maximum, a multiplication, an exponential at a quarter of the rate, an addition and half a rounding, and only two products of 64):
 // 16 sequences of 512, 16 heads, 29 us, of which the rows' way out, 33 MB behind one round of work-groups, is about 7.
-template <int DP, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const AttentionArgs p) {
+template <int DP, int WAVES, bool SHARES>
+__global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const AttentionArgs p, RangePlan plan) {
   typedef Tile<DP> L;
   typedef Mma<bf16> M;
   constexpr int KS = DP / 16, ND = DP / 32, SLOT = 2 * L::BYTES, K_AHEAD = 2 * KS < 6 ? 2 * KS : 6, V_AHEAD = 4;
@@ -177,6 +200,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const Atte
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int b, hk, tile;
   locate(p, b, hk, tile);
+  const int share = SHARES ? tile % plan.splits : 0;
+  if (SHARES) tile /= plan.splits;
   if (p.causal) tile = (p.q_len * p.group + WAVES * 32 - 1) / (WAVES * 32) - 1 - tile;
   const Sequence q(p, b);
   const int r0 = tile * WAVES * 32;
@@ -184,6 +209,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const Atte
   const int limit = row.there ? q.limit(row.i) : 0;
   // the work-group's keys, and the wave's: all rows see those before `common`, none those from `most` on
   const int keys = q.seen(r0 / p.group, (r0 + WAVES * 32 - 1) / p.group);
+  const Keys range(keys, share, SHARES ? plan.splits : 1);
   const int first_i = (r0 + wave * 32) / p.group, last_i = (r0 + wave * 32 + 31) / p.group;
   const int most = __builtin_amdgcn_readfirstlane(first_i < p.q_len ? q.seen(first_i, last_i) : 0);
   const int common = __builtin_amdgcn_readfirstlane(last_i < q.n ? q.limit(first_i) : 0);
@@ -202,18 +228,18 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const Atte
   const bf16* const vb = static_cast<const bf16*>(p.v) + b * p.vs[0] + hk * p.vs[2];
   const typename L::template Loader<WAVES> load_k(wave, lane, p.ks[1], p.D), load_v(wave, lane, p.vs[1], p.D);
   const unsigned k_at = L::along_address(lane), v_at = L::across_address(lane);
-  Walk<TILE_ROWS> walk_k(kb, p.ks[1], 0, p.D), walk_v(vb, p.vs[1], 0, p.D);
-  if (keys > 0) {
-    load_k.load(walk_k.window(q.m), 0u, wave);
-    load_v.load(walk_v.window(q.m), L::BYTES, wave);
+  Walk<TILE_ROWS> walk_k(kb, p.ks[1], range.begin, p.D), walk_v(vb, p.vs[1], range.begin, p.D);
+  if (range.begin < range.end) {
+    load_k.load(walk_k.window(q.m - range.begin), 0u, wave);
+    load_v.load(walk_v.window(q.m - range.begin), L::BYTES, wave);
   }
 
   unsigned slot = 0;
-  for (int j0 = 0; j0 < keys; j0 += TILE_ROWS, slot ^= SLOT) {
+  for (int j0 = range.begin; j0 < range.end; j0 += TILE_ROWS, slot ^= SLOT) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // this tile is there, and nobody reads the other slot
     walk_k.skip(TILE_ROWS);
     walk_v.skip(TILE_ROWS);
-    const int left = j0 + TILE_ROWS < keys ? q.m - j0 - TILE_ROWS : 0;   // (behind the last tile nothing is fetched)
+    const int left = j0 + TILE_ROWS < range.end ? q.m - j0 - TILE_ROWS : 0;   // (behind the last tile nothing is fetched)
     const u32x4 next_k = walk_k.window(left), next_v = walk_v.window(left);
     // The next tile is asked for an instruction at a time under the scores' products: its 32 KB are half a thousand cycles of the CU's path
     // from memory, in which a wave that asked for all of its own at once would do nothing else.
@@ -263,6 +289,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const Atte
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing may land in LDS any more)
   const float sum = sm.sum + other_half(sm.sum);
+  if (SHARES) {
+    if (!row.there) return;
+    const int64_t slot = ((int64_t)(b * p.kv_heads + hk) * plan.splits + share) * p.q_len * p.group + r0 + wave * 32 + (lane & 31);
+    store_sums<DP>(plan.sums + slot * p.D, o, p.D, lane);
+    if (lane < 32) *reinterpret_cast<float2*>(plan.stats + slot * 2) = make_float2(sm.top, sum);
+    return;
+  }
   const int64_t at = (((int64_t)b * p.q_len + row.i) * p.heads + row.h) * p.D;
   store_row_and_rest<DP>(static_cast<bf16*>(p.o) + at, p.o_rest != nullptr ? static_cast<bf16*>(p.o_rest) + at : nullptr, row.there, o, sum == 0.f ? 0.f : 1.f / sum, p.D,
                          lane);
@@ -276,7 +309,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const Atte
 // has half of it), and 5 of the join.  Ranges twice and half as long, and grids of three and four work-groups a CU, were level or slower.  With several
 // ranges the sums, their maxima and the weights' sums go to the workspace and attention_join_kernel puts them together.
 template <int DP>
-__global__ __launch_bounds__(256, 2) void attention_few_kernel(const AttentionArgs p, FewPlan plan) {
+__global__ __launch_bounds__(256, 2) void attention_few_kernel(const AttentionArgs p, RangePlan plan) {
   typedef Tile<DP, 32> L;
   typedef Mma<bf16> M;
   constexpr int KS = DP / 16, ND = DP / 32, LD = DP + 4, EACH = L::INSTRUCTIONS;
@@ -400,65 +433,69 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(const AttentionAr
   }
 }
 
-// A wave to a row: the ranges' sums in order, each brought to the largest maximum.  64 ranges at a time: a lane to a range's maximum and
-// sum, then a lane to two features with eight ranges on their way.
-__global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs p, FewPlan plan) {
-  const int lane = threadIdx.x & 63, rows = p.q_len * p.group, bh = blockIdx.y;
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
+// The ranges' sums of a row in order, each brought to the largest maximum: a thread to four features, eight ranges on their way.
+__global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs p, RangePlan plan) {
+  const int rows = p.q_len * p.group, per = p.D / 4, bh = blockIdx.y;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int r = (int)(id / per), c = (int)(id - (int64_t)r * per) * 4;
   if (r >= rows) return;
   const int b = bh / p.kv_heads, hk = bh - b * p.kv_heads;
-  const Sequence q(p, b);
-  const int r0 = r / 32 * 32, last = r0 + 31 < rows ? r0 + 31 : rows - 1;
-  const int keys = q.seen(r0 / p.group, last / p.group);
-  const int splits = keys > 0 ? (keys + plan.chunk - 1) / plan.chunk : 1;
-  const int c = lane * 2;
-  float top = -INFINITY, total = 0.f, x = 0.f, y = 0.f;
-  for (int s0 = 0; s0 < splits; s0 += 64) {
-    const int n = splits - s0 < 64 ? splits - s0 : 64;
-    const int64_t slot = ((int64_t)bh * plan.splits + s0) * rows + r;
-    const float2 stat = lane < n ? *reinterpret_cast<const float2*>(plan.stats + (slot + (int64_t)lane * rows) * 2) : make_float2(-INFINITY, 0.f);
-    float m = fmaxf(top, stat.x);
+  int splits = plan.splits;
+  if (plan.chunk > 0) {   // only those that the row's tile has
+    const Sequence q(p, b);
+    const int r0 = r / 32 * 32, last = r0 + 31 < rows ? r0 + 31 : rows - 1;
+    const int keys = q.seen(r0 / p.group, last / p.group);
+    splits = keys > 0 ? (keys + plan.chunk - 1) / plan.chunk : 1;
+  }
+  const int64_t first = (int64_t)bh * plan.splits * rows + r;
+  const float2* const stats = reinterpret_cast<const float2*>(plan.stats) + first;
+  const float* const sums = plan.sums + first * p.D + c;
+  float top = -INFINITY, total = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < splits; s0 += 8) {
+    float2 stat[8];
+    f32x4 x[8];
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+    for (int u = 0; u < 8; ++u) {
+      const int64_t at = (int64_t)(s0 + u < splits ? s0 + u : s0) * rows;
+      stat[u] = stats[at];
+      x[u] = *reinterpret_cast<const f32x4*>(sums + at * p.D);
+    }
+    float m = top;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) m = fmaxf(m, stat[u].x);
     const float base = m == -INFINITY ? 0.f : m, before = __builtin_amdgcn_exp2f(top - base);
-    const float keep = __builtin_amdgcn_exp2f(stat.x - base);
-    float sum = stat.y * keep;
+    total *= before;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-    total = total * before + sum;
-    x *= before;
-    y *= before;
+    for (int i = 0; i < 4; ++i) v[i] *= before;
     top = m;
-    const float* const sums = plan.sums + slot * p.D + (c < p.D ? c : 0);
-    for (int s = 0; s < n; s += 8) {
-      float2 v[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const float2*>(sums + (int64_t)(s + u < n ? s + u : s) * rows * p.D);
+    for (int u = 0; u < 8; ++u) {
+      const float keep = s0 + u < splits ? __builtin_amdgcn_exp2f(stat[u].x - base) : 0.f;
+      total += stat[u].y * keep;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const float k = s + u < n ? __shfl(keep, s + u) : 0.f;
-        x += v[u].x * k;
-        y += v[u].y * k;
-      }
+      for (int i = 0; i < 4; ++i) v[i] += x[u][i] * keep;
     }
   }
   const Row out(p, r, hk);
   const float scale = total == 0.f ? 0.f : 1.f / total;
-  if (c < p.D) {
-    const int64_t to = (((int64_t)b * p.q_len + out.i) * p.heads + out.h) * p.D + c;
-    x *= scale;
-    y *= scale;
-    *reinterpret_cast<unsigned*>(static_cast<bf16*>(p.o) + to) = pack_bf16x2(x, y);
-    if (p.o_rest != nullptr) *reinterpret_cast<unsigned*>(static_cast<bf16*>(p.o_rest) + to) = pack_bf16x2(x - (float)(bf16)x, y - (float)(bf16)y);
+  const int64_t to = (((int64_t)b * p.q_len + out.i) * p.heads + out.h) * p.D + c;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] *= scale;
+  store_values<bf16, 4>(static_cast<bf16*>(p.o) + to, v);
+  if (p.o_rest != nullptr) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] -= (float)(bf16)v[i];
+    store_values<bf16, 4>(static_cast<bf16*>(p.o_rest) + to, v);
   }
-  if (p.lse != nullptr && lane == 0) p.lse[((int64_t)b * p.heads + out.h) * p.q_len + out.i] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * LN2;
+  if (p.lse != nullptr && c == 0) p.lse[((int64_t)b * p.heads + out.h) * p.q_len + out.i] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * LN2;
 }
 
 // dq: the forward pass's walk over the keys, with the probabilities from lse: p = exp2(s c - lse2), dp = dO v, ds = p (dp - D), dq = scale ds k, where
 // -D = -sum dO o is what dp's accumulators begin with, so the subtraction is the product's.  726 us on the forward pass's 16384 tokens (1140
 // TFLOP/s of what is executed and seen, the matrix unit 67 % busy), 41 on its 16 sequences of 512 (a third of it the 117 MB that go in and out; 32 keys at a time
-// within the registers of four waves a SIMD were level there and 10 % slower at 32 features).  Leaves lse log2(e) and minus sum_d dO o of every row for dk and dv.
-template <int DP, int WAVES>
+// within the registers of four waves a SIMD were level there and 10 % slower at 32 features).  Leaves lse log2(e) and minus sum_d dO o of every row for dk and dv.  With SHARES each
+// share of the keys leaves fp32 sums, which attention_sum_parts_kernel adds up in order.
+template <int DP, int WAVES, bool SHARES>
 __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const AttentionArgs p) {
   typedef Tile<DP> L;
   typedef Mma<bf16> M;
@@ -468,12 +505,15 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int b, hk, tile;
   locate(p, b, hk, tile);
+  const int share = SHARES ? tile % p.q_shares : 0;
+  if (SHARES) tile /= p.q_shares;
   if (p.causal) tile = (p.q_len * p.group + WAVES * 32 - 1) / (WAVES * 32) - 1 - tile;
   const Sequence q(p, b);
   const int r0 = tile * WAVES * 32;
   const Row row(p, r0 + wave * 32 + (lane & 31), hk);
   const int limit = row.there ? q.limit(row.i) : 0;
   const int keys = q.seen(r0 / p.group, (r0 + WAVES * 32 - 1) / p.group);
+  const Keys range(keys, share, SHARES ? p.q_shares : 1);
   const int first_i = (r0 + wave * 32) / p.group, last_i = (r0 + wave * 32 + 31) / p.group;
   const int most = __builtin_amdgcn_readfirstlane(first_i < p.q_len ? q.seen(first_i, last_i) : 0);
   const int common = __builtin_amdgcn_readfirstlane(last_i < q.n ? q.limit(first_i) : 0);
@@ -483,10 +523,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
   const bf16* const vb = static_cast<const bf16*>(p.v) + b * p.vs[0] + hk * p.vs[2];
   const typename L::template Loader<WAVES> load_k(wave, lane, p.ks[1], p.D), load_v(wave, lane, p.vs[1], p.D);
   const unsigned k_at = L::along_address(lane), kt_at = L::across_address(lane);
-  Walk<TILE_ROWS> walk_k(kb, p.ks[1], 0, p.D), walk_v(vb, p.vs[1], 0, p.D);
-  if (keys > 0) {
-    load_k.load(walk_k.window(q.m), 0u, wave);
-    load_v.load(walk_v.window(q.m), L::BYTES, wave);
+  Walk<TILE_ROWS> walk_k(kb, p.ks[1], range.begin, p.D), walk_v(vb, p.vs[1], range.begin, p.D);
+  if (range.begin < range.end) {
+    load_k.load(walk_k.window(q.m - range.begin), 0u, wave);
+    load_v.load(walk_v.window(q.m - range.begin), L::BYTES, wave);
   }
 
   bf16x8 qf[KS], gf[KS];
@@ -513,7 +553,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
   // (a row that sees nothing has no probabilities, whatever its lse says)
   float lse = limit > 0 ? p.lse[stat] * LOG2E : INFINITY;
   asm volatile("" : "+v"(lse), "+v"(delta));
-  if (row.there && lane < 32) {
+  if (row.there && lane < 32 && share == 0) {
     p.lse2[stat] = lse;
     p.delta[stat] = delta;
   }
@@ -522,11 +562,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
   for (int d = 0; d < ND; ++d) dq[d] = zeros();
   const float factor = score_factor(p.scale);
   unsigned slot = 0;
-  for (int j0 = 0; j0 < keys; j0 += TILE_ROWS, slot ^= SLOT) {
+  for (int j0 = range.begin; j0 < range.end; j0 += TILE_ROWS, slot ^= SLOT) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     walk_k.skip(TILE_ROWS);
     walk_v.skip(TILE_ROWS);
-    const int left = j0 + TILE_ROWS < keys ? q.m - j0 - TILE_ROWS : 0;
+    const int left = j0 + TILE_ROWS < range.end ? q.m - j0 - TILE_ROWS : 0;
     const u32x4 next_k = walk_k.window(left), next_v = walk_v.window(left);
     constexpr int EACH = L::template Loader<WAVES>::EACH;
     auto ask = [&](auto ic) {   // (as the forward pass's, one to two products)
@@ -587,7 +627,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  store_row<DP>(static_cast<bf16*>(p.dq) + at, row.there, dq, p.scale, p.D, lane);
+  const int lane_out = lane_again();   // (where the row is need not lie in registers all the way)
+  const Row out(p, r0 + wave * 32 + (lane_out & 31), hk);
+  const int64_t to = (((int64_t)b * p.q_len + out.i) * p.heads + out.h) * p.D;
+  if (!SHARES) store_row<DP>(static_cast<bf16*>(p.dq) + to, out.there, dq, p.scale, p.D, lane_out);
+  else if (out.there) store_sums<DP>(p.q_partial + share * ((int64_t)p.batch * p.q_len * p.heads * p.D) + to, dq, p.D, lane_out);
 }
 
 // dk and dv: 32 keys a wave, their sums in registers over all queries of all heads that share them; tiles of 64 queries and their
@@ -725,25 +769,32 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dkv_kernel(const Atte
   } else if (j_out < p.k_len) {
     const int64_t values = (int64_t)p.batch * p.k_len * p.kv_heads * p.D;
     float* const to = p.partial + part * 2 * values + row * p.D;
-#pragma unroll
-    for (int d = 0; d < ND; ++d)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int c = d * 32 + 8 * g + 4 * (lane_again() >> 5);
-        if (c >= p.D) continue;
-        *reinterpret_cast<f32x4*>(to + c) = f32x4{dk[d][4 * g], dk[d][4 * g + 1], dk[d][4 * g + 2], dk[d][4 * g + 3]};
-        *reinterpret_cast<f32x4*>(to + values + c) = f32x4{dv[d][4 * g], dv[d][4 * g + 1], dv[d][4 * g + 2], dv[d][4 * g + 3]};
-      }
+    store_sums<DP>(to, dk, p.D, lane_again());
+    store_sums<DP>(to + values, dv, p.D, lane_again());
   }
 }
 
 double pairs(const AttentionArgs& a) { return (double)a.batch * a.q_len * a.heads * a.k_len * a.D; }
 unsigned groups_of(const AttentionArgs& a, int64_t rows, int per) { return (unsigned)((int64_t)a.batch * a.kv_heads * ((rows + per - 1) / per)); }
 
+// Even shares of each row tile's keys, for the forward pass by attention_fwd_kernel and for dq: where tiles of 128 rows leave CUs empty, so many that they
+// do not, of eight tiles of keys at least; under a causal mask, whose walks differ in length, up to two work-groups a CU, whose shorter ones even that out.  Below 24 tiles of
+// keys the fp32 sums and the launch that joins them cost more than they save.  Four sequences of 300 queries on 4000 keys, 8 heads on 2 of 128,
+// causal: 81 us in one share, 32 + 9 in five; one of 4096, 4 heads on 2 of 64, causal, forward 58 and 23 + 8, dq 63 and 29 + 2; one of 4096, 8 on 4 of 128, the most
+// work-groups that are cut, forward 72 and 51 + 15, dq 86 and 71 + 5.  Not cut: two of 1895, 16 heads on 4 of 64, causal: 39 in one share, 31 + 10 in two;
+// not causal, one of 2048, 16 heads of 128: 45 and 44 + 10.
+int query_shares(const AttentionArgs& a) {
+  const int64_t groups = (int64_t)a.batch * a.kv_heads * (((int64_t)a.q_len * a.group + 127) / 128), tiles = (a.k_len + TILE_ROWS - 1) / TILE_ROWS;
+  int64_t shares = (a.causal ? 2 : 1) * NUM_CUS / groups;
+  if (tiles < 24 || shares < 2) return 1;
+  if (shares > tiles / 8) shares = tiles / 8;
+  return shares > 16 ? 16 : (int)shares;
+}
+
 // Whether the forward pass goes by attention_few_kernel, and how: rows that fill one wave's tile at most, or so few that tiles of 32, whose four
 // waves share the way through the keys, leave no CU with two (two sequences of 355, eight heads of 64: 8.7 us where tiles of 128 took
 // 11.7; 640 queries of 16 heads, 320 tiles of 32: 24.8 and 13.7).
-bool few_rows(const AttentionArgs& a, FewPlan& plan) {
+bool few_rows(const AttentionArgs& a, RangePlan& plan) {
   const int64_t heads = (int64_t)a.batch * a.kv_heads, rows = (int64_t)a.q_len * a.group;
   if (rows > 32 && (heads * ((rows + 31) / 32) > NUM_CUS || a.k_len < 128)) return false;
   plan.row_tiles = (int)((rows + 31) / 32);
@@ -755,85 +806,131 @@ bool few_rows(const AttentionArgs& a, FewPlan& plan) {
   plan.chunk = (int)chunk;
   return true;
 }
-size_t few_sums(const AttentionArgs& a, const FewPlan& plan) {
+size_t range_sums(const AttentionArgs& a, const RangePlan& plan) {
   return plan.splits > 1 ? (size_t)a.batch * a.kv_heads * plan.splits * a.q_len * a.group * a.D * 4 : 0;
 }
-size_t few_bytes(const AttentionArgs& a, const FewPlan& plan) { return few_sums(a, plan) + few_sums(a, plan) / a.D * 2; }
+size_t range_bytes(const AttentionArgs& a, const RangePlan& plan) { return range_sums(a, plan) + range_sums(a, plan) / a.D * 2; }
+void place_ranges(const AttentionArgs& a, RangePlan& plan) {
+  plan.sums = static_cast<float*>(a.workspace);
+  plan.stats = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + range_sums(a, plan));
+}
+hipError_t join(const AttentionArgs& a, const RangePlan& plan, hipStream_t s) {
+  const size_t bytes = range_bytes(a, plan);
+  note_matrix(a.workspace, 1, bytes, bytes, 1, false);
+  note_attention_fwd(a, 2);
+  return launch_kernel("attention_join_kernel", Work{0.0, (double)bytes}, attention_join_kernel,
+                       dim3((unsigned)(((int64_t)a.q_len * a.group * (a.D / 4) + 255) / 256), a.batch * a.kv_heads), dim3(256), s, a, plan);
+}
 
 template <int DP>
-hipError_t few(const AttentionArgs& a, FewPlan plan, hipStream_t s) {
-  const size_t sums = few_sums(a, plan), bytes = few_bytes(a, plan);
-  const int heads = a.batch * a.kv_heads, rows = a.q_len * a.group;
+hipError_t few(const AttentionArgs& a, RangePlan plan, hipStream_t s) {
+  const size_t bytes = range_bytes(a, plan);
   const int64_t units = (int64_t)a.batch * plan.row_tiles * plan.splits;
   plan.xcds = units < 8 ? (int)units : 8;
-  plan.sums = static_cast<float*>(a.workspace);
-  plan.stats = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + sums);
+  place_ranges(a, plan);
   note_attention_inputs(a, 2);
   if (plan.splits == 1) note_attention_fwd(a, 2);
   else note_matrix(a.workspace, 1, bytes, bytes, 1, true);
   hipError_t e = launch_kernel(SK_LABEL_BY_WIDTH("attention_few_kernel", DP), Work{4 * pairs(a), 0.0}, attention_few_kernel<DP>,
                                dim3((unsigned)((units + plan.xcds - 1) / plan.xcds * plan.xcds * a.kv_heads)), dim3(256), s, a, plan);
-  if (e != hipSuccess || plan.splits == 1) return e;
-  note_matrix(a.workspace, 1, bytes, bytes, 1, false);
-  note_attention_fwd(a, 2);
-  return launch_kernel("attention_join_kernel", Work{0.0, (double)bytes}, attention_join_kernel, dim3((rows + 3) / 4, heads), dim3(256), s, a, plan);
+  return e != hipSuccess || plan.splits == 1 ? e : join(a, plan, s);
 }
 
 template <int DP>
 hipError_t fwd(const AttentionArgs& a, hipStream_t s) {
-  FewPlan plan;
+  RangePlan plan{};
   if (few_rows(a, plan)) return few<DP>(a, plan, s);
   constexpr int WAVES = 4;
+  plan.splits = query_shares(a);
+  if (plan.splits > 1) {
+    const size_t bytes = range_bytes(a, plan);
+    place_ranges(a, plan);
+    note_attention_inputs(a, 2);
+    note_matrix(a.workspace, 1, bytes, bytes, 1, true);
+    hipError_t e = launch_kernel(SK_LABEL_BY_WIDTH("attention_fwd_shares_kernel", DP), Work{4 * pairs(a), 0.0}, attention_fwd_kernel<DP, WAVES, true>,
+                                 dim3(groups_of(a, (int64_t)a.q_len * a.group, WAVES * 32) * plan.splits), dim3(WAVES * 64), s, a, plan);
+    return e != hipSuccess ? e : join(a, plan, s);
+  }
   note_attention_fwd(a, 2);
-  return launch_kernel(SK_LABEL_BY_WIDTH("attention_fwd_kernel", DP), Work{4 * pairs(a), 0.0}, attention_fwd_kernel<DP, WAVES>,
-                       dim3(groups_of(a, (int64_t)a.q_len * a.group, WAVES * 32)), dim3(WAVES * 64), s, a);
+  return launch_kernel(SK_LABEL_BY_WIDTH("attention_fwd_kernel", DP), Work{4 * pairs(a), 0.0}, attention_fwd_kernel<DP, WAVES, false>,
+                       dim3(groups_of(a, (int64_t)a.q_len * a.group, WAVES * 32)), dim3(WAVES * 64), s, a, plan);
 }
 
 template <int DP>
 hipError_t bwd(const AttentionArgs& a, hipStream_t s) {
   constexpr int WAVES = 4;
   note_attention_dq(a, 2);
-  hipError_t e = launch_kernel(SK_LABEL_BY_WIDTH("attention_dq_kernel", DP), Work{6 * pairs(a), 0.0}, attention_dq_kernel<DP, WAVES>,
-                               dim3(groups_of(a, (int64_t)a.q_len * a.group, WAVES * 32)), dim3(WAVES * 64), s, a);
+  const unsigned groups = groups_of(a, (int64_t)a.q_len * a.group, WAVES * 32);
+  const Work work{6 * pairs(a), 0.0};
+  hipError_t e = a.q_shares > 1 ? launch_kernel(SK_LABEL_BY_WIDTH("attention_dq_shares_kernel", DP), work, attention_dq_kernel<DP, WAVES, true>, dim3(groups * a.q_shares), dim3(WAVES * 64), s, a)
+                                : launch_kernel(SK_LABEL_BY_WIDTH("attention_dq_kernel", DP), work, attention_dq_kernel<DP, WAVES, false>, dim3(groups), dim3(WAVES * 64), s, a);
   if (e != hipSuccess) return e;
   note_attention_dkv(a, 2);
   e = launch_kernel(SK_LABEL_BY_WIDTH("attention_dkv_kernel", DP), Work{8 * pairs(a), 0.0}, attention_dkv_kernel<DP, WAVES>,
                        dim3(groups_of(a, a.k_len, WAVES * 32) * a.parts), dim3(WAVES * 64), s, a);
-  return e != hipSuccess || a.parts == 1 ? e : launch_attention_sum_parts(a, false, s);
+  return e != hipSuccess ? e : launch_attention_sum_parts(a, false, s);
 }
 
 }  // namespace
 
+// Results in parts, [part][values] a `step` apart, that are added up in order, scaled and rounded; one to a row of the grid.
+struct PartSums {
+  struct {
+    const float* from;
+    void* to;
+    int64_t values, step;
+    int parts;
+    float scale;
+  } of[3];
+};
 template <typename T>
-__global__ __launch_bounds__(256) void attention_sum_parts_kernel(const AttentionArgs p, int64_t values) {
+__global__ __launch_bounds__(256) void attention_sum_parts_kernel(const PartSums p) {
+  const auto& r = p.of[blockIdx.y];
   const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-  const bool v = blockIdx.y == 1;
-  if (at >= values) return;
+  if (at >= r.values) return;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-  const float* const from = p.partial + (v ? values : 0) + at;
 #pragma unroll 4
-  for (int part = 0; part < p.parts; ++part) {
-    const float4 x = *reinterpret_cast<const float4*>(from + part * 2 * values);
+  for (int part = 0; part < r.parts; ++part) {
+    const float4 x = *reinterpret_cast<const float4*>(r.from + at + part * r.step);
     s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
   }
-  const float scale = v ? 1.f : p.scale, out[4] = {s.x * scale, s.y * scale, s.z * scale, s.w * scale};
-  store_values<T, 4>(static_cast<T*>(v ? p.dv : p.dk) + at, out);
+  const float out[4] = {s.x * r.scale, s.y * r.scale, s.z * r.scale, s.w * r.scale};
+  store_values<T, 4>(static_cast<T*>(r.to) + at, out);
 }
 
 size_t attention_fwd_bytes_bf16(const AttentionArgs& a) {
-  FewPlan plan;
-  return few_rows(a, plan) ? few_bytes(a, plan) : 0;
+  RangePlan plan{};
+  if (!few_rows(a, plan)) plan.splits = query_shares(a);
+  return range_bytes(a, plan);
 }
 hipError_t launch_attention_fwd_bf16(const AttentionArgs& a, hipStream_t s) { return by_width(a.D, [&](auto dp) { return fwd<decltype(dp)::value>(a, s); }); }
 hipError_t launch_attention_sum_parts(const AttentionArgs& a, bool f32, hipStream_t s) {
-  const int64_t values = (int64_t)a.batch * a.k_len * a.kv_heads * a.D;
-  note_matrix(a.partial, 2 * a.parts, values, values, 4, false);
-  note_matrix(a.dk, 1, values, values, f32 ? 4 : 2, true);
-  note_matrix(a.dv, 1, values, values, f32 ? 4 : 2, true);
-  const dim3 grid((unsigned)((values / 4 + 255) / 256), 2);
-  const Work work{0.0, (8.0 * a.parts + (f32 ? 8 : 4)) * values};
-  if (f32) return launch_kernel("attention_sum_parts_kernel", work, attention_sum_parts_kernel<float>, grid, dim3(256), s, a, values);
-  return launch_kernel("attention_sum_parts_kernel", work, attention_sum_parts_kernel<bf16>, grid, dim3(256), s, a, values);
+  const int64_t keys = (int64_t)a.batch * a.k_len * a.kv_heads * a.D, queries = rows_of(a) * a.D;
+  const int esize = f32 ? 4 : 2;
+  PartSums p{};
+  int n = 0;
+  if (a.parts > 1) {
+    p.of[n++] = {a.partial, a.dk, keys, 2 * keys, a.parts, a.scale};
+    p.of[n++] = {a.partial + keys, a.dv, keys, 2 * keys, a.parts, 1.f};
+    note_matrix(a.partial, 2 * a.parts, keys, keys, 4, false);
+    note_matrix(a.dk, 1, keys, keys, esize, true);
+    note_matrix(a.dv, 1, keys, keys, esize, true);
+  }
+  if (a.q_shares > 1) {
+    p.of[n++] = {a.q_partial, a.dq, queries, queries, a.q_shares, a.scale};
+    note_matrix(a.q_partial, a.q_shares, queries, queries, 4, false);
+    note_matrix(a.dq, 1, queries, queries, esize, true);
+  }
+  if (n == 0) return hipSuccess;
+  double bytes = 0.0;
+  int64_t most = 0;
+  for (int i = 0; i < n; ++i) {
+    bytes += (4.0 * p.of[i].parts + esize) * p.of[i].values;
+    most = p.of[i].values > most ? p.of[i].values : most;
+  }
+  const dim3 grid((unsigned)((most / 4 + 255) / 256), n);
+  return f32 ? launch_kernel("attention_sum_parts_kernel", Work{0.0, bytes}, attention_sum_parts_kernel<float>, grid, dim3(256), s, p)
+             : launch_kernel("attention_sum_parts_kernel", Work{0.0, bytes}, attention_sum_parts_kernel<bf16>, grid, dim3(256), s, p);
 }
 
 // dk and dv's kernel gets as many work-groups as there are tiles of 128 keys, which with few key heads leaves CUs without one while
@@ -841,6 +938,7 @@ hipError_t launch_attention_sum_parts(const AttentionArgs& a, bool f32, hipStrea
 // costs), whose fp32 results a second kernel adds up in order: for two a CU, or under a causal mask, whose tiles differ in length,
 // three.  One sequence of 2048 tokens, 32 heads on 8 of 128, causal: 317 us in one part, 106 + 14 at two a CU, 92 + 19 at three; of 4096 on 4,
 // not causal: 1250, 549 + 15, 583 + 19.
+int attention_query_shares(const AttentionArgs& a) { return query_shares(a); }
 int attention_parts(const AttentionArgs& a, bool f32) {
   const int64_t groups = (int64_t)a.batch * a.kv_heads * ((a.k_len + 127) / 128), tiles = (int64_t)a.group * ((a.q_len + (f32 ? 31 : 63)) / (f32 ? 32 : 64));
   if (groups >= 2 * NUM_CUS) return 1;

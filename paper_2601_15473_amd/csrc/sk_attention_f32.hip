@@ -301,7 +301,7 @@ hipError_t bwd(const AttentionArgs& a, hipStream_t s) {
   note_attention_dkv(a, 4);
   e = launch_kernel(SK_LABEL_BY_WIDTH("attention_dkv_f32_kernel", DP), Work{8 * pairs(a), 0.0},
                        attention_dkv_f32_kernel<DP>, dim3(a.batch * a.kv_heads * k_tiles * a.parts), dim3(256), s, a, k_tiles);
-  return e != hipSuccess || a.parts == 1 ? e : launch_attention_sum_parts(a, true, s);
+  return e != hipSuccess ? e : launch_attention_sum_parts(a, true, s);
 }
 
 }  // namespace

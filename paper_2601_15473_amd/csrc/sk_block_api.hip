@@ -61,10 +61,11 @@ sk_status attention_args(const sk_attention_shape* s, AttentionArgs& a) {
 }
 bool lengths_aligned(const AttentionArgs& a) { return ((reinterpret_cast<uintptr_t>(a.q_lengths) | reinterpret_cast<uintptr_t>(a.k_lengths)) & 3u) == 0; }
 size_t stat_bytes(const AttentionArgs& a) { return align_up((size_t)a.batch * a.heads * a.q_len * 4); }
+size_t parts_bytes(const AttentionArgs& a, int parts) { return parts > 1 ? align_up((size_t)parts * 2 * a.batch * a.k_len * a.kv_heads * a.D * 4) : 0; }
+size_t query_shares_bytes(const AttentionArgs& a, int shares) { return shares > 1 ? align_up((size_t)shares * a.batch * a.q_len * a.heads * a.D * 4) : 0; }
 size_t attention_bytes(const AttentionArgs& a, bool f32, bool backward) {
   if (!backward) return f32 ? 0 : align_up(attention_fwd_bytes_bf16(a));
-  const int parts = attention_parts(a, f32);
-  return 2 * stat_bytes(a) + (parts > 1 ? align_up((size_t)parts * 2 * a.batch * a.k_len * a.kv_heads * a.D * 4) : 0);
+  return 2 * stat_bytes(a) + parts_bytes(a, attention_parts(a, f32)) + query_shares_bytes(a, f32 ? 1 : attention_query_shares(a));
 }
 
 sk_status norm_rope_args(const sk_norm_rope_shape* s, NormRopeArgs& a, bool back) {
@@ -160,6 +161,8 @@ sk_status sk_attention_bwd(const sk_attention_shape* shape, const void* q, const
   a.delta = reinterpret_cast<float*>(w + stat_bytes(a));
   a.parts = attention_parts(a, shape->dtype == SK_F32);
   a.partial = reinterpret_cast<float*>(w + 2 * stat_bytes(a));
+  a.q_shares = shape->dtype == SK_F32 ? 1 : attention_query_shares(a);
+  a.q_partial = reinterpret_cast<float*>(w + 2 * stat_bytes(a) + parts_bytes(a, a.parts));
   return launched(launch_attention_bwd(a, shape->dtype == SK_F32, static_cast<hipStream_t>(stream)), "sk_attention_bwd");
 }
 

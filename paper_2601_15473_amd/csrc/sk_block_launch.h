@@ -25,8 +25,13 @@ struct AttentionArgs {
   // backward: parts that dk and dv are summed in, and room for [parts][dk, dv] in fp32 where there are several
   int parts;
   float* partial;
+  // ... shares of the keys that dq is summed in (bf16), and room for [shares][dq]
+  int q_shares;
+  float* q_partial;
 };
 int attention_parts(const AttentionArgs& a, bool f32);
+int attention_query_shares(const AttentionArgs& a);
+// Sums up what is in parts (nothing where nothing is).
 hipError_t launch_attention_sum_parts(const AttentionArgs& a, bool f32, hipStream_t s);
 
 size_t attention_fwd_bytes_bf16(const AttentionArgs& a);

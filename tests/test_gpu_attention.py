@@ -58,6 +58,7 @@ SHAPES = [  # batch, q_len, k_len, heads, kv_heads, head_dim
     (2, 3, 515, 8, 2, 80), (1, 515, 640, 2, 2, 64), (1, 300, 300, 5, 1, 40),
     (1, 70, 1500, 4, 2, 128), (2, 9, 2100, 12, 1, 64),   # ranges of the keys, over one tile of rows
     (1, 600, 330, 8, 1, 64), (2, 333, 260, 6, 2, 128),   # parts of the queries for few key heads
+    (1, 1100, 1100, 8, 1, 64), (1, 1050, 1700, 16, 2, 104), (1, 3, 2100, 8, 4, 32),   # shares of the keys, for both directions or dq
 ]
 
 
@@ -78,6 +79,8 @@ RAGGED = [  # shape, queries', keys' lengths
     ((3, 130, 260, 3, 3, 64), [130, 128, -4], [260, 1000, 17]),   # out of range: clamped
     ((2, 257, 257, 2, 1, 128), [129, 257], [129, 256]),
     ((3, 520, 300, 8, 1, 64), [0, 520, 65], [300, 200, 3]),
+    ((2, 1030, 1100, 8, 1, 64), [1030, 300], [1100, 700]),
+    ((3, 1030, 1030, 4, 1, 128), [1030, 0, 64], [17, 1030, 961]),
 ]
 
 
