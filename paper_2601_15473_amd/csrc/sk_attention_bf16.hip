@@ -5,6 +5,8 @@
 namespace sk {
 namespace {
 
+constexpr int WAVES = 4;   // of 32 rows (queries, or keys) each, to a work-group or half of one
+
 // How the keys are cut where rows alone do not fill the chip, and where the ranges' results are.
 struct RangePlan {
   int row_tiles, splits, chunk;   // few rows: tiles of 32 rows, ranges of `chunk` keys; 0: each tile of rows has its keys in `splits` even shares
@@ -34,13 +36,15 @@ struct Row {
 };
 
 // Share `share` of `shares` of a tile of rows' keys, by whole tiles (none where there are fewer tiles than shares).
+template <int HALVES>
 struct Keys {
-  int begin, end;
+  int begin, end, steps;   // steps: tiles of it; of halves, which wait for each other, of the longer one
   __device__ __forceinline__ Keys(int keys, int share, int shares) {
     const int tiles = (keys + TILE_ROWS - 1) / TILE_ROWS;
     begin = tiles * share / shares * TILE_ROWS;
     end = tiles * (share + 1) / shares * TILE_ROWS;
     end = end < keys ? end : keys;
+    steps = HALVES > 1 ? (tiles + shares - 1) / shares : tiles * (share + 1) / shares - tiles * share / shares;
   }
 };
 
@@ -131,6 +135,23 @@ __device__ __forceinline__ void store_sums(float* row, const f32x16 (&acc)[DP / 
     }
 }
 
+// Sums of one half of a work-group's waves through LDS to the other half's waves of the same rows: 16 bytes a lane side by side.
+template <int ND>
+__device__ __forceinline__ void sums_to_lds(unsigned char* lds, const f32x16 (&acc)[ND], int lane) {
+#pragma unroll
+  for (int i = 0; i < 4 * ND; ++i)
+    *reinterpret_cast<f32x4*>(lds + i * 1024 + lane * 16) = f32x4{acc[i / 4][4 * (i % 4)], acc[i / 4][4 * (i % 4) + 1], acc[i / 4][4 * (i % 4) + 2], acc[i / 4][4 * (i % 4) + 3]};
+}
+template <int ND>
+__device__ __forceinline__ void add_from_lds(f32x16 (&acc)[ND], float keep, const unsigned char* lds, float factor, int lane) {
+#pragma unroll
+  for (int i = 0; i < 4 * ND; ++i) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(lds + i * 1024 + lane * 16);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) acc[i / 4][4 * (i % 4) + u] = acc[i / 4][4 * (i % 4) + u] * keep + v[u] * factor;
+  }
+}
+
 // Running softmax of a lane's row (the lane 32 further has the row's other keys): the maximum and its own keys' sum.
 struct Softmax {
   float top = -INFINITY, sum = 0.f, base = 0.f;
@@ -183,21 +204,22 @@ __device__ __forceinline__ void read_first(bf16x8 (&f)[AHEAD], Read&& read) {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// Forward: WAVES x 32 rows a work-group (with SHARES a share of their keys, whose sums attention_join_kernel puts together), tiles of 64 keys and values through a ring of two slots in LDS, asked for a tile
+// Forward: WAVES x 32 rows a work-group, or with two HALVES twice the waves, each half of which takes half of the keys (with SHARES: a share of their keys, whose
+// sums attention_join_kernel puts together), tiles of 64 keys and values through a ring of two slots in LDS, asked for a tile
 // ahead; one barrier a tile.  s^T = K q^T, p = exp2(s c - m), o^T = o^T exp2(m' - m) + V^T p^T, in the end o / sum p; a key tile is read by all
 // four waves.  At 128 features two waves a SIMD, one's exponentials under the other's products: 16384 tokens in sequences of 4096, 32 heads on 8,
 // causal, 543 us = 1010 TFLOP/s of the 4 flops a pair that is seen and feature, the matrix unit 58 % busy at the clock that the power limit
 // leaves (zeros for inputs take two thirds as long).  At 64 features four waves a SIMD and the vector unit is the bound (65 % busy, the matrix unit 32 %:
 // a score costs it a maximum, a multiplication, an exponential at a quarter of the rate, an addition and half a rounding, and only two products of 64):
 // 16 sequences of 512, 16 heads, 29 us, of which the rows' way out, 33 MB behind one round of work-groups, is about 7.
-template <int DP, int WAVES, bool SHARES>
-__global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const AttentionArgs p, RangePlan plan) {
+template <int DP, int HALVES, bool SHARES>
+__global__ __launch_bounds__(HALVES * WAVES * 64, 2) void attention_fwd_kernel(const AttentionArgs p, RangePlan plan) {
   typedef Tile<DP> L;
   typedef Mma<bf16> M;
   constexpr int KS = DP / 16, ND = DP / 32, SLOT = 2 * L::BYTES, K_AHEAD = 2 * KS < 6 ? 2 * KS : 6, V_AHEAD = 4;
-  __shared__ __align__(1024) unsigned char smem[2 * SLOT];
+  __shared__ __align__(1024) unsigned char smem[HALVES * 2 * SLOT];
   asm volatile("" ::"v"((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem) : "memory");
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave_id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = HALVES > 1 ? wave_id / WAVES : 0, wave = wave_id % WAVES;
   int b, hk, tile;
   locate(p, b, hk, tile);
   const int share = SHARES ? tile % plan.splits : 0;
@@ -209,7 +231,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const Atte
   const int limit = row.there ? q.limit(row.i) : 0;
   // the work-group's keys, and the wave's: all rows see those before `common`, none those from `most` on
   const int keys = q.seen(r0 / p.group, (r0 + WAVES * 32 - 1) / p.group);
-  const Keys range(keys, share, SHARES ? plan.splits : 1);
+  const Keys<HALVES> range(keys, share * HALVES + half, HALVES * (SHARES ? plan.splits : 1));
   const int first_i = (r0 + wave * 32) / p.group, last_i = (r0 + wave * 32 + 31) / p.group;
   const int most = __builtin_amdgcn_readfirstlane(first_i < p.q_len ? q.seen(first_i, last_i) : 0);
   const int common = __builtin_amdgcn_readfirstlane(last_i < q.n ? q.limit(first_i) : 0);
@@ -230,12 +252,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const Atte
   const unsigned k_at = L::along_address(lane), v_at = L::across_address(lane);
   Walk<TILE_ROWS> walk_k(kb, p.ks[1], range.begin, p.D), walk_v(vb, p.vs[1], range.begin, p.D);
   if (range.begin < range.end) {
-    load_k.load(walk_k.window(q.m - range.begin), 0u, wave);
-    load_v.load(walk_v.window(q.m - range.begin), L::BYTES, wave);
+    load_k.load(walk_k.window(q.m - range.begin), half * 2 * SLOT, wave);
+    load_v.load(walk_v.window(q.m - range.begin), half * 2 * SLOT + L::BYTES, wave);
   }
 
-  unsigned slot = 0;
-  for (int j0 = range.begin; j0 < range.end; j0 += TILE_ROWS, slot ^= SLOT) {
+  unsigned slot = half * 2 * SLOT;
+  int j0 = range.begin;
+  for (int step = 0; step < range.steps; ++step, j0 += TILE_ROWS, slot ^= SLOT) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // this tile is there, and nobody reads the other slot
     walk_k.skip(TILE_ROWS);
     walk_v.skip(TILE_ROWS);
@@ -251,7 +274,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const Atte
         else load_v.template load_one<n - EACH>(next_v, (slot ^ SLOT) + L::BYTES, wave);
       }
     };
-    if (j0 >= most) {
+    if (j0 >= most || (HALVES > 1 && j0 >= range.end)) {
       static_for<0, 2 * KS>(ask);
       continue;
     }
@@ -288,6 +311,22 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_fwd_kernel(const Atte
                       });
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing may land in LDS any more)
+  if (HALVES > 1) {
+    __syncthreads();
+    float2* const stats = reinterpret_cast<float2*>(smem + WAVES * ND * 4096);
+    if (half > 0) {
+      sums_to_lds(smem + wave * ND * 4096, o, lane);
+      stats[wave * 64 + lane] = make_float2(sm.top, sm.sum);
+    }
+    __syncthreads();
+    if (half > 0) return;
+    const float2 other = stats[wave * 64 + lane];
+    const float top = fmaxf(sm.top, other.x), base = top == -INFINITY ? 0.f : top;
+    const float keep = __builtin_amdgcn_exp2f(sm.top - base), factor = __builtin_amdgcn_exp2f(other.x - base);
+    add_from_lds(o, keep, smem + wave * ND * 4096, factor, lane);
+    sm.sum = sm.sum * keep + other.y * factor;
+    sm.top = top;
+  }
   const float sum = sm.sum + other_half(sm.sum);
   if (SHARES) {
     if (!row.there) return;
@@ -495,14 +534,14 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs
 // TFLOP/s of what is executed and seen, the matrix unit 67 % busy), 41 on its 16 sequences of 512 (a third of it the 117 MB that go in and out; 32 keys at a time
 // within the registers of four waves a SIMD were level there and 10 % slower at 32 features).  Leaves lse log2(e) and minus sum_d dO o of every row for dk and dv.  With SHARES each
 // share of the keys leaves fp32 sums, which attention_sum_parts_kernel adds up in order.
-template <int DP, int WAVES, bool SHARES>
-__global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const AttentionArgs p) {
+template <int DP, int HALVES, bool SHARES>
+__global__ __launch_bounds__(HALVES * WAVES * 64, 2) void attention_dq_kernel(const AttentionArgs p) {
   typedef Tile<DP> L;
   typedef Mma<bf16> M;
   constexpr int KS = DP / 16, ND = DP / 32, SLOT = 2 * L::BYTES, AHEAD = 4;
-  __shared__ __align__(1024) unsigned char smem[2 * SLOT];
+  __shared__ __align__(1024) unsigned char smem[HALVES * 2 * SLOT];
   asm volatile("" ::"v"((unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem) : "memory");
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave_id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = HALVES > 1 ? wave_id / WAVES : 0, wave = wave_id % WAVES;
   int b, hk, tile;
   locate(p, b, hk, tile);
   const int share = SHARES ? tile % p.q_shares : 0;
@@ -513,7 +552,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
   const Row row(p, r0 + wave * 32 + (lane & 31), hk);
   const int limit = row.there ? q.limit(row.i) : 0;
   const int keys = q.seen(r0 / p.group, (r0 + WAVES * 32 - 1) / p.group);
-  const Keys range(keys, share, SHARES ? p.q_shares : 1);
+  const Keys<HALVES> range(keys, share * HALVES + half, HALVES * (SHARES ? p.q_shares : 1));
   const int first_i = (r0 + wave * 32) / p.group, last_i = (r0 + wave * 32 + 31) / p.group;
   const int most = __builtin_amdgcn_readfirstlane(first_i < p.q_len ? q.seen(first_i, last_i) : 0);
   const int common = __builtin_amdgcn_readfirstlane(last_i < q.n ? q.limit(first_i) : 0);
@@ -525,8 +564,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
   const unsigned k_at = L::along_address(lane), kt_at = L::across_address(lane);
   Walk<TILE_ROWS> walk_k(kb, p.ks[1], range.begin, p.D), walk_v(vb, p.vs[1], range.begin, p.D);
   if (range.begin < range.end) {
-    load_k.load(walk_k.window(q.m - range.begin), 0u, wave);
-    load_v.load(walk_v.window(q.m - range.begin), L::BYTES, wave);
+    load_k.load(walk_k.window(q.m - range.begin), half * 2 * SLOT, wave);
+    load_v.load(walk_v.window(q.m - range.begin), half * 2 * SLOT + L::BYTES, wave);
   }
 
   bf16x8 qf[KS], gf[KS];
@@ -553,7 +592,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
   // (a row that sees nothing has no probabilities, whatever its lse says)
   float lse = limit > 0 ? p.lse[stat] * LOG2E : INFINITY;
   asm volatile("" : "+v"(lse), "+v"(delta));
-  if (row.there && lane < 32 && share == 0) {
+  if (row.there && lane < 32 && share == 0 && half == 0) {
     p.lse2[stat] = lse;
     p.delta[stat] = delta;
   }
@@ -561,8 +600,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
 #pragma unroll
   for (int d = 0; d < ND; ++d) dq[d] = zeros();
   const float factor = score_factor(p.scale);
-  unsigned slot = 0;
-  for (int j0 = range.begin; j0 < range.end; j0 += TILE_ROWS, slot ^= SLOT) {
+  unsigned slot = half * 2 * SLOT;
+  int j0 = range.begin;
+  for (int step = 0; step < range.steps; ++step, j0 += TILE_ROWS, slot ^= SLOT) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     walk_k.skip(TILE_ROWS);
     walk_v.skip(TILE_ROWS);
@@ -576,7 +616,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
         else load_v.template load_one<n - EACH>(next_v, (slot ^ SLOT) + L::BYTES, wave);
       }
     };
-    if (j0 >= most) {
+    if (j0 >= most || (HALVES > 1 && j0 >= range.end)) {
       static_for<0, 4 * KS>(ask);
       continue;
     }
@@ -627,6 +667,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  if (HALVES > 1) {
+    __syncthreads();
+    if (half > 0) sums_to_lds(smem + wave * ND * 4096, dq, lane_again());
+    __syncthreads();
+    if (half > 0) return;
+    add_from_lds(dq, 1.f, smem + wave * ND * 4096, 1.f, lane_again());
+  }
   const int lane_out = lane_again();   // (where the row is need not lie in registers all the way)
   const Row out(p, r0 + wave * 32 + (lane_out & 31), hk);
   const int64_t to = (((int64_t)b * p.q_len + out.i) * p.heads + out.h) * p.D;
@@ -638,7 +685,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dq_kernel(const Atten
 // dO through the ring, with what dq's kernel left of their rows.  Two waves a SIMD, so that one's exponentials run under the other's
 // products, is what the registers are kept to: one wave of 330 took 1572 us where two take 1081 (16384 tokens in sequences of 4096, 32 heads on 8 of 128,
 // causal; the matrix unit 59 % busy).  256 keys a work-group instead of 128 load half as much for 1 % there, and cost 17 to 25 % at 128 to 512 keys of 64.
-template <int DP, int WAVES>
+template <int DP>
 __global__ __launch_bounds__(WAVES * 64, 2) void attention_dkv_kernel(const AttentionArgs p) {
   typedef Tile<DP> L;
   typedef Mma<bf16> M;
@@ -791,6 +838,16 @@ int query_shares(const AttentionArgs& a) {
   return shares > 16 ? 16 : (int)shares;
 }
 
+// Whether a work-group of eight waves, four to each half of the keys, takes a tile of rows (forward, dq), joined through LDS: where a round of work-groups leaves
+// SIMDs with one wave, or the walks under a causal mask differ so much that it soon does.  Two sequences of 1800, 8 heads on 4 of 64: forward 36
+// and with halves 30 us, dq 42 and 33; two of 1895, 16 on 4 of 64, causal: 39 and 34, 46 and 37; three of up to 3875, 4 on 1 of 128, causal: 79 and 61, 88
+// and 72.  At more than 64 features its LDS leaves room for one on a CU: one sequence of 2048, 32 heads on 8 of 128, 512 tiles, causal, 58 and 53, but dq 69 and
+// 72; 1001 queries of 64 heads on 8, 504 tiles, 96 and 99; two of 1024, 16 on 8 of 128, 27 and 25, 32 and 33: these stay with four waves.
+bool query_halves(const AttentionArgs& a) {
+  const int64_t groups = (int64_t)a.batch * a.kv_heads * (((int64_t)a.q_len * a.group + 127) / 128), tiles = a.k_len / TILE_ROWS;
+  return a.D <= 64 ? tiles >= 16 && groups <= 2 * NUM_CUS : tiles >= 32 && 2 * groups <= 3 * NUM_CUS;
+}
+
 // Whether the forward pass goes by attention_few_kernel, and how: rows that fill one wave's tile at most, or so few that tiles of 32, whose four
 // waves share the way through the keys, leave no CU with two (two sequences of 355, eight heads of 64: 8.7 us where tiles of 128 took
 // 11.7; 640 queries of 16 heads, 320 tiles of 32: 24.8 and 13.7).
@@ -840,34 +897,34 @@ template <int DP>
 hipError_t fwd(const AttentionArgs& a, hipStream_t s) {
   RangePlan plan{};
   if (few_rows(a, plan)) return few<DP>(a, plan, s);
-  constexpr int WAVES = 4;
   plan.splits = query_shares(a);
   if (plan.splits > 1) {
     const size_t bytes = range_bytes(a, plan);
     place_ranges(a, plan);
     note_attention_inputs(a, 2);
     note_matrix(a.workspace, 1, bytes, bytes, 1, true);
-    hipError_t e = launch_kernel(SK_LABEL_BY_WIDTH("attention_fwd_shares_kernel", DP), Work{4 * pairs(a), 0.0}, attention_fwd_kernel<DP, WAVES, true>,
+    hipError_t e = launch_kernel(SK_LABEL_BY_WIDTH("attention_fwd_shares_kernel", DP), Work{4 * pairs(a), 0.0}, attention_fwd_kernel<DP, 1, true>,
                                  dim3(groups_of(a, (int64_t)a.q_len * a.group, WAVES * 32) * plan.splits), dim3(WAVES * 64), s, a, plan);
     return e != hipSuccess ? e : join(a, plan, s);
   }
   note_attention_fwd(a, 2);
-  return launch_kernel(SK_LABEL_BY_WIDTH("attention_fwd_kernel", DP), Work{4 * pairs(a), 0.0}, attention_fwd_kernel<DP, WAVES, false>,
-                       dim3(groups_of(a, (int64_t)a.q_len * a.group, WAVES * 32)), dim3(WAVES * 64), s, a, plan);
+  const dim3 groups(groups_of(a, (int64_t)a.q_len * a.group, WAVES * 32));
+  const Work work{4 * pairs(a), 0.0};
+  if (query_halves(a)) return launch_kernel(SK_LABEL_BY_WIDTH("attention_fwd_halves_kernel", DP), work, attention_fwd_kernel<DP, 2, false>, groups, dim3(2 * WAVES * 64), s, a, plan);
+  return launch_kernel(SK_LABEL_BY_WIDTH("attention_fwd_kernel", DP), work, attention_fwd_kernel<DP, 1, false>, groups, dim3(WAVES * 64), s, a, plan);
 }
 
 template <int DP>
 hipError_t bwd(const AttentionArgs& a, hipStream_t s) {
-  constexpr int WAVES = 4;
   note_attention_dq(a, 2);
   const unsigned groups = groups_of(a, (int64_t)a.q_len * a.group, WAVES * 32);
   const Work work{6 * pairs(a), 0.0};
-  hipError_t e = a.q_shares > 1 ? launch_kernel(SK_LABEL_BY_WIDTH("attention_dq_shares_kernel", DP), work, attention_dq_kernel<DP, WAVES, true>, dim3(groups * a.q_shares), dim3(WAVES * 64), s, a)
-                                : launch_kernel(SK_LABEL_BY_WIDTH("attention_dq_kernel", DP), work, attention_dq_kernel<DP, WAVES, false>, dim3(groups), dim3(WAVES * 64), s, a);
+  hipError_t e = a.q_shares > 1 ? launch_kernel(SK_LABEL_BY_WIDTH("attention_dq_shares_kernel", DP), work, attention_dq_kernel<DP, 1, true>, dim3(groups * a.q_shares), dim3(WAVES * 64), s, a)
+                 : query_halves(a) ? launch_kernel(SK_LABEL_BY_WIDTH("attention_dq_halves_kernel", DP), work, attention_dq_kernel<DP, 2, false>, dim3(groups), dim3(2 * WAVES * 64), s, a)
+                                   : launch_kernel(SK_LABEL_BY_WIDTH("attention_dq_kernel", DP), work, attention_dq_kernel<DP, 1, false>, dim3(groups), dim3(WAVES * 64), s, a);
   if (e != hipSuccess) return e;
   note_attention_dkv(a, 2);
-  e = launch_kernel(SK_LABEL_BY_WIDTH("attention_dkv_kernel", DP), Work{8 * pairs(a), 0.0}, attention_dkv_kernel<DP, WAVES>,
-                       dim3(groups_of(a, a.k_len, WAVES * 32) * a.parts), dim3(WAVES * 64), s, a);
+  e = launch_kernel(SK_LABEL_BY_WIDTH("attention_dkv_kernel", DP), Work{8 * pairs(a), 0.0}, attention_dkv_kernel<DP>, dim3(groups_of(a, a.k_len, WAVES * 32) * a.parts), dim3(WAVES * 64), s, a);
   return e != hipSuccess ? e : launch_attention_sum_parts(a, false, s);
 }
 
@@ -937,13 +994,16 @@ hipError_t launch_attention_sum_parts(const AttentionArgs& a, bool f32, hipStrea
 // each walks over the queries of a whole group: below two a CU the walk is cut into parts of eight tiles at least (what the sum's launch
 // costs), whose fp32 results a second kernel adds up in order: for two a CU, or under a causal mask, whose tiles differ in length,
 // three.  One sequence of 2048 tokens, 32 heads on 8 of 128, causal: 317 us in one part, 106 + 14 at two a CU, 92 + 19 at three; of 4096 on 4,
-// not causal: 1250, 549 + 15, 583 + 19.
+// not causal: 1250, 549 + 15, 583 + 19.  Under a causal mask parts of four tiles up to two a CU still pay: six sequences of 401, 8 heads on 4 of 128: 43 in one,
+// 25 + 8 in three; one of 344, 64 on 8: 33 + 6 in six, 25 + 8 in twelve.
 int attention_query_shares(const AttentionArgs& a) { return query_shares(a); }
 int attention_parts(const AttentionArgs& a, bool f32) {
   const int64_t groups = (int64_t)a.batch * a.kv_heads * ((a.k_len + 127) / 128), tiles = (int64_t)a.group * ((a.q_len + (f32 ? 31 : 63)) / (f32 ? 32 : 64));
   if (groups >= 2 * NUM_CUS) return 1;
   int64_t parts = ((a.causal ? 3 : 2) * NUM_CUS + groups - 1) / groups;
   if (parts > tiles / 8) parts = tiles / 8;
+  const int64_t evened = a.causal ? 2 * NUM_CUS / groups : 1;
+  if (!f32 && parts < evened) parts = evened < tiles / 4 ? evened : tiles / 4 > parts ? tiles / 4 : parts;
   return parts < 1 ? 1 : parts > 16 ? 16 : (int)parts;
 }
 

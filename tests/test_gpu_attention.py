@@ -59,6 +59,8 @@ SHAPES = [  # batch, q_len, k_len, heads, kv_heads, head_dim
     (1, 70, 1500, 4, 2, 128), (2, 9, 2100, 12, 1, 64),   # ranges of the keys, over one tile of rows
     (1, 600, 330, 8, 1, 64), (2, 333, 260, 6, 2, 128),   # parts of the queries for few key heads
     (1, 1100, 1100, 8, 1, 64), (1, 1050, 1700, 16, 2, 104), (1, 3, 2100, 8, 4, 32),   # shares of the keys, for both directions or dq
+    (2, 1100, 1100, 16, 8, 64), (3, 1030, 1090, 10, 5, 24), (1, 2100, 2100, 16, 16, 72), (1, 2060, 2060, 18, 18, 128),   # halves of a work-group
+    (3, 200, 200, 8, 2, 64),   # parts of four tiles
 ]
 
 
@@ -81,6 +83,7 @@ RAGGED = [  # shape, queries', keys' lengths
     ((3, 520, 300, 8, 1, 64), [0, 520, 65], [300, 200, 3]),
     ((2, 1030, 1100, 8, 1, 64), [1030, 300], [1100, 700]),
     ((3, 1030, 1030, 4, 1, 128), [1030, 0, 64], [17, 1030, 961]),
+    ((4, 1030, 1030, 8, 8, 64), [1030, 0, 64, 700], [1030, 1030, 65, 129]),
 ]
 
 
