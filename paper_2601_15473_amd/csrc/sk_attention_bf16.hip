@@ -1000,10 +1000,18 @@ int attention_query_shares(const AttentionArgs& a) { return query_shares(a); }
 int attention_parts(const AttentionArgs& a, bool f32) {
   const int64_t groups = (int64_t)a.batch * a.kv_heads * ((a.k_len + 127) / 128), tiles = (int64_t)a.group * ((a.q_len + (f32 ? 31 : 63)) / (f32 ? 32 : 64));
   if (groups >= 2 * NUM_CUS) return 1;
-  int64_t parts = ((a.causal ? 3 : 2) * NUM_CUS + groups - 1) / groups;
-  if (parts > tiles / 8) parts = tiles / 8;
-  const int64_t evened = a.causal ? 2 * NUM_CUS / groups : 1;
-  if (!f32 && parts < evened) parts = evened < tiles / 4 ? evened : tiles / 4 > parts ? tiles / 4 : parts;
+  int64_t parts;
+  if (f32) {
+    // a tile takes 3 to 7 us, so two to a part do; no more parts than one round of the work-groups that the registers leave room for (14 sequences of 512,
+    // eight heads of 96, causal: 294 + 21 us in two rounds, 277 in one; one of 55, 4 heads on 1 of 32: 34 in one part, 13 + 6 in four)
+    parts = (a.D <= 64 ? 2 : 1) * NUM_CUS / groups;
+    parts = parts < tiles / 2 ? parts : tiles / 2;
+  } else {
+    parts = ((a.causal ? 3 : 2) * NUM_CUS + groups - 1) / groups;
+    parts = parts < tiles / 8 ? parts : tiles / 8;
+    const int64_t evened = a.causal ? 2 * NUM_CUS / groups : 1;
+    if (parts < evened) parts = evened < tiles / 4 ? evened : tiles / 4 > parts ? tiles / 4 : parts;
+  }
   return parts < 1 ? 1 : parts > 16 ? 16 : (int)parts;
 }
 
