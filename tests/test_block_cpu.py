@@ -151,7 +151,8 @@ def traced(call):
 
 
 ATTENTION = [(1, 1, 1, 1, 1, 8), (2, 1, 5000, 64, 8, 128), (32, 128, 128, 12, 12, 64), (4, 4096, 4096, 32, 8, 128), (1, 1001, 3001, 64, 8, 128), (3, 17, 100, 6, 2, 80),
-             (1, 2, 32768, 8, 1, 96), (7, 1, 33, 5, 5, 32)]
+             (1, 2, 32768, 8, 1, 96), (7, 1, 33, 5, 5, 32),
+             (1, 4096, 4096, 4, 2, 64), (2, 2292, 2292, 4, 1, 32), (4, 300, 4000, 8, 2, 128), (1, 2493, 2493, 1, 1, 64), (3, 3875, 3875, 4, 1, 128), (1, 55, 55, 4, 1, 40)]
 
 
 @pytest.mark.parametrize("dtype, e", [(sk.SK_BF16, 2), (sk.SK_F32, 4)], ids=["bf16", "f32"])
