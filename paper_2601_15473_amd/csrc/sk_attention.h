@@ -31,6 +31,15 @@ struct Mma<bf16> {
     u.w = pack_bf16x2(p[8 * s + 6], p[8 * s + 7]);
     return __builtin_bit_cast(Frag, u);
   }
+  // What rounding left off fragment s of them
+  static __device__ __forceinline__ Frag rest_of_acc(const f32x16& p, int s, Frag rounded) {
+    uint4 u;
+    u.x = pack_bf16x2(p[8 * s + 0] - (float)rounded[0], p[8 * s + 1] - (float)rounded[1]);
+    u.y = pack_bf16x2(p[8 * s + 2] - (float)rounded[2], p[8 * s + 3] - (float)rounded[3]);
+    u.z = pack_bf16x2(p[8 * s + 4] - (float)rounded[4], p[8 * s + 5] - (float)rounded[5]);
+    u.w = pack_bf16x2(p[8 * s + 6] - (float)rounded[6], p[8 * s + 7] - (float)rounded[7]);
+    return __builtin_bit_cast(Frag, u);
+  }
   static __device__ __forceinline__ float dot(Frag a, Frag b) {
     float s = 0.f;
 #pragma unroll

@@ -533,8 +533,11 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs
 // -D = -sum dO o is what dp's accumulators begin with, so the subtraction is the product's.  726 us on the forward pass's 16384 tokens (1140
 // TFLOP/s of what is executed and seen, the matrix unit 67 % busy), 41 on its 16 sequences of 512 (a third of it the 117 MB that go in and out; 32 keys at a time
 // within the registers of four waves a SIMD were level there and 10 % slower at 32 features).  Leaves lse log2(e) and minus sum_d dO o of every row for dk and dv.  With SHARES each
-// share of the keys leaves fp32 sums, which attention_sum_parts_kernel adds up in order.
-template <int DP, int HALVES, bool SHARES>
+// share of the keys leaves fp32 sums, which attention_sum_parts_kernel adds up in order.  FINE: ds goes into the product in two bf16, rounded and what that left off, so
+// that dq is rounded once (off by 0.0017 of 64 bits instead of 0.0024 to 0.0025): for up to 128 keys, where it costs 1 us of 14 (32 sentences of 128, 12 heads of 64),
+// and for heads of 32, where a wave has products to spare (33 and 38 us of a pass of 93 to 98, 16 sequences of 512, 16 heads).  With more of both the second rounding stays: it
+// would be a third more products.
+template <int DP, int HALVES, bool SHARES, bool FINE>
 __global__ __launch_bounds__(HALVES * WAVES * 64, 2) void attention_dq_kernel(const AttentionArgs p) {
   typedef Tile<DP> L;
   typedef Mma<bf16> M;
@@ -662,8 +665,14 @@ __global__ __launch_bounds__(HALVES * WAVES * 64, 2) void attention_dq_kernel(co
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const bf16x8 w = M::of_acc(s[t >> 1], t & 1);
+      bf16x8 rest;
+      if constexpr (FINE) rest = M::rest_of_acc(s[t >> 1], t & 1, w);
 #pragma unroll
-      for (int d = 0; d < ND; ++d) dq[d] = M::mma(L::across(slot + kt_at, d, t), w, dq[d]);
+      for (int d = 0; d < ND; ++d) {
+        const bf16x8 k = L::across(slot + kt_at, d, t);
+        dq[d] = M::mma(k, w, dq[d]);
+        if constexpr (FINE) dq[d] = M::mma(k, rest, dq[d]);
+      }
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -919,9 +928,11 @@ hipError_t bwd(const AttentionArgs& a, hipStream_t s) {
   note_attention_dq(a, 2);
   const unsigned groups = groups_of(a, (int64_t)a.q_len * a.group, WAVES * 32);
   const Work work{6 * pairs(a), 0.0};
-  hipError_t e = a.q_shares > 1 ? launch_kernel(SK_LABEL_BY_WIDTH("attention_dq_shares_kernel", DP), work, attention_dq_kernel<DP, 1, true>, dim3(groups * a.q_shares), dim3(WAVES * 64), s, a)
-                 : query_halves(a) ? launch_kernel(SK_LABEL_BY_WIDTH("attention_dq_halves_kernel", DP), work, attention_dq_kernel<DP, 2, false>, dim3(groups), dim3(2 * WAVES * 64), s, a)
-                                   : launch_kernel(SK_LABEL_BY_WIDTH("attention_dq_kernel", DP), work, attention_dq_kernel<DP, 1, false>, dim3(groups), dim3(WAVES * 64), s, a);
+  constexpr bool FINE = DP == 32;
+  hipError_t e = a.q_shares > 1 ? launch_kernel(SK_LABEL_BY_WIDTH("attention_dq_shares_kernel", DP), work, attention_dq_kernel<DP, 1, true, FINE>, dim3(groups * a.q_shares), dim3(WAVES * 64), s, a)
+                 : query_halves(a) ? launch_kernel(SK_LABEL_BY_WIDTH("attention_dq_halves_kernel", DP), work, attention_dq_kernel<DP, 2, false, FINE>, dim3(groups), dim3(2 * WAVES * 64), s, a)
+                 : a.k_len <= 2 * TILE_ROWS ? launch_kernel(SK_LABEL_BY_WIDTH("attention_dq_fine_kernel", DP), work, attention_dq_kernel<DP, 1, false, true>, dim3(groups), dim3(WAVES * 64), s, a)
+                                   : launch_kernel(SK_LABEL_BY_WIDTH("attention_dq_kernel", DP), work, attention_dq_kernel<DP, 1, false, FINE>, dim3(groups), dim3(WAVES * 64), s, a);
   if (e != hipSuccess) return e;
   note_attention_dkv(a, 2);
   e = launch_kernel(SK_LABEL_BY_WIDTH("attention_dkv_kernel", DP), Work{8 * pairs(a), 0.0}, attention_dkv_kernel<DP>, dim3(groups_of(a, a.k_len, WAVES * 32) * a.parts), dim3(WAVES * 64), s, a);
