@@ -37,6 +37,8 @@ extern "C" {
  *     lse_i = log sum_j exp(s_ij)   over the keys that i sees.
  * A query that sees no key, and a row i >= n, has o = 0 and lse = -infinity.  What lies in keys
  * and values past m and in queries past n is not used, whatever it is.
+ * (Tokens of k or v that overlap in memory, a token stride below head_dim: what is not finite in the
+ * last that counts may come out as NaN where it would be infinity.)
  *
  * Limits (else SK_ERR_UNSUPPORTED): head_dim a multiple of 8 up to 128, heads a multiple of
  * kv_heads, token strides and heads * head_dim up to 2^22, q_len * heads / kv_heads and k_len up to 2^27, and batch * kv_heads times the tiles of 128 rows of

@@ -86,6 +86,13 @@ def _strided(t: torch.Tensor, token: int) -> torch.Tensor:
     return t.clone(memory_format=torch.contiguous_format)
 
 
+def _apart(t: torch.Tensor) -> torch.Tensor:
+    """Keys or values [batch, tokens, heads, head_dim] as the library takes them: copied too where tokens overlap in memory (expanded ones), since
+    what a kernel reads past the last token is then that token again."""
+    t = _strided(t, 1)
+    return t if t.size(1) <= 1 or t.stride(1) >= t.size(3) else t.clone(memory_format=torch.contiguous_format)
+
+
 # ---------------------------------------------------------------------------
 # attention
 # ---------------------------------------------------------------------------
@@ -129,7 +136,7 @@ class AttentionFunction(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, q, k, v, q_lengths, k_lengths, causal, scale):
-        qs, ks, vs = (_strided(t, 1) for t in (q, k, v))
+        qs, ks, vs = _strided(q, 1), _apart(k), _apart(v)
         o, lse, rest = _attention_forward(qs, ks, vs, q_lengths, k_lengths, causal, scale, True)
         ctx.save_for_backward(qs, ks, vs, o, lse, rest, q_lengths, k_lengths)
         ctx.causal, ctx.scale = causal, scale
@@ -183,7 +190,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lengths: torc
     scale = q.shape[3] ** -0.5 if scale is None else float(scale)
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
         return AttentionFunction.apply(q, k, v, *lengths, bool(causal), scale)
-    return _attention_forward(*(_strided(t, 1) for t in (q, k, v)), *lengths, bool(causal), scale, False)[0]
+    return _attention_forward(_strided(q, 1), _apart(k), _apart(v), *lengths, bool(causal), scale, False)[0]
 
 
 # ---------------------------------------------------------------------------

@@ -53,6 +53,9 @@ sk_status attention_args(const sk_attention_shape* s, AttentionArgs& a) {
     if (!stride_ok(q_sizes[i], s->q_strides[i], s->dtype, most[i], a.qs[i], st) || !stride_ok(k_sizes[i], s->k_strides[i], s->dtype, most[i], a.ks[i], st) ||
         !stride_ok(k_sizes[i], s->v_strides[i], s->dtype, most[i], a.vs[i], st))
       return st;
+  // (a lone token's tile has nothing behind it: the window of a tile's rows ends with the last only where rows do not overlap)
+  if (s->q_len == 1) a.qs[1] = s->head_dim;
+  if (s->k_len == 1) a.ks[1] = a.vs[1] = s->head_dim;
   a.batch = (int)s->batch; a.q_len = (int)s->q_len; a.k_len = (int)s->k_len;
   a.heads = s->heads; a.kv_heads = s->kv_heads; a.group = group; a.D = s->head_dim;
   a.causal = s->causal; a.scale = s->scale;

@@ -27,6 +27,9 @@ bool strided(const Tensor& t, int64_t token) {
   return true;
 }
 
+// Tokens that do not overlap in memory (block.py's _apart)
+bool apart(const Tensor& t) { return t.size(1) <= 1 || t.stride(1) >= t.size(3); }
+
 // Gradients that cannot be differentiated again say so where that is tried.
 variable_list once(variable_list grads) {
   if (!at::GradMode::is_enabled()) return grads;
@@ -261,7 +264,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!q || !k || !v || !floating(*q) || !no_tangent(*q) || !same(*q, *k) || !same(*q, *v)) Py_RETURN_NONE;
   if (q->dim() != 4 || k->dim() != 4 || v->dim() != 4 || q->numel() == 0 || k->numel() == 0 || k->sizes() != v->sizes() || q->size(0) != k->size(0) || q->size(3) != k->size(3))
     Py_RETURN_NONE;
-  if (q->size(2) > INT32_MAX || q->size(3) > INT32_MAX || !strided(*q, 1) || !strided(*k, 1) || !strided(*v, 1)) Py_RETURN_NONE;
+  if (q->size(2) > INT32_MAX || q->size(3) > INT32_MAX || !strided(*q, 1) || !strided(*k, 1) || !strided(*v, 1) || !apart(*k) || !apart(*v)) Py_RETURN_NONE;
   Tensor lengths[2];
   for (int i = 0; i < 2; ++i) {
     if (a[3 + i] == Py_None) continue;
