@@ -51,7 +51,7 @@ Tensor forward_pass(const Tensor& x, const Tensor& x2, const Tensor& S, const Te
   sk_status st;
   {
     const std::lock_guard<std::mutex> lock(w.mutex);
-    const Tensor& ws = w.get(x2.device(), stream, need);
+    const Tensor ws = w.get(x2.device(), stream, need);
     st = sk_linear_fwd(x2.data_ptr(), S.data_ptr(), U.data_ptr(), bias.has_value() ? bias->data_ptr() : nullptr, y.data_ptr(), tokens, in,
                        out, l, k, dt, ws.data_ptr(), (size_t)ws.numel(), stream);
   }
@@ -122,7 +122,7 @@ struct Linear : torch::autograd::Function<Linear> {
       sk_status st;
       {
         const std::lock_guard<std::mutex> lock(w.mutex);
-        const Tensor& ws = w.get(x2.device(), stream, need);
+        const Tensor ws = w.get(x2.device(), stream, need);
         void* const wp = ws.data_ptr();
         const size_t wn = (size_t)ws.numel();
         if (need_dx && need_w && round.count > 0)
@@ -182,7 +182,8 @@ struct LinearTwoSided : torch::autograd::Function<LinearTwoSided> {
       const Tensor own = behind ? Tensor() : at::empty({sums}, f32);
       const size_t at_sums = (need + 255) / 256 * 256;
       const std::lock_guard<std::mutex> lock(w.mutex);
-      unsigned char* const ws = static_cast<unsigned char*>(w.get(x2.device(), stream, behind ? at_sums + (size_t)sums * 4 : need).data_ptr());
+      const Tensor held = w.get(x2.device(), stream, behind ? at_sums + (size_t)sums * 4 : need);
+      unsigned char* const ws = static_cast<unsigned char*>(held.data_ptr());
       float* const sum_dB = behind ? reinterpret_cast<float*>(ws + at_sums) : own.data_ptr<float>();
       float* const sum_dA = sum_dB + 2 * half * out;
       st = sk_linear_bwd_rounded(x2.data_ptr(), dY.data_ptr(), A.data_ptr(), B.data_ptr(), dX.data_ptr(), sum_dB, kept.bias ? sum_dA + in * half : nullptr, sum_dA,
@@ -193,7 +194,7 @@ struct LinearTwoSided : torch::autograd::Function<LinearTwoSided> {
       dB = whole.narrow(0, 0, half);
       if (kept.bias) db = at::empty({out}, f32);
       const std::lock_guard<std::mutex> lock(w.mutex);
-      const Tensor& ws = w.get(x2.device(), stream, need);
+      const Tensor ws = w.get(x2.device(), stream, need);
       st = sk_linear_bwd_two_sided(x2.data_ptr(), dY.data_ptr(), A.data_ptr(), B.data_ptr(), dX.data_ptr(), whole.data_ptr<float>(),
                                    kept.bias ? db.data_ptr<float>() : nullptr, dA.data_ptr<float>(), tokens, in, out, l2, kept.k, dt, ws.data_ptr(),
                                    (size_t)ws.numel(), stream);

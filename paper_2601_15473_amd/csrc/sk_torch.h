@@ -33,6 +33,8 @@ using torch::autograd::variable_list;
 // One scratch buffer per (device, stream), grown to the largest request; the least recently used of more
 // than MAX_STREAMS goes back to the allocator, which keeps it until the work queued on it is done.
 // Calls queue their kernels under the lock: two threads that share a stream share its buffer.
+// A call that is being recorded into a graph gets a buffer of its own, out of the graph's memory: every replay writes there,
+// long after a stream's buffer may have been replaced or given back.
 struct Workspaces {
   static constexpr size_t MAX_STREAMS = 8;
   // Most that a pass keeps here beside its workspace: an allocation a pass is 1 us of host, 1 to 2 % of a small two-sided layer's step, and the sums
@@ -46,14 +48,27 @@ struct Workspaces {
   std::mutex mutex;
   std::list<Entry> entries;   // most recently used first
 
-  const Tensor& get(const at::Device& device, void* stream, size_t bytes) {   // (with the lock held)
+  static Tensor made(const at::Device& device, size_t bytes) {
+    return at::empty({(int64_t)(bytes < 256 ? 256 : bytes)}, at::TensorOptions().dtype(at::kByte).device(device));
+  }
+  static bool recording(void* stream) {
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(static_cast<hipStream_t>(stream), &status) != hipSuccess) {   // (the null stream's answer while another one is recorded)
+      (void)hipGetLastError();
+      return false;
+    }
+    return status != hipStreamCaptureStatusNone;
+  }
+
+  // For calls that are queued before the tensor and the lock go (the lock is held).
+  Tensor get(const at::Device& device, void* stream, size_t bytes) {
+    if (recording(stream)) return made(device, bytes);
     auto it = entries.begin();
     while (it != entries.end() && !(it->device == device.index() && it->stream == stream)) ++it;
     if (it == entries.end()) entries.push_front(Entry{device.index(), stream, Tensor()});
     else if (it != entries.begin()) entries.splice(entries.begin(), entries, it);
     Entry& e = entries.front();
-    if (!e.buffer.defined() || (size_t)e.buffer.numel() < bytes)
-      e.buffer = at::empty({(int64_t)(bytes < 256 ? 256 : bytes)}, at::TensorOptions().dtype(at::kByte).device(device));
+    if (!e.buffer.defined() || (size_t)e.buffer.numel() < bytes) e.buffer = made(device, bytes);
     if (entries.size() > MAX_STREAMS) entries.pop_back();
     return e.buffer;
   }

@@ -86,7 +86,7 @@ Tensor attention_forward(const Tensor& q, const Tensor& k, const Tensor& v, cons
   sk_status st;
   {
     const std::lock_guard<std::mutex> lock(w.mutex);
-    const Tensor& ws = w.get(q.device(), stream, need);
+    const Tensor ws = w.get(q.device(), stream, need);
     st = sk_attention_fwd(&c.s, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse ? lse->data_ptr<float>() : nullptr,
                           rest && rest->defined() ? rest->data_ptr() : nullptr, ws.data_ptr(), (size_t)ws.numel(), stream);
   }
@@ -119,7 +119,7 @@ struct Attention : torch::autograd::Function<Attention> {
     sk_status st;
     {
       const std::lock_guard<std::mutex> lock(w.mutex);
-      const Tensor& ws = w.get(q.device(), stream, need);
+      const Tensor ws = w.get(q.device(), stream, need);
       st = sk_attention_bwd(&c.s, q.data_ptr(), k.data_ptr(), v.data_ptr(), saved[3].data_ptr(), saved[4].data_ptr<float>(), saved[5].defined() ? saved[5].data_ptr() : nullptr, dO.data_ptr(), dq.data_ptr(), dk.data_ptr(),
                             dv.data_ptr(), ws.data_ptr(), (size_t)ws.numel(), stream);
     }
@@ -174,7 +174,7 @@ struct NormRope : torch::autograd::Function<NormRope> {
     sk_status st;
     {
       const std::lock_guard<std::mutex> lock(w.mutex);
-      const Tensor& ws = w.get(q.device(), stream, need);
+      const Tensor ws = w.get(q.device(), stream, need);
       st = sk_norm_rope_bwd(&c.s, q.data_ptr(), k.data_ptr(), wq.data_ptr(), wk.data_ptr(), t[4].data_ptr<float>(), t[5].data_ptr<float>(), t[6].data_ptr(), dqo.data_ptr(),
                             dko.data_ptr(), dq.data_ptr(), dk.data_ptr(), dwq.data_ptr(), dwk.data_ptr(), ws.data_ptr(), (size_t)ws.numel(), stream);
     }
@@ -216,7 +216,7 @@ struct Embedding : torch::autograd::Function<Embedding> {
     sk_status st;
     {
       const std::lock_guard<std::mutex> lock(w.mutex);
-      const Tensor& ws = w.get(ids.device(), stream, need);
+      const Tensor ws = w.get(ids.device(), stream, need);
       st = sk_embedding_bwd(ids.data_ptr(), (int32_t)ids.element_size(), dy.data_ptr(), dtable.data_ptr(), ids.numel(), rows, width, (float)ctx->saved_data["scale"].toDouble(),
                             dtype_of(dy), ws.data_ptr(), (size_t)ws.numel(), stream);
     }

@@ -44,7 +44,10 @@ def _workspace(device: torch.device, stream: int, nbytes: int) -> torch.Tensor:
     share it.  A buffer grows to the largest request seen on its stream; at most
     ``_MAX_WORKSPACES`` streams keep one (least recently used dropped first: torch's caching
     allocator keeps a dropped buffer alive until the work queued on it is done), and
-    ``release_workspaces()`` drops them all."""
+    ``release_workspaces()`` drops them all.  A call that is being recorded into a graph gets a buffer of
+    its own, out of the graph's memory: every replay writes there, long after a stream's may be gone."""
+    if torch.cuda.is_current_stream_capturing():
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
     key = (device.index, stream)
     ws = _workspaces.get(key)
     if ws is None or ws.numel() < nbytes:
