@@ -14,6 +14,7 @@ from __future__ import annotations
 import functools
 
 import torch
+from torch.autograd import forward_ad
 
 from . import libsk as sk
 from .nn import _DTYPES, _native, _on, _stream, _workspace
@@ -25,6 +26,14 @@ def _natively() -> bool:
     """Whether a call may try its native function (csrc/sk_torch_block.cpp), which computes the same for plain tensors outside of
     compilation, tracing and torch's modes and transforms, and gives None for anything else."""
     return _native is not None and not torch.compiler.is_compiling()
+
+
+def _training(*tensors) -> bool:
+    """Whether a call has to keep what its backward pass needs.  (A traced call does: the trace's own calls may want gradients.)
+
+    Whatever the native functions leave goes through an operator's autograd function, gradients or not: a trace records that call, where it would see
+    none of a kernel's launches, and a tangent, for which there is no rule, is refused there."""
+    return torch.jit.is_tracing() or (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors))
 
 
 def _once(backward):
@@ -135,9 +144,9 @@ class AttentionFunction(torch.autograd.Function):
     recomputes the probabilities."""
 
     @staticmethod
-    def forward(ctx, q, k, v, q_lengths, k_lengths, causal, scale):
+    def forward(ctx, q, k, v, q_lengths, k_lengths, causal, scale, training):
         qs, ks, vs = _strided(q, 1), _apart(k), _apart(v)
-        o, lse, rest = _attention_forward(qs, ks, vs, q_lengths, k_lengths, causal, scale, True)
+        o, lse, rest = _attention_forward(qs, ks, vs, q_lengths, k_lengths, causal, scale, training)
         ctx.save_for_backward(qs, ks, vs, o, lse, rest, q_lengths, k_lengths)
         ctx.causal, ctx.scale = causal, scale
         return o
@@ -148,14 +157,14 @@ class AttentionFunction(torch.autograd.Function):
         q, k, v, o, lse, rest, q_lengths, k_lengths = ctx.saved_tensors
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
         if q.numel() == 0 or k.numel() == 0:
-            return dq.zero_(), dk.zero_(), dv.zero_(), None, None, None, None
+            return dq.zero_(), dk.zero_(), dv.zero_(), None, None, None, None, None
         do = _dense(do)
         shape = _attention_shape(q, k, v, q_lengths, k_lengths, ctx.causal, ctx.scale)
         with _on(q.device):
             stream = _stream(q.device)
             ws = _attention_workspace(shape, 1, q.device, stream)
             sk.check(sk.sk_attention_bwd(shape, q, k, v, o, lse, rest, do, dq, dk, dv, ws, ws.numel(), stream))
-        return dq, dk, dv, None, None, None, None
+        return dq, dk, dv, None, None, None, None, None
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lengths: torch.Tensor | None = None,
@@ -187,10 +196,8 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lengths: torc
                 raise ValueError(f"attention: {name} has shape {tuple(t.shape)}, not [{q.shape[0]}]")
             t = t.to(torch.int32).contiguous()
         lengths.append(t)
-    scale = q.shape[3] ** -0.5 if scale is None else float(scale)
-    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
-        return AttentionFunction.apply(q, k, v, *lengths, bool(causal), scale)
-    return _attention_forward(_strided(q, 1), _apart(k), _apart(v), *lengths, bool(causal), scale, False)[0]
+    scale = float(q.shape[3]) ** -0.5 if scale is None else float(scale)
+    return AttentionFunction.apply(q, k, v, *lengths, bool(causal), scale, _training(q, k, v))
 
 
 # ---------------------------------------------------------------------------
@@ -281,22 +288,24 @@ def head_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: torch.Tensor, k_w
     lead = q.shape[:-2]
     q3, k3 = (t if t.dim() == 3 else t.flatten(0, -3) for t in (q, k))
     args = (_dense(cos), _dense(sin), _dense(positions.reshape(-1)), float(eps), bool(interleaved))
-    if torch.is_grad_enabled() and any(t.requires_grad for t in (q, k, q_weight, k_weight)):
-        if out is not None:
+    if out is not None:
+        floating = (q, k, q_weight, k_weight)
+        if torch.is_grad_enabled() and any(t.requires_grad for t in floating):
             raise RuntimeError("head_norm_rope: out is for calls without gradients")
-        q_out, k_out = NormRopeFunction.apply(q3, k3, q_weight, k_weight, *args)
-    else:
-        if out is not None:
-            for t, like, name in zip(out, (q, k), ("q_out", "k_out")):
-                _checked("head_norm_rope", q, **{name: t})
-                if t.shape != like.shape:
-                    raise ValueError(f"head_norm_rope: {name} has shape {tuple(t.shape)}, not {tuple(like.shape)}")
-            views = tuple(t if t.dim() == 3 else t.view(-1, *t.shape[-2:]) for t in out)
-            if any(_strided(t, -1) is not t for t in views):
-                raise ValueError("head_norm_rope: out needs heads of consecutive values at 16-byte boundaries")
+        for t, like, name in zip(out, (q, k), ("q_out", "k_out")):
+            _checked("head_norm_rope", q, **{name: t})
+            if t.shape != like.shape:
+                raise ValueError(f"head_norm_rope: {name} has shape {tuple(t.shape)}, not {tuple(like.shape)}")
+        views = tuple(t if t.dim() == 3 else t.view(-1, *t.shape[-2:]) for t in out)
+        if any(_strided(t, -1) is not t for t in views):
+            raise ValueError("head_norm_rope: out needs heads of consecutive values at 16-byte boundaries")
+        if torch.jit.is_tracing() or any(forward_ad.unpack_dual(t).tangent is not None for t in floating):   # (as _training says)
+            for t, result in zip(views, NormRopeFunction.apply(q3, k3, q_weight, k_weight, *args)):
+                t.copy_(result)
+        else:
             _norm_rope_forward(_strided(q3, -1), _strided(k3, -1), _dense(q_weight), _dense(k_weight), *args, views)
-            return tuple(out)
-        q_out, k_out = _norm_rope_forward(_strided(q3, -1), _strided(k3, -1), _dense(q_weight), _dense(k_weight), *args)
+        return tuple(out)
+    q_out, k_out = NormRopeFunction.apply(q3, k3, q_weight, k_weight, *args)
     return (q_out, k_out) if len(lead) == 1 else (q_out.view(q.shape), k_out.view(k.shape))
 
 
@@ -354,10 +363,7 @@ def embedding(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0) -> tor
     _integers("embedding", "ids", ids, table.device)
     if table.dim() != 2 or table.shape[0] == 0 or table.shape[1] == 0:
         raise ValueError("embedding: the table is [rows, width]")
-    ids, scale = _dense(ids), float(scale)
-    if torch.is_grad_enabled() and table.requires_grad:
-        return EmbeddingFunction.apply(ids, table, scale)
-    return _embedding_forward(ids, _dense(table), scale)
+    return EmbeddingFunction.apply(_dense(ids), table, float(scale))
 
 
 # ---------------------------------------------------------------------------
@@ -404,6 +410,4 @@ def dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, residual: tor
         raise ValueError("dropout: seed and offset are 64-bit unsigned numbers")
     if residual is not None and residual.shape != x.shape:
         raise ValueError(f"dropout: residual has shape {tuple(residual.shape)}, not {tuple(x.shape)}")
-    if torch.is_grad_enabled() and (x.requires_grad or (residual is not None and residual.requires_grad)):
-        return DropoutFunction.apply(x, residual, float(p), int(seed), int(offset))
-    return _dropout(_dense(x), float(p), int(seed), int(offset), None if residual is None else _dense(residual))
+    return DropoutFunction.apply(x, residual, float(p), int(seed), int(offset))
