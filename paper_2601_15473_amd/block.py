@@ -17,7 +17,7 @@ import torch
 from torch.autograd import forward_ad
 
 from . import libsk as sk
-from .nn import _DTYPES, _native, _on, _stream, _workspace
+from .nn import _DTYPES, _native, _on, _queueing, _stream, _workspace
 
 _REFUSED = 2 ** 64 - 1
 
@@ -132,7 +132,7 @@ def _attention_forward(q, k, v, q_lengths, k_lengths, causal, scale, training):
     if q.numel() == 0 or k.numel() == 0:
         return o.zero_(), lse, rest
     shape = _attention_shape(q, k, v, q_lengths, k_lengths, causal, scale)
-    with _on(q.device):
+    with _on(q.device), _queueing:
         stream = _stream(q.device)
         ws = _attention_workspace(shape, 0, q.device, stream)
         sk.check(sk.sk_attention_fwd(shape, q, k, v, o, lse, rest, ws, ws.numel(), stream))
@@ -160,7 +160,7 @@ class AttentionFunction(torch.autograd.Function):
             return dq.zero_(), dk.zero_(), dv.zero_(), None, None, None, None, None
         do = _dense(do)
         shape = _attention_shape(q, k, v, q_lengths, k_lengths, ctx.causal, ctx.scale)
-        with _on(q.device):
+        with _on(q.device), _queueing:
             stream = _stream(q.device)
             ws = _attention_workspace(shape, 1, q.device, stream)
             sk.check(sk.sk_attention_bwd(shape, q, k, v, o, lse, rest, do, dq, dk, dv, ws, ws.numel(), stream))
@@ -243,7 +243,7 @@ class NormRopeFunction(torch.autograd.Function):
             return dq, dk, dwq.zero_(), dwk.zero_(), None, None, None, None, None
         shape = _norm_rope_shape(q, k, cos, positions, ctx.eps, ctx.interleaved, q, k)
         dq_out, dk_out = _dense(dq_out), _dense(dk_out)
-        with _on(q.device):
+        with _on(q.device), _queueing:
             stream = _stream(q.device)
             ws = _workspace(q.device, stream, sk.sk_norm_rope_workspace_bytes(shape))
             sk.check(sk.sk_norm_rope_bwd(shape, q, k, wq, wk, cos, sin, positions, dq_out, dk_out, dq, dk, dwq, dwk, ws, ws.numel(), stream))
@@ -341,7 +341,7 @@ class EmbeddingFunction(torch.autograd.Function):
             return None, dtable.zero_(), None
         dy = _dense(dy)
         args = (ids.numel(), rows, width)
-        with _on(dy.device):
+        with _on(dy.device), _queueing:
             stream, dt = _stream(dy.device), _DTYPES[dy.dtype]
             need = sk.sk_embedding_workspace_bytes(*args, dt)
             if need == _REFUSED:

@@ -18,6 +18,7 @@ from __future__ import annotations
 import collections
 import contextlib
 import math
+import threading
 import warnings
 
 import torch
@@ -37,11 +38,14 @@ _DTYPES = {torch.float32: sk.SK_F32, torch.bfloat16: sk.SK_BF16}
 _workspaces: "collections.OrderedDict" = collections.OrderedDict()
 _MAX_WORKSPACES = 8
 _HERE = contextlib.nullcontext()
+# Held from when a call takes its scratch buffer until its kernels are queued: threads on one stream share the buffer, and the library's
+# call lets another thread run (a gradient's second kernel would read what that thread's first one left).
+_queueing = threading.RLock()
 
 
 def _workspace(device: torch.device, stream: int, nbytes: int) -> torch.Tensor:
     """One scratch buffer per (device, stream): calls on a stream run in order, so they can
-    share it.  A buffer grows to the largest request seen on its stream; at most
+    share it (with ``_queueing`` held).  A buffer grows to the largest request seen on its stream; at most
     ``_MAX_WORKSPACES`` streams keep one (least recently used dropped first: torch's caching
     allocator keeps a dropped buffer alive until the work queued on it is done), and
     ``release_workspaces()`` drops them all.  A call that is being recorded into a graph gets a buffer of
@@ -61,7 +65,8 @@ def _workspace(device: torch.device, stream: int, nbytes: int) -> torch.Tensor:
 
 def release_workspaces() -> None:
     """Give the layers' scratch buffers back to the allocator (they are re-created on demand)."""
-    _workspaces.clear()
+    with _queueing:
+        _workspaces.clear()
     if _native is not None:
         _native.release_workspaces()
 
@@ -128,7 +133,7 @@ class SKLinearFunction(torch.autograd.Function):
         tokens = x2.shape[0]
         y = torch.empty((tokens, d_out), dtype=dtype, device=x.device)
         args = (tokens, d_in, d_out, l, k, _DTYPES[dtype])
-        with _on(x.device):
+        with _on(x.device), _queueing:
             stream = _stream(x.device)
             need = sk.sk_linear_workspace_bytes(sk.SK_OP_FWD, *args)
             if need == 2 ** 64 - 1:
@@ -149,7 +154,7 @@ class SKLinearFunction(torch.autograd.Function):
         dY2 = _rows(dY if dY.dtype == dtype else dY.to(dtype), d_out)
         need_dx, _, need_du, need_db = ctx.needs_input_grad[:4]
         dX = dU = db = None
-        with _on(dY.device):
+        with _on(dY.device), _queueing:
             stream = _stream(dY.device)
             want_w = need_du or (need_db and ctx.has_bias)
             # (never less than that of either gradient by itself)
@@ -289,7 +294,7 @@ class SKLinearTwoSidedFunction(torch.autograd.Function):
         tokens = x2.shape[0]
         y = torch.empty((tokens, d_out), dtype=dtype, device=x.device)
         args = (tokens, d_in, d_out, 2 * l, k, _DTYPES[dtype])
-        with _on(x.device):
+        with _on(x.device), _queueing:
             stream = _stream(x.device)
             need = sk.sk_linear_workspace_bytes(sk.SK_OP_FWD, *args)
             if need == 2 ** 64 - 1:
@@ -307,7 +312,7 @@ class SKLinearTwoSidedFunction(torch.autograd.Function):
         dtype, half = A_cat.dtype, ctx.half
         dY2 = _rows(dY if dY.dtype == dtype else dY.to(dtype), d_out)
         dev = dY.device
-        with _on(dev):
+        with _on(dev), _queueing:
             stream = _stream(dev)
             need = sk.sk_linear_workspace_bytes(sk.SK_OP_BWD_TWO_SIDED, *ctx.args)
             ws = _workspace(dev, stream, need)
