@@ -36,20 +36,26 @@ def _training(*tensors) -> bool:
     return torch.jit.is_tracing() or (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors))
 
 
+class _Underivable(torch.autograd.Function):
+    """Results of ``compute`` that depend on something, with no rule for how."""
+
+    @staticmethod
+    def forward(ctx, anchor, compute):
+        return compute()
+
+    @staticmethod
+    def backward(ctx, *unused):
+        raise RuntimeError("libsk: a gradient of a gradient was asked for; these operators are differentiated once, not twice")
+
+
 def _once(backward):
-    """A backward pass whose gradients cannot be differentiated again, and say so where that is tried, whatever the gradients it was
-    given depend on (they themselves do on what it has saved)."""
+    """A backward pass whose gradients refuse to be differentiated, where a graph of it is made (create_graph): all of them do, also
+    those that depend on nothing that has a gradient, so that a program is told the same whatever it differentiates."""
     @functools.wraps(backward)
     def wrapper(ctx, *grads):
-        with torch.no_grad():
-            out = backward(ctx, *grads)
         if not torch.is_grad_enabled():
-            return out
-        there = [g.detach().requires_grad_() for g in out if g is not None]
-        fail = torch._C._functions.DelayedError(b"trying to differentiate twice a function that was marked with @once_differentiable", len(there))
-        marked = fail(*there)
-        left = iter(marked if isinstance(marked, tuple) else (marked,))
-        return tuple(None if g is None else next(left) for g in out)
+            return backward(ctx, *grads)
+        return _Underivable.apply(torch.empty(0, requires_grad=True), lambda: backward(ctx, *grads))
     return wrapper
 
 

@@ -5,7 +5,7 @@
 // sk_torch.cpp's leave out, tensors that have to be copied first, arguments that are to be refused -- gives None, and block.py goes on from there.
 #include "sk_torch_block.h"
 
-#include <torch/csrc/autograd/functions/basic_ops.h>
+#include <functional>
 
 #include "../../include/sk_block.h"
 
@@ -30,18 +30,18 @@ bool strided(const Tensor& t, int64_t token) {
 // Tokens that do not overlap in memory (block.py's _apart)
 bool apart(const Tensor& t) { return t.size(1) <= 1 || t.stride(1) >= t.size(3); }
 
-// Gradients that cannot be differentiated again say so where that is tried.
-variable_list once(variable_list grads) {
-  if (!at::GradMode::is_enabled()) return grads;
-  variable_list inputs;
-  for (const Tensor& g : grads)
-    if (g.defined()) inputs.push_back(g.detach().set_requires_grad(true));
-  const auto error = std::make_shared<torch::autograd::DelayedError>("trying to differentiate twice a function that was marked with @once_differentiable", (int64_t)inputs.size());
-  variable_list out = (*error)(std::move(inputs));
-  size_t at = 0;
-  for (Tensor& g : grads)
-    if (g.defined()) g = out[at++];
-  return grads;
+// Results that depend on something, with no rule for how (block.py's _Underivable).
+struct Underivable : torch::autograd::Function<Underivable> {
+  static variable_list forward(AutogradContext*, const Tensor&, const std::function<variable_list()>& compute) { return compute(); }
+  static variable_list backward(AutogradContext*, variable_list) {
+    TORCH_CHECK(false, "libsk: a gradient of a gradient was asked for; these operators are differentiated once, not twice");
+  }
+};
+// A backward pass's gradients; where a graph of it is made they refuse to be differentiated.
+template <typename Compute>
+variable_list once(const Compute& compute) {
+  if (!at::GradMode::is_enabled()) return compute();
+  return Underivable::apply(at::empty({0}, at::kFloat).set_requires_grad(true), std::function<variable_list()>(compute));
 }
 
 // (a function's arguments are tensors that are there, or options)
@@ -107,6 +107,11 @@ struct Attention : torch::autograd::Function<Attention> {
   }
 
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    const variable_list out = once([&] { return gradients(ctx, grads); });
+    return {out[0], out[1], out[2], Tensor(), Tensor(), Tensor(), Tensor()};
+  }
+
+  static variable_list gradients(AutogradContext* ctx, const variable_list& grads) {
     const variable_list saved = ctx->get_saved_variables();
     const Tensor &q = saved[0], &k = saved[1], &v = saved[2];
     const c10::DeviceGuard guard(q.device());
@@ -124,8 +129,7 @@ struct Attention : torch::autograd::Function<Attention> {
                             dv.data_ptr(), ws.data_ptr(), (size_t)ws.numel(), stream);
     }
     check(st);
-    variable_list out = once({dq, dk, dv});
-    return {out[0], out[1], out[2], Tensor(), Tensor(), Tensor(), Tensor()};
+    return {dq, dk, dv};
   }
 };
 
@@ -162,6 +166,11 @@ struct NormRope : torch::autograd::Function<NormRope> {
   }
 
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    const variable_list out = once([&] { return gradients(ctx, grads); });
+    return {out[0], out[1], out[2], out[3], Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+  }
+
+  static variable_list gradients(AutogradContext* ctx, const variable_list& grads) {
     const variable_list t = ctx->get_saved_variables();
     const Tensor &q = t[0], &k = t[1], &wq = t[2], &wk = t[3];
     const c10::DeviceGuard guard(q.device());
@@ -179,8 +188,7 @@ struct NormRope : torch::autograd::Function<NormRope> {
                             dko.data_ptr(), dq.data_ptr(), dk.data_ptr(), dwq.data_ptr(), dwk.data_ptr(), ws.data_ptr(), (size_t)ws.numel(), stream);
     }
     check(st);
-    variable_list out = once({dq, dk, dwq, dwk});
-    return {out[0], out[1], out[2], out[3], Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+    return {dq, dk, dwq, dwk};
   }
 };
 
@@ -205,6 +213,10 @@ struct Embedding : torch::autograd::Function<Embedding> {
   }
 
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    return {Tensor(), once([&] { return gradients(ctx, grads); })[0], Tensor()};
+  }
+
+  static variable_list gradients(AutogradContext* ctx, const variable_list& grads) {
     const Tensor ids = ctx->get_saved_variables()[0];
     const c10::DeviceGuard guard(ids.device());
     const Tensor dy = made_dense(grads[0]);
@@ -221,7 +233,7 @@ struct Embedding : torch::autograd::Function<Embedding> {
                             dtype_of(dy), ws.data_ptr(), (size_t)ws.numel(), stream);
     }
     check(st);
-    return {Tensor(), once({dtable})[0], Tensor()};
+    return {dtable};
   }
 };
 
