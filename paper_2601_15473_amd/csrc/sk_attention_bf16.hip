@@ -559,7 +559,7 @@ __global__ __launch_bounds__(HALVES * WAVES * 64, 2) void attention_dq_kernel(co
   const int first_i = (r0 + wave * 32) / p.group, last_i = (r0 + wave * 32 + 31) / p.group;
   const int most = __builtin_amdgcn_readfirstlane(first_i < p.q_len ? q.seen(first_i, last_i) : 0);
   const int common = __builtin_amdgcn_readfirstlane(last_i < q.n ? q.limit(first_i) : 0);
-  const bool counts = row.there && row.i < q.n;
+  const bool counts = limit > 0;   // (of a row that sees nothing, not what came back for it either)
 
   const bf16* const kb = static_cast<const bf16*>(p.k) + b * p.ks[0] + hk * p.ks[2];
   const bf16* const vb = static_cast<const bf16*>(p.v) + b * p.vs[0] + hk * p.vs[2];
@@ -593,7 +593,7 @@ __global__ __launch_bounds__(HALVES * WAVES * 64, 2) void attention_dq_kernel(co
   settle(qf);
   settle(gf);
   // (a row that sees nothing has no probabilities, whatever its lse says)
-  float lse = limit > 0 ? p.lse[stat] * LOG2E : INFINITY;
+  float lse = counts ? p.lse[stat] * LOG2E : INFINITY;
   asm volatile("" : "+v"(lse), "+v"(delta));
   if (row.there && lane < 32 && share == 0 && half == 0) {
     p.lse2[stat] = lse;
@@ -710,8 +710,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dkv_kernel(const Atte
   const Sequence q(p, b);
   const int j0 = tile * WAVES * 32, jw = j0 + wave * 32, j = jw + (lane & 31);
   const bool there = j < q.m;
-  // the first tile that the work-group and the wave look at (the first query that sees a key; past the end none does)
-  const int i_begin = q.causal && j0 - q.shift + 1 > 0 ? (j0 - q.shift + 1) / TILE_ROWS * TILE_ROWS : 0;
+  // the first query that the work-group and the wave look at: that sees their first key, and no earlier one, whose dO need not be a number if it
+  // sees nothing (past the end none does)
+  const int i_begin = q.causal && j0 - q.shift + 1 > 0 ? j0 - q.shift + 1 : 0;
   const int i_wave = jw < q.m ? (q.causal ? jw - q.shift + 1 : 0) : INT32_MAX;
   const int i_whole = jw + 31 < q.m ? (q.causal ? jw + 31 - q.shift + 1 : 0) : INT32_MAX;   // from here on queries see all the wave's keys
   const int per_head = j0 < q.m && q.n > i_begin ? (q.n - i_begin + TILE_ROWS - 1) / TILE_ROWS : 0;

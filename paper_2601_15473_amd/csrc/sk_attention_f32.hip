@@ -151,7 +151,7 @@ __global__ __launch_bounds__(256) void attention_dq_f32_kernel(const AttentionAr
   const Row row(p, r0 + wave * 32 + (lane & 31), hk);
   const int limit = row.there ? q.limit(row.i) : 0;
   const int keys = q.seen(r0 / p.group, (r0 + 127) / p.group);
-  const bool counts = row.there && row.i < q.n;
+  const bool counts = limit > 0;   // (of a row that sees nothing, not what came back for it either)
 
   typename M::Frag qf[KS], gf[KS];
   const int64_t at = (((int64_t)b * p.q_len + row.i) * p.heads + row.h) * p.D;
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(256) void attention_dq_f32_kernel(const AttentionAr
   }
   delta += other_half(delta);
   // (a row that sees nothing has no probabilities, whatever its lse says)
-  const float lse = limit > 0 ? p.lse[stat] * LOG2E : INFINITY;
+  const float lse = counts ? p.lse[stat] * LOG2E : INFINITY;
   if (row.there && lane < 32) {
     p.lse2[stat] = lse;
     p.delta[stat] = delta;
@@ -217,9 +217,9 @@ __global__ __launch_bounds__(256) void attention_dkv_f32_kernel(const AttentionA
   const Sequence q(p, b);
   const int j0 = tile * 128, j = j0 + wave * 32 + (lane & 31);
   const bool there = j < q.m;
-  // the first query that sees key j, and the work-group's first
+  // the first query that sees key j, and the work-group's first (no earlier one, whose dO need not be a number if it sees nothing)
   const int first = q.causal ? j - q.shift + 1 : 0;
-  const int i_begin = j0 >= q.m ? q.n : q.causal && j0 - q.shift + 1 > 0 ? (j0 - q.shift + 1) / ROWS * ROWS : 0;
+  const int i_begin = j0 >= q.m ? q.n : q.causal && j0 - q.shift + 1 > 0 ? j0 - q.shift + 1 : 0;
 
   typename M::Frag kf[KS], vf[KS];
   load_row<DP>(kf, static_cast<const float*>(p.k) + b * p.ks[0] + j * p.ks[1] + hk * p.ks[2], there, p.D, lane);
