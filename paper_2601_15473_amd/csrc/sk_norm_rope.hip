@@ -175,7 +175,7 @@ __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(const NormRopeArgs p
 #pragma unroll
         for (int i = 0; i < 8; ++i) ss += x[i] * x[i];
         ss = sum_lanes<L>(ss);
-        const float r = 1.f / sqrtf(ss / p.D + p.eps);
+        const float r = there ? 1.f / sqrtf(ss / p.D + p.eps) : 0.f;   // (a head that is not there: not 1 / 0 where eps is 0)
         float gx = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {   // the rotation back, then the norm's
