@@ -195,12 +195,12 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lengths: torc
     if k.shape[2] == 0 or q.shape[2] % k.shape[2] != 0:
         raise ValueError(f"attention: {q.shape[2]} query heads are not a multiple of {k.shape[2]} key heads")
     lengths = []
-    for name, t in (("q_lengths", q_lengths), ("k_lengths", k_lengths)):
+    for name, t, most in (("q_lengths", q_lengths, q.shape[1]), ("k_lengths", k_lengths, k.shape[1])):
         if t is not None:
             _integers("attention", name, t, q.device)
             if t.shape != (q.shape[0],):
                 raise ValueError(f"attention: {name} has shape {tuple(t.shape)}, not [{q.shape[0]}]")
-            t = t.to(torch.int32).contiguous()
+            t = (t if t.dtype == torch.int32 else t.clamp(0, most).to(torch.int32)).contiguous()   # (not the low halves of what does not fit)
         lengths.append(t)
     scale = float(q.shape[3]) ** -0.5 if scale is None else float(scale)
     return AttentionFunction.apply(q, k, v, *lengths, bool(causal), scale, _training(q, k, v))
