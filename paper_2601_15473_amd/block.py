@@ -11,6 +11,7 @@ Tensors are float32 or bfloat16, all floating ones of a call alike; sums are fp3
 """
 from __future__ import annotations
 
+import ctypes
 import functools
 
 import torch
@@ -112,15 +113,15 @@ def _apart(t: torch.Tensor) -> torch.Tensor:
 # attention
 # ---------------------------------------------------------------------------
 
+# (The library's structures are made in one call each: a compiler that looks at these functions takes an assignment to an array in one for one to its class.)
+_2, _3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
+
+
 def _attention_shape(q, k, v, q_lengths, k_lengths, causal, scale):
-    s = sk.AttentionShape()
-    s.batch, s.q_len, s.heads, s.head_dim = q.shape
-    s.k_len, s.kv_heads = k.shape[1], k.shape[2]
-    s.causal, s.scale, s.dtype = int(causal), scale, _DTYPES[q.dtype]
-    s.q_strides[:], s.k_strides[:], s.v_strides[:] = q.stride()[:3], k.stride()[:3], v.stride()[:3]
-    s.q_lengths = None if q_lengths is None else q_lengths.data_ptr()
-    s.k_lengths = None if k_lengths is None else k_lengths.data_ptr()
-    return s
+    batch, q_len, heads, head_dim = q.shape
+    return sk.AttentionShape(batch, q_len, k.shape[1], heads, k.shape[2], head_dim, int(causal), scale, _DTYPES[q.dtype],
+                             _3(*q.stride()[:3]), _3(*k.stride()[:3]), _3(*v.stride()[:3]),
+                             None if q_lengths is None else q_lengths.data_ptr(), None if k_lengths is None else k_lengths.data_ptr())
 
 
 def _attention_workspace(shape, backward, device, stream):
@@ -211,14 +212,9 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lengths: torc
 # ---------------------------------------------------------------------------
 
 def _norm_rope_shape(q, k, cos, positions, eps, interleaved, q_out, k_out):
-    s = sk.NormRopeShape()
-    s.tokens, s.heads, s.head_dim = q.shape
-    s.kv_heads = k.shape[1]
-    s.table_rows, s.rotary_dim = cos.shape[0], 2 * cos.shape[1]
-    s.interleaved, s.position_bytes, s.eps, s.dtype = int(interleaved), positions.element_size(), eps, _DTYPES[q.dtype]
-    s.q_strides[:], s.k_strides[:] = q.stride()[:2], k.stride()[:2]
-    s.q_out_strides[:], s.k_out_strides[:] = q_out.stride()[:2], k_out.stride()[:2]
-    return s
+    tokens, heads, head_dim = q.shape
+    return sk.NormRopeShape(tokens, heads, k.shape[1], head_dim, 2 * cos.shape[1], int(interleaved), positions.element_size(), cos.shape[0], eps, _DTYPES[q.dtype],
+                            _2(*q.stride()[:2]), _2(*k.stride()[:2]), _2(*q_out.stride()[:2]), _2(*k_out.stride()[:2]))
 
 
 def _norm_rope_forward(q, k, wq, wk, cos, sin, positions, eps, interleaved, out=None):
