@@ -103,7 +103,7 @@ typedef struct {
   int64_t q_out_strides[2], k_out_strides[2];   /* of the results (a cache's slots, say); the gradients are dense */
 } sk_norm_rope_shape;
 
-/* The results may be the inputs (same pointer and strides). */
+/* The results may be the inputs (same pointer and strides).  A result's rows must not lie on one another (SK_ERR_INVALID_ARG: a stride of 0, say). */
 sk_status sk_norm_rope_fwd(const sk_norm_rope_shape* shape, const void* q, const void* k, const void* q_weight, const void* k_weight,
                            const float* cos, const float* sin, const void* positions, void* q_out, void* k_out, void* stream);
 

@@ -71,6 +71,19 @@ size_t attention_bytes(const AttentionArgs& a, bool f32, bool backward) {
   return 2 * stat_bytes(a) + parts_bytes(a, attention_parts(a, f32)) + query_shares_bytes(a, f32 ? 1 : attention_query_shares(a));
 }
 
+// Whether two of `tokens` x `heads` rows of D values lie on the same place.
+bool rows_overlap(int64_t tokens, int64_t heads, int64_t D, int64_t token_stride, int64_t head_stride) {
+  if (tokens > 1 && token_stride < D) return true;
+  if (heads > 1 && head_stride < D) return true;
+  // (one inside the other's step, as any slice of a tensor is)
+  if (tokens == 1 || heads == 1 || token_stride >= (heads - 1) * head_stride + D || head_stride >= (tokens - 1) * token_stride + D) return false;
+  for (int64_t h = 1; h < heads; ++h) {   // the tokens whose rows begin next to head h's, on either side
+    const int64_t t = h * head_stride / token_stride, past = h * head_stride - t * token_stride;
+    if ((t < tokens && past < D) || (t + 1 < tokens && token_stride - past < D)) return true;
+  }
+  return false;
+}
+
 sk_status norm_rope_args(const sk_norm_rope_shape* s, NormRopeArgs& a, bool back) {
   if (s == nullptr) return SK_ERR_INVALID_ARG;
   if (s->tokens < 1 || s->heads < 1 || s->kv_heads < 0 || s->head_dim < 1 || s->rotary_dim < 0 || s->rotary_dim > s->head_dim || s->interleaved < 0 ||
@@ -92,6 +105,9 @@ sk_status norm_rope_args(const sk_norm_rope_shape* s, NormRopeArgs& a, bool back
                   !stride_ok(keys ? k_sizes[i] : 1, s->k_out_strides[i], s->dtype, most, a.kos[i], st)))
       return st;
   }
+  if (!back && (rows_overlap(s->tokens, s->heads, s->head_dim, a.qos[0], a.qos[1]) ||
+                (s->kv_heads > 0 && rows_overlap(s->tokens, s->kv_heads, s->head_dim, a.kos[0], a.kos[1]))))
+    return SK_ERR_INVALID_ARG;
   a.tokens = s->tokens; a.table_rows = s->table_rows;
   a.heads = s->heads; a.kv_heads = s->kv_heads; a.D = s->head_dim; a.rotary = s->rotary_dim;
   a.interleaved = s->interleaved; a.pos64 = s->position_bytes == 8;
