@@ -306,6 +306,7 @@ def head_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: torch.Tensor, k_w
                 t.copy_(result)
         else:
             _norm_rope_forward(_strided(q3, -1), _strided(k3, -1), _dense(q_weight), _dense(k_weight), *args, views)
+            torch.autograd.graph.increment_version([t for t in out if not t.is_inference()])   # (as a change in place: who has saved them finds out)
         return tuple(out)
     q_out, k_out = NormRopeFunction.apply(q3, k3, q_weight, k_weight, *args)
     return (q_out, k_out) if len(lead) == 1 else (q_out.view(q.shape), k_out.view(k.shape))
