@@ -292,7 +292,7 @@ def head_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: torch.Tensor, k_w
     args = (_dense(cos), _dense(sin), _dense(positions.reshape(-1)), float(eps), bool(interleaved))
     if out is not None:
         floating = (q, k, q_weight, k_weight)
-        if torch.is_grad_enabled() and any(t.requires_grad for t in floating):
+        if torch.is_grad_enabled() and any(t.requires_grad for t in (*floating, *out)):
             raise RuntimeError("head_norm_rope: out is for calls without gradients")
         for t, like, name in zip(out, (q, k), ("q_out", "k_out")):
             _checked("head_norm_rope", q, **{name: t})

@@ -26,6 +26,16 @@ def test_who_has_saved_them_finds_out(which):
         y.sum().backward()
 
 
+def test_results_with_gradients_are_refused():
+    from paper_2601_15473_amd import block
+    args = _inputs()
+    out = torch.empty_like(args[0]).requires_grad_() * 1, torch.empty_like(args[1])
+    with pytest.raises(RuntimeError, match="without gradients"):
+        block.head_norm_rope(*args, out=out)
+    with torch.no_grad():
+        assert torch.equal(block.head_norm_rope(*args, out=out)[0], block.head_norm_rope(*args)[0])
+
+
 def test_in_inference_mode_and_expanded():
     from paper_2601_15473_amd import block
     from paper_2601_15473_amd import libsk as sk
