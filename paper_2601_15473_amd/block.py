@@ -258,7 +258,7 @@ def head_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: torch.Tensor, k_w
                    sin: torch.Tensor, positions: torch.Tensor, *, eps: float = 1e-6, interleaved: bool = False, out=None):
     """RMS norm of every head of ``q [..., heads, head_dim]`` and ``k [..., kv_heads, head_dim]`` with weights ``[head_dim]``, then
     the rotation of its first features by the token's position: row ``positions[...]`` of the fp32 tables ``cos`` and ``sin
-    [rows, rotated / 2]`` (positions outside the tables take their first or last row).  Pairs are a feature and the one
+    [rows, rotated / 2]`` (positions outside the tables take their first or last row; the tables get no gradient).  Pairs are a feature and the one
     rotated / 2 further, or with ``interleaved`` neighbours.  Returns the two results, dense; outside of
     autograd they go into ``out = (q_out, k_out)`` if given (a cache's slots, or q and k themselves).
 
@@ -282,6 +282,8 @@ def head_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: torch.Tensor, k_w
             raise TypeError(f"head_norm_rope: {name} has dtype {t.dtype}, not float32")
         if t.device != q.device:
             raise RuntimeError(f"head_norm_rope: {name} is on {t.device}, not on {q.device}")
+        if torch.is_grad_enabled() and t.requires_grad:
+            raise RuntimeError(f"head_norm_rope: {name} gets no gradient; pass it detached")
     if cos.dim() != 2 or cos.shape != sin.shape or 2 * cos.shape[1] > D or (cos.shape[0] == 0 and cos.shape[1] > 0):
         raise ValueError("head_norm_rope: cos and sin are [rows, rotated / 2], of one row at least")
     _integers("head_norm_rope", "positions", positions, q.device)
@@ -301,7 +303,7 @@ def head_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: torch.Tensor, k_w
         views = tuple(t if t.dim() == 3 else t.view(-1, *t.shape[-2:]) for t in out)
         if any(_strided(t, -1) is not t for t in views):
             raise ValueError("head_norm_rope: out needs heads of consecutive values at 16-byte boundaries")
-        if torch.jit.is_tracing() or any(forward_ad.unpack_dual(t).tangent is not None for t in floating):   # (as _training says)
+        if torch.jit.is_tracing() or any(forward_ad.unpack_dual(t).tangent is not None for t in (*floating, cos, sin)):   # (as _training says)
             for t, result in zip(views, NormRopeFunction.apply(q3, k3, q_weight, k_weight, *args)):
                 t.copy_(result)
         else:

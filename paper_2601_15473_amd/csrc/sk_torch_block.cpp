@@ -316,7 +316,7 @@ PyObject* head_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
   if (cos.scalar_type() != at::kFloat || sin.scalar_type() != at::kFloat || cos.device() != q.device() || sin.device() != q.device() || cos.dim() != 2 || cos.numel() == 0 ||
       cos.sizes() != sin.sizes() || 2 * cos.size(1) > D || !dense(cos) || !dense(sin) || !integers(positions, q.device()) || positions.dim() != 1 ||
-      positions.size(0) != q.size(0) || !dense(positions))
+      positions.size(0) != q.size(0) || !dense(positions) || (at::GradMode::is_enabled() && (cos.requires_grad() || sin.requires_grad())))
     Py_RETURN_NONE;
   const bool interleaved = a[8] == Py_True;
   const NormRopeCall c(q, k, cos, positions, eps, interleaved);
