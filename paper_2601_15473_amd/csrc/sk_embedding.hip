@@ -25,7 +25,7 @@ template <typename T, int ROWS>
 __global__ __launch_bounds__(256) void embedding_fwd_kernel(const EmbeddingArgs p, int threads) {
   constexpr int V = 16 / sizeof(T), STEPS = 4 / ROWS;
   const int subs = 256 / threads, sub = threadIdx.x / threads, first = (threadIdx.x - sub * threads) * V, step = threads * V;
-  const int64_t t0 = (int64_t)blockIdx.x * subs * ROWS + sub;
+  const int64_t t0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * subs * ROWS + sub;
   const T* from[ROWS];
   bool there[ROWS];
 #pragma unroll
@@ -282,9 +282,10 @@ hipError_t fwd(const EmbeddingArgs& a, hipStream_t s) {
   // rows to a thread: as many as leave it four steps, and every CU eight work-groups
   const int steps = (a.width * (int)sizeof(T) / 16 + threads - 1) / threads, subs = 256 / threads;
   const int most = (int)(a.tokens / (8 * NUM_CUS * subs)), rows = steps == 1 && most >= 4 ? 4 : steps <= 2 && most >= 2 ? 2 : 1;
+  const int64_t groups = (a.tokens + subs * rows - 1) / (subs * rows), along = groups < 1 << 23 ? groups : 1 << 23;   // (a dimension takes 2^32 threads)
   return launch_kernel("embedding_fwd_kernel", Work{0.0, 2.0 * a.tokens * a.width * sizeof(T)},
                        rows == 4 ? embedding_fwd_kernel<T, 4> : rows == 2 ? embedding_fwd_kernel<T, 2> : embedding_fwd_kernel<T, 1>,
-                       dim3((unsigned)((a.tokens + subs * rows - 1) / (subs * rows))), dim3(256), s, a, threads);
+                       dim3((unsigned)along, (unsigned)((groups + along - 1) / along)), dim3(256), s, a, threads);
 }
 
 template <typename T>

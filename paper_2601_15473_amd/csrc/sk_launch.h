@@ -51,6 +51,8 @@ inline hipError_t launch_kernel(const char* name, Work work, void (*kernel)(KArg
   LaunchHooks* h = launch_hooks();
   if (h != nullptr && h->tracing()) {
     h->launch_recorded(name, grid.x * grid.y * grid.z);
+    // (what HIP would refuse: 2^32 threads along a dimension, 2^16 work-groups along the second or third)
+    if ((uint64_t)grid.x * block.x > 0xffffffffull || grid.y > 0xffff || grid.z > 0xffff) return hipErrorInvalidConfiguration;
     return hipSuccess;
   }
   if (h != nullptr) h->before(name, grid.x * grid.y * grid.z, work.flops, work.bytes, s);
