@@ -49,6 +49,12 @@ class DecoderLayer(torch.nn.Module):
         return dropout(h, p, seed, offset + 1, residual=x)
 
 
+class Cache(tuple):
+    """(keys and values [layers, batch, tokens, 2, kv_heads, head_dim], how many there are of each sequence: int32 [batch]), both on the GPU."""
+
+    most = 0     # as many as any sequence can have by what was appended: known here, where the numbers themselves are a copy away
+
+
 class Decoder(torch.nn.Module):
     def __init__(self, rows: int, width: int = 256, layers: int = 2, heads: int = 4, kv_heads: int = 2, head_dim: int = 64, hidden: int = 512,
                  terms: int = 1, rank: int = 128, context: int = 512, p: float = 0.1, dtype: torch.dtype = torch.bfloat16, seed: int = 0):
@@ -65,6 +71,8 @@ class Decoder(torch.nn.Module):
     def forward(self, ids, lengths=None, step: int = 0):
         """Logits [batch, tokens, rows]; ``lengths`` (int32 [batch]) of padded sequences, whose padding is an id outside the
         table.  ``step``: the training step, whose dropouts are its own."""
+        if ids.shape[1] > len(self.tables[0]):
+            raise ValueError(f"decoder: {ids.shape[1]} tokens, but positions for {len(self.tables[0])}")
         positions = torch.arange(ids.shape[1], device=ids.device).expand(ids.shape)
         p = self.p if self.training else 0.0
         x = embedding(ids, self.table, self.scale)
@@ -77,19 +85,28 @@ class Decoder(torch.nn.Module):
         """Empty room for ``tokens`` keys and values of each sequence, and how many there are of each."""
         layer = self.layers[0]
         kv = torch.zeros((len(self.layers), batch, tokens, 2, layer.kv_heads, layer.head_dim), dtype=self.table.dtype, device="cuda")
-        return kv, torch.zeros(batch, dtype=torch.int32, device="cuda")
+        return Cache((kv, torch.zeros(batch, dtype=torch.int32, device="cuda")))
 
     @torch.no_grad()
     def append(self, ids, cache):
         """Logits of ids [batch, n] behind what the cache holds of each sequence; their keys and values join it."""
         kv, lengths = cache
-        positions = lengths[:, None] + torch.arange(ids.shape[1], dtype=torch.int32, device=ids.device)
-        sequence = torch.arange(len(ids), device=ids.device)[:, None]
-        lengths += ids.shape[1]
+        n, room = ids.shape[1], min(kv.shape[2], len(self.tables[0]))
+        most = cache.most if isinstance(cache, Cache) else room
+        if most + n > room:
+            most = int(lengths.max())           # (not known, or the program may have emptied sequences since)
+        if most + n > room:
+            raise ValueError(f"decoder: {n} tokens behind {most}, but room for {kv.shape[2]} and positions for {len(self.tables[0])}")
+        if isinstance(cache, Cache):
+            cache.most = most + n
+        positions = lengths[:, None] + torch.arange(n, dtype=torch.int32, device=ids.device)
+        # (inside the cache whatever the lengths are: a program that sets them itself must not write elsewhere)
+        sequence, slots = torch.arange(len(ids), device=ids.device)[:, None], positions.clamp(0, kv.shape[2] - 1)
+        lengths += n
         x = embedding(ids, self.table, self.scale)
         for i, layer in enumerate(self.layers):
             q, k, v = layer.heads_of(x, self.tables, positions)
-            kv[i, sequence, positions, 0], kv[i, sequence, positions, 1] = k, v
+            kv[i, sequence, slots, 0], kv[i, sequence, slots, 1] = k, v
             x = layer.finish(x, attention(q, kv[i, :, :, 0], kv[i, :, :, 1], k_lengths=lengths, causal=True), 0.0, 0, 0)
         return self.logits(x)
 
