@@ -30,7 +30,7 @@ using at::Tensor;
 using torch::autograd::AutogradContext;
 using torch::autograd::variable_list;
 
-// One scratch buffer per (device, stream), grown to the largest request; the least recently used of more
+// One scratch buffer per (device, stream), grown to the largest request up to MAX_KEPT; the least recently used of more
 // than MAX_STREAMS goes back to the allocator, which keeps it until the work queued on it is done.
 // Calls queue their kernels under the lock: two threads that share a stream share its buffer.
 // A call that is being recorded into a graph gets a buffer of its own, out of the graph's memory: every replay writes there,
@@ -40,6 +40,9 @@ struct Workspaces {
   // Most that a pass keeps here beside its workspace: an allocation a pass is 1 us of host, 1 to 2 % of a small two-sided layer's step, and the sums
   // of a large one (4096 -> 11008, 2048 columns: 107 MB) would stay on every stream.
   static constexpr size_t MAX_SUMS = 4 << 20;
+  // Most that a stream keeps: a call that needs more (attention's parts can be 130 MB) has its own, which the allocator hands on when the call is queued.
+  // It does not notice the allocation.
+  static constexpr size_t MAX_KEPT = 64 << 20;
   struct Entry {
     c10::DeviceIndex device;
     void* stream;
@@ -62,7 +65,7 @@ struct Workspaces {
 
   // For calls that are queued before the tensor and the lock go (the lock is held).
   Tensor get(const at::Device& device, void* stream, size_t bytes) {
-    if (recording(stream)) return made(device, bytes);
+    if (bytes > MAX_KEPT || recording(stream)) return made(device, bytes);
     auto it = entries.begin();
     while (it != entries.end() && !(it->device == device.index() && it->stream == stream)) ++it;
     if (it == entries.end()) entries.push_front(Entry{device.index(), stream, Tensor()});

@@ -37,6 +37,7 @@ else:
 _DTYPES = {torch.float32: sk.SK_F32, torch.bfloat16: sk.SK_BF16}
 _workspaces: "collections.OrderedDict" = collections.OrderedDict()
 _MAX_WORKSPACES = 8
+_MAX_KEPT = 64 << 20
 _HERE = contextlib.nullcontext()
 # Held from when a call takes its scratch buffer until its kernels are queued: threads on one stream share the buffer, and the library's
 # call lets another thread run (a gradient's second kernel would read what that thread's first one left).
@@ -45,12 +46,13 @@ _queueing = threading.RLock()
 
 def _workspace(device: torch.device, stream: int, nbytes: int) -> torch.Tensor:
     """One scratch buffer per (device, stream): calls on a stream run in order, so they can
-    share it (with ``_queueing`` held).  A buffer grows to the largest request seen on its stream; at most
+    share it (with ``_queueing`` held).  A buffer grows to the largest request seen on its stream, up to ``_MAX_KEPT`` bytes (a call that
+    needs more has a buffer of its own); at most
     ``_MAX_WORKSPACES`` streams keep one (least recently used dropped first: torch's caching
     allocator keeps a dropped buffer alive until the work queued on it is done), and
     ``release_workspaces()`` drops them all.  A call that is being recorded into a graph gets a buffer of
     its own, out of the graph's memory: every replay writes there, long after a stream's may be gone."""
-    if torch.cuda.is_current_stream_capturing():
+    if nbytes > _MAX_KEPT or torch.cuda.is_current_stream_capturing():
         return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
     key = (device.index, stream)
     ws = _workspaces.get(key)
