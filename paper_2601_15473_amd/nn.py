@@ -58,6 +58,8 @@ def _workspace(device: torch.device, stream: int, nbytes: int) -> torch.Tensor:
     ws = _workspaces.get(key)
     if ws is None or ws.numel() < nbytes:
         ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+        if type(ws) is not torch.Tensor:    # (a mode's stand-in, with no memory: for this call, which will be refused, and no other)
+            return ws
         _workspaces[key] = ws
     _workspaces.move_to_end(key)
     while len(_workspaces) > _MAX_WORKSPACES:
