@@ -127,6 +127,8 @@ sk_status sk_embedding_fwd(const void* ids, int32_t id_bytes, const void* table,
 /*
  * dtable[v] = scale * sum over t with ids[t] = v of dy[t], in fp32, added up by sorted tokens (token order within a row,
  * in runs of a fixed length); rows without a token are zeros.  Workspace: sk_embedding_workspace_bytes.
+ * (Made for a step's tokens: they are sorted in runs of up to 16384, each token's place among the other runs found by search, whose number grows with
+ * the square of the tokens.)
  */
 sk_status sk_embedding_bwd(const void* ids, int32_t id_bytes, const void* dy, void* dtable, int64_t tokens, int64_t rows,
                            int64_t width, float scale, sk_dtype dtype, void* workspace, size_t workspace_bytes, void* stream);

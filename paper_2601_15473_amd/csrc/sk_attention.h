@@ -5,6 +5,10 @@
 // dimension of the next along the registers, and a contraction may run in any order, so they go into the next one as
 // they lie, only rounded: register r is element r % 8 of k step r / 8, for which the other operand's rows are read in
 // the same order.  No probability passes through LDS or another lane.
+//
+// Rounded: in bf16 a probability (and ds) is off by up to 2^-9 of itself there, as any bf16 product's operand, and what is summed of it by 0.0022 to
+// 0.0024 of 64 bits, where one rounding of an exact result is 0.0017.  In two bf16 parts it would be another product for each that takes it, where products are the
+// bound.  The sum that divides, and lse, are of the weights before rounding: of 32 bits throughout.
 #pragma once
 #include "sk_bf16_tile.h"
 #include "sk_block_launch.h"

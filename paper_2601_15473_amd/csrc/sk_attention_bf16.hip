@@ -344,7 +344,7 @@ __global__ __launch_bounds__(HALVES * WAVES * 64, 2) void attention_fwd_kernel(c
 
 // Forward for few rows: 32 rows a work-group, a range of the keys, of which every wave takes every fourth tile of 32
 // by itself (no barrier; 64 KB of LDS, so that eight waves a CU have 8 to 16 KB each on their way), joined through LDS.  Bound by reading: eight
-// sequences of 0 to 16384 keys, one query, 64 heads on 8 of 128, 268 MB: 67 us = 4.0 TB/s, what a sum over 2 GB reaches here too (51 where the Infinity Cache
+// sequences of 0 to 16384 keys, one query, 64 heads on 8 of 128, 268 MB: 67 us = 4.0 TB/s, where a plain read of 2 GB by stretches reaches 6.3 (51 where the Infinity Cache
 // has half of it), and 5 of the join.  Ranges twice and half as long, and grids of three and four work-groups a CU, were level or slower.  With several
 // ranges the sums, their maxima and the weights' sums go to the workspace and attention_join_kernel puts them together.
 template <int DP>

@@ -5,8 +5,8 @@
 // further), so the running maximum and sum of the softmax are registers; o^T += V^T p^T.  Backward, no atomics: dq by the same walk
 // over the keys with p from lse, dk and dv by a walk over the queries for 32 keys a wave.  Tiles of 32 keys (queries) go through
 // registers into LDS, one at a time: with fp32 products at a sixteenth of the bf16 ones' rate a wave has 4096 cycles of them a tile at 64 features,
-// and the matrix unit is the bound (16 sequences of 512, eight heads of 64, forward and backward: 407 us, 74 TFLOP/s of the 14 flops a pair and feature,
-// 95 of what is executed, where the library's product reaches 146).
+// and the matrix unit is the bound (16 sequences of 512, eight heads of 64, forward and backward: 389 us, 77 TFLOP/s of the 14 flops a pair and feature,
+// 99 of what is executed, where the library's product reaches 146).
 #include "sk_attention.h"
 
 namespace sk {
