@@ -36,7 +36,8 @@ extern "C" {
  *     o_i = sum_j p_ij v_j,   p_ij = exp(s_ij - lse_i),   s_ij = scale * q_i . k_j,
  *     lse_i = log sum_j exp(s_ij)   over the keys that i sees.
  * A query that sees no key, and a row i >= n, has o = 0 and lse = -infinity.  What lies in keys
- * and values past m and in queries past n is not used, whatever it is.
+ * and values past m and in queries past n is not used, whatever it is.  (Of what counts for some
+ * query, a value that is not finite may reach queries that see other keys but not its own, as zero times it.)
  * (Tokens of k or v that overlap in memory, a token stride below head_dim: what is not finite in the
  * last that counts may come out as NaN where it would be infinity.)
  *

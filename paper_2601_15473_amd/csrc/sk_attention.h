@@ -82,6 +82,15 @@ __device__ __forceinline__ f32x16 zeros() {
   return z;
 }
 
+// Rows (a row of the result to a lane) that do not count are zeros whatever was summed for them: a weight of zero times what is not a number is none.
+template <int ND>
+__device__ __forceinline__ void zeros_unless(bool counts, f32x16 (&acc)[ND]) {
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[d][r] = counts ? acc[d][r] : 0.f;
+}
+
 // Row of register r in the C operand's lane layout.
 __device__ __forceinline__ int acc_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
 

@@ -336,6 +336,7 @@ __global__ __launch_bounds__(HALVES * WAVES * 64, 2) void attention_fwd_kernel(c
     return;
   }
   const int64_t at = (((int64_t)b * p.q_len + row.i) * p.heads + row.h) * p.D;
+  if (__any(sum == 0.f)) zeros_unless(sum != 0.f, o);   // (selects in every wave would be 1 % of 16 sequences of 512)
   store_row_and_rest<DP>(static_cast<bf16*>(p.o) + at, p.o_rest != nullptr ? static_cast<bf16*>(p.o_rest) + at : nullptr, row.there, o, sum == 0.f ? 0.f : 1.f / sum, p.D,
                          lane);
   if (p.lse != nullptr && row.there && lane < 32)
@@ -459,7 +460,7 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(const AttentionAr
       const Row out(p, r0 + r, hk);
       const float scale = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] *= scale;
+      for (int i = 0; i < 8; ++i) v[i] = total == 0.f ? 0.f : v[i] * scale;   // (as zeros_unless)
       const int64_t to = (((int64_t)b * p.q_len + out.i) * p.heads + out.h) * p.D + c;
       store_values<bf16, 8>(static_cast<bf16*>(p.o) + to, v);
       if (p.o_rest != nullptr) {
@@ -519,7 +520,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs
   const float scale = total == 0.f ? 0.f : 1.f / total;
   const int64_t to = (((int64_t)b * p.q_len + out.i) * p.heads + out.h) * p.D + c;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] *= scale;
+  for (int i = 0; i < 4; ++i) v[i] = total == 0.f ? 0.f : v[i] * scale;   // (as zeros_unless)
   store_values<bf16, 4>(static_cast<bf16*>(p.o) + to, v);
   if (p.o_rest != nullptr) {
 #pragma unroll
@@ -686,6 +687,8 @@ __global__ __launch_bounds__(HALVES * WAVES * 64, 2) void attention_dq_kernel(co
   const int lane_out = lane_again();   // (where the row is need not lie in registers all the way)
   const Row out(p, r0 + wave * 32 + (lane_out & 31), hk);
   const int64_t to = (((int64_t)b * p.q_len + out.i) * p.heads + out.h) * p.D;
+  const bool counts_out = out.there && q.limit(out.i) > 0;
+  if (__any(!counts_out)) zeros_unless(counts_out, dq);
   if (!SHARES) store_row<DP>(static_cast<bf16*>(p.dq) + to, out.there, dq, p.scale, p.D, lane_out);
   else if (out.there) store_sums<DP>(p.q_partial + share * ((int64_t)p.batch * p.q_len * p.heads * p.D) + to, dq, p.D, lane_out);
 }
@@ -824,6 +827,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dkv_kernel(const Atte
   }
   const int j_out = jw + (lane_again() & 31);
   const int64_t row = ((int64_t)b * p.k_len + j_out) * p.kv_heads + hk;
+  if (jw + 32 > q.m) {
+    zeros_unless(j_out < q.m, dk);
+    zeros_unless(j_out < q.m, dv);
+  }
   if (p.parts == 1) {
     store_row<DP>(static_cast<bf16*>(p.dk) + row * p.D, j_out < p.k_len, dk, p.scale, p.D, lane_again());
     store_row<DP>(static_cast<bf16*>(p.dv) + row * p.D, j_out < p.k_len, dv, 1.f, p.D, lane_again());

@@ -130,6 +130,7 @@ __global__ __launch_bounds__(256) void attention_fwd_f32_kernel(const AttentionA
     }
   }
   sum += other_half(sum);
+  zeros_unless(sum != 0.f, o);
   if (row.there) {
     store_row<DP>(static_cast<float*>(p.o) + (((int64_t)b * p.q_len + row.i) * p.heads + row.h) * p.D, o, sum == 0.f ? 0.f : 1.f / sum, p.D, lane);
     if (p.lse != nullptr && lane < 32)
@@ -199,6 +200,7 @@ __global__ __launch_bounds__(256) void attention_dq_f32_kernel(const AttentionAr
 #pragma unroll
       for (int t = 0; t < 32 / M::STEP; ++t) dq[d] = M::mma(M::across(k_tile, LD, 0, t, d * 32, lane), M::of_acc(s, t), dq[d]);
   }
+  zeros_unless(counts, dq);
   store_row<DP>(row.there ? static_cast<float*>(p.dq) + at : nullptr, dq, p.scale, p.D, lane);
 }
 
@@ -270,6 +272,8 @@ __global__ __launch_bounds__(256) void attention_dkv_f32_kernel(const AttentionA
     }
   }
   const int64_t at = (((int64_t)b * p.k_len + j) * p.kv_heads + hk) * p.D;
+  zeros_unless(there, dk);
+  zeros_unless(there, dv);
   if (p.parts > 1) {
     const int64_t values = (int64_t)p.batch * p.k_len * p.kv_heads * p.D;
     float* const to = p.partial + part * 2 * values + at;
