@@ -801,15 +801,18 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_dkv_kernel(const Atte
 #pragma unroll
         for (int u = 0; u < 4; ++u) s[r + u] = __builtin_amdgcn_exp2f(s[r + u] * factor - lse[u]);
       }
-      // (past the last query the tile has zeros, or where queries overlap in memory that query again: with lse = 0 its weight may be infinite, which
-      // the zeros of dO would make NaN)
-      if (i_now < i_whole || i_now + TILE_ROWS > q.n) {
+      if (i_now < i_whole) {
         const int j = jw + (lane & 31), first = j < q.m ? (q.causal ? j - q.shift + 1 : 0) : INT32_MAX;   // the first query that sees key j
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int i = i_now + t * 32 + acc_row(r, lane);
-          if (i < first || i >= q.n) s[r] = 0.f;
-        }
+        for (int r = 0; r < 16; ++r)
+          if (i_now + t * 32 + acc_row(r, lane) < first) s[r] = 0.f;
+      }
+      // (past the last query the tile has zeros, or where queries overlap in memory that query again: with lse = 0 its weight may be infinite, which
+      // the zeros of dO would make NaN)
+      if (i_now + TILE_ROWS > q.n) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (i_now + t * 32 + acc_row(r, lane) >= q.n) s[r] = 0.f;
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) g[r] *= s[r];
