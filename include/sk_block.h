@@ -41,6 +41,9 @@ extern "C" {
  * (Tokens of k or v that overlap in memory, a token stride below head_dim: what is not finite in the
  * last that counts may come out as NaN where it would be infinity.)
  *
+ * Scores are fp32: from some 2^24 on they do not tell neighbours apart, and from 2^31 on weights may
+ * overflow, and what is formed of them be NaN.
+ *
  * Limits (else SK_ERR_UNSUPPORTED): head_dim a multiple of 8 up to 128, heads a multiple of
  * kv_heads, token strides and heads * head_dim up to 2^22, q_len * heads / kv_heads and k_len up to 2^27, and batch * kv_heads times the tiles of 128 rows of
  * either below 2^24.
