@@ -1,7 +1,8 @@
 /*
  * libsk -- the operators of a transformer block that stand between its sketched layers
  * (include/sk.h), on AMD MI355X (gfx950): attention, the norms and the position rotation of
- * queries and keys, the token embedding, dropout; each with its gradients.
+ * queries and keys, the token embedding, dropout, layer norm, layers that stay dense, and the loss
+ * against a teacher's largest logits; each with its gradients.
  *
  * Common rules (those of include/sk.h unless said otherwise)
  *   - Every pointer is a DEVICE pointer, 16-byte aligned.  Arrays are dense and row-major
@@ -148,6 +149,94 @@ size_t sk_embedding_workspace_bytes(int64_t tokens, int64_t rows, int64_t width,
  */
 sk_status sk_dropout(const void* x, const void* residual, void* y, int64_t n, float p, uint64_t seed, uint64_t offset,
                      sk_dtype dtype, void* stream);
+
+/*
+ * Layer norm of rows, with a residual added first:
+ *     s = x + residual,   y = (s - mean s) / sqrt(mean (s - mean s)^2 + eps) * weight + bias
+ *   x and residual [rows, width] with row strides, weight and bias [width], y and sum (s) [rows, width] dense.  residual, weight, bias and
+ * sum may be NULL.  stats [rows, 2] fp32 for a backward pass, or NULL: the mean and what the deviation is divided by, inverted.
+ * y is formed of s before its rounding.
+ *   width a multiple of 8 up to 2^15, rows below 2^24.
+ */
+typedef struct {
+  int64_t rows, width;
+  float eps;                 /* >= 0 */
+  sk_dtype dtype;
+  int64_t x_stride, residual_stride;   /* elements between rows */
+} sk_layer_norm_shape;
+
+sk_status sk_layer_norm_fwd(const sk_layer_norm_shape* shape, const void* x, const void* residual, const void* weight, const void* bias,
+                            void* y, void* sum, float* stats, void* stream);
+
+/*
+ * Its gradients: x [rows, width] is what was normed (the sum, where there was a residual), with row stride x_stride; dy and d_sum dense, d_sum the
+ * gradient of the sum or NULL; dx (of x, and of the residual) dense, dweight and dbias in `dtype`, or NULL.  Workspace: sk_layer_norm_workspace_bytes,
+ * needed for dweight and dbias.
+ */
+sk_status sk_layer_norm_bwd(const sk_layer_norm_shape* shape, const void* x, const void* weight, const float* stats, const void* dy, const void* d_sum,
+                            void* dx, void* dweight, void* dbias, void* workspace, size_t workspace_bytes, void* stream);
+size_t sk_layer_norm_workspace_bytes(const sk_layer_norm_shape* shape);
+
+/*
+ * A dense layer:  y = act(z) + residual,  z = x weight^T + bias.
+ *   x [tokens, in] and residual [tokens, out] with row strides, weight [out, in], bias [out], y [tokens, out] dense.  bias and residual may be NULL.
+ * z [tokens, out] dense, for a backward pass of a layer with an activation, or NULL (not looked at without one).
+ *   in and out multiples of 8 up to 2^20, up to 2^24 tokens, strides up to 2^20 and not below a row, each matrix below 2^34 values.
+ */
+typedef enum {
+  SK_ACT_NONE = 0,
+  SK_ACT_RELU = 1,       /* max(z, 0) */
+  SK_ACT_GELU = 2,       /* z Phi(z), Phi the normal distribution's */
+  SK_ACT_GELU_TANH = 3,  /* z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) */
+  SK_ACT_SILU = 4        /* z / (1 + exp(-z)) */
+} sk_activation;
+
+typedef struct {
+  int64_t tokens, in, out;
+  int32_t activation;        /* sk_activation */
+  sk_dtype dtype;
+  int64_t x_stride, residual_stride;   /* elements between rows */
+} sk_dense_shape;
+
+size_t sk_dense_workspace_bytes(const sk_dense_shape* shape, int32_t backward);
+sk_status sk_dense_fwd(const sk_dense_shape* shape, const void* x, const void* weight, const void* bias, const void* residual, void* y, void* z,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradients:  dz = dy act'(z),  dx = dz weight,  dweight = dz^T x,  dbias = sum of dz over tokens  (the residual's is dy).
+ *   z: the forward pass's (NULL without an activation), dy [tokens, out], dx [tokens, in], dweight [out, in], dbias [out] dense, in `dtype`; each gradient may be
+ * NULL.  In bf16 dz is rounded once, as an operand of both products.
+ */
+sk_status sk_dense_bwd(const sk_dense_shape* shape, const void* x, const void* weight, const void* z, const void* dy, void* dx, void* dweight,
+                       void* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The loss of logits z [rows, vocabulary] against a teacher's `top` largest logits t at the places c, and against labels:
+ *     loss = (1 - label_weight) temperature^2 sum_k p_k (log p_k - log q_c(k)) + label_weight (log sum_j exp z_j - z_label),
+ *     p = softmax(t / temperature) over the row's entries,  q = softmax(z / temperature).
+ * An entry whose id is outside the vocabulary or whose logit is -infinity is not there (lists may be of different lengths); a place that is named twice has
+ * both entries.  A row without an entry has no first term, one whose label is outside the vocabulary (or all, with labels NULL) no second.
+ *   logits on any boundary of a value, with a row stride of any number of elements, teacher_logits [rows, top] in `dtype`, teacher_ids [rows, top], labels [rows], loss [rows] fp32.
+ * stats [rows, 4] fp32 for a backward pass, or NULL.  (A row whose logits are all -infinity has no softmax: NaN.)
+ *   rows and vocabulary up to 2^24 (rows below it), top up to 2^16 (0: no teacher; its pointers may be NULL), temperature from 10^-3 to 10^3.
+ */
+typedef struct {
+  int64_t rows, vocabulary, logits_stride;
+  int32_t top;
+  int32_t id_bytes, label_bytes;   /* 4 or 8 */
+  float temperature, label_weight; /* label_weight in 0 .. 1 */
+  sk_dtype dtype;
+} sk_distill_shape;
+
+sk_status sk_distill_fwd(const sk_distill_shape* shape, const void* logits, const void* teacher_logits, const void* teacher_ids, const void* labels,
+                         float* loss, float* stats, void* stream);
+/*
+ * Its gradient, from the inputs, the forward pass's stats and the gradient dloss [rows] of every row's loss:
+ *     dz_j = dloss [ (1 - label_weight) temperature (q_j - sum_{k: c(k) = j} p_k) + label_weight (softmax(z)_j - [j = label]) ],
+ * dlogits [rows, vocabulary] dense in `dtype`; zeros in a row without an entry and a label, whatever its logits are.
+ */
+sk_status sk_distill_bwd(const sk_distill_shape* shape, const void* logits, const void* teacher_logits, const void* teacher_ids, const void* labels,
+                         const float* stats, const float* dloss, void* dlogits, void* stream);
 
 #ifdef __cplusplus
 }

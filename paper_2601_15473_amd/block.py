@@ -4,6 +4,9 @@
 ``head_norm_rope``   RMS norm of every query and key head with the position rotation in the same pass
 ``embedding``        rows of a table by token, scaled
 ``dropout``          dropout by a counter-based generator whose mask is never stored, with a residual added
+``layer_norm``       layer norm of rows, with a residual added first
+``linear``           a layer that stays dense, with bias, activation and residual
+``distillation_loss``  the loss of logits against a teacher's largest ones and against labels
 
 Each has its gradients.  Everything that computes runs in libsk's HIP kernels (include/sk_block.h says what, in full);
 PyTorch provides the tensors, the current stream and the autograd graph.  There is no CPU path: tensors that are not on a GPU raise.
@@ -416,3 +419,250 @@ def dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, residual: tor
     if residual is not None and residual.shape != x.shape:
         raise ValueError(f"dropout: residual has shape {tuple(residual.shape)}, not {tuple(x.shape)}")
     return DropoutFunction.apply(x, residual, float(p), int(seed), int(offset))
+
+
+# ---------------------------------------------------------------------------
+# layer norm
+# ---------------------------------------------------------------------------
+
+def _rows_of(t: torch.Tensor, least: int = 0, most: int = 1 << 40) -> torch.Tensor:
+    """t as a matrix of its rows, in place where they lie a stride of ``least`` to ``most`` elements apart that the library takes."""
+    t = t.reshape(-1, t.shape[-1])
+    if _strided(t, -1) is not t or (t.shape[0] > 1 and not least <= t.stride(0) <= most):
+        return t.clone(memory_format=torch.contiguous_format)
+    return t
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _layer_norm_shape(x, residual, eps):
+    return sk.LayerNormShape(x.shape[0], x.shape[1], eps, _DTYPES[x.dtype], _row_stride(x), x.shape[1] if residual is None else _row_stride(residual))
+
+
+class LayerNormFunction(torch.autograd.Function):
+    """See ``layer_norm``, on rows; keeps what was normed, and each row's mean and deviation."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, residual, eps, training):
+        x2 = _rows_of(x)
+        r2 = None if residual is None else _rows_of(residual)
+        w, b = (None if t is None else _dense(t) for t in (weight, bias))
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        total = None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        stats = torch.empty((x2.shape[0], 2), dtype=torch.float32, device=x.device) if training else None
+        if x.numel() > 0:
+            with _on(x.device):
+                sk.check(sk.sk_layer_norm_fwd(_layer_norm_shape(x2, r2, eps), x2, r2, w, b, y, total, stats, _stream(x.device)))
+        ctx.save_for_backward(x2 if total is None else total, w, stats)
+        ctx.shape, ctx.bias = x.shape, bias is not None
+        ctx.set_materialize_grads(False)
+        return y if total is None else (y, total)
+
+    @staticmethod
+    @_once
+    def backward(ctx, dy, ds=None):
+        x, w, stats = ctx.saved_tensors
+        x = x.reshape(-1, ctx.shape[-1])
+        dx = torch.empty(ctx.shape, dtype=x.dtype, device=x.device)
+        dw, db = (torch.empty(ctx.shape[-1], dtype=x.dtype, device=x.device) if there else None for there in (w is not None, ctx.bias))
+        if x.numel() == 0:
+            for t in (dw, db):
+                if t is not None:
+                    t.zero_()
+            return dx, dw, db, dx if ctx.needs_input_grad[3] else None, None, None
+        dy = torch.zeros_like(dx) if dy is None else _dense(dy)
+        ds = None if ds is None else _dense(ds)
+        shape = _layer_norm_shape(x, None, 0.0)
+        with _on(x.device), _queueing:
+            stream = _stream(x.device)
+            ws = _workspace(x.device, stream, sk.sk_layer_norm_workspace_bytes(shape))
+            sk.check(sk.sk_layer_norm_bwd(shape, x, w, stats, dy, ds, dx, dw, db, ws, ws.numel(), stream))
+        return dx, dw, db, dx if ctx.needs_input_grad[3] else None, None, None
+
+
+def _vector(what: str, name: str, t: torch.Tensor | None, n: int):
+    if t is not None and t.shape != (n,):
+        raise ValueError(f"{what}: {name} has shape {tuple(t.shape)}, not [{n}]")
+
+
+def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, residual: torch.Tensor | None = None, *,
+               eps: float = 1e-5):
+    """Layer norm over the last dimension of ``x [..., width]``, times ``weight`` and plus ``bias [width]`` where they are given.
+
+    With a ``residual`` (as x) the norm is of ``x + residual``, and the sum comes back too: ``(y, sum)``, the stream that a block goes on with.  What is
+    normed is the sum before it is rounded.  Rows of a strided matrix are read in place.  width: a multiple of 8 up to 32768.
+    """
+    if _natively():
+        out = _native.layer_norm(x, weight, bias, residual, eps)
+        if out is not None:
+            return out
+    _checked("layer_norm", x, x=x, weight=weight, bias=bias, residual=residual)
+    if x.dim() == 0 or x.shape[-1] == 0:
+        raise ValueError("layer_norm: x is [..., width]")
+    for name, t in (("weight", weight), ("bias", bias)):
+        _vector("layer_norm", name, t, x.shape[-1])
+    if residual is not None and residual.shape != x.shape:
+        raise ValueError(f"layer_norm: residual has shape {tuple(residual.shape)}, not {tuple(x.shape)}")
+    return LayerNormFunction.apply(x, weight, bias, residual, float(eps), _training(x, weight, bias, residual))
+
+
+# ---------------------------------------------------------------------------
+# dense layers
+# ---------------------------------------------------------------------------
+
+_ACTIVATIONS = {None: sk.SK_ACT_NONE, "relu": sk.SK_ACT_RELU, "gelu": sk.SK_ACT_GELU, "gelu_tanh": sk.SK_ACT_GELU_TANH, "silu": sk.SK_ACT_SILU}
+
+
+def _dense_shape(x, weight, residual, activation):
+    return sk.DenseShape(x.shape[0], weight.shape[1], weight.shape[0], activation, _DTYPES[x.dtype], _row_stride(x),
+                         weight.shape[0] if residual is None else _row_stride(residual))
+
+
+def _dense_workspace(shape, backward, device, stream):
+    need = sk.sk_dense_workspace_bytes(shape, backward)
+    if need == _REFUSED:
+        raise sk.SkError(sk.SK_ERR_UNSUPPORTED)
+    return _workspace(device, stream, need)
+
+
+class LinearFunction(torch.autograd.Function):
+    """See ``linear``; keeps x, the weight, and with an activation what goes into it."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, residual, activation, training):
+        x2, w = _rows_of(x, x.shape[-1], 1 << 20), _dense(weight)
+        b = None if bias is None else _dense(bias)
+        r2 = None if residual is None else _rows_of(residual, residual.shape[-1], 1 << 20)
+        y = torch.empty((*x.shape[:-1], w.shape[0]), dtype=x.dtype, device=x.device)
+        z = torch.empty((x2.shape[0], w.shape[0]), dtype=x.dtype, device=x.device) if training and activation != sk.SK_ACT_NONE else None
+        if y.numel() > 0:
+            shape = _dense_shape(x2, w, r2, activation)
+            with _on(x.device), _queueing:
+                stream = _stream(x.device)
+                ws = _dense_workspace(shape, 0, x.device, stream)
+                sk.check(sk.sk_dense_fwd(shape, x2, w, b, r2, y, z, ws, ws.numel(), stream))
+        ctx.save_for_backward(x2, w, z)
+        ctx.shape, ctx.activation, ctx.bias = x.shape, activation, bias is not None
+        return y
+
+    @staticmethod
+    @_once
+    def backward(ctx, dy):
+        x, w, z = ctx.saved_tensors
+        wanted = ctx.needs_input_grad
+        dx = torch.empty(ctx.shape, dtype=x.dtype, device=x.device) if wanted[0] else None
+        dw = torch.empty(w.shape, dtype=x.dtype, device=x.device) if wanted[1] else None
+        db = torch.empty(w.shape[0], dtype=x.dtype, device=x.device) if wanted[2] else None
+        if x.numel() == 0:
+            for t in (dw, db):
+                if t is not None:
+                    t.zero_()
+        elif any(wanted[:3]):
+            d = _dense(dy)
+            shape = _dense_shape(x, w, None, ctx.activation)
+            with _on(x.device), _queueing:
+                stream = _stream(x.device)
+                ws = _dense_workspace(shape, 1, x.device, stream)
+                sk.check(sk.sk_dense_bwd(shape, x, w, z, d, dx, dw, db, ws, ws.numel(), stream))
+        return dx, dw, db, dy if wanted[3] else None, None, None
+
+
+def linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = None, residual: torch.Tensor | None = None, *,
+           activation: str | None = None) -> torch.Tensor:
+    """``activation(x @ weight.t() + bias) + residual``: a layer that stays dense, ``x [..., in]``, ``weight [out, in]`` and ``bias [out]`` as
+    ``torch.nn.Linear`` has them, ``residual [..., out]``.
+
+    ``activation``: None, "relu", "gelu" (z Phi(z)), "gelu_tanh" (its approximation by tanh) or "silu".  A backward pass has what goes into
+    it, in the tensors' type.  Rows of strided matrices x and residual are read in place.  in and out: multiples of 8.
+    """
+    if activation not in _ACTIVATIONS:
+        raise ValueError(f"linear: no activation {activation!r}; there are {', '.join(map(repr, _ACTIVATIONS))}")
+    act = _ACTIVATIONS[activation]
+    if _natively():
+        y = _native.dense_layer(x, weight, bias, residual, act)
+        if y is not None:
+            return y
+    _checked("linear", x, x=x, weight=weight, bias=bias, residual=residual)
+    if x.dim() == 0 or weight.dim() != 2 or weight.numel() == 0 or x.shape[-1] != weight.shape[1]:
+        raise ValueError("linear: shapes do not match (x [..., in], weight [out, in])")
+    _vector("linear", "bias", bias, weight.shape[0])
+    if residual is not None and residual.shape != (*x.shape[:-1], weight.shape[0]):
+        raise ValueError(f"linear: residual has shape {tuple(residual.shape)}, not {(*x.shape[:-1], weight.shape[0])}")
+    return LinearFunction.apply(x, weight, bias, residual, act, _training(x, weight, bias, residual))
+
+
+# ---------------------------------------------------------------------------
+# distillation
+# ---------------------------------------------------------------------------
+
+def _distill_shape(z, ids, labels, temperature, label_weight):
+    return sk.DistillShape(z.shape[0], z.shape[1], _row_stride(z), ids.shape[-1], ids.element_size(), 8 if labels is None else labels.element_size(),
+                           temperature, label_weight, _DTYPES[z.dtype])
+
+
+class DistillationFunction(torch.autograd.Function):
+    """See ``distillation_loss``; keeps its inputs and each row's largest logit and sums."""
+
+    @staticmethod
+    def forward(ctx, logits, teacher_logits, teacher_ids, labels, temperature, label_weight, training):
+        z = logits.reshape(-1, logits.shape[-1])
+        if z.stride(1) != 1 or z.stride(0) > 1 << 40:
+            z = z.contiguous()
+        loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
+        stats = torch.empty((z.shape[0], 4), dtype=torch.float32, device=logits.device) if training else None
+        if z.shape[0] > 0:
+            shape = _distill_shape(z, teacher_ids, labels, temperature, label_weight)
+            with _on(logits.device):
+                sk.check(sk.sk_distill_fwd(shape, z, teacher_logits, teacher_ids, labels, loss, stats, _stream(logits.device)))
+        ctx.save_for_backward(z, teacher_logits, teacher_ids, labels, stats)
+        ctx.shape, ctx.args = logits.shape, (temperature, label_weight)
+        return loss
+
+    @staticmethod
+    @_once
+    def backward(ctx, dloss):
+        z, t, ids, labels, stats = ctx.saved_tensors
+        dz = torch.empty(ctx.shape, dtype=z.dtype, device=z.device)
+        if z.shape[0] > 0:
+            with _on(z.device):
+                sk.check(sk.sk_distill_bwd(_distill_shape(z, ids, labels, *ctx.args), z, t, ids, labels, stats, _dense(dloss), dz, _stream(z.device)))
+        return dz, None, None, None, None, None, None
+
+
+def distillation_loss(logits: torch.Tensor, teacher_logits: torch.Tensor, teacher_ids: torch.Tensor, labels: torch.Tensor | None = None, *,
+                      temperature: float = 1.0, label_weight: float = 0.0) -> torch.Tensor:
+    """The loss of every row of ``logits [..., vocabulary]`` (fp32 ``[...]``; sum or average it as the program does) against a teacher's largest
+    logits ``teacher_logits [..., top]`` at the places ``teacher_ids [..., top]``, and against ``labels [...]``:
+
+        (1 - label_weight) temperature^2 KL(p || q) + label_weight (log sum exp z - z_label)
+
+    with p the softmax of the teacher's entries over the temperature and q that of all of a row's logits.  An entry whose id is outside the vocabulary or
+    whose logit is -infinity is not there (a list that ends early), an id that is named twice has both entries; a row without an entry has no first
+    term, one whose label is outside the vocabulary no second.  The logits alone get a gradient.  Ids and labels are int32 or int64.  Any size of
+    vocabulary; rows of a strided matrix are read in place.
+    """
+    if _natively():
+        loss = _native.distillation_loss(logits, teacher_logits, teacher_ids, labels, temperature, label_weight)
+        if loss is not None:
+            return loss
+    what = "distillation_loss"
+    _checked(what, logits, logits=logits, teacher_logits=teacher_logits)
+    if logits.dim() == 0 or logits.shape[-1] == 0 or teacher_logits.dim() != logits.dim() or teacher_logits.shape[:-1] != logits.shape[:-1]:
+        raise ValueError(f"{what}: shapes do not match (logits [..., vocabulary], teacher_logits [..., top])")
+    if torch.is_grad_enabled() and teacher_logits.requires_grad:
+        raise RuntimeError(f"{what}: teacher_logits get no gradient; pass them detached")
+    _integers(what, "teacher_ids", teacher_ids, logits.device)
+    if teacher_ids.shape != teacher_logits.shape:
+        raise ValueError(f"{what}: teacher_ids have shape {tuple(teacher_ids.shape)}, not {tuple(teacher_logits.shape)}")
+    if labels is not None:
+        _integers(what, "labels", labels, logits.device)
+        if labels.shape != logits.shape[:-1]:
+            raise ValueError(f"{what}: labels have shape {tuple(labels.shape)}, not {tuple(logits.shape[:-1])}")
+        labels = _dense(labels)
+    if not 0.0 < temperature < float("inf"):
+        raise ValueError(f"{what}: a temperature of {temperature}")
+    if not 0.0 <= label_weight <= 1.0:
+        raise ValueError(f"{what}: a label_weight of {label_weight} is not between 0 and 1")
+    return DistillationFunction.apply(logits, _dense(teacher_logits), _dense(teacher_ids), labels, float(temperature), float(label_weight), _training(logits))

@@ -19,7 +19,8 @@ OUT_TORCH = os.path.join(HERE, "lib", "_sktorch.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 SOURCES = ["sk_api.hip", "sk_bf16_gemm.hip", "sk_bf16_gemm256.hip", "sk_bf16_few_rows.hip",
            "sk_f32_gemm.hip", "sk_chain.hip", "sk_bwd_narrow.hip",
-           "sk_block_api.hip", "sk_attention_f32.hip", "sk_attention_bf16.hip", "sk_norm_rope.hip", "sk_embedding.hip", "sk_dropout.hip"]
+           "sk_block_api.hip", "sk_attention_f32.hip", "sk_attention_bf16.hip", "sk_norm_rope.hip", "sk_embedding.hip", "sk_dropout.hip",
+           "sk_layer_norm.hip", "sk_dense.hip", "sk_distill.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # packed fp32 VALU forms are kept off on the test machines
@@ -55,7 +56,7 @@ def build_torch(verbose: bool = True) -> str:
            "-DUSE_ROCM=1", "-D__HIP_PLATFORM_AMD__=1", f'-DSK_TORCH_VERSION="{torch.__version__}"', f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
            "-isystem", include, "-isystem", os.path.join(include, "torch", "csrc", "api", "include"),
            "-isystem", "/opt/rocm/include", "-isystem", sysconfig.get_paths()["include"],
-           os.path.join(CSRC, "sk_torch.cpp"), os.path.join(CSRC, "sk_torch_block.cpp"), OUT, "-L" + os.path.join(root, "lib"),
+           os.path.join(CSRC, "sk_torch.cpp"), os.path.join(CSRC, "sk_torch_block.cpp"), os.path.join(CSRC, "sk_torch_layers.cpp"), OUT, "-L" + os.path.join(root, "lib"),
            "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch", "-ltorch_python", "-Wl,-rpath,$ORIGIN", "-o", OUT_TORCH]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

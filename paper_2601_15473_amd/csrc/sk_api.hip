@@ -842,6 +842,68 @@ hipError_t first_gemm(const Shape& s, GemmKind kind, GemmKind kind_slabs, GemmAr
   return launch_reduce_to_bf16(static_cast<const float*>(slabs), out, (int64_t)a.M * a.N, f.splits, st);
 }
 
+}  // namespace
+
+namespace sk {
+
+size_t product_bytes(GemmKind kind, int64_t M, int64_t N, int64_t K, bool f32) {
+  const size_t slab = (size_t)M * N * 4;
+  if (kind == GEMM_TN_F32_PLAIN) {
+    const TokenPlan t = plan_tokens(M, N, K, f32 ? SK_F32 : SK_BF16, false, 0);
+    return f32 && t.splits == 1 ? 0 : align_up(slab * t.splits);
+  }
+  if (f32) return plan_f32_first(M, N, K).slab_bytes;
+  return plan_first(kind, M, N, K).slab_bytes;
+}
+
+hipError_t launch_product(GemmKind kind, GemmArgs a, bool f32, void* slabs, hipStream_t st) {
+  Shape s{};
+  s.dtype = f32 ? SK_F32 : SK_BF16;
+  a.scale = 1.f;
+  a.splits = 1;
+  a.k_per_split = (a.K + 63) / 64 * 64;
+  if (kind != GEMM_TN_F32_PLAIN) {
+    const GemmKind in_slabs = kind == GEMM_NT ? GEMM_NT_F32 : GEMM_NN_F32;
+    if (a.bias != nullptr || product_bytes(kind, a.M, a.N, a.K, f32) == 0) return gemm(s, kind, a, st);
+    return first_gemm(s, kind, in_slabs, a, slabs, st);
+  }
+  const TokenPlan t = plan_tokens(a.M, a.N, a.K, s.dtype, false, 0);
+  void* const out = a.C;
+  a.splits = t.splits;
+  a.k_per_split = t.k_per_split;
+  if (!f32 || t.splits > 1) a.C = slabs;
+  const hipError_t e = f32 ? launch_gemm_f32(GEMM_TN_F32, t.tile, a, st) : launch_gemm_bf16(GEMM_TN_F32_PLAIN, t.tile, a, st);
+  if (e != hipSuccess) return e;
+  const int64_t n = (int64_t)a.M * a.N;
+  if (!f32) return launch_reduce_to_bf16(static_cast<const float*>(slabs), out, n, t.splits, st);
+  if (t.splits == 1) return hipSuccess;
+  ReduceArgs r{};
+  r.part = static_cast<const float*>(slabs); r.out = static_cast<float*>(out); r.n = n; r.splits = t.splits; r.scale = 1.f;
+  r.splits2 = 1; r.scale2 = 1.f;
+  return launch_reduce_splits(r, st);
+}
+
+int product_slabs(int64_t M, int64_t N, int64_t K, bool f32) { return f32 ? plan_f32_first(M, N, K).splits : plan_first(GEMM_NT, M, N, K).splits; }
+
+hipError_t launch_product_slabs(GemmArgs a, bool f32, void* slabs, hipStream_t st) {
+  a.C = slabs;
+  a.bias = nullptr;
+  a.scale = 1.f;
+  if (f32) {
+    const F32Plan f = plan_f32_first(a.M, a.N, a.K);
+    a.splits = f.splits; a.k_per_split = f.k_per_split;
+    return launch_gemm_f32(GEMM_NT, f.tile, a, st);
+  }
+  const FirstPlan f = plan_first(GEMM_NT, a.M, a.N, a.K);
+  a.splits = f.splits; a.k_per_split = f.k_per_split;
+  if (f.few && f.splits > 1) return launch_gemm_few_rows_bf16(GEMM_NT, a, st);
+  return launch_gemm_bf16(GEMM_NT_F32, f.few ? TILE_64x64 : f.tile == TILE_256x256 ? TILE_128x128 : f.tile, a, st);
+}
+
+}  // namespace sk
+
+namespace {
+
 // C[M,N] = scale * (A[M,K] . B) + bias through the workspace-free single GEMM.
 GemmArgs dense_args(const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc,
                     int64_t M, int64_t N, int64_t K, float scale, const void* bias) {

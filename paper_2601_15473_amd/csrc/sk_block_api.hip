@@ -139,6 +139,78 @@ struct EmbeddingRoom {
   }
 };
 
+// Of rows `width` long: dense ones, or further apart; false as stride_ok.
+bool row_stride_ok(int64_t rows, int64_t width, int64_t stride, sk_dtype t, int64_t most, int64_t& out, sk_status& st) {
+  if (!stride_ok(rows, stride, t, most, out, st)) return false;
+  if (rows <= 1) out = width;
+  return true;
+}
+
+sk_status layer_norm_args(const sk_layer_norm_shape* s, LayerNormArgs& a) {
+  if (s == nullptr) return SK_ERR_INVALID_ARG;
+  if (s->rows < 1 || s->width < 1 || !(s->eps >= 0.f) || !std::isfinite(s->eps)) return SK_ERR_INVALID_ARG;
+  if (!known(s->dtype) || s->width % 8 != 0 || s->width > LAYER_NORM_MAX_WIDTH || s->rows >= (1 << 24)) return SK_ERR_UNSUPPORTED;
+  sk_status st = SK_OK;
+  if (!row_stride_ok(s->rows, s->width, s->x_stride, s->dtype, MOST_STRIDE, a.x_stride, st) ||
+      !row_stride_ok(s->rows, s->width, s->residual_stride, s->dtype, MOST_STRIDE, a.residual_stride, st))
+    return st;
+  a.rows = s->rows; a.width = (int)s->width; a.eps = s->eps;
+  return SK_OK;
+}
+size_t layer_norm_bytes(const LayerNormArgs& a) { return align_up((size_t)(a.rows < LAYER_NORM_MAX_GROUPS ? a.rows : LAYER_NORM_MAX_GROUPS) * 2 * a.width * 4); }
+
+sk_status dense_layer_args(const sk_dense_shape* s, DenseArgs& a) {
+  if (s == nullptr) return SK_ERR_INVALID_ARG;
+  if (s->tokens < 1 || s->in < 1 || s->out < 1 || s->activation < 0) return SK_ERR_INVALID_ARG;
+  if (!known(s->dtype) || s->activation > SK_ACT_SILU || s->in % 8 != 0 || s->out % 8 != 0 || s->tokens > (1 << 24) || s->in > (1 << 20) || s->out > (1 << 20)) return SK_ERR_UNSUPPORTED;
+  const int64_t most = (int64_t)1 << 34;   // values of any of the matrices: work-groups of 256 threads in a launch
+  if (s->tokens * s->in >= most || s->tokens * s->out >= most || s->in * s->out >= most) return SK_ERR_UNSUPPORTED;
+  sk_status st = SK_OK;
+  if (!row_stride_ok(s->tokens, s->in, s->x_stride, s->dtype, 1 << 20, a.x_stride, st) ||
+      !row_stride_ok(s->tokens, s->out, s->residual_stride, s->dtype, 1 << 20, a.residual_stride, st))
+    return st;
+  // (the windows that rows are read through take them for apart)
+  if (a.x_stride < s->in || a.residual_stride < s->out) return SK_ERR_UNSUPPORTED;
+  a.tokens = (int)s->tokens; a.in = (int)s->in; a.out = (int)s->out; a.activation = s->activation;
+  return SK_OK;
+}
+struct DenseRoom {   // backward: dz | column sums | the products' slabs, one product after the other
+  size_t dz, partial, slabs, total;
+  DenseRoom(const DenseArgs& a, bool f32) {
+    partial = a.activation != SK_ACT_NONE ? align_up((size_t)a.tokens * a.out * (f32 ? 4 : 2)) : 0;
+    dz = 0;
+    slabs = partial + align_up((size_t)DenseRuns(a.tokens, a.out).runs * a.out * 4);
+    const size_t dx = product_bytes(GEMM_NN, a.tokens, a.in, a.out, f32), dw = product_bytes(GEMM_TN_F32_PLAIN, a.out, a.in, a.tokens, f32);
+    total = slabs + (dx > dw ? dx : dw);
+  }
+};
+size_t dense_forward_bytes(const DenseArgs& a, bool f32) { return align_up((size_t)product_slabs(a.tokens, a.out, a.in, f32) * a.tokens * a.out * 4); }
+GemmArgs product(const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t M, int64_t N, int64_t K, const void* bias) {
+  GemmArgs g{};
+  g.A = A; g.B = B; g.C = C; g.bias = bias;
+  g.lda = lda; g.ldb = ldb; g.ldc = N;
+  g.M = (int)M; g.N = (int)N; g.K = (int)K;
+  return g;
+}
+
+sk_status distill_args(const sk_distill_shape* s, const void* logits, DistillArgs& a) {
+  if (s == nullptr) return SK_ERR_INVALID_ARG;
+  if (s->rows < 1 || s->vocabulary < 1 || s->top < 0 || s->logits_stride < 0 || !(s->temperature > 0.f) || !std::isfinite(s->temperature) ||
+      !(s->label_weight >= 0.f && s->label_weight <= 1.f))
+    return SK_ERR_INVALID_ARG;
+  if (!known(s->dtype) || (s->id_bytes != 4 && s->id_bytes != 8) || (s->label_bytes != 4 && s->label_bytes != 8) || s->rows >= (1 << 24) || s->vocabulary > (1 << 24) ||
+      s->top > (1 << 16) || s->logits_stride > MOST_STRIDE || !(s->temperature >= 1e-3f && s->temperature <= 1e3f))
+    return SK_ERR_UNSUPPORTED;
+  // (rows begin anywhere; values where values do)
+  if (reinterpret_cast<uintptr_t>(logits) % esize(s->dtype) != 0) return SK_ERR_INVALID_ARG;
+  a.logits = logits;
+  a.rows = s->rows; a.logits_stride = s->logits_stride;
+  a.vocabulary = (int)s->vocabulary; a.top = s->top;
+  a.ids64 = s->id_bytes == 8; a.labels64 = s->label_bytes == 8;
+  a.temperature = s->temperature; a.label_weight = s->label_weight;
+  return SK_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -266,6 +338,101 @@ sk_status sk_dropout(const void* x, const void* residual, void* y, int64_t n, fl
   a.key[0] = (unsigned)seed; a.key[1] = (unsigned)(seed >> 32);
   a.offset[0] = (unsigned)offset; a.offset[1] = (unsigned)(offset >> 32);
   return launched(launch_dropout(a, dtype == SK_F32, static_cast<hipStream_t>(stream)), "sk_dropout");
+}
+
+sk_status sk_layer_norm_fwd(const sk_layer_norm_shape* shape, const void* x, const void* residual, const void* weight, const void* bias,
+                            void* y, void* sum, float* stats, void* stream) {
+  if (!x || !y || !aligned16(x, residual, weight, bias, y, sum, stats)) return SK_ERR_INVALID_ARG;
+  LayerNormArgs a{};
+  const sk_status st = layer_norm_args(shape, a);
+  if (st != SK_OK) return st;
+  a.x = x; a.residual = residual; a.weight = weight; a.bias = bias; a.y = y; a.s = sum; a.stats = stats;
+  return launched(launch_layer_norm_fwd(a, shape->dtype == SK_F32, static_cast<hipStream_t>(stream)), "sk_layer_norm_fwd");
+}
+
+size_t sk_layer_norm_workspace_bytes(const sk_layer_norm_shape* shape) {
+  LayerNormArgs a{};
+  if (layer_norm_args(shape, a) != SK_OK) return (size_t)-1;
+  return layer_norm_bytes(a);
+}
+
+sk_status sk_layer_norm_bwd(const sk_layer_norm_shape* shape, const void* x, const void* weight, const float* stats, const void* dy, const void* d_sum,
+                            void* dx, void* dweight, void* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!x || !stats || !dy || !dx || !aligned16(x, weight, stats, dy, d_sum, dx, dweight, dbias, workspace)) return SK_ERR_INVALID_ARG;
+  LayerNormArgs a{};
+  const sk_status st = layer_norm_args(shape, a);
+  if (st != SK_OK) return st;
+  if ((dweight || dbias) && (!workspace || workspace_bytes < layer_norm_bytes(a))) return SK_ERR_WORKSPACE;
+  a.x = x; a.weight = weight; a.stats = const_cast<float*>(stats); a.dy = dy; a.ds = d_sum; a.dx = dx; a.dweight = dweight; a.dbias = dbias;
+  a.partial = dweight || dbias ? static_cast<float*>(workspace) : nullptr;
+  return launched(launch_layer_norm_bwd(a, shape->dtype == SK_F32, static_cast<hipStream_t>(stream)), "sk_layer_norm_bwd");
+}
+
+size_t sk_dense_workspace_bytes(const sk_dense_shape* shape, int32_t backward) {
+  DenseArgs a{};
+  if (dense_layer_args(shape, a) != SK_OK) return (size_t)-1;
+  return backward ? DenseRoom(a, shape->dtype == SK_F32).total : dense_forward_bytes(a, shape->dtype == SK_F32);
+}
+
+sk_status sk_dense_fwd(const sk_dense_shape* shape, const void* x, const void* weight, const void* bias, const void* residual, void* y, void* z,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+  if (!x || !weight || !y || !aligned16(x, weight, bias, residual, y, z, workspace)) return SK_ERR_INVALID_ARG;
+  DenseArgs a{};
+  const sk_status st = dense_layer_args(shape, a);
+  if (st != SK_OK) return st;
+  const bool f32 = shape->dtype == SK_F32;
+  if (!workspace || workspace_bytes < dense_forward_bytes(a, f32)) return SK_ERR_WORKSPACE;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  a.x = x; a.weight = weight; a.bias = bias; a.residual = residual; a.y = y; a.z = z;
+  a.slabs = static_cast<const float*>(workspace);
+  a.splits = product_slabs(a.tokens, a.out, a.in, f32);
+  hipError_t e = launch_product_slabs(product(x, a.x_stride, weight, a.in, nullptr, a.tokens, a.out, a.in, nullptr), f32, workspace, s);
+  if (e == hipSuccess) e = launch_dense_finish(a, f32, s);
+  return launched(e, "sk_dense_fwd");
+}
+
+sk_status sk_dense_bwd(const sk_dense_shape* shape, const void* x, const void* weight, const void* z, const void* dy, void* dx, void* dweight,
+                       void* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!x || !weight || !dy || !aligned16(x, weight, z, dy, dx, dweight, dbias, workspace)) return SK_ERR_INVALID_ARG;
+  DenseArgs a{};
+  const sk_status st = dense_layer_args(shape, a);
+  if (st != SK_OK) return st;
+  const bool f32 = shape->dtype == SK_F32, act = a.activation != SK_ACT_NONE;
+  if (act && !z) return SK_ERR_INVALID_ARG;
+  const DenseRoom room(a, f32);
+  if (room.total > 0 && (!workspace || workspace_bytes < room.total)) return SK_ERR_WORKSPACE;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  char* const w = static_cast<char*>(workspace);
+  a.x = x; a.weight = weight; a.z = const_cast<void*>(z); a.dy = dy; a.dx = dx; a.dweight = dweight; a.dbias = dbias;
+  a.dz = act ? w + room.dz : const_cast<void*>(dy);
+  a.partial = dbias ? reinterpret_cast<float*>(w + room.partial) : nullptr;
+  hipError_t e = launch_dense_dz(a, f32, s);
+  if (e == hipSuccess) e = launch_dense_dbias(a, f32, s);
+  if (e == hipSuccess && dx) e = launch_product(GEMM_NN, product(a.dz, a.out, weight, a.in, dx, a.tokens, a.in, a.out, nullptr), f32, w + room.slabs, s);
+  if (e == hipSuccess && dweight) e = launch_product(GEMM_TN_F32_PLAIN, product(a.dz, a.out, x, a.x_stride, dweight, a.out, a.in, a.tokens, nullptr), f32, w + room.slabs, s);
+  return launched(e, "sk_dense_bwd");
+}
+
+sk_status sk_distill_fwd(const sk_distill_shape* shape, const void* logits, const void* teacher_logits, const void* teacher_ids, const void* labels,
+                         float* loss, float* stats, void* stream) {
+  if (!logits || !loss || !aligned16(teacher_logits, teacher_ids, labels, loss, stats)) return SK_ERR_INVALID_ARG;
+  DistillArgs a{};
+  const sk_status st = distill_args(shape, logits, a);
+  if (st != SK_OK) return st;
+  if (a.top > 0 && (!teacher_logits || !teacher_ids)) return SK_ERR_INVALID_ARG;
+  a.teacher = teacher_logits; a.ids = teacher_ids; a.labels = labels; a.loss = loss; a.stats = stats;
+  return launched(launch_distill_fwd(a, shape->dtype == SK_F32, static_cast<hipStream_t>(stream)), "sk_distill_fwd");
+}
+
+sk_status sk_distill_bwd(const sk_distill_shape* shape, const void* logits, const void* teacher_logits, const void* teacher_ids, const void* labels,
+                         const float* stats, const float* dloss, void* dlogits, void* stream) {
+  if (!logits || !stats || !dloss || !dlogits || !aligned16(teacher_logits, teacher_ids, labels, stats, dloss, dlogits)) return SK_ERR_INVALID_ARG;
+  DistillArgs a{};
+  const sk_status st = distill_args(shape, logits, a);
+  if (st != SK_OK) return st;
+  if (a.top > 0 && (!teacher_logits || !teacher_ids)) return SK_ERR_INVALID_ARG;
+  a.teacher = teacher_logits; a.ids = teacher_ids; a.labels = labels; a.stats = const_cast<float*>(stats); a.dloss = dloss; a.dlogits = dlogits;
+  return launched(launch_distill_bwd(a, shape->dtype == SK_F32, static_cast<hipStream_t>(stream)), "sk_distill_bwd");
 }
 
 }  // extern "C"

@@ -96,4 +96,60 @@ struct DropoutArgs {
 };
 hipError_t launch_dropout(const DropoutArgs& a, bool f32, hipStream_t s);
 
+struct LayerNormArgs {
+  const void *x, *residual, *weight, *bias;   // forward: x and the residual (or null); backward: x is what was normed
+  void *y, *s;                                // forward: the result, and the sum (or null)
+  float* stats;                               // [rows][mean, 1 / deviation]: forward written unless null, backward read
+  const void *dy, *ds;                        // backward; ds or null
+  void *dx, *dweight, *dbias;                 // backward; weights' or null
+  float* partial;                             // backward: [groups][dweight, dbias][width], null where neither is wanted
+  int64_t rows, x_stride, residual_stride;
+  int width;
+  float eps;
+};
+constexpr int LAYER_NORM_MAX_GROUPS = 512;
+constexpr int LAYER_NORM_MAX_WIDTH = 1 << 15;   // a row on one work-group's registers
+hipError_t launch_layer_norm_fwd(const LayerNormArgs& a, bool f32, hipStream_t s);
+hipError_t launch_layer_norm_bwd(const LayerNormArgs& a, bool f32, hipStream_t s);
+
+struct DistillArgs {
+  const void *logits, *teacher;               // rows logits_stride elements apart, [rows][top] dense
+  const void *ids, *labels;                   // labels or null
+  float* loss;                                // forward
+  float* stats;                               // [rows][4]: the largest logit, 1 / sum exp((z - it) / temperature), 1 / sum exp(z - it), 0; forward written unless null, backward read
+  const float* dloss;                         // backward
+  void* dlogits;                              // backward: dense
+  int64_t rows, logits_stride;
+  int vocabulary, top, ids64, labels64;
+  float temperature, label_weight;
+};
+hipError_t launch_distill_fwd(const DistillArgs& a, bool f32, hipStream_t s);
+hipError_t launch_distill_bwd(const DistillArgs& a, bool f32, hipStream_t s);
+
+struct DenseArgs {
+  const void *x, *weight, *bias, *residual;   // bias and residual or null
+  void *y, *z;                                // z: what goes into the activation, dense; forward written unless null, backward read
+  const void* dy;                             // backward
+  void *dz, *dx, *dweight, *dbias;            // backward; dz: room for it where there is an activation; the others or null
+  const float* slabs;                         // forward: the product in fp32 slabs [splits][tokens, out]
+  int splits;
+  float* partial;                             // backward: [runs][out] sums of dz, null where dbias is not wanted
+  int64_t x_stride, residual_stride;
+  int tokens, in, out, activation;
+};
+// Runs of rows that dz's column sums are formed in: of groups of 512 columns about four work-groups to a CU, 16 rows at least.
+struct DenseRuns {
+  int groups, runs, rows;
+  DenseRuns(int64_t tokens, int64_t out) {
+    groups = (int)((out + 511) / 512);
+    const int64_t wanted = (4 * NUM_CUS + groups - 1) / groups, most = (tokens + 15) / 16;
+    const int64_t n = wanted < most ? wanted : most;
+    rows = (int)(((tokens + n - 1) / n + 15) / 16 * 16);
+    runs = (int)((tokens + rows - 1) / rows);
+  }
+};
+hipError_t launch_dense_finish(const DenseArgs& a, bool f32, hipStream_t s);
+hipError_t launch_dense_dz(const DenseArgs& a, bool f32, hipStream_t s);
+hipError_t launch_dense_dbias(const DenseArgs& a, bool f32, hipStream_t s);
+
 }  // namespace sk

@@ -1,0 +1,284 @@
+// Layer norm of rows, with a residual added first, and its gradients.
+//
+//   s = x + residual,  mu = mean s,  r = 1 / sqrt(mean (s - mu)^2 + eps),  u = (s - mu) r,  y = u w + b
+//   g = dy w,  dx = ds + r (g - mean g - u mean(g u)),  dw = sum dy u,  db = sum dy
+//
+// Bound by memory: a row is read once into registers, eight values to a lane and piece, and both of its sums are taken there (the mean first, the
+// squares about it second: a stream whose mean is large beside its spread loses nothing).  y is formed of the sum before s is rounded.
+#include "sk_block_launch.h"
+#include "sk_rows.h"
+
+namespace sk {
+namespace {
+
+constexpr int PIECE = 8;   // values
+
+// Sums of a row's lanes: L of a wave, or all of a work-group's (`shared`: a float a wave and sum).  Every lane gets them.
+template <int L, int N>
+__device__ __forceinline__ void sum_row(float (&v)[N], float* shared) {
+#pragma unroll
+  for (int m = 1; m < (L < 64 ? L : 64); m <<= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], m);
+  if constexpr (L > 64) {
+    constexpr int WAVES = L / 64;
+    __syncthreads();   // (what the sum before left has been read)
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i) shared[i * WAVES + (threadIdx.x >> 6)] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) s += shared[i * WAVES + w];
+      v[i] = s;
+    }
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void load_piece(float (&v)[PIECE], const T* row, int piece, int width) {
+#pragma unroll
+  for (int i = 0; i < PIECE; ++i) v[i] = 0.f;
+  if (piece * PIECE < width) load_values<T, PIECE>(v, row + piece * PIECE);
+}
+
+// L lanes to a row, N pieces to a lane: piece n of a lane is the row's n L + lane.
+template <typename T, int L, int N>
+__global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_fwd_kernel(const LayerNormArgs p) {
+  constexpr int THREADS = L > 256 ? L : 256, ROWS = THREADS / L;
+  __shared__ float shared[L > 64 ? L / 64 : 1];
+  const int lane = threadIdx.x % L;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / L;
+  if (row >= p.rows) return;   // (L > 64: a work-group's threads all, or none)
+  const T* const x = static_cast<const T*>(p.x) + row * p.x_stride;
+  const T* const residual = p.residual ? static_cast<const T*>(p.residual) + row * p.residual_stride : nullptr;
+  float v[N][PIECE];
+#pragma unroll
+  for (int n = 0; n < N; ++n) load_piece<T>(v[n], x, n * L + lane, p.width);
+  if (residual) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      float add[PIECE];
+      load_piece<T>(add, residual, n * L + lane, p.width);
+#pragma unroll
+      for (int i = 0; i < PIECE; ++i) v[n][i] += add[i];
+    }
+  }
+  float sum[1] = {0.f};
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int i = 0; i < PIECE; ++i) sum[0] += v[n][i];
+  sum_row<L, 1>(sum, shared);
+  const float mean = sum[0] / p.width;
+  sum[0] = 0.f;
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+    if ((n * L + lane) * PIECE < p.width)
+#pragma unroll
+      for (int i = 0; i < PIECE; ++i) sum[0] += (v[n][i] - mean) * (v[n][i] - mean);
+  sum_row<L, 1>(sum, shared);
+  const float r = 1.f / sqrtf(sum[0] / p.width + p.eps);
+  if (p.stats && lane == 0) *reinterpret_cast<float2*>(p.stats + row * 2) = make_float2(mean, r);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int at = (n * L + lane) * PIECE;
+    if (at >= p.width) continue;
+    if (p.s) store_values<T, PIECE>(static_cast<T*>(p.s) + row * p.width + at, v[n]);
+    float w[PIECE], b[PIECE], y[PIECE];
+#pragma unroll
+    for (int i = 0; i < PIECE; ++i) { w[i] = 1.f; b[i] = 0.f; }
+    if (p.weight) load_values<T, PIECE>(w, static_cast<const T*>(p.weight) + at);
+    if (p.bias) load_values<T, PIECE>(b, static_cast<const T*>(p.bias) + at);
+#pragma unroll
+    for (int i = 0; i < PIECE; ++i) y[i] = (v[n][i] - mean) * r * w[i] + b[i];
+    store_values<T, PIECE>(static_cast<T*>(p.y) + row * p.width + at, y);
+  }
+}
+
+// Gradients: work-groups walk over the rows with their lanes' terms of dw and db in registers, and leave one row of each, [group][dw, db][width].
+template <typename T, int L, int N>
+__global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_bwd_kernel(const LayerNormArgs p) {
+  constexpr int THREADS = L > 256 ? L : 256, ROWS = THREADS / L;
+  __shared__ float shared[L > 64 ? 2 * (L / 64) : 1];
+  __shared__ float rows[ROWS > 1 ? THREADS * N * PIECE : 1];
+  const int lane = threadIdx.x % L, sub = threadIdx.x / L;
+  float dw[N][PIECE], db[N][PIECE];
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int i = 0; i < PIECE; ++i) dw[n][i] = db[n][i] = 0.f;
+  // (ROWS > 1: the lanes of a row that is not there go along with zeros)
+  for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < p.rows; row0 += (int64_t)gridDim.x * ROWS) {
+    const int64_t row = row0 + sub;
+    const bool there = row < p.rows;
+    const int64_t at_row = there ? row : p.rows - 1;
+    const float2 stat = *reinterpret_cast<const float2*>(p.stats + at_row * 2);
+    const T* const s = static_cast<const T*>(p.x) + at_row * p.x_stride;
+    const T* const dy = static_cast<const T*>(p.dy) + at_row * p.width;
+    float u[N][PIECE], g[N][PIECE];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      load_piece<T>(u[n], s, n * L + lane, p.width);
+      load_piece<T>(g[n], dy, n * L + lane, p.width);
+    }
+    float sums[2] = {0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int at = (n * L + lane) * PIECE;
+      const bool in = there && at < p.width;
+      float w[PIECE];
+#pragma unroll
+      for (int i = 0; i < PIECE; ++i) w[i] = 1.f;
+      if (p.weight && at < p.width) load_values<T, PIECE>(w, static_cast<const T*>(p.weight) + at);
+#pragma unroll
+      for (int i = 0; i < PIECE; ++i) {
+        u[n][i] = in ? (u[n][i] - stat.x) * stat.y : 0.f;
+        const float d = in ? g[n][i] : 0.f;
+        dw[n][i] += d * u[n][i];
+        db[n][i] += d;
+        g[n][i] = d * w[i];
+        sums[0] += g[n][i];
+        sums[1] += g[n][i] * u[n][i];
+      }
+    }
+    sum_row<L, 2>(sums, shared);
+    const float mg = sums[0] / p.width, mgu = sums[1] / p.width;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int at = (n * L + lane) * PIECE;
+      if (!there || at >= p.width) continue;
+      float dx[PIECE];
+#pragma unroll
+      for (int i = 0; i < PIECE; ++i) dx[i] = stat.y * (g[n][i] - mg - u[n][i] * mgu);
+      if (p.ds) {
+        float add[PIECE];
+        load_values<T, PIECE>(add, static_cast<const T*>(p.ds) + row * p.width + at);
+#pragma unroll
+        for (int i = 0; i < PIECE; ++i) dx[i] += add[i];
+      }
+      store_values<T, PIECE>(static_cast<T*>(p.dx) + row * p.width + at, dx);
+    }
+  }
+  if (!p.partial) return;
+  float* const out = p.partial + (int64_t)blockIdx.x * 2 * p.width;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    float (&d)[N][PIECE] = which ? db : dw;
+    if constexpr (ROWS > 1) {   // the rows side by side, added in their order
+      __syncthreads();
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < PIECE; ++i) rows[sub * (L * N * PIECE) + (n * L + lane) * PIECE + i] = d[n][i];
+      __syncthreads();
+      for (int c = threadIdx.x; c < p.width; c += THREADS) {
+        float t = 0.f;
+#pragma unroll
+        for (int q = 0; q < ROWS; ++q) t += rows[q * (L * N * PIECE) + c];
+        out[which * p.width + c] = t;
+      }
+    } else {
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const int at = (n * L + lane) * PIECE;
+        if (at < p.width) store_values<float, PIECE>(out + which * p.width + at, d[n]);
+      }
+    }
+  }
+}
+
+// The work-groups' rows summed: 32 columns a work-group, rows dealt over 32 threads a column and joined in order.
+template <typename T>
+__global__ __launch_bounds__(1024) void layer_norm_sum_kernel(const LayerNormArgs p, int groups) {
+  __shared__ float sums[32][33];
+  const int c = threadIdx.x & 31, part = threadIdx.x >> 5, column = blockIdx.x * 32 + c, columns = 2 * p.width;
+  float s = 0.f;
+  if (column < columns)
+#pragma unroll 8
+    for (int g = part; g < groups; g += 32) s += p.partial[(int64_t)g * columns + column];
+  sums[part][c] = s;
+  __syncthreads();
+  if (part == 0 && column < columns) {
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) s += sums[i][c];
+    if (column < p.width) {
+      if (p.dweight) store_one(static_cast<T*>(p.dweight) + column, s);
+    } else if (p.dbias) {
+      store_one(static_cast<T*>(p.dbias) + column - p.width, s);
+    }
+  }
+}
+
+double values_of(const LayerNormArgs& a) { return (double)a.rows * a.width; }
+
+template <typename T, int L, int N>
+hipError_t fwd(const LayerNormArgs& a, hipStream_t s) {
+  constexpr int THREADS = L > 256 ? L : 256, ROWS = THREADS / L;
+  note_matrix(a.x, a.rows, a.width, a.x_stride, sizeof(T), false);
+  if (a.residual) note_matrix(a.residual, a.rows, a.width, a.residual_stride, sizeof(T), false);
+  note_matrix(a.weight, 1, a.width, a.width, sizeof(T), false);
+  note_matrix(a.bias, 1, a.width, a.width, sizeof(T), false);
+  note_matrix(a.y, a.rows, a.width, a.width, sizeof(T), true);
+  note_matrix(a.s, a.rows, a.width, a.width, sizeof(T), true);
+  note_matrix(a.stats, a.rows, 2, 2, 4, true);
+  const int tensors = 2 + (a.residual != nullptr) + (a.s != nullptr);
+  return launch_kernel("layer_norm_fwd_kernel", Work{8 * values_of(a), tensors * values_of(a) * sizeof(T)}, layer_norm_fwd_kernel<T, L, N>,
+                       dim3((unsigned)((a.rows + ROWS - 1) / ROWS)), dim3(THREADS), s, a);
+}
+
+template <typename T, int L, int N>
+hipError_t bwd(const LayerNormArgs& a, hipStream_t s) {
+  constexpr int THREADS = L > 256 ? L : 256, ROWS = THREADS / L;
+  const int64_t most = (a.rows + ROWS - 1) / ROWS;
+  const int groups = (int)(most < LAYER_NORM_MAX_GROUPS ? most : LAYER_NORM_MAX_GROUPS);
+  note_matrix(a.x, a.rows, a.width, a.x_stride, sizeof(T), false);
+  note_matrix(a.weight, 1, a.width, a.width, sizeof(T), false);
+  note_matrix(a.stats, a.rows, 2, 2, 4, false);
+  note_matrix(a.dy, a.rows, a.width, a.width, sizeof(T), false);
+  note_matrix(a.ds, a.rows, a.width, a.width, sizeof(T), false);
+  note_matrix(a.dx, a.rows, a.width, a.width, sizeof(T), true);
+  note_matrix(a.partial, groups, 2 * a.width, 2 * a.width, 4, true);
+  const hipError_t e = launch_kernel("layer_norm_bwd_kernel", Work{14 * values_of(a), (a.ds ? 4 : 3) * values_of(a) * sizeof(T)}, layer_norm_bwd_kernel<T, L, N>,
+                                     dim3(groups), dim3(THREADS), s, a);
+  if (e != hipSuccess || !a.partial) return e;
+  note_matrix(a.partial, groups, 2 * a.width, 2 * a.width, 4, false);
+  note_matrix(a.dweight, 1, a.width, a.width, sizeof(T), true);
+  note_matrix(a.dbias, 1, a.width, a.width, sizeof(T), true);
+  return launch_kernel("layer_norm_sum_kernel", Work{0.0, 8.0 * groups * a.width}, layer_norm_sum_kernel<T>, dim3((2 * a.width + 31) / 32), dim3(1024), s, a, groups);
+}
+
+template <typename T, bool BACK>
+hipError_t by_width(const LayerNormArgs& a, hipStream_t s) {
+  auto go = [&](auto l, auto n) {
+    if constexpr (BACK) return bwd<T, decltype(l)::value, decltype(n)::value>(a, s);
+    else return fwd<T, decltype(l)::value, decltype(n)::value>(a, s);
+  };
+  const int pieces = a.width / PIECE;
+  if (pieces <= 8) return go(IntC<8>{}, IntC<1>{});
+  if (pieces <= 16) return go(IntC<16>{}, IntC<1>{});
+  if (pieces <= 32) return go(IntC<32>{}, IntC<1>{});
+  if (pieces <= 64) return go(IntC<64>{}, IntC<1>{});
+  if (pieces <= 128) return go(IntC<64>{}, IntC<2>{});
+  if (pieces <= 256) return go(IntC<256>{}, IntC<1>{});
+  if (pieces <= 512) return go(IntC<256>{}, IntC<2>{});
+  if (pieces <= 768) return go(IntC<256>{}, IntC<3>{});
+  if (pieces <= 1024) return go(IntC<256>{}, IntC<4>{});
+  if (pieces <= 2048) return go(IntC<1024>{}, IntC<2>{});
+  if (pieces <= 4096) return go(IntC<1024>{}, IntC<4>{});
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_layer_norm_fwd(const LayerNormArgs& a, bool f32, hipStream_t s) {
+  return f32 ? by_width<float, false>(a, s) : by_width<bf16, false>(a, s);
+}
+hipError_t launch_layer_norm_bwd(const LayerNormArgs& a, bool f32, hipStream_t s) {
+  return f32 ? by_width<float, true>(a, s) : by_width<bf16, true>(a, s);
+}
+
+}  // namespace sk

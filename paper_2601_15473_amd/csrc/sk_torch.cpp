@@ -289,6 +289,9 @@ PyMethodDef methods[] = {
     {"head_norm_rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(sk_torch::head_norm_rope)), METH_FASTCALL, "(q, k), or None for a call it does not take"},
     {"embedding", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(sk_torch::embedding)), METH_FASTCALL, "y, or None for a call it does not take"},
     {"dropout", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(sk_torch::dropout)), METH_FASTCALL, "y, or None for a call it does not take"},
+    {"layer_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(sk_torch::layer_norm)), METH_FASTCALL, "y or (y, sum), or None for a call it does not take"},
+    {"dense_layer", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(sk_torch::dense_layer)), METH_FASTCALL, "y, or None for a call it does not take"},
+    {"distillation_loss", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(sk_torch::distillation_loss)), METH_FASTCALL, "the loss, or None for a call it does not take"},
     {"raise_as", raise_as, METH_O, "the exception type of a refused call, made from its status"},
     {"release_workspaces", release_workspaces, METH_NOARGS, "gives the scratch buffers back to the allocator"},
     {nullptr, nullptr, 0, nullptr}};

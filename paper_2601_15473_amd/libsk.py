@@ -89,8 +89,29 @@ class NormRopeShape(ctypes.Structure):
                 ("q_out_strides", _i64 * 2), ("k_out_strides", _i64 * 2)]
 
 
+class LayerNormShape(ctypes.Structure):
+    """sk_layer_norm_shape"""
+    _fields_ = [("rows", _i64), ("width", _i64), ("eps", ctypes.c_float), ("dtype", ctypes.c_int),
+                ("x_stride", _i64), ("residual_stride", _i64)]
+
+
+class DenseShape(ctypes.Structure):
+    """sk_dense_shape"""
+    _fields_ = [("tokens", _i64), ("d_in", _i64), ("d_out", _i64), ("activation", _i32), ("dtype", ctypes.c_int),
+                ("x_stride", _i64), ("residual_stride", _i64)]
+
+
+class DistillShape(ctypes.Structure):
+    """sk_distill_shape"""
+    _fields_ = [("rows", _i64), ("vocabulary", _i64), ("logits_stride", _i64), ("top", _i32), ("id_bytes", _i32), ("label_bytes", _i32),
+                ("temperature", ctypes.c_float), ("label_weight", ctypes.c_float), ("dtype", ctypes.c_int)]
+
+
+SK_ACT_NONE, SK_ACT_RELU, SK_ACT_GELU, SK_ACT_GELU_TANH, SK_ACT_SILU = range(5)
+
 _shape, _f32, _u64 = ctypes.POINTER(AttentionShape), ctypes.c_float, ctypes.c_uint64
 _norm_shape = ctypes.POINTER(NormRopeShape)
+_layer_norm_shape, _dense_shape, _distill_shape = (ctypes.POINTER(_s) for _s in (LayerNormShape, DenseShape, DistillShape))
 for _name, _restype, _argtypes in (
         ("sk_attention_workspace_bytes", _sz, [_shape, _i32]),
         ("sk_attention_fwd", ctypes.c_int, [_shape] + [_vp] * 7 + [_sz, _vp]),
@@ -101,12 +122,22 @@ for _name, _restype, _argtypes in (
         ("sk_embedding_fwd", ctypes.c_int, [_vp, _i32, _vp, _vp, _i64, _i64, _i64, _f32, ctypes.c_int, _vp]),
         ("sk_embedding_workspace_bytes", _sz, [_i64, _i64, _i64, ctypes.c_int]),
         ("sk_embedding_bwd", ctypes.c_int, [_vp, _i32, _vp, _vp, _i64, _i64, _i64, _f32, ctypes.c_int, _vp, _sz, _vp]),
-        ("sk_dropout", ctypes.c_int, [_vp, _vp, _vp, _i64, _f32, _u64, _u64, ctypes.c_int, _vp])):
+        ("sk_dropout", ctypes.c_int, [_vp, _vp, _vp, _i64, _f32, _u64, _u64, ctypes.c_int, _vp]),
+        ("sk_layer_norm_fwd", ctypes.c_int, [_layer_norm_shape] + [_vp] * 8),
+        ("sk_layer_norm_workspace_bytes", _sz, [_layer_norm_shape]),
+        ("sk_layer_norm_bwd", ctypes.c_int, [_layer_norm_shape] + [_vp] * 9 + [_sz, _vp]),
+        ("sk_dense_workspace_bytes", _sz, [_dense_shape, _i32]),
+        ("sk_dense_fwd", ctypes.c_int, [_dense_shape] + [_vp] * 7 + [_sz, _vp]),
+        ("sk_dense_bwd", ctypes.c_int, [_dense_shape] + [_vp] * 8 + [_sz, _vp]),
+        ("sk_distill_fwd", ctypes.c_int, [_distill_shape] + [_vp] * 7),
+        ("sk_distill_bwd", ctypes.c_int, [_distill_shape] + [_vp] * 8)):
     getattr(_lib, _name).restype = _restype
     getattr(_lib, _name).argtypes = _argtypes
 
 BLOCK_EXPORTS = ("sk_attention_workspace_bytes", "sk_attention_fwd", "sk_attention_bwd", "sk_norm_rope_fwd", "sk_norm_rope_bwd",
-                 "sk_norm_rope_workspace_bytes", "sk_embedding_fwd", "sk_embedding_bwd", "sk_embedding_workspace_bytes", "sk_dropout")
+                 "sk_norm_rope_workspace_bytes", "sk_embedding_fwd", "sk_embedding_bwd", "sk_embedding_workspace_bytes", "sk_dropout",
+                 "sk_layer_norm_fwd", "sk_layer_norm_bwd", "sk_layer_norm_workspace_bytes", "sk_dense_fwd", "sk_dense_bwd", "sk_dense_workspace_bytes",
+                 "sk_distill_fwd", "sk_distill_bwd")
 
 # ---- testing / tuning / measurement aids (include/sk_debug.h) ----
 (SK_TUNE_TILE, SK_TUNE_WTILE, SK_TUNE_WSPLITS, SK_TUNE_BM, SK_TUNE_SLICES, SK_TUNE_STILE, SK_TUNE_SSPLITS,
@@ -276,6 +307,42 @@ def sk_embedding_bwd(ids, id_bytes, dy, dtable, tokens, rows, width, scale, dtyp
 
 def sk_dropout(x, residual, y, n, p, seed, offset, dtype, stream=None):
     return _lib.sk_dropout(_ptr(x), _ptr(residual), _ptr(y), n, p, seed, offset, dtype, _stream(stream))
+
+
+def sk_layer_norm_fwd(shape, x, residual, weight, bias, y, sum, stats, stream=None):
+    return _lib.sk_layer_norm_fwd(shape, _ptr(x), _ptr(residual), _ptr(weight), _ptr(bias), _ptr(y), _ptr(sum), _ptr(stats), _stream(stream))
+
+
+def sk_layer_norm_workspace_bytes(shape):
+    return _lib.sk_layer_norm_workspace_bytes(shape)
+
+
+def sk_layer_norm_bwd(shape, x, weight, stats, dy, d_sum, dx, dweight, dbias, workspace, workspace_bytes, stream=None):
+    return _lib.sk_layer_norm_bwd(shape, _ptr(x), _ptr(weight), _ptr(stats), _ptr(dy), _ptr(d_sum), _ptr(dx), _ptr(dweight), _ptr(dbias),
+                                  _ptr(workspace), workspace_bytes, _stream(stream))
+
+
+def sk_dense_workspace_bytes(shape, backward):
+    return _lib.sk_dense_workspace_bytes(shape, backward)
+
+
+def sk_dense_fwd(shape, x, weight, bias, residual, y, z, workspace, workspace_bytes, stream=None):
+    return _lib.sk_dense_fwd(shape, _ptr(x), _ptr(weight), _ptr(bias), _ptr(residual), _ptr(y), _ptr(z), _ptr(workspace), workspace_bytes,
+                             _stream(stream))
+
+
+def sk_dense_bwd(shape, x, weight, z, dy, dx, dweight, dbias, workspace, workspace_bytes, stream=None):
+    return _lib.sk_dense_bwd(shape, _ptr(x), _ptr(weight), _ptr(z), _ptr(dy), _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(workspace),
+                             workspace_bytes, _stream(stream))
+
+
+def sk_distill_fwd(shape, logits, teacher_logits, teacher_ids, labels, loss, stats, stream=None):
+    return _lib.sk_distill_fwd(shape, _ptr(logits), _ptr(teacher_logits), _ptr(teacher_ids), _ptr(labels), _ptr(loss), _ptr(stats), _stream(stream))
+
+
+def sk_distill_bwd(shape, logits, teacher_logits, teacher_ids, labels, stats, dloss, dlogits, stream=None):
+    return _lib.sk_distill_bwd(shape, _ptr(logits), _ptr(teacher_logits), _ptr(teacher_ids), _ptr(labels), _ptr(stats), _ptr(dloss),
+                               _ptr(dlogits), _stream(stream))
 
 
 def sk_status_string(status):
