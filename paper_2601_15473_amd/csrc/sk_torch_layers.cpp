@@ -7,7 +7,7 @@
 namespace sk_torch {
 namespace {
 
-// Which inputs' gradients a backward pass forms: those that had one at the forward pass; every one where a graph of it is made.
+// Which inputs' gradients a backward pass forms: those that had one at the forward pass; where a graph of it is made, every one (a function's results are all there).
 enum Wanted : int64_t { WANT_X = 1, WANT_WEIGHT = 2, WANT_BIAS = 4, WANT_RESIDUAL = 8 };
 bool wants(const std::optional<Tensor>& t) { return t.has_value() && t->requires_grad(); }
 int64_t wanted(const Tensor& x, const std::optional<Tensor>& weight, const std::optional<Tensor>& bias, const std::optional<Tensor>& residual) {
@@ -78,13 +78,14 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
   }
 
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
-    const variable_list out = once([&] { return gradients(ctx, grads); });
+    const bool all = at::GradMode::is_enabled();   // (off inside)
+    const variable_list out = once([&] { return gradients(ctx, grads, all); });
     const int64_t want = ctx->saved_data["wanted"].toInt();
     const bool residual = ctx->saved_data["residual"].toBool();
     return {want & WANT_X ? out[0] : Tensor(), want & WANT_WEIGHT ? out[1] : Tensor(), want & WANT_BIAS ? out[2] : Tensor(), residual && (want & WANT_RESIDUAL) ? out[0] : Tensor(), Tensor()};
   }
 
-  static variable_list gradients(AutogradContext* ctx, const variable_list& grads) {
+  static variable_list gradients(AutogradContext* ctx, const variable_list& grads, bool all) {
     const variable_list saved = ctx->get_saved_variables();
     const Tensor &x = saved[0], &w = saved[1], &stats = saved[2];
     const c10::DeviceGuard guard(x.device());
@@ -92,7 +93,6 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
     const Tensor ds = grads.size() > 1 && grads[1].defined() ? made_dense(grads[1]) : Tensor();
     const sk_layer_norm_shape s = norm_shape(x, Tensor(), 0.0);
     const int64_t want = ctx->saved_data["wanted"].toInt();
-    const bool all = at::GradMode::is_enabled();
     const Tensor none = all ? at::zeros({0}, x.options()) : Tensor();
     const Tensor dx = at::empty(x.sizes(), x.options());
     const Tensor dw = w.defined() && (all || (want & WANT_WEIGHT)) ? at::empty({s.width}, x.options()) : none;
@@ -141,18 +141,18 @@ struct Dense : torch::autograd::Function<Dense> {
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
     const int64_t want = ctx->saved_data["wanted"].toInt();
     variable_list out{Tensor(), Tensor(), Tensor()};
-    if (want & ~WANT_RESIDUAL) out = once([&] { return gradients(ctx, grads); });
+    const bool all = at::GradMode::is_enabled();   // (off inside)
+    if (want & ~WANT_RESIDUAL) out = once([&] { return gradients(ctx, grads, all); });
     return {want & WANT_X ? out[0] : Tensor(), want & WANT_WEIGHT ? out[1] : Tensor(), want & WANT_BIAS ? out[2] : Tensor(), want & WANT_RESIDUAL ? grads[0] : Tensor(), Tensor()};
   }
 
-  static variable_list gradients(AutogradContext* ctx, const variable_list& grads) {
+  static variable_list gradients(AutogradContext* ctx, const variable_list& grads, bool all) {
     const variable_list saved = ctx->get_saved_variables();
     const Tensor &x = saved[0], &w = saved[1], &z = saved[2];
     const c10::DeviceGuard guard(x.device());
     const Tensor dy = made_dense(grads[0]);
     const sk_dense_shape s = layer_shape(x, w, Tensor(), ctx->saved_data["activation"].toInt());
     const int64_t want = ctx->saved_data["wanted"].toInt();
-    const bool all = at::GradMode::is_enabled();
     const Tensor none = all ? at::zeros({0}, x.options()) : Tensor();
     const Tensor dx = all || (want & WANT_X) ? at::empty(x.sizes(), x.options()) : none;
     const Tensor dw = all || (want & WANT_WEIGHT) ? at::empty(w.sizes(), x.options()) : none;
