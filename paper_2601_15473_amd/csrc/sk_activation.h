@@ -64,6 +64,17 @@ __device__ __forceinline__ float activation(float z) {
   if constexpr (ACT == ACT_SILU) return z * logistic(z);
   return z;
 }
+// ... by a number that is the same in all lanes, where an activation is not worth a kernel
+template <bool PRECISE>
+__device__ __forceinline__ float activation(int act, float z) {
+  switch (act) {
+    case ACT_RELU: return activation<ACT_RELU, PRECISE>(z);
+    case ACT_GELU: return activation<ACT_GELU, PRECISE>(z);
+    case ACT_GELU_TANH: return activation<ACT_GELU_TANH, PRECISE>(z);
+    case ACT_SILU: return activation<ACT_SILU, PRECISE>(z);
+    default: return z;
+  }
+}
 template <int ACT, bool PRECISE>
 __device__ __forceinline__ float activation_slope(float z) {
   if constexpr (ACT == ACT_RELU) return z <= 0.f ? 0.f : 1.f;

@@ -883,7 +883,19 @@ hipError_t launch_product(GemmKind kind, GemmArgs a, bool f32, void* slabs, hipS
   return launch_reduce_splits(r, st);
 }
 
-int product_slabs(int64_t M, int64_t N, int64_t K, bool f32) { return f32 ? plan_f32_first(M, N, K).splits : plan_first(GEMM_NT, M, N, K).splits; }
+DensePlan plan_dense(int64_t M, int64_t N, int64_t K, bool f32) {
+  DensePlan d{};
+  if (f32) {
+    d.splits = plan_f32_first(M, N, K).splits;
+    return d;
+  }
+  const FirstPlan f = plan_first(GEMM_NT, M, N, K);
+  d.splits = f.splits;
+  d.fused = f.splits == 1;
+  d.few = f.few;
+  d.tile = f.few ? f.tile : choose_expansion_tile(GEMM_NT, M, N, K);
+  return d;
+}
 
 hipError_t launch_product_slabs(GemmArgs a, bool f32, void* slabs, hipStream_t st) {
   a.C = slabs;
@@ -896,8 +908,7 @@ hipError_t launch_product_slabs(GemmArgs a, bool f32, void* slabs, hipStream_t s
   }
   const FirstPlan f = plan_first(GEMM_NT, a.M, a.N, a.K);
   a.splits = f.splits; a.k_per_split = f.k_per_split;
-  if (f.few && f.splits > 1) return launch_gemm_few_rows_bf16(GEMM_NT, a, st);
-  return launch_gemm_bf16(GEMM_NT_F32, f.few ? TILE_64x64 : f.tile == TILE_256x256 ? TILE_128x128 : f.tile, a, st);
+  return f.few ? launch_gemm_few_rows_bf16(GEMM_NT, a, st) : launch_gemm_bf16(GEMM_NT_F32, f.tile, a, st);
 }
 
 }  // namespace sk

@@ -10,7 +10,7 @@
 // planner's few_rows_splits) is cut into two to eight ranges, each on XCDs of its own, that leave fp32
 // slabs for another launch to sum; everything else is one launch without slabs.
 #include "sk_bf16_lds.h"
-#include "sk_launch.h"
+#include "sk_dense_launch.h"
 
 namespace sk {
 
@@ -28,8 +28,14 @@ struct FewRows {
   static_assert(A8 * 8 <= 64 && NB <= 2, "one panel each");
 };
 
-template <int A8, int NB, bool B_KC>
-__global__ __launch_bounds__(256) void gemm_bf16_few_rows_kernel(const GemmArgs p) {
+// Of a dense layer: its result, act(C) + residual, in place of the product's.
+struct DenseFewArgs : GemmArgs {
+  FinishArgs f;
+  int act;
+};
+
+template <int A8, int NB, bool B_KC, typename Args = GemmArgs>
+__global__ __launch_bounds__(256) void gemm_bf16_few_rows_kernel(const Args p) {
   typedef FewRows<A8, NB, B_KC> G;
   constexpr int MB = G::MB;
   constexpr bool HALF = NB == 1 && !B_KC;   // 32 columns: lines of 64 bytes, which need no swizzle
@@ -159,6 +165,17 @@ __global__ __launch_bounds__(256) void gemm_bf16_few_rows_kernel(const GemmArgs 
     }
     uint2 b = make_uint2(0u, 0u);
     if (p.bias != nullptr) b = *reinterpret_cast<const uint2*>(static_cast<const bf16*>(p.bias) + gn);
+    if constexpr (!std::is_same<Args, GemmArgs>::value) {
+      const FinishArgs& f = p.f;
+      float v[4] = {s.x + bf16_bits_to_float(b.x & 0xffffu), s.y + bf16_bits_to_float(b.x >> 16), s.z + bf16_bits_to_float(b.y & 0xffffu), s.w + bf16_bits_to_float(b.y >> 16)};
+      if (f.z != nullptr) *reinterpret_cast<uint2*>(static_cast<bf16*>(f.z) + (int64_t)gm * p.ldc + gn) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+      uint2 r = make_uint2(0u, 0u);
+      if (f.residual != nullptr) r = *reinterpret_cast<const uint2*>(static_cast<const bf16*>(f.residual) + (int64_t)gm * f.residual_ld + gn);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = activation<false>(p.act, v[e]) + bf16_bits_to_float(e < 2 ? (e ? r.x >> 16 : r.x & 0xffffu) : (e > 2 ? r.y >> 16 : r.y & 0xffffu));
+      *reinterpret_cast<uint2*>(static_cast<bf16*>(p.C) + (int64_t)gm * p.ldc + gn) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+      continue;
+    }
     uint2 o;
     o.x = pack_bf16x2(s.x * p.scale + bf16_bits_to_float(b.x & 0xffffu), s.y * p.scale + bf16_bits_to_float(b.x >> 16));
     o.y = pack_bf16x2(s.z * p.scale + bf16_bits_to_float(b.y & 0xffffu), s.w * p.scale + bf16_bits_to_float(b.y >> 16));
@@ -197,6 +214,26 @@ hipError_t launch_gemm_few_rows_bf16(GemmKind kind, const GemmArgs& a, hipStream
   const bool wide = a.splits > 1 || (long long)((a.M + 63) / 64) * ((a.N + 31) / 32) > NUM_CUS;
   if (kind == GEMM_NN) return wide ? launch_rows<2, false>(a, s) : launch_rows<1, false>(a, s);
   return wide ? launch_rows<2, true>(a, s) : launch_rows<1, true>(a, s);
+}
+
+template <int A8, int NB>
+static hipError_t launch_dense(const GemmArgs& g, const FinishArgs& f, int act, hipStream_t s) {
+  typedef FewRows<A8, NB, true> G;
+  DenseFewArgs a{g, f, act};
+  a.tiles_m = (a.M + G::BM - 1) / G::BM;
+  a.tiles_n = (a.N + G::BN - 1) / G::BN;
+  const long long grid = (long long)a.tiles_m * a.tiles_n;
+  if (a.splits != 1 || grid <= 0 || grid > 0x7fffffffLL) return hipErrorInvalidValue;
+  note_dense(a, f);
+  static const std::string name = kernel_label("dense_bf16_few_rows_kernel", {lbl(A8), lbl(NB)});
+  return launch_kernel(name.c_str(), dense_work(a, f), gemm_bf16_few_rows_kernel<A8, NB, true, DenseFewArgs>, dim3((unsigned)grid), dim3(256), s, a);
+}
+hipError_t launch_dense_few_rows(int act, const GemmArgs& a, const FinishArgs& f, hipStream_t s) {
+  const bool wide = (long long)((a.M + 63) / 64) * ((a.N + 31) / 32) > NUM_CUS;   // (as above)
+  if (a.M <= 8) return wide ? launch_dense<1, 2>(a, f, act, s) : launch_dense<1, 1>(a, f, act, s);
+  if (a.M <= 16) return wide ? launch_dense<2, 2>(a, f, act, s) : launch_dense<2, 1>(a, f, act, s);
+  if (a.M <= 32) return wide ? launch_dense<4, 2>(a, f, act, s) : launch_dense<4, 1>(a, f, act, s);
+  return wide ? launch_dense<8, 2>(a, f, act, s) : launch_dense<8, 1>(a, f, act, s);
 }
 
 }  // namespace sk

@@ -1,6 +1,7 @@
 // The bf16 GEMM tiles (same contract as sk_bf16_gemm.hip) on a ring of chunks in LDS: for launches of one round,
 // whose work-groups have a CU to themselves or share it with one other.
 #pragma once
+#include "sk_bf16_finish.h"
 #include "sk_bf16_lds.h"
 
 namespace sk {
@@ -17,7 +18,8 @@ namespace sk {
 // neither reads nor MFMAs the same loops take 80 to 95 % of the time (35 to 57 GB/s a CU, a chunk of a
 // 128 x 128 tile 0.58 us), and neither more slots nor tiles that start at different k changed that.  A 256 x 128 tile, a wave's part 128 x 64,
 // fills three quarters as much for the same products, 0.83 us a chunk: for expansions of one round (choose_expansion_tile).
-template <int BM, int BN, bool A_KC, bool B_KC, typename OutT, bool COLSUM>
+// ACT: 0 and more for a dense layer's results (sk_bf16_finish.h) in place of the product's.
+template <int BM, int BN, bool A_KC, bool B_KC, typename OutT, bool COLSUM, int ACT = -1>
 struct RingTile {
   static constexpr int WM = BM / 2, WN = BN / 2, TM = WM / 32, TN = WN / 32;   // waves 2 x 2
   static constexpr int SLOTS = BM == BN ? 4 : 3;
@@ -28,12 +30,13 @@ struct RingTile {
   static constexpr int AHEAD = (SLOTS - 2) * LOADS;                           // loads in flight at a barrier
   static constexpr int STRIP = 32 * WN * 2;                                   // a wave's, for bf16 results
   static_assert(LDS_BYTES <= 160 * 1024 && 4 * STRIP <= LDS_BYTES && AHEAD + LOADS <= 63, "LDS of a compute unit, the load counter");
-  static __device__ __forceinline__ void run(const GemmArgs& p, int block, unsigned char* smem);   // (smem: the kernel's only LDS, from address 0)
+  static_assert(ACT < 0 || (sizeof(OutT) == 2 && 4 * FinishStrip<TN>::BYTES <= LDS_BYTES), "a dense layer's strips");
+  static __device__ __forceinline__ void run(const GemmArgs& p, int block, unsigned char* smem, const FinishArgs& f = FinishArgs{});   // (smem: the kernel's only LDS, from address 0)
 };
 
-template <int BM, int BN, bool A_KC, bool B_KC, typename OutT, bool COLSUM>
+template <int BM, int BN, bool A_KC, bool B_KC, typename OutT, bool COLSUM, int ACT>
 __device__ __forceinline__ void
-RingTile<BM, BN, A_KC, B_KC, OutT, COLSUM>::run(const GemmArgs& p, const int block, unsigned char* const smem) {
+RingTile<BM, BN, A_KC, B_KC, OutT, COLSUM, ACT>::run(const GemmArgs& p, const int block, unsigned char* const smem, const FinishArgs& f) {
   typedef Panels<A_KC> PA;
   typedef Panels<B_KC> PB;
   // (what the loads write is invisible to the compiler: it must not take smem for unwritten)
@@ -50,8 +53,8 @@ RingTile<BM, BN, A_KC, B_KC, OutT, COLSUM>::run(const GemmArgs& p, const int blo
 
   // This lane's bias values (see sk_bf16_gemm.hip), through a buffer window of N elements (none without a bias)
   constexpr bool BF16_OUT = sizeof(OutT) == 2;
-  uint2 bias_r[BF16_OUT ? TN : 1][4];
-  if constexpr (BF16_OUT) {
+  uint2 bias_r[BF16_OUT && ACT < 0 ? TN : 1][4];
+  if constexpr (BF16_OUT && ACT < 0) {
     const GWindow bias_w = make_window(p.bias, 0, p.bias != nullptr ? p.N : 0, 2);
 #pragma unroll
     for (int j = 0; j < TN; ++j)
@@ -191,7 +194,13 @@ RingTile<BM, BN, A_KC, B_KC, OutT, COLSUM>::run(const GemmArgs& p, const int blo
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
   const float scale = p.scale;
   const int wn0 = n0 + wn * WN, n_store = p.n_store > 0 ? p.n_store : p.N;
-  if constexpr (!BF16_OUT) {
+  if constexpr (ACT >= 0) {
+    uint4 bias[FinishStrip<TN>::STEPS];
+    finish_bias<TN>(bias, p.bias, wn0, p.N, lane);
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+      finish_rows<ACT, TN>(acc[i], f, bias, p.C, p.ldc, m0 + wm * WM + i * 32, wn0, p.M, p.N, smem + wave * FinishStrip<TN>::BYTES, lane);
+  } else if constexpr (!BF16_OUT) {
     float* const C = static_cast<float*>(p.C);
 #pragma unroll
     for (int i = 0; i < TM; ++i) {

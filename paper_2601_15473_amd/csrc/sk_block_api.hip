@@ -3,6 +3,7 @@
 
 #include "../../include/sk_block.h"
 #include "sk_block_launch.h"
+#include "sk_dense_launch.h"
 
 namespace {
 
@@ -184,7 +185,10 @@ struct DenseRoom {   // backward: dz | column sums | the products' slabs, one pr
     total = slabs + (dx > dw ? dx : dw);
   }
 };
-size_t dense_forward_bytes(const DenseArgs& a, bool f32) { return align_up((size_t)product_slabs(a.tokens, a.out, a.in, f32) * a.tokens * a.out * 4); }
+size_t dense_forward_bytes(const DenseArgs& a, bool f32) {
+  const DensePlan d = plan_dense(a.tokens, a.out, a.in, f32);
+  return d.fused ? 0 : align_up((size_t)d.splits * a.tokens * a.out * 4);
+}
 GemmArgs product(const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t M, int64_t N, int64_t K, const void* bias) {
   GemmArgs g{};
   g.A = A; g.B = B; g.C = C; g.bias = bias;
@@ -381,13 +385,24 @@ sk_status sk_dense_fwd(const sk_dense_shape* shape, const void* x, const void* w
   const sk_status st = dense_layer_args(shape, a);
   if (st != SK_OK) return st;
   const bool f32 = shape->dtype == SK_F32;
-  if (!workspace || workspace_bytes < dense_forward_bytes(a, f32)) return SK_ERR_WORKSPACE;
+  const size_t need = dense_forward_bytes(a, f32);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return SK_ERR_WORKSPACE;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  a.x = x; a.weight = weight; a.bias = bias; a.residual = residual; a.y = y; a.z = z;
-  a.slabs = static_cast<const float*>(workspace);
-  a.splits = product_slabs(a.tokens, a.out, a.in, f32);
-  hipError_t e = launch_product_slabs(product(x, a.x_stride, weight, a.in, nullptr, a.tokens, a.out, a.in, nullptr), f32, workspace, s);
-  if (e == hipSuccess) e = launch_dense_finish(a, f32, s);
+  const DensePlan d = plan_dense(a.tokens, a.out, a.in, f32);
+  GemmArgs g = product(x, a.x_stride, weight, a.in, y, a.tokens, a.out, a.in, bias);
+  hipError_t e;
+  if (d.fused) {
+    g.splits = 1;
+    g.k_per_split = (g.K + 63) / 64 * 64;
+    const FinishArgs f = {residual, a.activation != SK_ACT_NONE ? z : nullptr, a.residual_stride};
+    e = d.few ? launch_dense_few_rows(a.activation, g, f, s) : launch_dense_bf16(d.tile, a.activation, g, f, s);
+  } else {
+    a.x = x; a.weight = weight; a.bias = bias; a.residual = residual; a.y = y; a.z = z;
+    a.slabs = static_cast<const float*>(workspace);
+    a.splits = d.splits;
+    e = launch_product_slabs(g, f32, workspace, s);
+    if (e == hipSuccess) e = launch_dense_finish(a, f32, s);
+  }
   return launched(e, "sk_dense_fwd");
 }
 

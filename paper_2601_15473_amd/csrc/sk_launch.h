@@ -176,8 +176,14 @@ constexpr int F32_BK = 32;
 // (GEMM_NN) or [N, K] (GEMM_NT); of A [K, M] and B [K, N] (GEMM_TN_F32_PLAIN), a contraction over rows.  `slabs`: product_bytes of room (none with a bias).
 size_t product_bytes(GemmKind kind, int64_t M, int64_t N, int64_t K, bool f32);
 hipError_t launch_product(GemmKind kind, GemmArgs a, bool f32, void* slabs, hipStream_t s);
-// ... A [M, K] . B [N, K] in fp32 slabs [splits][M, N] for a launch of the caller's that sums them
-int product_slabs(int64_t M, int64_t N, int64_t K, bool f32);
+// A dense layer's forward product, planned: with all that follows it in its epilogue (bf16; `few`: the few-rows kernel, else on `tile`), or in fp32 slabs [splits][M, N]
+// for a launch of the caller's that sums and finishes them.
+struct DensePlan {
+  bool fused, few;
+  int tile, splits;
+};
+DensePlan plan_dense(int64_t M, int64_t N, int64_t K, bool f32);
+// A [M, K] . B [N, K] in fp32 slabs [splits][M, N] for a launch of the caller's that sums them
 hipError_t launch_product_slabs(GemmArgs a, bool f32, void* slabs, hipStream_t s);
 
 hipError_t launch_reduce_splits(const ReduceArgs& a, hipStream_t s);
