@@ -847,10 +847,9 @@ hipError_t first_gemm(const Shape& s, GemmKind kind, GemmKind kind_slabs, GemmAr
 namespace sk {
 
 size_t product_bytes(GemmKind kind, int64_t M, int64_t N, int64_t K, bool f32) {
-  const size_t slab = (size_t)M * N * 4;
-  if (kind == GEMM_TN_F32_PLAIN) {
+  if (kind == GEMM_TN) {
     const TokenPlan t = plan_tokens(M, N, K, f32 ? SK_F32 : SK_BF16, false, 0);
-    return f32 && t.splits == 1 ? 0 : align_up(slab * t.splits);
+    return t.splits == 1 ? 0 : align_up((size_t)t.splits * M * N * 4);
   }
   if (f32) return plan_f32_first(M, N, K).slab_bytes;
   return plan_first(kind, M, N, K).slab_bytes;
@@ -862,7 +861,7 @@ hipError_t launch_product(GemmKind kind, GemmArgs a, bool f32, void* slabs, hipS
   a.scale = 1.f;
   a.splits = 1;
   a.k_per_split = (a.K + 63) / 64 * 64;
-  if (kind != GEMM_TN_F32_PLAIN) {
+  if (kind != GEMM_TN) {
     const GemmKind in_slabs = kind == GEMM_NT ? GEMM_NT_F32 : GEMM_NN_F32;
     if (a.bias != nullptr || product_bytes(kind, a.M, a.N, a.K, f32) == 0) return gemm(s, kind, a, st);
     return first_gemm(s, kind, in_slabs, a, slabs, st);
@@ -871,12 +870,12 @@ hipError_t launch_product(GemmKind kind, GemmArgs a, bool f32, void* slabs, hipS
   void* const out = a.C;
   a.splits = t.splits;
   a.k_per_split = t.k_per_split;
-  if (!f32 || t.splits > 1) a.C = slabs;
+  if (t.splits == 1) return f32 ? launch_gemm_f32(GEMM_TN_F32, t.tile, a, st) : launch_gemm_bf16(GEMM_TN, t.tile, a, st);
+  a.C = slabs;
   const hipError_t e = f32 ? launch_gemm_f32(GEMM_TN_F32, t.tile, a, st) : launch_gemm_bf16(GEMM_TN_F32_PLAIN, t.tile, a, st);
   if (e != hipSuccess) return e;
   const int64_t n = (int64_t)a.M * a.N;
   if (!f32) return launch_reduce_to_bf16(static_cast<const float*>(slabs), out, n, t.splits, st);
-  if (t.splits == 1) return hipSuccess;
   ReduceArgs r{};
   r.part = static_cast<const float*>(slabs); r.out = static_cast<float*>(out); r.n = n; r.splits = t.splits; r.scale = 1.f;
   r.splits2 = 1; r.scale2 = 1.f;

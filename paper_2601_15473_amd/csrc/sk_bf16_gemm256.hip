@@ -154,6 +154,7 @@ hipError_t launch_gemm256_bf16(GemmKind kind, const GemmArgs& a, hipStream_t s) 
     case GEMM_TT: return launch_crew<false, true, bf16>(a, s);
     case GEMM_NN_F32: return launch_crew<true, false, float>(a, s);
     case GEMM_TN_F32_PLAIN: return launch_crew<false, false, float>(a, s);
+    case GEMM_TN: return launch_crew<false, false, bf16>(a, s);
     default: return hipErrorInvalidValue;
   }
 }

@@ -181,7 +181,7 @@ struct DenseRoom {   // backward: dz | column sums | the products' slabs, one pr
     partial = a.activation != SK_ACT_NONE ? align_up((size_t)a.tokens * a.out * (f32 ? 4 : 2)) : 0;
     dz = 0;
     slabs = partial + align_up((size_t)DenseRuns(a.tokens, a.out).runs * a.out * 4);
-    const size_t dx = product_bytes(GEMM_NN, a.tokens, a.in, a.out, f32), dw = product_bytes(GEMM_TN_F32_PLAIN, a.out, a.in, a.tokens, f32);
+    const size_t dx = product_bytes(GEMM_NN, a.tokens, a.in, a.out, f32), dw = product_bytes(GEMM_TN, a.out, a.in, a.tokens, f32);
     total = slabs + (dx > dw ? dx : dw);
   }
 };
@@ -424,7 +424,7 @@ sk_status sk_dense_bwd(const sk_dense_shape* shape, const void* x, const void* w
   hipError_t e = launch_dense_dz(a, f32, s);
   if (e == hipSuccess) e = launch_dense_dbias(a, f32, s);
   if (e == hipSuccess && dx) e = launch_product(GEMM_NN, product(a.dz, a.out, weight, a.in, dx, a.tokens, a.in, a.out, nullptr), f32, w + room.slabs, s);
-  if (e == hipSuccess && dweight) e = launch_product(GEMM_TN_F32_PLAIN, product(a.dz, a.out, x, a.x_stride, dweight, a.out, a.in, a.tokens, nullptr), f32, w + room.slabs, s);
+  if (e == hipSuccess && dweight) e = launch_product(GEMM_TN, product(a.dz, a.out, x, a.x_stride, dweight, a.out, a.in, a.tokens, nullptr), f32, w + room.slabs, s);
   return launched(e, "sk_dense_bwd");
 }
 

@@ -88,12 +88,13 @@ enum GemmKind : int {
   GEMM_NN_F32_COLSUM = 6,  // as GEMM_NN_F32, plus the column sums of B
   GEMM_TN_F32_PLAIN = 7,   // as GEMM_TN_F32 without the column sums (any tile)
   GEMM_TT_F32 = 8,         // as GEMM_TT, split-K          -> fp32 slabs
+  GEMM_TN = 9,             // A [K,M], B [K,N]            -> storage type
 };
 
 inline void gemm_kind_traits(GemmKind kind, bool& a_kc, bool& b_kc, bool& out_f32) {
-  a_kc = !(kind == GEMM_TN_F32 || kind == GEMM_TN_F32_PLAIN || kind == GEMM_TT || kind == GEMM_TT_F32);
+  a_kc = !(kind == GEMM_TN_F32 || kind == GEMM_TN_F32_PLAIN || kind == GEMM_TN || kind == GEMM_TT || kind == GEMM_TT_F32);
   b_kc = kind == GEMM_NT || kind == GEMM_NT_F32 || kind == GEMM_TT || kind == GEMM_TT_F32;
-  out_f32 = !(kind == GEMM_NN || kind == GEMM_NT || kind == GEMM_TT);
+  out_f32 = !(kind == GEMM_NN || kind == GEMM_NT || kind == GEMM_TT || kind == GEMM_TN);
 }
 
 enum TileCfg : int {
@@ -173,7 +174,7 @@ hipError_t launch_dual_gemm_f32(GemmKind kind_a, const GemmArgs& a, GemmKind kin
 constexpr int F32_BK = 32;
 
 // Products of the dense layers, planned as the sketched layers' are (sk_api.hip), the result in the storage type: C [M, N] = A . B (+ bias) of A [M, K] and B [K, N]
-// (GEMM_NN) or [N, K] (GEMM_NT); of A [K, M] and B [K, N] (GEMM_TN_F32_PLAIN), a contraction over rows.  `slabs`: product_bytes of room (none with a bias).
+// (GEMM_NN) or [N, K] (GEMM_NT); of A [K, M] and B [K, N] (GEMM_TN), a contraction over rows.  `slabs`: product_bytes of room (none with a bias).
 size_t product_bytes(GemmKind kind, int64_t M, int64_t N, int64_t K, bool f32);
 hipError_t launch_product(GemmKind kind, GemmArgs a, bool f32, void* slabs, hipStream_t s);
 // A dense layer's forward product, planned: with all that follows it in its epilogue (bf16; `few`: the few-rows kernel, else on `tile`), or in fp32 slabs [splits][M, N]

@@ -13,28 +13,19 @@ namespace {
 
 constexpr int PIECE = 8;   // values
 
-// Sums of a row's lanes: L of a wave, or all of a work-group's (`shared`: a float a wave and sum).  Every lane gets them.
-template <int L, int N>
-__device__ __forceinline__ void sum_row(float (&v)[N], float* shared) {
+// The sum of a row's lanes, L of a wave or all of a work-group's (`shared`: a float a wave, another place for each sum).  Every lane gets it.
+template <int L>
+__device__ __forceinline__ float sum_row(float v, float* shared) {
 #pragma unroll
-  for (int m = 1; m < (L < 64 ? L : 64); m <<= 1)
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], m);
+  for (int m = 1; m < (L < 64 ? L : 64); m <<= 1) v += __shfl_xor(v, m);
   if constexpr (L > 64) {
-    constexpr int WAVES = L / 64;
-    __syncthreads();   // (what the sum before left has been read)
-    if ((threadIdx.x & 63) == 0)
-#pragma unroll
-      for (int i = 0; i < N; ++i) shared[i * WAVES + (threadIdx.x >> 6)] = v[i];
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
     __syncthreads();
+    v = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      float s = 0.f;
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) s += shared[i * WAVES + w];
-      v[i] = s;
-    }
+    for (int w = 0; w < L / 64; ++w) v += shared[w];
   }
+  return v;
 }
 
 template <typename T>
@@ -48,7 +39,7 @@ __device__ __forceinline__ void load_piece(float (&v)[PIECE], const T* row, int 
 template <typename T, int L, int N>
 __global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_fwd_kernel(const LayerNormArgs p) {
   constexpr int THREADS = L > 256 ? L : 256, ROWS = THREADS / L;
-  __shared__ float shared[L > 64 ? L / 64 : 1];
+  __shared__ float shared[2][L > 64 ? L / 64 : 1];
   const int lane = threadIdx.x % L;
   const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / L;
   if (row >= p.rows) return;   // (L > 64: a work-group's threads all, or none)
@@ -66,21 +57,19 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_fwd_kernel(const
       for (int i = 0; i < PIECE; ++i) v[n][i] += add[i];
     }
   }
-  float sum[1] = {0.f};
+  float sum = 0.f;
 #pragma unroll
   for (int n = 0; n < N; ++n)
 #pragma unroll
-    for (int i = 0; i < PIECE; ++i) sum[0] += v[n][i];
-  sum_row<L, 1>(sum, shared);
-  const float mean = sum[0] / p.width;
-  sum[0] = 0.f;
+    for (int i = 0; i < PIECE; ++i) sum += v[n][i];
+  const float mean = sum_row<L>(sum, shared[0]) / p.width;
+  sum = 0.f;
 #pragma unroll
   for (int n = 0; n < N; ++n)
     if ((n * L + lane) * PIECE < p.width)
 #pragma unroll
-      for (int i = 0; i < PIECE; ++i) sum[0] += (v[n][i] - mean) * (v[n][i] - mean);
-  sum_row<L, 1>(sum, shared);
-  const float r = 1.f / sqrtf(sum[0] / p.width + p.eps);
+      for (int i = 0; i < PIECE; ++i) sum += (v[n][i] - mean) * (v[n][i] - mean);
+  const float r = 1.f / sqrtf(sum_row<L>(sum, shared[1]) / p.width + p.eps);
   if (p.stats && lane == 0) *reinterpret_cast<float2*>(p.stats + row * 2) = make_float2(mean, r);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
@@ -98,44 +87,81 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_fwd_kernel(const
   }
 }
 
+// A row's pieces as they lie in memory, for loads that are not waited for yet.
+template <typename T, int N>
+struct Raw {
+  uint4 v[N][sizeof(T) / 2];
+  template <int L>
+  __device__ __forceinline__ void load(const T* row, int lane, int width) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int at = (n * L + lane) * PIECE;
+#pragma unroll
+      for (int h = 0; h < (int)sizeof(T) / 2; ++h) v[n][h] = at < width ? reinterpret_cast<const uint4*>(row + at)[h] : make_uint4(0u, 0u, 0u, 0u);
+    }
+  }
+  __device__ __forceinline__ void values(float (&f)[PIECE], int n) const {
+    const unsigned u[4] = {v[n][0].x, v[n][0].y, v[n][0].z, v[n][0].w};
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __builtin_bit_cast(float, u[i] << 16);
+        f[2 * i + 1] = __builtin_bit_cast(float, u[i] & 0xffff0000u);
+      }
+    } else {
+      const uint4 w = v[n][sizeof(T) / 2 - 1];
+      const unsigned x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f[i] = __builtin_bit_cast(float, u[i]);
+        f[4 + i] = __builtin_bit_cast(float, x[i]);
+      }
+    }
+  }
+};
+
 // Gradients: work-groups walk over the rows with their lanes' terms of dw and db in registers, and leave one row of each, [group][dw, db][width].
-template <typename T, int L, int N>
+// What the next row needs is on its way while this one's sums are formed.
+template <typename T, int L, int N, bool SUM>
 __global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_bwd_kernel(const LayerNormArgs p) {
-  constexpr int THREADS = L > 256 ? L : 256, ROWS = THREADS / L;
-  __shared__ float shared[L > 64 ? 2 * (L / 64) : 1];
+  constexpr int THREADS = L > 256 ? L : 256, ROWS = THREADS / L, WAVES = L > 64 ? L / 64 : 1;
+  __shared__ float shared[2][2 * WAVES];
   __shared__ float rows[ROWS > 1 ? THREADS * N * PIECE : 1];
   const int lane = threadIdx.x % L, sub = threadIdx.x / L;
   float dw[N][PIECE], db[N][PIECE];
+  Raw<T, N> weight;
+  if (p.weight) weight.template load<L>(static_cast<const T*>(p.weight), lane, p.width);
 #pragma unroll
   for (int n = 0; n < N; ++n)
 #pragma unroll
     for (int i = 0; i < PIECE; ++i) dw[n][i] = db[n][i] = 0.f;
-  // (ROWS > 1: the lanes of a row that is not there go along with zeros)
-  for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < p.rows; row0 += (int64_t)gridDim.x * ROWS) {
-    const int64_t row = row0 + sub;
-    const bool there = row < p.rows;
-    const int64_t at_row = there ? row : p.rows - 1;
-    const float2 stat = *reinterpret_cast<const float2*>(p.stats + at_row * 2);
-    const T* const s = static_cast<const T*>(p.x) + at_row * p.x_stride;
-    const T* const dy = static_cast<const T*>(p.dy) + at_row * p.width;
-    float u[N][PIECE], g[N][PIECE];
+  struct Row {
+    Raw<T, N> s, dy, ds;
+    float2 stat;
+  };
+  auto fetch = [&](Row& r, int64_t row) {   // (past the last row: it again, for nothing)
+    const int64_t at = row < p.rows ? row : p.rows - 1;
+    r.stat = *reinterpret_cast<const float2*>(p.stats + at * 2);
+    r.s.template load<L>(static_cast<const T*>(p.x) + at * p.x_stride, lane, p.width);
+    r.dy.template load<L>(static_cast<const T*>(p.dy) + at * p.width, lane, p.width);
+    if constexpr (SUM) r.ds.template load<L>(static_cast<const T*>(p.ds) + at * p.width, lane, p.width);
+  };
+  int turn = 0;
+  auto one = [&](const Row& r, int64_t row) {
+    const bool there = row < p.rows;   // (ROWS > 1: the lanes of a row that is not there go along with zeros)
+    float u[N][PIECE], g[N][PIECE], sums[2] = {0.f, 0.f};
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      load_piece<T>(u[n], s, n * L + lane, p.width);
-      load_piece<T>(g[n], dy, n * L + lane, p.width);
-    }
-    float sums[2] = {0.f, 0.f};
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-      const int at = (n * L + lane) * PIECE;
-      const bool in = there && at < p.width;
+      const bool in = there && (n * L + lane) * PIECE < p.width;
       float w[PIECE];
 #pragma unroll
       for (int i = 0; i < PIECE; ++i) w[i] = 1.f;
-      if (p.weight && at < p.width) load_values<T, PIECE>(w, static_cast<const T*>(p.weight) + at);
+      if (p.weight) weight.values(w, n);
+      r.s.values(u[n], n);
+      r.dy.values(g[n], n);
 #pragma unroll
       for (int i = 0; i < PIECE; ++i) {
-        u[n][i] = in ? (u[n][i] - stat.x) * stat.y : 0.f;
+        u[n][i] = in ? (u[n][i] - r.stat.x) * r.stat.y : 0.f;
         const float d = in ? g[n][i] : 0.f;
         dw[n][i] += d * u[n][i];
         db[n][i] += d;
@@ -144,23 +170,50 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_bwd_kernel(const
         sums[1] += g[n][i] * u[n][i];
       }
     }
-    sum_row<L, 2>(sums, shared);
+#pragma unroll
+    for (int m = 1; m < (L < 64 ? L : 64); m <<= 1) {
+      sums[0] += __shfl_xor(sums[0], m);
+      sums[1] += __shfl_xor(sums[1], m);
+    }
+    if constexpr (L > 64) {   // (two places in turn: what is written now was read two barriers ago)
+      float* const place = shared[turn];
+      turn ^= 1;
+      if ((threadIdx.x & 63) == 0) {
+        place[threadIdx.x >> 6] = sums[0];
+        place[WAVES + (threadIdx.x >> 6)] = sums[1];
+      }
+      __syncthreads();
+      sums[0] = sums[1] = 0.f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) { sums[0] += place[w]; sums[1] += place[WAVES + w]; }
+    }
     const float mg = sums[0] / p.width, mgu = sums[1] / p.width;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const int at = (n * L + lane) * PIECE;
-      if (!there || at >= p.width) continue;
       float dx[PIECE];
 #pragma unroll
-      for (int i = 0; i < PIECE; ++i) dx[i] = stat.y * (g[n][i] - mg - u[n][i] * mgu);
-      if (p.ds) {
+      for (int i = 0; i < PIECE; ++i) dx[i] = r.stat.y * (g[n][i] - mg - u[n][i] * mgu);
+      if constexpr (SUM) {
         float add[PIECE];
-        load_values<T, PIECE>(add, static_cast<const T*>(p.ds) + row * p.width + at);
+        r.ds.values(add, n);
 #pragma unroll
         for (int i = 0; i < PIECE; ++i) dx[i] += add[i];
       }
-      store_values<T, PIECE>(static_cast<T*>(p.dx) + row * p.width + at, dx);
+      if (there && at < p.width) store_values<T, PIECE>(static_cast<T*>(p.dx) + row * p.width + at, dx);
     }
+  };
+  const int64_t step = (int64_t)gridDim.x * ROWS;
+  Row here, next;
+  int64_t row = (int64_t)blockIdx.x * ROWS + sub;
+  fetch(here, row);
+  for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < p.rows; row0 += 2 * step) {
+    fetch(next, row + step);
+    one(here, row);
+    if (row0 + step >= p.rows) break;
+    fetch(here, row + 2 * step);
+    one(next, row + step);
+    row += 2 * step;
   }
   if (!p.partial) return;
   float* const out = p.partial + (int64_t)blockIdx.x * 2 * p.width;
@@ -242,8 +295,8 @@ hipError_t bwd(const LayerNormArgs& a, hipStream_t s) {
   note_matrix(a.ds, a.rows, a.width, a.width, sizeof(T), false);
   note_matrix(a.dx, a.rows, a.width, a.width, sizeof(T), true);
   note_matrix(a.partial, groups, 2 * a.width, 2 * a.width, 4, true);
-  const hipError_t e = launch_kernel("layer_norm_bwd_kernel", Work{14 * values_of(a), (a.ds ? 4 : 3) * values_of(a) * sizeof(T)}, layer_norm_bwd_kernel<T, L, N>,
-                                     dim3(groups), dim3(THREADS), s, a);
+  const hipError_t e = launch_kernel("layer_norm_bwd_kernel", Work{14 * values_of(a), (a.ds ? 4 : 3) * values_of(a) * sizeof(T)},
+                                     a.ds ? layer_norm_bwd_kernel<T, L, N, true> : layer_norm_bwd_kernel<T, L, N, false>, dim3(groups), dim3(THREADS), s, a);
   if (e != hipSuccess || !a.partial) return e;
   note_matrix(a.partial, groups, 2 * a.width, 2 * a.width, 4, false);
   note_matrix(a.dweight, 1, a.width, a.width, sizeof(T), true);
