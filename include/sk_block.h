@@ -217,7 +217,7 @@ sk_status sk_dense_bwd(const sk_dense_shape* shape, const void* x, const void* w
  * An entry whose id is outside the vocabulary or whose logit is -infinity is not there (lists may be of different lengths); a place that is named twice has
  * both entries.  A row without an entry has no first term, one whose label is outside the vocabulary (or all, with labels NULL) no second.
  *   logits on any boundary of a value, with a row stride of any number of elements, teacher_logits [rows, top] in `dtype`, teacher_ids [rows, top], labels [rows], loss [rows] fp32.
- * stats [rows, 4] fp32 for a backward pass, or NULL.  (A row whose logits are all -infinity has no softmax: NaN.)
+ * stats [rows, 8] fp32 for a backward pass, or NULL.  (A row whose logits are all -infinity has no softmax: NaN.)
  *   rows and vocabulary up to 2^24 (rows below it), top up to 2^16 (0: no teacher; its pointers may be NULL), temperature from 10^-3 to 10^3.
  */
 typedef struct {

@@ -611,7 +611,7 @@ class DistillationFunction(torch.autograd.Function):
         if z.stride(1) != 1 or z.stride(0) > 1 << 40:
             z = z.contiguous()
         loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
-        stats = torch.empty((z.shape[0], 4), dtype=torch.float32, device=logits.device) if training else None
+        stats = torch.empty((z.shape[0], 8), dtype=torch.float32, device=logits.device) if training else None
         if z.shape[0] > 0:
             shape = _distill_shape(z, teacher_ids, labels, temperature, label_weight)
             with _on(logits.device):

@@ -112,11 +112,14 @@ constexpr int LAYER_NORM_MAX_WIDTH = 1 << 15;   // a row on one work-group's reg
 hipError_t launch_layer_norm_fwd(const LayerNormArgs& a, bool f32, hipStream_t s);
 hipError_t launch_layer_norm_bwd(const LayerNormArgs& a, bool f32, hipStream_t s);
 
+constexpr int DISTILL_STATS = 8;
 struct DistillArgs {
   const void *logits, *teacher;               // rows logits_stride elements apart, [rows][top] dense
   const void *ids, *labels;                   // labels or null
   float* loss;                                // forward
-  float* stats;                               // [rows][4]: the largest logit, 1 / sum exp((z - it) / temperature), 1 / sum exp(z - it), 0; forward written unless null, backward read
+  // [rows][DISTILL_STATS], forward written unless null, backward read: the largest logit, 1 / sum exp((z - it) / temperature), 1 / sum exp(z - it); the teacher's
+  // largest, 1 / sum exp((t - it) / temperature) or 0 where there is no entry
+  float* stats;
   const float* dloss;                         // backward
   void* dlogits;                              // backward: dense
   int64_t rows, logits_stride;

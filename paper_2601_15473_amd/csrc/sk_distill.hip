@@ -16,29 +16,27 @@ namespace sk {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int LISTS = 256;   // entries that a work-group has in LDS at once
 
 __device__ __forceinline__ int64_t index_of(const void* p, int wide, int64_t at) {
   return wide ? static_cast<const int64_t*>(p)[at] : (int64_t)static_cast<const int32_t*>(p)[at];
 }
 
-// A row's 16-byte pieces: piece i has the row's values i E - lead .. + E - 1.
+// A row as its values before the first 16-byte boundary, its whole pieces, and its values behind the last.
 template <typename T>
 struct RowPieces {
   static constexpr int E = 16 / sizeof(T);
-  const T* row;
-  int lead, n, pieces;
-  __device__ __forceinline__ RowPieces(const T* r, int width) : row(r), lead((int)((reinterpret_cast<uintptr_t>(r) & 15) / sizeof(T))), n(width), pieces((lead + width + E - 1) / E) {}
-  __device__ __forceinline__ bool whole(int i) const { return i * E >= lead && i * E - lead + E <= n; }
-  // values outside the row: `outside`
-  __device__ __forceinline__ void load(float (&v)[E], int i, float outside) const {
-    const int at = i * E - lead;
-    if (i < pieces && whole(i)) {
-      load_values<T, E>(v, row + at);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = i < pieces && at + e >= 0 && at + e < n ? load_one(row + at + e) : outside;
-    }
+  int before, pieces, behind, body;   // body: values up to the last whole piece
+  __device__ __forceinline__ RowPieces(const T* row, int width) {
+    const int off = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+    before = off == 0 ? 0 : E - off;
+    if (before > width) before = width;
+    pieces = (width - before) / E;
+    body = before + pieces * E;
+    behind = width - body;
+  }
+  // The place of the lone value that falls to a thread (there are less than 2 E of them), or -1
+  __device__ __forceinline__ int lone(int thread) const {
+    return thread < before ? thread : thread >= E && thread < E + behind ? body + thread - E : -1;
   }
 };
 
@@ -65,36 +63,6 @@ __device__ __forceinline__ void join(Sums& s, Sums o, float c) {
   if (HARD) s.hard += o.hard;
 }
 
-// The sum (of 64 bits) of a work-group's threads, in all of them.
-template <int THREADS>
-__device__ __forceinline__ double sum_threads(double v, double* shared) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m);
-  if constexpr (THREADS > 64) {
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0.0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) v += shared[w];
-  }
-  return v;
-}
-template <int THREADS>
-__device__ __forceinline__ float max_threads(float v, double* shared) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) v = fmaxf(v, __shfl_xor(v, m));
-  if constexpr (THREADS > 64) {
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) v = fmaxf(v, (float)shared[w]);
-  }
-  return v;
-}
-
 // An entry of the teacher's list: where it stands, and how large it is.  One outside the vocabulary or of -infinity is not there.
 struct Entry {
   int id;
@@ -111,53 +79,82 @@ __device__ __forceinline__ Entry entry_of(const DistillArgs& p, int64_t row, int
   if (e.there) e.id = (int)id;
   return e;
 }
-// The largest of a row's entries, and the sum of their exponentials below it (0: there is none)
-template <typename T, int THREADS>
-__device__ __forceinline__ float teacher_sum(const DistillArgs& p, int64_t row, float c, float& high, double* shared) {
-  high = -INFINITY;
-  for (int k = threadIdx.x; k < p.top; k += THREADS) {
-    const Entry e = entry_of<T>(p, row, k);
-    if (e.there) high = fmaxf(high, e.t);   // (a NaN is no largest, and comes out in the sum)
-  }
-  high = max_threads<THREADS>(high, shared);
-  double sum = 0.0;
-  for (int k = threadIdx.x; k < p.top; k += THREADS) {
-    const Entry e = entry_of<T>(p, row, k);
-    if (e.there) sum += below(e.t, high, c);
-  }
-  return (float)sum_threads<THREADS>(sum, shared);
-}
-
-// THREADS to a row
+// THREADS to a row.  A thread's first entry of the teacher's list, the student's logit there and the label's are asked for ahead of the row, and what is
+// left to do behind it is two sums over the work-group: every row has that tail, and it is as long as 16000 values take.
 template <typename T, int THREADS, bool HARD>
 __global__ __launch_bounds__(THREADS) void distill_fwd_kernel(const DistillArgs p) {
-  constexpr int E = RowPieces<T>::E, AHEAD = 4;
-  __shared__ double shared[THREADS / 64];
-  __shared__ Sums waves[THREADS / 64];
+  constexpr int E = RowPieces<T>::E, AHEAD = 2, WAVES = THREADS / 64;
+  __shared__ Sums waves[WAVES];
+  __shared__ float highs[WAVES];
+  __shared__ double parts[2][WAVES];
   const int64_t row = blockIdx.x;
   const T* const z = static_cast<const T*>(p.logits) + row * p.logits_stride;
   const RowPieces<T> pieces(z, p.vocabulary);
-  const float c = LOG2E / p.temperature;
+  const float tau = p.temperature, weight = p.label_weight, c = LOG2E / tau;
+  const bool teaches = weight != 1.f;
+  // groups of pieces THREADS apart, the next one's loads under this one's exponentials
+  const uint4* const body = reinterpret_cast<const uint4*>(z + pieces.before);
+  uint4 here[AHEAD], next[AHEAD];
+  auto fetch = [&](uint4 (&raw)[AHEAD], int i) {   // (past the row: its last piece, for nothing)
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) raw[a] = body[i + a * THREADS < pieces.pieces ? i + a * THREADS : pieces.pieces - 1];
+  };
+  int64_t label = p.labels && weight != 0.f ? index_of(p.labels, p.labels64, row) : -1;
+  const Entry mine = entry_of<T>(p, row, teaches ? (int)threadIdx.x : p.top);
+  if (pieces.pieces > 0) fetch(here, threadIdx.x);
+  if (label >= p.vocabulary) label = -1;
+  const float at_label = label >= 0 ? load_one(z + label) : 0.f, at_mine = mine.there ? load_one(z + mine.id) : 0.f;
+
   Sums s{-INFINITY, 0.f, 0.f};
-  for (int i = threadIdx.x; i < pieces.pieces; i += AHEAD * THREADS) {
-    float v[AHEAD][E];
+  auto take = [&](auto n_c, const uint4* raw) {   // n pieces
+    constexpr int A = decltype(n_c)::value;
+    float v[A][E], top = s.top;
 #pragma unroll
-    for (int a = 0; a < AHEAD; ++a) pieces.load(v[a], i + a * THREADS, -INFINITY);
-    float top = s.top;
+    for (int a = 0; a < A; ++a) load_values<T, E>(v[a], reinterpret_cast<const T*>(raw + a));
 #pragma unroll
-    for (int a = 0; a < AHEAD; ++a)
+    for (int a = 0; a < A; ++a)
 #pragma unroll
       for (int e = 0; e < E; ++e) top = fmaxf(top, v[a][e]);
     raise<HARD>(s, top, c);
     const float from = top == -INFINITY ? 0.f : top;   // (nothing but -infinities: their exponentials are zeros)
 #pragma unroll
-    for (int a = 0; a < AHEAD; ++a)
+    for (int a = 0; a < A; ++a)
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         s.soft += below(v[a][e], from, c);
         if (HARD) s.hard += below(v[a][e], from, LOG2E);
       }
+  };
+  int i = threadIdx.x;
+  if (pieces.pieces > 0) {
+    constexpr int GROUP = AHEAD * THREADS, LAST = (AHEAD - 1) * THREADS;
+    while (i + GROUP + LAST < pieces.pieces) {   // two whole groups
+      fetch(next, i + GROUP);
+      take(IntC<AHEAD>{}, here);
+      fetch(here, i + 2 * GROUP);
+      take(IntC<AHEAD>{}, next);
+      i += 2 * GROUP;
+    }
+    if (i + LAST < pieces.pieces) {
+      take(IntC<AHEAD>{}, here);
+      i += GROUP;
+    }
+    for (; i < pieces.pieces; i += THREADS) {
+      const uint4 one = body[i];
+      take(IntC<1>{}, &one);
+    }
   }
+  if (const int at = pieces.lone(threadIdx.x); at >= 0) {
+    const float v = load_one(z + at);
+    join<HARD>(s, Sums{v, v == -INFINITY ? 0.f : below(v, v, c), v == -INFINITY ? 0.f : below(v, v, c)}, c);   // (1, or NaN of a NaN or an infinity)
+  }
+  // the teacher's largest entry (a NaN is no largest, and comes out in the sum), with the row's sums
+  float high = mine.there ? fmaxf(mine.t, -INFINITY) : -INFINITY;
+  if (teaches)
+    for (int k = threadIdx.x + THREADS; k < p.top; k += THREADS) {
+      const Entry e = entry_of<T>(p, row, k);
+      if (e.there) high = fmaxf(high, e.t);
+    }
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) {
     Sums o;
@@ -165,126 +162,250 @@ __global__ __launch_bounds__(THREADS) void distill_fwd_kernel(const DistillArgs 
     o.soft = __shfl_xor(s.soft, m);
     o.hard = HARD ? __shfl_xor(s.hard, m) : 0.f;
     join<HARD>(s, o, c);
+    high = fmaxf(high, __shfl_xor(high, m));
   }
-  if constexpr (THREADS > 64) {
-    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = s;
+  if constexpr (WAVES > 1) {
+    if ((threadIdx.x & 63) == 0) {
+      waves[threadIdx.x >> 6] = s;
+      highs[threadIdx.x >> 6] = high;
+    }
     __syncthreads();
     s = waves[0];
+    high = highs[0];
 #pragma unroll
-    for (int w = 1; w < THREADS / 64; ++w) join<HARD>(s, waves[w], c);
-  }
-  const float tau = p.temperature, weight = p.label_weight;
-  // the teacher's part: log p - log q is a difference of numbers much larger than it, in 64 bits
-  float high;
-  const float total = teacher_sum<T, THREADS>(p, row, c, high, shared);
-  double loss = 0.0;
-  const bool some = total != 0.f;   // (NaN: there is something)
-  if (some && weight != 1.f) {
-    const double logs = log((double)s.soft) - log((double)total);
-    for (int k = threadIdx.x; k < p.top; k += THREADS) {
-      const Entry e = entry_of<T>(p, row, k);
-      if (!e.there) continue;
-      const float share = below(e.t, high, c) / total;
-      if (share == 0.f) continue;     // (what it would be the logarithm of may be anything)
-      loss += (double)share * ((((double)e.t - (double)high) - ((double)load_one(z + e.id) - (double)s.top)) / (double)tau + logs);
+    for (int w = 1; w < WAVES; ++w) {
+      join<HARD>(s, waves[w], c);
+      high = fmaxf(high, highs[w]);
     }
-    loss = sum_threads<THREADS>(loss, shared) * ((1.0 - (double)weight) * (double)tau * (double)tau);
+  }
+  // With e_k = exp((t_k - high) / tau): the sum of e_k, and that of e_k (t_k - high - (z_k - top)) / tau.  log p - log q is a difference of numbers much
+  // larger than it: in 64 bits.
+  double total = 0.0, apart = 0.0;
+  auto add = [&](float t, float at) {
+    const float e = below(t, high, c);
+    total += (double)e;
+    if (e != 0.f) apart += (double)e * ((((double)t - (double)high) - ((double)at - (double)s.top)) / (double)tau);   // (what does not weigh may be anywhere)
+  };
+  if (mine.there) add(mine.t, at_mine);
+  if (teaches)
+    for (int k = threadIdx.x + THREADS; k < p.top; k += THREADS) {
+      const Entry e = entry_of<T>(p, row, k);
+      if (e.there) add(e.t, load_one(z + e.id));
+    }
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    total += __shfl_xor(total, m);
+    apart += __shfl_xor(apart, m);
+  }
+  if constexpr (WAVES > 1) {
+    if ((threadIdx.x & 63) == 0) {
+      parts[0][threadIdx.x >> 6] = total;
+      parts[1][threadIdx.x >> 6] = apart;
+    }
+    __syncthreads();
+    total = apart = 0.0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) { total += parts[0][w]; apart += parts[1][w]; }
   }
   if (threadIdx.x != 0) return;
-  if (p.labels && weight != 0.f) {
-    const int64_t label = index_of(p.labels, p.labels64, row);
-    if (label >= 0 && label < p.vocabulary)
-      loss += (double)weight * (log((double)(HARD ? s.hard : s.soft)) + ((double)s.top - (double)load_one(z + label)));
-  }
+  double loss = 0.0;
+  if (total != 0.0)   // (NaN: there is something)
+    loss = (apart / total + log((double)s.soft) - log(total)) * ((1.0 - (double)weight) * (double)tau * (double)tau);
+  if (label >= 0) loss += (double)weight * (log((double)(HARD ? s.hard : s.soft)) + ((double)s.top - (double)at_label));
   p.loss[row] = (float)loss;
-  if (p.stats) *reinterpret_cast<float4*>(p.stats + row * 4) = make_float4(s.top, 1.f / s.soft, 1.f / (HARD ? s.hard : s.soft), 0.f);
+  if (p.stats) {
+    float4* const stats = reinterpret_cast<float4*>(p.stats + row * DISTILL_STATS);
+    stats[0] = make_float4(s.top, 1.f / s.soft, 1.f / (HARD ? s.hard : s.soft), high);
+    stats[1] = make_float4(total != 0.0 ? (float)(1.0 / total) : 0.f, 0.f, 0.f, 0.f);
+  }
 }
 
-// The row of dz by its pieces first, then the values at the teacher's entries and at the label once more with what they have subtracted: by one thread each,
-// the first of those with the same place, behind a wait for the work-group's stores.
+// What the entries and the label subtract, by place, for the thread that writes the place: lists in LDS, chained by thread.
+struct alignas(16) Places {
+  static constexpr int MOST = 256;
+  int id[MOST], next[MOST];
+  float less[MOST];
+};
+
+// dz by pieces; what is subtracted at a place is by the thread that has its piece, before it goes.  (As a pass over the entries behind the row, whose lines had left
+// the L2, 128 of them cost 8192 rows of 65536 90 us of 484.)  Lists that do not fit LDS are taken that way, a stretch at a time, behind a wait for the
+// work-group's stores.
 template <typename T, int THREADS, bool HARD>
 __global__ __launch_bounds__(THREADS) void distill_bwd_kernel(const DistillArgs p) {
-  constexpr int E = RowPieces<T>::E, AHEAD = 4;
-  __shared__ double shared[THREADS / 64];
-  __shared__ int ids[LISTS];
-  __shared__ float less[LISTS];
+  constexpr int E = RowPieces<T>::E, AHEAD = 2, NONE = 0x7fffffff;
+  __shared__ Places places;
+  __shared__ int heads[THREADS];
   const int64_t row = blockIdx.x;
   const T* const z = static_cast<const T*>(p.logits) + row * p.logits_stride;
   T* const out = static_cast<T*>(p.dlogits) + row * p.vocabulary;
   const RowPieces<T> pieces(z, p.vocabulary);
   const bool together = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;   // (pieces of both are the same)
   const float tau = p.temperature, c = LOG2E / tau;
-  const float4 stat = *reinterpret_cast<const float4*>(p.stats + row * 4);
-  const float top = stat.x, g = p.dloss[row];
-  float high;
-  const float total = teacher_sum<T, THREADS>(p, row, c, high, shared);
-  int64_t label = -1;
+  // what does not wait for anything, on its way at once: the first pieces, and the thread's first entry
+  const uint4* const body = reinterpret_cast<const uint4*>(z + pieces.before);
+  uint4 here[AHEAD], next[AHEAD];
+  auto fetch = [&](uint4 (&raw)[AHEAD], int i) {   // (past the row: its last piece, for nothing)
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) raw[a] = body[i + a * THREADS < pieces.pieces ? i + a * THREADS : pieces.pieces - 1];
+  };
+  const Entry mine = entry_of<T>(p, row, threadIdx.x);
+  if (pieces.pieces > 0) fetch(here, threadIdx.x);
+  const float4 stat = reinterpret_cast<const float4*>(p.stats + row * DISTILL_STATS)[0];
+  const float top = stat.x, high = stat.w, rest = p.stats[row * DISTILL_STATS + 4], g = p.dloss[row];   // rest: 1 / the sum of the teacher's exponentials, 0 where there is none
+  int label = -1;
   if (p.labels && p.label_weight != 0.f) {
-    label = index_of(p.labels, p.labels64, row);
-    if (label < 0 || label >= p.vocabulary) label = -1;
+    const int64_t at = index_of(p.labels, p.labels64, row);
+    if (at >= 0 && at < p.vocabulary) label = (int)at;
   }
-  const bool teaches = total != 0.f && p.label_weight != 1.f, counts = teaches || label >= 0;
+  const bool teaches = rest != 0.f, counts = teaches || label >= 0;
   const float share = teaches ? g * (1.f - p.label_weight) * tau : 0.f;   // of the entries
   const float right = label >= 0 ? g * p.label_weight : 0.f;              // of the label
   // what q and softmax(z) are multiplied by, over their sums
   const float soft = HARD ? share * stat.y : (share + right) * stat.y, hard = HARD ? right * stat.z : 0.f;
   auto dense = [&](float v) { return soft * below(v, top, c) + (HARD ? hard * below(v, top, LOG2E) : 0.f); };
-  for (int i = threadIdx.x; i < pieces.pieces; i += AHEAD * THREADS) {
-    float v[AHEAD][E];
+
+  // The list: the teacher's entries, the label behind them.
+  const int n = teaches ? p.top : 0;
+  const float each = teaches ? share * rest : 0.f;
+  const bool chained = n + 1 <= Places::MOST;
+  auto stretch = [&](int j0) {   // entries j0 .. of the list into LDS
+    __syncthreads();
+    for (int j = threadIdx.x; j < Places::MOST; j += THREADS) {
+      int id = -1;
+      float w = 0.f;
+      if (j0 + j < n) {
+        const Entry e = j0 + j == (int)threadIdx.x ? mine : entry_of<T>(p, row, j0 + j);
+        id = e.id;
+        if (e.there) w = below(e.t, high, c) * each;
+      } else if (j0 + j == n) {
+        id = label;
+        w = right;
+      }
+      places.id[j] = id;
+      places.less[j] = w;
+    }
+    __syncthreads();
+  };
+  // What is subtracted at entry k's place by the stretch in LDS; whether no entry before k has it
+  auto gather = [&](int j0, int k, int id, float& sum, bool& first) {
+    const int m = n + 1 - j0 < Places::MOST ? n + 1 - j0 : Places::MOST;
+    for (int j = 0; j < m; j += 4) {   // (ids of -1 behind the last)
+      const int4 four = *reinterpret_cast<const int4*>(places.id + j);
+      if (four.x != id && four.y != id && four.z != id && four.w != id) continue;
+      const int all[4] = {four.x, four.y, four.z, four.w};
 #pragma unroll
-    for (int a = 0; a < AHEAD; ++a) pieces.load(v[a], i + a * THREADS, 0.f);
-#pragma unroll
-    for (int a = 0; a < AHEAD; ++a) {
-      const int piece = i + a * THREADS, at = piece * E - pieces.lead;
-      if (piece >= pieces.pieces) break;
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[a][e] = counts ? dense(v[a][e]) : 0.f;
-      if (together && pieces.whole(piece)) {
-        store_values<T, E>(out + at, v[a]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (at + e >= 0 && at + e < p.vocabulary) store_one(out + at + e, v[a][e]);
+      for (int e = 0; e < 4; ++e) {
+        if (all[e] != id) continue;
+        sum += places.less[j + e];
+        if (j0 + j + e < k) first = false;
       }
     }
+  };
+  // The piece that a place is in (the lone values: one behind the last), and the thread that writes it
+  auto piece_of = [&](int id) { return id < pieces.before || id >= pieces.body ? pieces.pieces : (id - pieces.before) / E; };
+  auto writer_of = [&](int id) { return id < pieces.before ? id : id >= pieces.body ? E + id - pieces.body : (id - pieces.before) / E % THREADS; };
+  int pending = NONE;
+  auto look = [&](int from) {   // the thread's next piece from `from` on
+    pending = NONE;
+    for (int k = heads[threadIdx.x]; k >= 0; k = places.next[k]) {
+      const int at = piece_of(places.id[k]);
+      if (at >= from && at < pending) pending = at;
+    }
+  };
+  if (chained && counts) {
+    heads[threadIdx.x] = -1;
+    stretch(0);
+    float sum[(Places::MOST + THREADS - 1) / THREADS];
+    bool first[(Places::MOST + THREADS - 1) / THREADS];
+#pragma unroll
+    for (int q = 0; q < (Places::MOST + THREADS - 1) / THREADS; ++q) {
+      const int k = q * THREADS + (int)threadIdx.x;
+      sum[q] = 0.f;
+      first[q] = k <= n && places.id[k] >= 0;
+      if (q * THREADS <= n) gather(0, k, first[q] ? places.id[k] : -2, sum[q], first[q]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < (Places::MOST + THREADS - 1) / THREADS; ++q) {
+      const int k = q * THREADS + (int)threadIdx.x;
+      if (!first[q]) continue;
+      places.less[k] = sum[q];
+      places.next[k] = atomicExch(&heads[writer_of(places.id[k])], k);
+    }
+    __syncthreads();
+    look(0);
   }
-  if (!counts) return;
+  auto give = [&](auto n_c, const uint4* raw, int i) {   // n pieces from i on
+    constexpr int A = decltype(n_c)::value;
+    float v[A][E];
+#pragma unroll
+    for (int a = 0; a < A; ++a) load_values<T, E>(v[a], reinterpret_cast<const T*>(raw + a));
+#pragma unroll
+    for (int a = 0; a < A; ++a)
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[a][e] = counts ? dense(v[a][e]) : 0.f;
+    if (pending <= i + (A - 1) * THREADS) {
+      for (int k = heads[threadIdx.x]; k >= 0; k = places.next[k]) {
+        const int id = places.id[k], at = piece_of(id) - i;      // (a multiple of THREADS)
+        if (at < 0 || at > (A - 1) * THREADS) continue;
+        const int place = at / THREADS * E + (id - pieces.before) % E;
+        const float w = places.less[k];
+#pragma unroll
+        for (int a = 0; a < A; ++a)
+#pragma unroll
+          for (int e = 0; e < E; ++e) v[a][e] -= place == a * E + e ? w : 0.f;
+      }
+      look(i + (A - 1) * THREADS + 1);
+    }
+#pragma unroll
+    for (int a = 0; a < A; ++a) {
+      T* const to = out + pieces.before + (i + a * THREADS) * E;
+      if (together) {
+        store_values<T, E>(to, v[a]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) store_one(to + e, v[a][e]);
+      }
+    }
+  };
+  int i = threadIdx.x;
+  if (pieces.pieces > 0) {
+    constexpr int GROUP = AHEAD * THREADS, LAST = (AHEAD - 1) * THREADS;
+    while (i + GROUP + LAST < pieces.pieces) {   // two whole groups
+      fetch(next, i + GROUP);
+      give(IntC<AHEAD>{}, here, i);
+      fetch(here, i + 2 * GROUP);
+      give(IntC<AHEAD>{}, next, i + GROUP);
+      i += 2 * GROUP;
+    }
+    if (i + LAST < pieces.pieces) {
+      give(IntC<AHEAD>{}, here, i);
+      i += GROUP;
+    }
+    for (; i < pieces.pieces; i += THREADS) {
+      const uint4 one = body[i];
+      give(IntC<1>{}, &one, i);
+    }
+  }
+  if (const int at = pieces.lone(threadIdx.x); at >= 0) {
+    float v = counts ? dense(load_one(z + at)) : 0.f;
+    if (pending != NONE)
+      for (int k = heads[threadIdx.x]; k >= 0; k = places.next[k])
+        if (places.id[k] == at) v -= places.less[k];
+    store_one(out + at, v);
+  }
+  if (chained || !counts) return;
   // (a piece's store and a place's of another wave: the first has to have arrived)
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  const int n = teaches ? p.top : 0;
-  const float each = teaches ? share / total : 0.f;
-  // the list's entries, the label behind them, against all of them a stretch at a time
   for (int k0 = 0; k0 <= n; k0 += THREADS) {
     const int k = k0 + (int)threadIdx.x;
-    int id = -1;
-    if (k < n) id = entry_of<T>(p, row, k).id;
-    else if (k == n) id = (int)label;
+    const int id = k < n ? entry_of<T>(p, row, k).id : k == n ? label : -1;
     float sum = 0.f;
     bool first = id >= 0;
-    for (int j0 = 0; j0 <= n; j0 += LISTS) {
-      __syncthreads();
-      for (int j = threadIdx.x; j < LISTS; j += THREADS) {
-        int other = -1;
-        float w = 0.f;
-        if (j0 + j < n) {
-          const Entry e = entry_of<T>(p, row, j0 + j);
-          other = e.id;
-          if (e.there) w = below(e.t, high, c) * each;
-        } else if (j0 + j == n) {
-          other = (int)label;
-          w = right;
-        }
-        ids[j] = other;
-        less[j] = w;
-      }
-      __syncthreads();
-      const int m = n + 1 - j0 < LISTS ? n + 1 - j0 : LISTS;
-      for (int j = 0; j < m; ++j) {
-        const bool same = ids[j] == id;
-        sum += same ? less[j] : 0.f;
-        if (same && j0 + j < k) first = false;
-      }
+    for (int j0 = 0; j0 <= n; j0 += Places::MOST) {
+      stretch(j0);
+      gather(j0, k, first ? id : -2, sum, first);
     }
     if (first) store_one(out + id, dense(load_one(z + id)) - sum);
   }
@@ -297,7 +418,7 @@ void note_io(const DistillArgs& a, int esize, bool back) {
   note_matrix(a.teacher, a.rows, a.top, a.top, esize, false);
   note_matrix(a.ids, a.rows, a.top, a.top, a.ids64 ? 8 : 4, false);
   note_matrix(a.labels, 1, a.rows, a.rows, a.labels64 ? 8 : 4, false);
-  note_matrix(a.stats, a.rows, 4, 4, 4, !back);
+  note_matrix(a.stats, a.rows, DISTILL_STATS, DISTILL_STATS, 4, !back);
   if (back) {
     note_matrix(a.dloss, 1, a.rows, a.rows, 4, false);
     note_matrix(a.dlogits, a.rows, a.vocabulary, a.vocabulary, esize, true);
@@ -315,22 +436,25 @@ hipError_t go(const DistillArgs& a, hipStream_t s) {
     return launch_kernel("distill_fwd_kernel", Work{4 * values_of(a), values_of(a) * sizeof(T)}, distill_fwd_kernel<T, THREADS, HARD>, dim3((unsigned)a.rows), dim3(THREADS), s, a);
 }
 
+// Threads to a row.  Short rows are the price of what each has behind (forward) or ahead of (back) its values, and many small work-groups hide it better;
+// long ones want few rows at a time.  Bf16, us, 64 : 256 : 512 threads: forward 16384 rows of 1000 25 : 51 : 102, 3000 of 9000 16 : 20 : 27, 4001 of 32001 80 : 83 : 82,
+// 8192 of 65536 232 : 227 : 220; back 16384 of 200 20 : 27 : 53, 16384 of 1000 80 : 67 : 121, 4001 of 32001 114 : 96 : 96, 8192 of 65536 466 : 413 : 398.
+// Few rows (less than two waves a SIMD at 64 threads): 256, forward 100 of 32000 13 : 8 : 8.
 template <typename T, bool HARD, bool BACK>
 hipError_t by_size(const DistillArgs& a, hipStream_t s) {
-  if (a.vocabulary <= 2048) return go<T, 64, HARD, BACK>(a, s);
-  return go<T, 256, HARD, BACK>(a, s);
+  if (a.vocabulary <= (BACK ? 512 : 12288) && (a.rows >= 8 * NUM_CUS || a.vocabulary <= 512)) return go<T, 64, HARD, BACK>(a, s);
+  if (a.vocabulary <= 49152) return go<T, 256, HARD, BACK>(a, s);
+  return go<T, 512, HARD, BACK>(a, s);
 }
-template <bool BACK>
-hipError_t by_type(const DistillArgs& a, bool f32, hipStream_t s) {
+template <typename T, bool BACK>
+hipError_t by_sums(const DistillArgs& a, hipStream_t s) {
   // (one sum serves both parts where the temperature is 1, or where one of them is not there)
-  const bool hard = a.labels && a.label_weight != 0.f && a.temperature != 1.f;
-  if (f32) return hard ? by_size<float, true, BACK>(a, s) : by_size<float, false, BACK>(a, s);
-  return hard ? by_size<bf16, true, BACK>(a, s) : by_size<bf16, false, BACK>(a, s);
+  return a.labels && a.label_weight != 0.f && a.temperature != 1.f ? by_size<T, true, BACK>(a, s) : by_size<T, false, BACK>(a, s);
 }
 
 }  // namespace
 
-hipError_t launch_distill_fwd(const DistillArgs& a, bool f32, hipStream_t s) { return by_type<false>(a, f32, s); }
-hipError_t launch_distill_bwd(const DistillArgs& a, bool f32, hipStream_t s) { return by_type<true>(a, f32, s); }
+hipError_t launch_distill_fwd(const DistillArgs& a, bool f32, hipStream_t s) { return f32 ? by_sums<float, false>(a, s) : by_sums<bf16, false>(a, s); }
+hipError_t launch_distill_bwd(const DistillArgs& a, bool f32, hipStream_t s) { return f32 ? by_sums<float, true>(a, s) : by_sums<bf16, true>(a, s); }
 
 }  // namespace sk

@@ -179,7 +179,7 @@ Tensor distill_forward(const Tensor& z, const Tensor& t, const Tensor& ids, cons
   const c10::DeviceGuard guard(z.device());
   const at::TensorOptions f32 = z.options().dtype(at::kFloat);
   Tensor loss = at::empty(z.sizes().slice(0, z.dim() - 1), f32);
-  if (stats) *stats = at::empty({s.rows, 4}, f32);
+  if (stats) *stats = at::empty({s.rows, 8}, f32);
   check(sk_distill_fwd(&s, z.data_ptr(), data(t), data(ids), data(labels), loss.data_ptr<float>(), stats ? stats->data_ptr<float>() : nullptr, stream_of(z.device())));
   return loss;
 }

@@ -192,7 +192,7 @@ def test_distill_accesses(rows, vocabulary, top, dtype, e):
         z = buf.new(((rows - 1) * (vocabulary + 3) + vocabulary) * e)
         t, ids = (buf.new(rows * top * e), buf.new(rows * top * 4)) if top else (None, None)
         y = buf.new(rows * 8) if labels else None
-        loss, stats = buf.new(rows * 4, write=True), buf.new(rows * 16, both=True)
+        loss, stats = buf.new(rows * 4, write=True), buf.new(rows * 32, both=True)
         buf.check(traced(lambda: sk.sk_distill_fwd(s, z, t, ids, y, loss, stats))[0])
         dz = buf.new(rows * vocabulary * e, write=True)
         buf.check(traced(lambda: sk.sk_distill_bwd(s, z, t, ids, y, stats, buf.new(rows * 4), dz))[0])
