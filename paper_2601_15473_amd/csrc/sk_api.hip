@@ -885,7 +885,10 @@ hipError_t launch_product(GemmKind kind, GemmArgs a, bool f32, void* slabs, hipS
 DensePlan plan_dense(int64_t M, int64_t N, int64_t K, bool f32) {
   DensePlan d{};
   if (f32) {
-    d.splits = plan_f32_first(M, N, K).splits;
+    const F32Plan f = plan_f32_first(M, N, K);
+    d.splits = f.splits;
+    d.fused = f.splits == 1;
+    d.tile = f.tile;
     return d;
   }
   const FirstPlan f = plan_first(GEMM_NT, M, N, K);

@@ -395,7 +395,7 @@ sk_status sk_dense_fwd(const sk_dense_shape* shape, const void* x, const void* w
     g.splits = 1;
     g.k_per_split = (g.K + 63) / 64 * 64;
     const FinishArgs f = {residual, a.activation != SK_ACT_NONE ? z : nullptr, a.residual_stride};
-    e = d.few ? launch_dense_few_rows(a.activation, g, f, s) : launch_dense_bf16(d.tile, a.activation, g, f, s);
+    e = f32 ? launch_dense_f32(d.tile, a.activation, g, f, s) : d.few ? launch_dense_few_rows(a.activation, g, f, s) : launch_dense_bf16(d.tile, a.activation, g, f, s);
   } else {
     a.x = x; a.weight = weight; a.bias = bias; a.residual = residual; a.y = y; a.z = z;
     a.slabs = static_cast<const float*>(workspace);

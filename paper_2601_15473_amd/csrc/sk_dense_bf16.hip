@@ -13,14 +13,14 @@ __global__ __launch_bounds__(256) void dense_bf16_kernel(const GemmArgs p, const
   G::run(p, blockIdx.x, smem, f);
 }
 
-void note_dense(const GemmArgs& a, const FinishArgs& f) {
-  note_gemm(a, true, true, 2, 2, false);
-  if (f.residual) note_matrix(f.residual, a.M, a.N, f.residual_ld, 2, false);
-  note_matrix(f.z, a.M, a.N, a.ldc, 2, true);
+void note_dense(const GemmArgs& a, const FinishArgs& f, int esize) {
+  note_gemm(a, true, true, esize, esize, false);
+  if (f.residual) note_matrix(f.residual, a.M, a.N, f.residual_ld, esize, false);
+  note_matrix(f.z, a.M, a.N, a.ldc, esize, true);
 }
-Work dense_work(const GemmArgs& a, const FinishArgs& f) {
-  Work w = gemm_work(a, 2, 2, false);
-  w.bytes += 2.0 * a.M * a.N * ((f.residual != nullptr) + (f.z != nullptr));
+Work dense_work(const GemmArgs& a, const FinishArgs& f, int esize) {
+  Work w = gemm_work(a, esize, esize, false);
+  w.bytes += (double)esize * a.M * a.N * ((f.residual != nullptr) + (f.z != nullptr));
   return w;
 }
 

@@ -22,7 +22,7 @@
 // read of a k-contiguous operand; an operand contiguous along m (n) with two blocks per wave
 // gives block i the rows 2 r + i, which makes its read one 8-byte read for both blocks.
 #include "sk_bf16_tile.h"
-#include "sk_launch.h"
+#include "sk_dense_launch.h"
 
 namespace sk {
 
@@ -85,16 +85,17 @@ struct F32Chunk {
 
 // The work of one work-group, index `block` of the product's own; a device function so that one launch
 // can carry the work-groups of two products.
-template <int T, bool A_KC, bool B_KC, bool COLSUM>
+// ACT: 0 and more for a dense layer's result, act(C) + residual, in place of the product's.
+template <int T, bool A_KC, bool B_KC, bool COLSUM, int ACT = -1>
 struct F32Tile {
   typedef F32Chunk<T, A_KC> CA;
   typedef F32Chunk<T, B_KC> CB;
   static constexpr int STAGE = CA::ELEMS + CB::ELEMS;
-  static __device__ __forceinline__ void run(const GemmArgs& p, int block, float* lds);
+  static __device__ __forceinline__ void run(const GemmArgs& p, int block, float* lds, const FinishArgs& f = FinishArgs{});
 };
 
-template <int T, bool A_KC, bool B_KC, bool COLSUM>
-__device__ __forceinline__ void F32Tile<T, A_KC, B_KC, COLSUM>::run(const GemmArgs& p, const int block, float* const lds) {
+template <int T, bool A_KC, bool B_KC, bool COLSUM, int ACT>
+__device__ __forceinline__ void F32Tile<T, A_KC, B_KC, COLSUM, ACT>::run(const GemmArgs& p, const int block, float* const lds, const FinishArgs& f) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave >> 1, wn = wave & 1;
   const int tiles = p.tiles_m * p.tiles_n;
@@ -206,6 +207,30 @@ __device__ __forceinline__ void F32Tile<T, A_KC, B_KC, COLSUM>::run(const GemmAr
   int gn[T];
 #pragma unroll
   for (int n = 0; n < T; ++n) gn[n] = n0 + wn * 32 * T + CB::place(n, lane & 31);
+  if constexpr (ACT >= 0) {
+    // a block's residual before its results: loads that the stores between would hold up
+    const GWindow zw = make_window(f.z, (int64_t)m0 * p.ldc, f.z != nullptr ? (int64_t)p.M * p.ldc : 0, 4);
+    const GWindow rw = make_window(f.residual, (int64_t)m0 * f.residual_ld, f.residual != nullptr ? (int64_t)p.M * f.residual_ld : 0, 4);
+#pragma unroll
+    for (int i = 0; i < T; ++i)
+#pragma unroll
+      for (int n = 0; n < T; ++n) {
+        float add[16];
+        auto at = [&](int r, int64_t ld) {
+          const int row = wm * 32 * T + CA::place(i, 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3));
+          return gn[n] < p.N ? (int)(((unsigned)row * (unsigned)ld + (unsigned)gn[n]) * 4u) : (int)OOB_OFFSET;
+        };
+#pragma unroll
+        for (int r = 0; r < 16; ++r) add[r] = f.residual == nullptr ? 0.f : __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw.rsrc, at(r, f.residual_ld), 0, 0));
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float v = acc[i][n][r] + bv[n];
+          if (ACT != ACT_NONE && f.z != nullptr) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), zw.rsrc, at(r, p.ldc), 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, activation<ACT, true>(v) + add[r]), cw.rsrc, at(r, p.ldc), 0, 0);
+        }
+      }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < T; ++i)
 #pragma unroll
@@ -316,6 +341,37 @@ hipError_t launch_dual_gemm_f32(GemmKind kind_a, const GemmArgs& a, GemmKind kin
     return big ? launch_pair<F32Tile<2, false, false, true>, F32Tile<2, true, true, false>>(2, a, b, work, s)
                : launch_pair<F32Tile<1, false, false, true>, F32Tile<1, true, true, false>>(1, a, b, work, s);
   return hipErrorInvalidValue;
+}
+
+template <int T, int ACT>
+__global__ __launch_bounds__(256) void dense_f32_kernel(const GemmArgs p, const FinishArgs f) {
+  typedef F32Tile<T, true, true, false, ACT> G;
+  __shared__ __attribute__((aligned(16))) float lds[2 * G::STAGE];
+  G::run(p, blockIdx.x, lds, f);
+}
+
+template <int ACT>
+static hipError_t launch_dense(int tile, GemmArgs a, const FinishArgs& f, hipStream_t s) {
+  const int side = tile == TILE_128x128 ? 128 : 64;
+  a.tiles_m = (a.M + side - 1) / side;
+  a.tiles_n = (a.N + side - 1) / side;
+  const long long grid = (long long)a.tiles_m * a.tiles_n;
+  if (a.splits != 1 || (tile != TILE_128x128 && tile != TILE_64x64) || grid <= 0 || grid > 0x7fffffffLL || !within_window(side, f.residual_ld, a.N, 4)) return hipErrorInvalidValue;
+  note_dense(a, f, 4);
+  static const std::string name = kernel_label("dense_f32_kernel", {lbl(1), lbl(ACT)}), big = kernel_label("dense_f32_kernel", {lbl(2), lbl(ACT)});
+  if (side == 128) return launch_kernel(big.c_str(), dense_work(a, f, 4), dense_f32_kernel<2, ACT>, dim3((unsigned)grid), dim3(256), s, a, f);
+  return launch_kernel(name.c_str(), dense_work(a, f, 4), dense_f32_kernel<1, ACT>, dim3((unsigned)grid), dim3(256), s, a, f);
+}
+
+hipError_t launch_dense_f32(int tile, int act, const GemmArgs& a, const FinishArgs& f, hipStream_t s) {
+  switch (act) {
+    case ACT_NONE: return launch_dense<ACT_NONE>(tile, a, f, s);
+    case ACT_RELU: return launch_dense<ACT_RELU>(tile, a, f, s);
+    case ACT_GELU: return launch_dense<ACT_GELU>(tile, a, f, s);
+    case ACT_GELU_TANH: return launch_dense<ACT_GELU_TANH>(tile, a, f, s);
+    case ACT_SILU: return launch_dense<ACT_SILU>(tile, a, f, s);
+    default: return hipErrorInvalidValue;
+  }
 }
 
 }  // namespace sk

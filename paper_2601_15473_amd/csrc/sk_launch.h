@@ -177,7 +177,7 @@ constexpr int F32_BK = 32;
 // (GEMM_NN) or [N, K] (GEMM_NT); of A [K, M] and B [K, N] (GEMM_TN), a contraction over rows.  `slabs`: product_bytes of room (none with a bias).
 size_t product_bytes(GemmKind kind, int64_t M, int64_t N, int64_t K, bool f32);
 hipError_t launch_product(GemmKind kind, GemmArgs a, bool f32, void* slabs, hipStream_t s);
-// A dense layer's forward product, planned: with all that follows it in its epilogue (bf16; `few`: the few-rows kernel, else on `tile`), or in fp32 slabs [splits][M, N]
+// A dense layer's forward product, planned: with all that follows it in its epilogue (`few`: the few-rows kernel, else on `tile`), or in fp32 slabs [splits][M, N]
 // for a launch of the caller's that sums and finishes them.
 struct DensePlan {
   bool fused, few;
