@@ -870,7 +870,7 @@ hipError_t launch_product(GemmKind kind, GemmArgs a, bool f32, void* slabs, hipS
   void* const out = a.C;
   a.splits = t.splits;
   a.k_per_split = t.k_per_split;
-  if (t.splits == 1) return f32 ? launch_gemm_f32(GEMM_TN_F32, t.tile, a, st) : launch_gemm_bf16(GEMM_TN, t.tile, a, st);
+  if (t.splits == 1) return f32 ? launch_gemm_f32(GEMM_TN_F32, t.tile, a, st) : launch_gemm_bf16(GEMM_TN, choose_expansion_tile(GEMM_TN, a.M, a.N, a.K), a, st);
   a.C = slabs;
   const hipError_t e = f32 ? launch_gemm_f32(GEMM_TN_F32, t.tile, a, st) : launch_gemm_bf16(GEMM_TN_F32_PLAIN, t.tile, a, st);
   if (e != hipSuccess) return e;

@@ -157,6 +157,7 @@ hipError_t launch_gemm_bf16(GemmKind kind, int tile, const GemmArgs& a, hipStrea
   if (tile == TILE_256x256) return launch_gemm256_bf16(kind, a, s);
   if (tile == TILE_256x128 && kind == GEMM_NN) return launch_ring<256, 128, true, false>(a, s);
   if (tile == TILE_256x128 && kind == GEMM_NT) return launch_ring<256, 128, true, true>(a, s);
+  if (tile == TILE_256x128 && kind == GEMM_TN) return launch_ring<256, 128, false, false>(a, s);
   switch (kind) {
     case GEMM_NN: return launch_tiles<true, false, bf16, false>(tile, a, s);
     case GEMM_NT: return launch_tiles<true, true, bf16, false>(tile, a, s);

@@ -104,7 +104,7 @@ enum TileCfg : int {
   TILE_64x128 = 3,
   TILE_64x64 = 4,
   TILE_COUNT = 5,        // (what sk_set_tuning can name)
-  TILE_256x128 = 5,      // on a ring only, GEMM_NN and GEMM_NT
+  TILE_256x128 = 5,      // on a ring only, GEMM_NN, GEMM_NT and GEMM_TN
 };
 
 inline void tile_dims(int tile, int& bm, int& bn) {
