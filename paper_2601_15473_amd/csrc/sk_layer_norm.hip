@@ -28,65 +28,6 @@ __device__ __forceinline__ float sum_row(float v, float* shared) {
   return v;
 }
 
-template <typename T>
-__device__ __forceinline__ void load_piece(float (&v)[PIECE], const T* row, int piece, int width) {
-#pragma unroll
-  for (int i = 0; i < PIECE; ++i) v[i] = 0.f;
-  if (piece * PIECE < width) load_values<T, PIECE>(v, row + piece * PIECE);
-}
-
-// L lanes to a row, N pieces to a lane: piece n of a lane is the row's n L + lane.
-template <typename T, int L, int N>
-__global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_fwd_kernel(const LayerNormArgs p) {
-  constexpr int THREADS = L > 256 ? L : 256, ROWS = THREADS / L;
-  __shared__ float shared[2][L > 64 ? L / 64 : 1];
-  const int lane = threadIdx.x % L;
-  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / L;
-  if (row >= p.rows) return;   // (L > 64: a work-group's threads all, or none)
-  const T* const x = static_cast<const T*>(p.x) + row * p.x_stride;
-  const T* const residual = p.residual ? static_cast<const T*>(p.residual) + row * p.residual_stride : nullptr;
-  float v[N][PIECE];
-#pragma unroll
-  for (int n = 0; n < N; ++n) load_piece<T>(v[n], x, n * L + lane, p.width);
-  if (residual) {
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-      float add[PIECE];
-      load_piece<T>(add, residual, n * L + lane, p.width);
-#pragma unroll
-      for (int i = 0; i < PIECE; ++i) v[n][i] += add[i];
-    }
-  }
-  float sum = 0.f;
-#pragma unroll
-  for (int n = 0; n < N; ++n)
-#pragma unroll
-    for (int i = 0; i < PIECE; ++i) sum += v[n][i];
-  const float mean = sum_row<L>(sum, shared[0]) / p.width;
-  sum = 0.f;
-#pragma unroll
-  for (int n = 0; n < N; ++n)
-    if ((n * L + lane) * PIECE < p.width)
-#pragma unroll
-      for (int i = 0; i < PIECE; ++i) sum += (v[n][i] - mean) * (v[n][i] - mean);
-  const float r = 1.f / sqrtf(sum_row<L>(sum, shared[1]) / p.width + p.eps);
-  if (p.stats && lane == 0) *reinterpret_cast<float2*>(p.stats + row * 2) = make_float2(mean, r);
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int at = (n * L + lane) * PIECE;
-    if (at >= p.width) continue;
-    if (p.s) store_values<T, PIECE>(static_cast<T*>(p.s) + row * p.width + at, v[n]);
-    float w[PIECE], b[PIECE], y[PIECE];
-#pragma unroll
-    for (int i = 0; i < PIECE; ++i) { w[i] = 1.f; b[i] = 0.f; }
-    if (p.weight) load_values<T, PIECE>(w, static_cast<const T*>(p.weight) + at);
-    if (p.bias) load_values<T, PIECE>(b, static_cast<const T*>(p.bias) + at);
-#pragma unroll
-    for (int i = 0; i < PIECE; ++i) y[i] = (v[n][i] - mean) * r * w[i] + b[i];
-    store_values<T, PIECE>(static_cast<T*>(p.y) + row * p.width + at, y);
-  }
-}
-
 // A row's pieces as they lie in memory, for loads that are not waited for yet.
 template <typename T, int N>
 struct Raw {
@@ -119,6 +60,62 @@ struct Raw {
     }
   }
 };
+
+// L lanes to a row, N pieces to a lane: piece n of a lane is the row's n L + lane.
+template <typename T, int L, int N>
+__global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_fwd_kernel(const LayerNormArgs p) {
+  constexpr int THREADS = L > 256 ? L : 256, ROWS = THREADS / L;
+  __shared__ float shared[2][L > 64 ? L / 64 : 1];
+  const int lane = threadIdx.x % L;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / L;
+  if (row >= p.rows) return;   // (L > 64: a work-group's threads all, or none)
+  // everything that the row needs, asked for at once
+  Raw<T, N> x, residual, weight, bias;
+  x.template load<L>(static_cast<const T*>(p.x) + row * p.x_stride, lane, p.width);
+  if (p.residual) residual.template load<L>(static_cast<const T*>(p.residual) + row * p.residual_stride, lane, p.width);
+  if (p.weight) weight.template load<L>(static_cast<const T*>(p.weight), lane, p.width);
+  if (p.bias) bias.template load<L>(static_cast<const T*>(p.bias), lane, p.width);
+  float v[N][PIECE];
+#pragma unroll
+  for (int n = 0; n < N; ++n) x.values(v[n], n);
+  if (p.residual) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      float add[PIECE];
+      residual.values(add, n);
+#pragma unroll
+      for (int i = 0; i < PIECE; ++i) v[n][i] += add[i];
+    }
+  }
+  float sum = 0.f;
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int i = 0; i < PIECE; ++i) sum += v[n][i];
+  const float mean = sum_row<L>(sum, shared[0]) / p.width;
+  sum = 0.f;
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+    if ((n * L + lane) * PIECE < p.width)
+#pragma unroll
+      for (int i = 0; i < PIECE; ++i) sum += (v[n][i] - mean) * (v[n][i] - mean);
+  const float r = 1.f / sqrtf(sum_row<L>(sum, shared[1]) / p.width + p.eps);
+  if (p.stats && lane == 0) *reinterpret_cast<float2*>(p.stats + row * 2) = make_float2(mean, r);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int at = (n * L + lane) * PIECE;
+    if (at >= p.width) continue;
+    if (p.s) store_values<T, PIECE>(static_cast<T*>(p.s) + row * p.width + at, v[n]);
+    float w[PIECE], b[PIECE], y[PIECE];
+#pragma unroll
+    for (int i = 0; i < PIECE; ++i) { w[i] = 1.f; b[i] = 0.f; }
+    if (p.weight) weight.values(w, n);
+    if (p.bias) bias.values(b, n);
+#pragma unroll
+    for (int i = 0; i < PIECE; ++i) y[i] = (v[n][i] - mean) * r * w[i] + b[i];
+    store_values<T, PIECE>(static_cast<T*>(p.y) + row * p.width + at, y);
+  }
+}
 
 // Gradients: work-groups walk over the rows with their lanes' terms of dw and db in registers, and leave one row of each, [group][dw, db][width].
 // What the next row needs is on its way while this one's sums are formed.
