@@ -158,7 +158,7 @@ sk_status layer_norm_args(const sk_layer_norm_shape* s, LayerNormArgs& a) {
   a.rows = s->rows; a.width = (int)s->width; a.eps = s->eps;
   return SK_OK;
 }
-size_t layer_norm_bytes(const LayerNormArgs& a) { return align_up((size_t)(a.rows < LAYER_NORM_MAX_GROUPS ? a.rows : LAYER_NORM_MAX_GROUPS) * 2 * a.width * 4); }
+size_t layer_norm_bytes(const LayerNormArgs& a) { return align_up((size_t)layer_norm_groups(a.rows, a.width) * 2 * a.width * 4); }
 
 sk_status dense_layer_args(const sk_dense_shape* s, DenseArgs& a) {
   if (s == nullptr) return SK_ERR_INVALID_ARG;

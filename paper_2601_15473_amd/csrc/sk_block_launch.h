@@ -107,7 +107,20 @@ struct LayerNormArgs {
   int width;
   float eps;
 };
-constexpr int LAYER_NORM_MAX_GROUPS = 512;
+// Lanes to a row: eight values a lane and piece, a row on part of a wave, a work-group's four, or sixteen waves.
+inline int layer_norm_lanes(int width) {
+  const int pieces = width / 8;
+  return pieces <= 8 ? 8 : pieces <= 16 ? 16 : pieces <= 32 ? 32 : pieces <= 128 ? 64 : pieces <= 1024 ? 256 : 1024;
+}
+// Work-groups of the backward pass, each of which leaves a row of partial sums: two to a CU (16383 x 4096 with a residual, 256 : 512 : 1024 of them, 141 : 113 : 112 us and 5 : 5 : 8
+// for their sum), but where a row is a work-group's not below eight rows each, down to one to a CU (2048 x 8192 33 + 4 : 39 + 7 : 51 + 12, 500 x 2048 6.5 + 3.0 : 8.0 + 5.0).
+inline int layer_norm_groups(int64_t rows, int width) {
+  const int lanes = layer_norm_lanes(width), together = lanes < 256 ? 256 / lanes : 1;
+  const int64_t groups = (rows + together - 1) / together;
+  int64_t most = 2 * NUM_CUS;
+  if (together == 1 && rows / 8 < most) most = rows / 8 < NUM_CUS ? NUM_CUS : rows / 8;
+  return (int)(groups < most ? groups : most);
+}
 constexpr int LAYER_NORM_MAX_WIDTH = 1 << 15;   // a row on one work-group's registers
 hipError_t launch_layer_norm_fwd(const LayerNormArgs& a, bool f32, hipStream_t s);
 hipError_t launch_layer_norm_bwd(const LayerNormArgs& a, bool f32, hipStream_t s);

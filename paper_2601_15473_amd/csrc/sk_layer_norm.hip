@@ -282,9 +282,8 @@ hipError_t fwd(const LayerNormArgs& a, hipStream_t s) {
 
 template <typename T, int L, int N>
 hipError_t bwd(const LayerNormArgs& a, hipStream_t s) {
-  constexpr int THREADS = L > 256 ? L : 256, ROWS = THREADS / L;
-  const int64_t most = (a.rows + ROWS - 1) / ROWS;
-  const int groups = (int)(most < LAYER_NORM_MAX_GROUPS ? most : LAYER_NORM_MAX_GROUPS);
+  constexpr int THREADS = L > 256 ? L : 256;
+  const int groups = layer_norm_groups(a.rows, a.width);
   note_matrix(a.x, a.rows, a.width, a.x_stride, sizeof(T), false);
   note_matrix(a.weight, 1, a.width, a.width, sizeof(T), false);
   note_matrix(a.stats, a.rows, 2, 2, 4, false);
@@ -308,18 +307,14 @@ hipError_t by_width(const LayerNormArgs& a, hipStream_t s) {
     else return fwd<T, decltype(l)::value, decltype(n)::value>(a, s);
   };
   const int pieces = a.width / PIECE;
-  if (pieces <= 8) return go(IntC<8>{}, IntC<1>{});
-  if (pieces <= 16) return go(IntC<16>{}, IntC<1>{});
-  if (pieces <= 32) return go(IntC<32>{}, IntC<1>{});
-  if (pieces <= 64) return go(IntC<64>{}, IntC<1>{});
-  if (pieces <= 128) return go(IntC<64>{}, IntC<2>{});
-  if (pieces <= 256) return go(IntC<256>{}, IntC<1>{});
-  if (pieces <= 512) return go(IntC<256>{}, IntC<2>{});
-  if (pieces <= 768) return go(IntC<256>{}, IntC<3>{});
-  if (pieces <= 1024) return go(IntC<256>{}, IntC<4>{});
-  if (pieces <= 2048) return go(IntC<1024>{}, IntC<2>{});
-  if (pieces <= 4096) return go(IntC<1024>{}, IntC<4>{});
-  return hipErrorInvalidValue;
+  switch (layer_norm_lanes(a.width)) {
+    case 8: return go(IntC<8>{}, IntC<1>{});
+    case 16: return go(IntC<16>{}, IntC<1>{});
+    case 32: return go(IntC<32>{}, IntC<1>{});
+    case 64: return pieces <= 64 ? go(IntC<64>{}, IntC<1>{}) : go(IntC<64>{}, IntC<2>{});
+    case 256: return pieces <= 256 ? go(IntC<256>{}, IntC<1>{}) : pieces <= 512 ? go(IntC<256>{}, IntC<2>{}) : pieces <= 768 ? go(IntC<256>{}, IntC<3>{}) : go(IntC<256>{}, IntC<4>{});
+    default: return pieces <= 2048 ? go(IntC<1024>{}, IntC<2>{}) : pieces <= 4096 ? go(IntC<1024>{}, IntC<4>{}) : hipErrorInvalidValue;
+  }
 }
 
 }  // namespace
