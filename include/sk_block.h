@@ -156,7 +156,7 @@ sk_status sk_dropout(const void* x, const void* residual, void* y, int64_t n, fl
  *   x and residual [rows, width] with row strides, weight and bias [width], y and sum (s) [rows, width] dense.  residual, weight, bias and
  * sum may be NULL.  stats [rows, 2] fp32 for a backward pass, or NULL: the mean and what the deviation is divided by, inverted.
  * y is formed of s before its rounding.
- *   width a multiple of 8 up to 2^15, rows below 2^24.
+ *   width a multiple of 8 up to 2^15, rows below 2^24 (2^22 from a width of 8200 on).
  */
 typedef struct {
   int64_t rows, width;
@@ -218,7 +218,7 @@ sk_status sk_dense_bwd(const sk_dense_shape* shape, const void* x, const void* w
  * both entries.  A row without an entry has no first term, one whose label is outside the vocabulary (or all, with labels NULL) no second.
  *   logits on any boundary of a value, with a row stride of any number of elements, teacher_logits [rows, top] in `dtype`, teacher_ids [rows, top], labels [rows], loss [rows] fp32.
  * stats [rows, 8] fp32 for a backward pass, or NULL.  (A row whose logits are all -infinity has no softmax: NaN.)
- *   rows and vocabulary up to 2^24 (rows below it), top up to 2^16 (0: no teacher; its pointers may be NULL), temperature from 10^-3 to 10^3.
+ *   rows below 2^23, vocabulary up to 2^24, top up to 2^16 (0: no teacher; its pointers may be NULL), temperature from 10^-3 to 10^3.
  */
 typedef struct {
   int64_t rows, vocabulary, logits_stride;

@@ -35,6 +35,7 @@ bool stride_ok(int64_t size, int64_t stride, sk_dtype t, int64_t most, int64_t& 
 constexpr int64_t MOST_ROWS = 1 << 27;          // queries times group, keys: positions are 32-bit in the kernels
 constexpr int64_t MOST_TOKEN_STRIDE = 1 << 22;  // a tile's offsets are 32-bit bytes
 constexpr int64_t MOST_GROUPS = (1 << 24) - 1;  // work-groups of 256 threads in a launch
+constexpr int64_t MOST_THREADS = (int64_t)1 << 32;  // of a launch
 constexpr int64_t MOST_STRIDE = (int64_t)1 << 40;
 
 sk_status attention_args(const sk_attention_shape* s, AttentionArgs& a) {
@@ -151,6 +152,7 @@ sk_status layer_norm_args(const sk_layer_norm_shape* s, LayerNormArgs& a) {
   if (s == nullptr) return SK_ERR_INVALID_ARG;
   if (s->rows < 1 || s->width < 1 || !(s->eps >= 0.f) || !std::isfinite(s->eps)) return SK_ERR_INVALID_ARG;
   if (!known(s->dtype) || s->width % 8 != 0 || s->width > LAYER_NORM_MAX_WIDTH || s->rows >= (1 << 24)) return SK_ERR_UNSUPPORTED;
+  if (s->rows * layer_norm_lanes((int)s->width) >= MOST_THREADS) return SK_ERR_UNSUPPORTED;
   sk_status st = SK_OK;
   if (!row_stride_ok(s->rows, s->width, s->x_stride, s->dtype, MOST_STRIDE, a.x_stride, st) ||
       !row_stride_ok(s->rows, s->width, s->residual_stride, s->dtype, MOST_STRIDE, a.residual_stride, st))
@@ -202,7 +204,7 @@ sk_status distill_args(const sk_distill_shape* s, const void* logits, DistillArg
   if (s->rows < 1 || s->vocabulary < 1 || s->top < 0 || s->logits_stride < 0 || !(s->temperature > 0.f) || !std::isfinite(s->temperature) ||
       !(s->label_weight >= 0.f && s->label_weight <= 1.f))
     return SK_ERR_INVALID_ARG;
-  if (!known(s->dtype) || (s->id_bytes != 4 && s->id_bytes != 8) || (s->label_bytes != 4 && s->label_bytes != 8) || s->rows >= (1 << 24) || s->vocabulary > (1 << 24) ||
+  if (!known(s->dtype) || (s->id_bytes != 4 && s->id_bytes != 8) || (s->label_bytes != 4 && s->label_bytes != 8) || s->rows >= (1 << 23) || s->vocabulary > (1 << 24) ||
       s->top > (1 << 16) || s->logits_stride > MOST_STRIDE || !(s->temperature >= 1e-3f && s->temperature <= 1e3f))
     return SK_ERR_UNSUPPORTED;
   // (rows begin anywhere; values where values do)

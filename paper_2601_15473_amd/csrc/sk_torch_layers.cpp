@@ -299,7 +299,7 @@ PyObject* distillation_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
     labels = *l;
   }
   const DistillCall c(*z, *ids, labels, temperature, label_weight);
-  if (!(temperature >= 1e-3 && temperature <= 1e3 && label_weight >= 0.0 && label_weight <= 1.0) || c.s.rows >= 1 << 24 || c.s.vocabulary > 1 << 24) Py_RETURN_NONE;
+  if (!(temperature >= 1e-3 && temperature <= 1e3 && label_weight >= 0.0 && label_weight <= 1.0) || c.s.rows >= 1 << 23 || c.s.vocabulary > 1 << 24) Py_RETURN_NONE;
   Tensor loss;
   {
     pybind11::gil_scoped_release no_gil;

@@ -30,7 +30,7 @@ def test_shapes_have_the_headers_layout():
 
 @pytest.mark.parametrize("change, want", [
     (dict(rows=0), 1), (dict(width=0), 1), (dict(width=-8), 1), (dict(eps=-1.0), 1), (dict(eps=math.nan), 1), (dict(eps=math.inf), 1), (dict(x_stride=-64), 1), (dict(residual_stride=-64), 1),
-    (dict(width=60), 2), (dict(width=(1 << 15) + 8), 2), (dict(rows=1 << 24), 2), (dict(dtype=4), 2), (dict(x_stride=68), 2), (dict(x_stride=(1 << 40) + 8), 2), (dict(residual_stride=65), 2),
+    (dict(width=60), 2), (dict(width=(1 << 15) + 8), 2), (dict(rows=1 << 24), 2), (dict(rows=1 << 22, width=8200), 2), (dict(dtype=4), 2), (dict(x_stride=68), 2), (dict(x_stride=(1 << 40) + 8), 2), (dict(residual_stride=65), 2),
 ])
 def test_layer_norm_refusals(change, want):
     s = norm_shape(**change)
@@ -98,7 +98,7 @@ def test_dense_pointers_and_workspace():
 @pytest.mark.parametrize("change, want", [
     (dict(rows=0), 1), (dict(vocabulary=0), 1), (dict(top=-1), 1), (dict(logits_stride=-1), 1), (dict(temperature=0.0), 1), (dict(temperature=-1.0), 1), (dict(temperature=math.nan), 1),
     (dict(temperature=math.inf), 1), (dict(label_weight=-0.1), 1), (dict(label_weight=1.1), 1), (dict(label_weight=math.nan), 1),
-    (dict(dtype=2), 2), (dict(id_bytes=2), 2), (dict(label_bytes=1), 2), (dict(rows=1 << 24), 2), (dict(vocabulary=(1 << 24) + 1), 2), (dict(top=(1 << 16) + 1), 2), (dict(temperature=1e-4), 2),
+    (dict(dtype=2), 2), (dict(id_bytes=2), 2), (dict(label_bytes=1), 2), (dict(rows=1 << 23), 2), (dict(vocabulary=(1 << 24) + 1), 2), (dict(top=(1 << 16) + 1), 2), (dict(temperature=1e-4), 2),
     (dict(temperature=2e3), 2), (dict(logits_stride=(1 << 40) + 1), 2),
 ])
 def test_distill_refusals(change, want):
@@ -125,7 +125,7 @@ def test_distill_pointers():
 
 
 @pytest.mark.parametrize("dtype, e", [(sk.SK_BF16, 2), (sk.SK_F32, 4)], ids=["bf16", "f32"])
-@pytest.mark.parametrize("rows, width", [(1, 8), (3, 64), (1000, 72), (5000, 768), (16384, 4096), (7, 32768), ((1 << 24) - 1, 8)])
+@pytest.mark.parametrize("rows, width", [(1, 8), (3, 64), (1000, 72), (5000, 768), (16384, 4096), (7, 32768), ((1 << 24) - 1, 8), ((1 << 24) - 1, 8192), ((1 << 22) - 1, 32768)])
 def test_layer_norm_accesses(rows, width, dtype, e):
     for residual in (False, True):
         buf = Buffers()
@@ -167,7 +167,7 @@ def test_dense_accesses(dtype, e):
     sizes += [(max(1, int(2 ** rng.uniform(0, 15))), 8 * max(1, int(2 ** rng.uniform(0, 10))), 8 * max(1, int(2 ** rng.uniform(0, 10)))) for _ in range(150)]
     for tokens, d_in, d_out in sizes:
         for act in (sk.SK_ACT_NONE, sk.SK_ACT_SILU):
-            stride = d_in + rng.choice([0, 0, 8, 264])
+            stride = rng.choice([d_in, d_in, d_in + 8, d_in + 264, 1 << 20])
             _dense_accesses(tokens, d_in, d_out, dtype, e, act, stride if stride <= 1 << 20 else d_in)
 
 
@@ -184,7 +184,7 @@ def test_dense_layers_of_the_most_values(dtype):
 
 
 @pytest.mark.parametrize("dtype, e", [(sk.SK_BF16, 2), (sk.SK_F32, 4)], ids=["bf16", "f32"])
-@pytest.mark.parametrize("rows, vocabulary, top", [(1, 1, 1), (3, 7, 0), (1000, 64, 8), (4001, 32001, 64), (5, 1 << 24, 1 << 16), ((1 << 24) - 1, 50, 3)])
+@pytest.mark.parametrize("rows, vocabulary, top", [(1, 1, 1), (3, 7, 0), (1000, 64, 8), (4001, 32001, 64), (5, 1 << 24, 1 << 16), ((1 << 23) - 1, 50, 3), ((1 << 23) - 1, 50000, 3)])
 def test_distill_accesses(rows, vocabulary, top, dtype, e):
     for labels in (False, True):
         buf = Buffers()
