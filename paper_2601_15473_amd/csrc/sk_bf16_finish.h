@@ -4,6 +4,12 @@
 // block of 32 rows over 64 columns at a time in fp32 through a strip of LDS of its own (no barrier: a wave's LDS operations execute in order): bias, activation and residual are applied to
 // eight consecutive columns of a row, and y, and z for a backward pass, are rounded once.  16-byte pieces are XOR-swizzled by row, so that neither the
 // column-wise writes nor the row-wise reads collide on banks.
+//
+// z is kept in bf16, as the operands are: what a backward pass needs of it is a derivative.
+//
+// Forward, us, with a bias alone (the plain product's epilogue, rounded in registers) : a residual : gelu : gelu with z stored: 4096 tokens, 1024 -> 4096 36 : 42 : 44 : 44; 16384, 512 -> 512
+// 15 : 15 : 19 : 20; 4096, 4096 -> 1024 36 : 39 : 39 : 40; 16384, 4096 -> 11008 1090 : 1131 : 1164 : 1217.  Where a CU has one tile, nothing runs under the turn and the activation.  On fp32
+// from the product, as a launch of its own, the last was 1835.
 #pragma once
 #include "sk_activation.h"
 #include "sk_bf16_tile.h"

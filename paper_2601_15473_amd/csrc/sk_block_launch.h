@@ -153,7 +153,8 @@ struct DenseArgs {
   int64_t x_stride, residual_stride;
   int tokens, in, out, activation;
 };
-// Runs of rows that dz's column sums are formed in: of groups of 512 columns about four work-groups to a CU, 16 rows at least.
+// Runs of rows that dz's column sums are formed in: of groups of 512 columns about four work-groups to a CU, 16 rows at least.  (Two, three and eight: dz of 4096 x 4096 behind gelu
+// 24.0, 20.8 and 19.2 us for 19.7, of 16384 x 11008 behind silu 265, 250 and 252 for 257; the sums' launch level.)
 struct DenseRuns {
   int groups, runs, rows;
   DenseRuns(int64_t tokens, int64_t out) {

@@ -1,4 +1,12 @@
-// Dense layers: y = act(x W^T + bias) + residual, and their gradients, around the products of sk_bf16_gemm*.hip and sk_f32_gemm.hip.
+// What stands around a dense layer's products: the second launch of a forward product that was split over its contraction, and dz = dy act'(z) with the bias's gradient ahead
+// of the two backward ones,  dx = dz W,  dW = dz^T x.
+//
+// Bound by memory.  dz of 4096 x 4096 behind gelu 19 us for 101 MB (5.3 TB/s; level for two to eight rows ahead and three to eight work-groups a CU), 16384 x 11008 behind silu 228 to 257 us for
+// 1.08 GB; the runs' sums 2 to 5 us, a launch.  In bf16 z comes back rounded (the derivative at z off by 2^-8 z act''(z): 0.0006 of dz, where dz's own rounding, as an operand of both products, is 0.0017; z in
+// fp32 would be twice the bytes here and in the forward pass), and the bias's sums are of dz before its rounding.
+//
+// Tried and slower: the bias's gradient on the weight's product, whose operand dz is, as MFMAs against ones (46 us for 36) or on the vector unit (48), where without an activation
+// its two launches here take 8 ([4001 x 1024]^T . [4001 x 4096]); dx beside dW in one launch on staged 128 x 128 tiles (84 for 38 + 37, 4096 tokens, 1024 -> 4096).
 #include "sk_activation.h"
 #include "sk_block_launch.h"
 #include "sk_rows.h"

@@ -6,6 +6,8 @@
 //
 // Bound by memory: forward z is read once, with the largest value so far and the sums of exponentials below it carried along (rescaled once in
 // some values), back it is read again and dz written (what the gradient is scaled by is known then only).  The entries are few: one thread each.
+// Bf16, 8192 rows of 65536: forward 179 us with one exponential a value (1.07 GB, 6.0 TB/s), 265 with two, back 398 with lists of 128 (2.15 GB, 5.4; a copy reaches 5.1).  Behind a backward pass
+// the forward one takes 215 and 267: it shares the memory with what that pass left to be written back.
 //
 // A row begins wherever the vocabulary's size puts it: its values are taken 16 bytes at a time at the places where memory has them, and one by one
 // in the pieces that it shares with its neighbours.
@@ -80,7 +82,7 @@ __device__ __forceinline__ Entry entry_of(const DistillArgs& p, int64_t row, int
   return e;
 }
 // THREADS to a row.  A thread's first entry of the teacher's list, the student's logit there and the label's are asked for ahead of the row, and what is
-// left to do behind it is two sums over the work-group: every row has that tail, and it is as long as 16000 values take.
+// left to do behind it is two sums over the work-group.
 template <typename T, int THREADS, bool HARD>
 __global__ __launch_bounds__(THREADS) void distill_fwd_kernel(const DistillArgs p) {
   constexpr int E = RowPieces<T>::E, AHEAD = 2, WAVES = THREADS / 64;
@@ -155,14 +157,24 @@ __global__ __launch_bounds__(THREADS) void distill_fwd_kernel(const DistillArgs 
       const Entry e = entry_of<T>(p, row, k);
       if (e.there) high = fmaxf(high, e.t);
     }
+  // The work-group's largest values, then its sums below the largest: one exponential a thread and sum, and one a wave.  (Joined a pair at a time, every pair with its own, and by all
+  // threads, that took 8192 rows of 65536 230 us for 217, 16384 of 1000 30 for 26.)
+  const float own = s.top;
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) {
-    Sums o;
-    o.top = __shfl_xor(s.top, m);
-    o.soft = __shfl_xor(s.soft, m);
-    o.hard = HARD ? __shfl_xor(s.hard, m) : 0.f;
-    join<HARD>(s, o, c);
+    s.top = fmaxf(s.top, __shfl_xor(s.top, m));
     high = fmaxf(high, __shfl_xor(high, m));
+  }
+  auto rescale = [&](float from) {   // (a thread or wave of -infinities has nothing to rescale)
+    const bool any = from != -INFINITY;
+    s.soft *= any ? below(from, s.top, c) : 1.f;
+    if (HARD) s.hard *= any ? below(from, s.top, LOG2E) : 1.f;
+  };
+  rescale(own);
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    s.soft += __shfl_xor(s.soft, m);
+    if (HARD) s.hard += __shfl_xor(s.hard, m);
   }
   if constexpr (WAVES > 1) {
     if ((threadIdx.x & 63) == 0) {
@@ -170,32 +182,42 @@ __global__ __launch_bounds__(THREADS) void distill_fwd_kernel(const DistillArgs 
       highs[threadIdx.x >> 6] = high;
     }
     __syncthreads();
-    s = waves[0];
-    high = highs[0];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) {
-      join<HARD>(s, waves[w], c);
+    for (int w = 0; w < WAVES; ++w) {
+      s.top = fmaxf(s.top, waves[w].top);
       high = fmaxf(high, highs[w]);
     }
+    if (threadIdx.x < 64) {   // (the first thread has use for them)
+      const Sums o = waves[threadIdx.x % WAVES];
+      s.soft = o.soft;
+      s.hard = o.hard;
+      rescale(o.top);
+#pragma unroll
+      for (int m = 1; m < WAVES; m <<= 1) {
+        s.soft += __shfl_xor(s.soft, m);
+        if (HARD) s.hard += __shfl_xor(s.hard, m);
+      }
+    }
   }
-  // With e_k = exp((t_k - high) / tau): the sum of e_k, and that of e_k (t_k - high - (z_k - top)) / tau.  log p - log q is a difference of numbers much
+  // With e_k = exp((t_k - high) / tau): the sum of e_k, and that of e_k (t_k - high - (z_k - top)).  log p - log q is a difference of numbers much
   // larger than it: in 64 bits.
   double total = 0.0, apart = 0.0;
   auto add = [&](float t, float at) {
     const float e = below(t, high, c);
     total += (double)e;
-    if (e != 0.f) apart += (double)e * ((((double)t - (double)high) - ((double)at - (double)s.top)) / (double)tau);   // (what does not weigh may be anywhere)
+    if (e != 0.f) apart += (double)e * (((double)t - (double)high) - ((double)at - (double)s.top));   // (what does not weigh may be anywhere)
   };
-  if (mine.there) add(mine.t, at_mine);
-  if (teaches)
+  if (teaches && (int)(threadIdx.x & ~63u) < p.top) {   // (a wave without entries has nothing to add up)
+    if (mine.there) add(mine.t, at_mine);
     for (int k = threadIdx.x + THREADS; k < p.top; k += THREADS) {
       const Entry e = entry_of<T>(p, row, k);
       if (e.there) add(e.t, load_one(z + e.id));
     }
 #pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    total += __shfl_xor(total, m);
-    apart += __shfl_xor(apart, m);
+    for (int m = 1; m < 64; m <<= 1) {
+      total += __shfl_xor(total, m);
+      apart += __shfl_xor(apart, m);
+    }
   }
   if constexpr (WAVES > 1) {
     if ((threadIdx.x & 63) == 0) {
@@ -203,14 +225,16 @@ __global__ __launch_bounds__(THREADS) void distill_fwd_kernel(const DistillArgs 
       parts[1][threadIdx.x >> 6] = apart;
     }
     __syncthreads();
+  }
+  if (threadIdx.x != 0) return;
+  if constexpr (WAVES > 1) {
     total = apart = 0.0;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) { total += parts[0][w]; apart += parts[1][w]; }
   }
-  if (threadIdx.x != 0) return;
   double loss = 0.0;
   if (total != 0.0)   // (NaN: there is something)
-    loss = (apart / total + log((double)s.soft) - log(total)) * ((1.0 - (double)weight) * (double)tau * (double)tau);
+    loss = (apart / total / (double)tau + log((double)s.soft) - log(total)) * ((1.0 - (double)weight) * (double)tau * (double)tau);
   if (label >= 0) loss += (double)weight * (log((double)(HARD ? s.hard : s.soft)) + ((double)s.top - (double)at_label));
   p.loss[row] = (float)loss;
   if (p.stats) {
@@ -221,6 +245,7 @@ __global__ __launch_bounds__(THREADS) void distill_fwd_kernel(const DistillArgs 
 }
 
 // What the entries and the label subtract, by place, for the thread that writes the place: lists in LDS, chained by thread.
+// (A place that is named twice stands in them once, with the sum in the list's order: what order the chains come out in changes nothing.)
 struct alignas(16) Places {
   static constexpr int MOST = 256;
   int id[MOST], next[MOST];
@@ -437,12 +462,12 @@ hipError_t go(const DistillArgs& a, hipStream_t s) {
 }
 
 // Threads to a row.  Short rows are the price of what each has behind (forward) or ahead of (back) its values, and many small work-groups hide it better;
-// long ones want few rows at a time.  Bf16, us, 64 : 256 : 512 threads: forward 16384 rows of 1000 25 : 51 : 102, 3000 of 9000 16 : 20 : 27, 4001 of 32001 80 : 83 : 82,
-// 8192 of 65536 232 : 227 : 220; back 16384 of 200 20 : 27 : 53, 16384 of 1000 80 : 67 : 121, 4001 of 32001 114 : 96 : 96, 8192 of 65536 466 : 413 : 398.
-// Few rows (less than two waves a SIMD at 64 threads): 256, forward 100 of 32000 13 : 8 : 8.
+// long ones want few rows at a time.  Bf16, us, 64 : 256 : 512 threads: forward 16384 rows of 1000 26 : 43 : 74, 3000 of 9000 22 : 20 : 22, 4001 of 32001 84 : 81 : 80,
+// 8192 of 65536 241 : 227 : 215; back 16384 of 200 20 : 27 : 53, 16384 of 1000 80 : 67 : 121, 4001 of 32001 114 : 96 : 96, 8192 of 65536 466 : 413 : 398.
+// Few rows (less than two waves a SIMD at 64 threads): 256, forward 100 of 32000 16 : 9 : 9.
 template <typename T, bool HARD, bool BACK>
 hipError_t by_size(const DistillArgs& a, hipStream_t s) {
-  if (a.vocabulary <= (BACK ? 512 : 12288) && (a.rows >= 8 * NUM_CUS || a.vocabulary <= 512)) return go<T, 64, HARD, BACK>(a, s);
+  if (a.vocabulary <= (BACK ? 512 : 6144) && (a.rows >= 8 * NUM_CUS || a.vocabulary <= 512)) return go<T, 64, HARD, BACK>(a, s);
   if (a.vocabulary <= 49152) return go<T, 256, HARD, BACK>(a, s);
   return go<T, 512, HARD, BACK>(a, s);
 }

@@ -4,7 +4,11 @@
 //   g = dy w,  dx = ds + r (g - mean g - u mean(g u)),  dw = sum dy u,  db = sum dy
 //
 // Bound by memory: a row is read once into registers, eight values to a lane and piece, and both of its sums are taken there (the mean first, the
-// squares about it second: a stream whose mean is large beside its spread loses nothing).  y is formed of the sum before s is rounded.
+// squares about it second: a stream whose mean is large beside its spread loses nothing).  y is formed of the sum before s is rounded; the gradients take s as it was
+// stored, in the storage type, with the mean and deviation of the sum itself: keeping it in fp32 for them would be half as much again to write and read.
+// Bf16, 16383 rows of 4096 with a residual: forward 93 us for 537 MB (5.8 TB/s; a copy reaches 5.1), back 112 us for 537 MB (4.8) and 5 for the sum of the partial
+// sums; 4096 rows of 768 6.4, 9.7 and 3.8.  What carried it: every load of a row ahead of its first sum, the weights' among them (forward 99 -> 93, eight rows of 8192 6.4 -> 4.5), and the
+// next row's loads under this one's sums (back 180 -> 112).
 #include "sk_block_launch.h"
 #include "sk_rows.h"
 
