@@ -437,6 +437,11 @@ def _row_stride(t: torch.Tensor) -> int:
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
+def _saved(t: torch.Tensor | None) -> torch.Tensor | None:
+    """What was saved dense: hooks may have laid it out differently."""
+    return None if t is None else _dense(t)
+
+
 def _layer_norm_shape(x, residual, eps):
     return sk.LayerNormShape(x.shape[0], x.shape[1], eps, _DTYPES[x.dtype], _row_stride(x), x.shape[1] if residual is None else _row_stride(residual))
 
@@ -464,7 +469,7 @@ class LayerNormFunction(torch.autograd.Function):
     @_once
     def backward(ctx, dy, ds=None):
         x, w, stats = ctx.saved_tensors
-        x = x.reshape(-1, ctx.shape[-1])
+        x, w, stats = _rows_of(x), _saved(w), _saved(stats)
         dx = torch.empty(ctx.shape, dtype=x.dtype, device=x.device)
         dw, db = (torch.empty(ctx.shape[-1], dtype=x.dtype, device=x.device) if there else None for there in (w is not None, ctx.bias))
         if x.numel() == 0:
@@ -551,6 +556,7 @@ class LinearFunction(torch.autograd.Function):
     @_once
     def backward(ctx, dy):
         x, w, z = ctx.saved_tensors
+        x, w, z = _rows_of(x, x.shape[-1], 1 << 20), _saved(w), _saved(z)
         wanted = ctx.needs_input_grad
         dx = torch.empty(ctx.shape, dtype=x.dtype, device=x.device) if wanted[0] else None
         dw = torch.empty(w.shape, dtype=x.dtype, device=x.device) if wanted[1] else None
@@ -602,14 +608,17 @@ def _distill_shape(z, ids, labels, temperature, label_weight):
                            temperature, label_weight, _DTYPES[z.dtype])
 
 
+def _logit_rows(z: torch.Tensor) -> torch.Tensor:
+    return z if z.stride(1) == 1 and z.stride(0) <= 1 << 40 else z.clone(memory_format=torch.contiguous_format)
+
+
 class DistillationFunction(torch.autograd.Function):
     """See ``distillation_loss``; keeps its inputs and each row's largest logit and sums."""
 
     @staticmethod
     def forward(ctx, logits, teacher_logits, teacher_ids, labels, temperature, label_weight, training):
         z = logits.reshape(-1, logits.shape[-1])
-        if z.stride(1) != 1 or z.stride(0) > 1 << 40:
-            z = z.contiguous()
+        z = _logit_rows(z)
         loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=logits.device)
         stats = torch.empty((z.shape[0], 8), dtype=torch.float32, device=logits.device) if training else None
         if z.shape[0] > 0:
@@ -623,7 +632,8 @@ class DistillationFunction(torch.autograd.Function):
     @staticmethod
     @_once
     def backward(ctx, dloss):
-        z, t, ids, labels, stats = ctx.saved_tensors
+        z, *rest = ctx.saved_tensors
+        z, (t, ids, labels, stats) = _logit_rows(z), map(_saved, rest)
         dz = torch.empty(ctx.shape, dtype=z.dtype, device=z.device)
         if z.shape[0] > 0:
             with _on(z.device):

@@ -21,6 +21,9 @@ bool rows_in_place(const Tensor& t, int64_t least, int64_t most) {
 }
 int64_t row_stride(const Tensor& t) { return t.is_contiguous() ? t.size(-1) : t.stride(0); }
 void* data(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+// What was saved, as the kernels take it: hooks may have laid it out differently.
+Tensor saved_dense(const Tensor& t) { return t.defined() ? made_dense(t) : t; }
+Tensor saved_rows(const Tensor& t, int64_t least, int64_t most) { return rows_in_place(t, least, most) ? t : made_dense(t); }
 
 template <typename Call>
 void with_workspace(const Tensor& t, size_t bytes, const Call& call) {
@@ -87,8 +90,8 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
 
   static variable_list gradients(AutogradContext* ctx, const variable_list& grads, bool all) {
     const variable_list saved = ctx->get_saved_variables();
-    const Tensor &x = saved[0], &w = saved[1], &stats = saved[2];
-    const c10::DeviceGuard guard(x.device());
+    const c10::DeviceGuard guard(saved[0].device());
+    const Tensor x = saved_rows(saved[0], 0, (int64_t)1 << 40), w = saved_dense(saved[1]), stats = saved_dense(saved[2]);
     const Tensor dy = grads[0].defined() ? made_dense(grads[0]) : at::zeros(x.sizes(), x.options());
     const Tensor ds = grads.size() > 1 && grads[1].defined() ? made_dense(grads[1]) : Tensor();
     const sk_layer_norm_shape s = norm_shape(x, Tensor(), 0.0);
@@ -148,8 +151,8 @@ struct Dense : torch::autograd::Function<Dense> {
 
   static variable_list gradients(AutogradContext* ctx, const variable_list& grads, bool all) {
     const variable_list saved = ctx->get_saved_variables();
-    const Tensor &x = saved[0], &w = saved[1], &z = saved[2];
-    const c10::DeviceGuard guard(x.device());
+    const c10::DeviceGuard guard(saved[0].device());
+    const Tensor x = saved_rows(saved[0], saved[0].size(-1), 1 << 20), w = saved_dense(saved[1]), z = saved_dense(saved[2]);
     const Tensor dy = made_dense(grads[0]);
     const sk_dense_shape s = layer_shape(x, w, Tensor(), ctx->saved_data["activation"].toInt());
     const int64_t want = ctx->saved_data["wanted"].toInt();
@@ -165,6 +168,10 @@ struct Dense : torch::autograd::Function<Dense> {
 };
 
 // ---- the distillation loss ----
+
+bool logits_in_place(const Tensor& z) {
+  return z.is_contiguous() || (z.dim() == 2 && z.stride(1) == 1 && z.stride(0) > 0 && z.stride(0) <= (int64_t)1 << 40);
+}
 
 struct DistillCall {
   sk_distill_shape s{};
@@ -201,11 +208,12 @@ struct Distill : torch::autograd::Function<Distill> {
 
   static variable_list gradients(AutogradContext* ctx, const variable_list& grads) {
     const variable_list saved = ctx->get_saved_variables();
-    const Tensor& z = saved[0];
-    const c10::DeviceGuard guard(z.device());
+    const c10::DeviceGuard guard(saved[0].device());
+    const Tensor z = logits_in_place(saved[0]) ? saved[0] : made_dense(saved[0]);
+    const Tensor t = saved_dense(saved[1]), ids = saved_dense(saved[2]), labels = saved_dense(saved[3]), stats = saved_dense(saved[4]);
     const Tensor dloss = made_dense(grads[0]), dz = at::empty(z.sizes(), z.options());
-    const DistillCall c(z, saved[2], saved[3], ctx->saved_data["temperature"].toDouble(), ctx->saved_data["label_weight"].toDouble());
-    check(sk_distill_bwd(&c.s, z.data_ptr(), data(saved[1]), data(saved[2]), data(saved[3]), saved[4].data_ptr<float>(), dloss.data_ptr<float>(), dz.data_ptr(), stream_of(z.device())));
+    const DistillCall c(z, ids, labels, ctx->saved_data["temperature"].toDouble(), ctx->saved_data["label_weight"].toDouble());
+    check(sk_distill_bwd(&c.s, z.data_ptr(), data(t), data(ids), data(labels), stats.data_ptr<float>(), dloss.data_ptr<float>(), dz.data_ptr(), stream_of(z.device())));
     return {dz};
   }
 };
@@ -288,7 +296,7 @@ PyObject* distillation_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 6 || !number(a[4], temperature) || !number(a[5], label_weight) || !unwatched()) Py_RETURN_NONE;
   const Tensor *z = plain(a[0]), *t = plain(a[1]), *ids = plain(a[2]);
   if (!z || !t || !ids || !floating(*z) || !no_tangent(*z) || !same(*z, *t) || !integers(*ids, z->device()) || z->dim() < 1 || z->numel() == 0) Py_RETURN_NONE;
-  if (!z->is_contiguous() && !(z->dim() == 2 && z->stride(1) == 1 && z->stride(0) > 0 && z->stride(0) <= (int64_t)1 << 40)) Py_RETURN_NONE;
+  if (!logits_in_place(*z)) Py_RETURN_NONE;
   if (t->dim() != z->dim() || ids->sizes() != t->sizes() || t->sizes().slice(0, t->dim() - 1) != z->sizes().slice(0, z->dim() - 1) || t->numel() == 0 || t->size(-1) > 1 << 16 || !dense(*t) || !dense(*ids) ||
       (at::GradMode::is_enabled() && t->requires_grad()))
     Py_RETURN_NONE;
