@@ -154,7 +154,8 @@ sk_status sk_dropout(const void* x, const void* residual, void* y, int64_t n, fl
  * Layer norm of rows, with a residual added first:
  *     s = x + residual,   y = (s - mean s) / sqrt(mean (s - mean s)^2 + eps) * weight + bias
  *   x and residual [rows, width] with row strides, weight and bias [width], y and sum (s) [rows, width] dense.  residual, weight, bias and
- * sum may be NULL.  stats [rows, 2] fp32 for a backward pass, or NULL: the mean and what the deviation is divided by, inverted.
+ * sum may be NULL.  For a backward pass, or NULL: stats [rows, 2] fp32, the mean and what the deviation is divided by, inverted; with a sum in bf16 also
+ * sum_rest [rows, width / 8] 32-bit words, what its rounding left off: four bits a value, a word's from the lowest on, signed, in 16ths of a step of the type.
  * y is formed of s before its rounding.
  *   width a multiple of 8 up to 2^15, rows below 2^24 (2^22 from a width of 8200 on).
  */
@@ -166,14 +167,14 @@ typedef struct {
 } sk_layer_norm_shape;
 
 sk_status sk_layer_norm_fwd(const sk_layer_norm_shape* shape, const void* x, const void* residual, const void* weight, const void* bias,
-                            void* y, void* sum, float* stats, void* stream);
+                            void* y, void* sum, void* sum_rest, float* stats, void* stream);
 
 /*
- * Its gradients: x [rows, width] is what was normed (the sum, where there was a residual), with row stride x_stride; dy and d_sum dense, d_sum the
+ * Its gradients: x [rows, width] is what was normed (the sum, where there was a residual, and sum_rest or NULL), with row stride x_stride; dy and d_sum dense, d_sum the
  * gradient of the sum or NULL; dx (of x, and of the residual) dense, dweight and dbias in `dtype`, or NULL.  Workspace: sk_layer_norm_workspace_bytes,
  * needed for dweight and dbias.
  */
-sk_status sk_layer_norm_bwd(const sk_layer_norm_shape* shape, const void* x, const void* weight, const float* stats, const void* dy, const void* d_sum,
+sk_status sk_layer_norm_bwd(const sk_layer_norm_shape* shape, const void* x, const void* sum_rest, const void* weight, const float* stats, const void* dy, const void* d_sum,
                             void* dx, void* dweight, void* dbias, void* workspace, size_t workspace_bytes, void* stream);
 size_t sk_layer_norm_workspace_bytes(const sk_layer_norm_shape* shape);
 

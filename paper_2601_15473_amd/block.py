@@ -447,7 +447,7 @@ def _layer_norm_shape(x, residual, eps):
 
 
 class LayerNormFunction(torch.autograd.Function):
-    """See ``layer_norm``, on rows; keeps what was normed, and each row's mean and deviation."""
+    """See ``layer_norm``, on rows; keeps what was normed, each row's mean and deviation, and for the gradient of a weight what a sum's rounding to bf16 left off."""
 
     @staticmethod
     def forward(ctx, x, weight, bias, residual, eps, training):
@@ -457,10 +457,13 @@ class LayerNormFunction(torch.autograd.Function):
         y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         total = None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
         stats = torch.empty((x2.shape[0], 2), dtype=torch.float32, device=x.device) if training else None
+        rest = None
+        if training and total is not None and weight is not None and weight.requires_grad and x.dtype == torch.bfloat16:
+            rest = torch.empty((x2.shape[0], x2.shape[1] // 8), dtype=torch.int32, device=x.device)
         if x.numel() > 0:
             with _on(x.device):
-                sk.check(sk.sk_layer_norm_fwd(_layer_norm_shape(x2, r2, eps), x2, r2, w, b, y, total, stats, _stream(x.device)))
-        ctx.save_for_backward(x2 if total is None else total, w, stats)
+                sk.check(sk.sk_layer_norm_fwd(_layer_norm_shape(x2, r2, eps), x2, r2, w, b, y, total, stats, _stream(x.device), rest))
+        ctx.save_for_backward(x2 if total is None else total, w, stats, rest)
         ctx.shape, ctx.bias = x.shape, bias is not None
         ctx.set_materialize_grads(False)
         return y if total is None else (y, total)
@@ -468,8 +471,8 @@ class LayerNormFunction(torch.autograd.Function):
     @staticmethod
     @_once
     def backward(ctx, dy, ds=None):
-        x, w, stats = ctx.saved_tensors
-        x, w, stats = _rows_of(x), _saved(w), _saved(stats)
+        x, *saved = ctx.saved_tensors
+        x, (w, stats, rest) = _rows_of(x), map(_saved, saved)
         dx = torch.empty(ctx.shape, dtype=x.dtype, device=x.device)
         dw, db = (torch.empty(ctx.shape[-1], dtype=x.dtype, device=x.device) if there else None for there in (w is not None, ctx.bias))
         if x.numel() == 0:
@@ -483,7 +486,7 @@ class LayerNormFunction(torch.autograd.Function):
         with _on(x.device), _queueing:
             stream = _stream(x.device)
             ws = _workspace(x.device, stream, sk.sk_layer_norm_workspace_bytes(shape))
-            sk.check(sk.sk_layer_norm_bwd(shape, x, w, stats, dy, ds, dx, dw, db, ws, ws.numel(), stream))
+            sk.check(sk.sk_layer_norm_bwd(shape, x, w, stats, dy, ds, dx, dw, db, ws, ws.numel(), stream, rest))
         return dx, dw, db, dx if ctx.needs_input_grad[3] else None, None, None
 
 

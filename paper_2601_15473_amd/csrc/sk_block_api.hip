@@ -182,7 +182,7 @@ struct DenseRoom {   // backward: dz | column sums | the products' slabs, one pr
   DenseRoom(const DenseArgs& a, bool f32) {
     partial = a.activation != SK_ACT_NONE ? align_up((size_t)a.tokens * a.out * (f32 ? 4 : 2)) : 0;
     dz = 0;
-    slabs = partial + align_up((size_t)DenseRuns(a.tokens, a.out).runs * a.out * 4);
+    slabs = partial + align_up((size_t)ColumnRuns(a.tokens, a.out).runs * a.out * 4);
     const size_t dx = product_bytes(GEMM_NN, a.tokens, a.in, a.out, f32), dw = product_bytes(GEMM_TN, a.out, a.in, a.tokens, f32);
     total = slabs + (dx > dw ? dx : dw);
   }
@@ -347,12 +347,13 @@ sk_status sk_dropout(const void* x, const void* residual, void* y, int64_t n, fl
 }
 
 sk_status sk_layer_norm_fwd(const sk_layer_norm_shape* shape, const void* x, const void* residual, const void* weight, const void* bias,
-                            void* y, void* sum, float* stats, void* stream) {
-  if (!x || !y || !aligned16(x, residual, weight, bias, y, sum, stats)) return SK_ERR_INVALID_ARG;
+                            void* y, void* sum, void* sum_rest, float* stats, void* stream) {
+  if (!x || !y || !aligned16(x, residual, weight, bias, y, sum, sum_rest, stats)) return SK_ERR_INVALID_ARG;
   LayerNormArgs a{};
   const sk_status st = layer_norm_args(shape, a);
   if (st != SK_OK) return st;
-  a.x = x; a.residual = residual; a.weight = weight; a.bias = bias; a.y = y; a.s = sum; a.stats = stats;
+  if (sum_rest && (!sum || shape->dtype == SK_F32)) return SK_ERR_INVALID_ARG;
+  a.x = x; a.residual = residual; a.weight = weight; a.bias = bias; a.y = y; a.s = sum; a.rest = static_cast<unsigned*>(sum_rest); a.stats = stats;
   return launched(launch_layer_norm_fwd(a, shape->dtype == SK_F32, static_cast<hipStream_t>(stream)), "sk_layer_norm_fwd");
 }
 
@@ -362,14 +363,15 @@ size_t sk_layer_norm_workspace_bytes(const sk_layer_norm_shape* shape) {
   return layer_norm_bytes(a);
 }
 
-sk_status sk_layer_norm_bwd(const sk_layer_norm_shape* shape, const void* x, const void* weight, const float* stats, const void* dy, const void* d_sum,
+sk_status sk_layer_norm_bwd(const sk_layer_norm_shape* shape, const void* x, const void* sum_rest, const void* weight, const float* stats, const void* dy, const void* d_sum,
                             void* dx, void* dweight, void* dbias, void* workspace, size_t workspace_bytes, void* stream) {
-  if (!x || !stats || !dy || !dx || !aligned16(x, weight, stats, dy, d_sum, dx, dweight, dbias, workspace)) return SK_ERR_INVALID_ARG;
+  if (!x || !stats || !dy || !dx || !aligned16(x, sum_rest, weight, stats, dy, d_sum, dx, dweight, dbias, workspace)) return SK_ERR_INVALID_ARG;
   LayerNormArgs a{};
   const sk_status st = layer_norm_args(shape, a);
   if (st != SK_OK) return st;
+  if (sum_rest && shape->dtype == SK_F32) return SK_ERR_INVALID_ARG;
   if ((dweight || dbias) && (!workspace || workspace_bytes < layer_norm_bytes(a))) return SK_ERR_WORKSPACE;
-  a.x = x; a.weight = weight; a.stats = const_cast<float*>(stats); a.dy = dy; a.ds = d_sum; a.dx = dx; a.dweight = dweight; a.dbias = dbias;
+  a.x = x; a.rest = static_cast<unsigned*>(const_cast<void*>(sum_rest)); a.weight = weight; a.stats = const_cast<float*>(stats); a.dy = dy; a.ds = d_sum; a.dx = dx; a.dweight = dweight; a.dbias = dbias;
   a.partial = dweight || dbias ? static_cast<float*>(workspace) : nullptr;
   return launched(launch_layer_norm_bwd(a, shape->dtype == SK_F32, static_cast<hipStream_t>(stream)), "sk_layer_norm_bwd");
 }

@@ -96,9 +96,23 @@ struct DropoutArgs {
 };
 hipError_t launch_dropout(const DropoutArgs& a, bool f32, hipStream_t s);
 
+// Runs of rows that column sums are formed in: of groups of 512 columns about four work-groups to a CU, 16 rows at least.  (Two, three and eight: a dense layer's dz of
+// 4096 x 4096 behind gelu 24.0, 20.8 and 19.2 us for 19.7, of 16384 x 11008 behind silu 265, 250 and 252 for 257; the sums' launch level.)
+struct ColumnRuns {
+  int groups, runs, rows;   // rows of a run
+  ColumnRuns(int64_t of_rows, int64_t columns) {
+    groups = (int)((columns + 511) / 512);
+    const int64_t wanted = (4 * NUM_CUS + groups - 1) / groups, most = (of_rows + 15) / 16;
+    const int64_t n = wanted < most ? wanted : most;
+    rows = (int)(((of_rows + n - 1) / n + 15) / 16 * 16);
+    runs = (int)((of_rows + rows - 1) / rows);
+  }
+};
+
 struct LayerNormArgs {
   const void *x, *residual, *weight, *bias;   // forward: x and the residual (or null); backward: x is what was normed
   void *y, *s;                                // forward: the result, and the sum (or null)
+  unsigned* rest;                             // [rows][width / 8] what a bf16 sum's rounding left off, or null: forward written, backward read
   float* stats;                               // [rows][mean, 1 / deviation]: forward written unless null, backward read
   const void *dy, *ds;                        // backward; ds or null
   void *dx, *dweight, *dbias;                 // backward; weights' or null
@@ -116,6 +130,7 @@ inline int layer_norm_lanes(int width) {
 // for their sum), but where a row is a work-group's not below eight rows each, down to one to a CU (2048 x 8192 33 + 4 : 39 + 7 : 51 + 12, 500 x 2048 6.5 + 3.0 : 8.0 + 5.0).
 inline int layer_norm_groups(int64_t rows, int width) {
   const int lanes = layer_norm_lanes(width), together = lanes < 256 ? 256 / lanes : 1;
+  if (lanes > 256) return ColumnRuns(rows, width).runs;   // (a launch of its own)
   const int64_t groups = (rows + together - 1) / together;
   int64_t most = 2 * NUM_CUS;
   if (together == 1 && rows / 8 < most) most = rows / 8 < NUM_CUS ? NUM_CUS : rows / 8;
@@ -152,18 +167,6 @@ struct DenseArgs {
   float* partial;                             // backward: [runs][out] sums of dz, null where dbias is not wanted
   int64_t x_stride, residual_stride;
   int tokens, in, out, activation;
-};
-// Runs of rows that dz's column sums are formed in: of groups of 512 columns about four work-groups to a CU, 16 rows at least.  (Two, three and eight: dz of 4096 x 4096 behind gelu
-// 24.0, 20.8 and 19.2 us for 19.7, of 16384 x 11008 behind silu 265, 250 and 252 for 257; the sums' launch level.)
-struct DenseRuns {
-  int groups, runs, rows;
-  DenseRuns(int64_t tokens, int64_t out) {
-    groups = (int)((out + 511) / 512);
-    const int64_t wanted = (4 * NUM_CUS + groups - 1) / groups, most = (tokens + 15) / 16;
-    const int64_t n = wanted < most ? wanted : most;
-    rows = (int)(((tokens + n - 1) / n + 15) / 16 * 16);
-    runs = (int)((tokens + rows - 1) / rows);
-  }
 };
 hipError_t launch_dense_finish(const DenseArgs& a, bool f32, hipStream_t s);
 hipError_t launch_dense_dz(const DenseArgs& a, bool f32, hipStream_t s);

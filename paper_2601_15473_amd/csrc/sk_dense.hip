@@ -129,7 +129,7 @@ template <typename T>
 hipError_t dz(const DenseArgs& a, hipStream_t s) {
   const bool act = a.activation != ACT_NONE;
   if (!act && !a.partial) return hipSuccess;
-  const DenseRuns r(a.tokens, a.out);
+  const ColumnRuns r(a.tokens, a.out);
   note_matrix(a.dy, a.tokens, a.out, a.out, sizeof(T), false);
   if (act) {
     note_matrix(a.z, a.tokens, a.out, a.out, sizeof(T), false);
@@ -145,7 +145,7 @@ hipError_t dz(const DenseArgs& a, hipStream_t s) {
 template <typename T>
 hipError_t dbias(const DenseArgs& a, hipStream_t s) {
   if (!a.partial) return hipSuccess;
-  const DenseRuns r(a.tokens, a.out);
+  const ColumnRuns r(a.tokens, a.out);
   note_matrix(a.partial, r.runs, a.out, a.out, 4, false);
   note_matrix(a.dbias, 1, a.out, a.out, sizeof(T), true);
   return launch_kernel("dense_dbias_kernel", Work{0.0, 4.0 * r.runs * a.out}, dense_dbias_kernel<T>, dim3((unsigned)((a.out + 31) / 32)), dim3(1024), s,

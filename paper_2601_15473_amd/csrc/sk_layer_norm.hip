@@ -4,10 +4,11 @@
 //   g = dy w,  dx = ds + r (g - mean g - u mean(g u)),  dw = sum dy u,  db = sum dy
 //
 // Bound by memory: a row is read once into registers, eight values to a lane and piece, and both of its sums are taken there (the mean first, the
-// squares about it second: a stream whose mean is large beside its spread loses nothing).  y is formed of the sum before s is rounded; the gradients take s as it was
-// stored, in the storage type, with the mean and deviation of the sum itself: keeping it in fp32 for them would be half as much again to write and read.
-// Bf16, 16383 rows of 4096 with a residual: forward 93 us for 537 MB (5.8 TB/s; a copy reaches 5.1), back 112 us for 537 MB (4.8) and 5 for the sum of the partial
-// sums; 4096 rows of 768 6.4, 9.7 and 3.8.  What carried it: every load of a row ahead of its first sum, the weights' among them (forward 99 -> 93, eight rows of 8192 6.4 -> 4.5), and the
+// squares about it second: a stream whose mean is large beside its spread loses nothing).  y is formed of the sum before s is rounded, and so are the gradients of the weights: s as it was
+// stored, off by up to 2^-9 of it, would make dw 0.0024 to 0.0027 off 64 bits where one rounding of an exact result is 0.0017.  Four bits more a value, a quarter of a tensor each way, leave
+// 2^-12 of it (s in fp32 would be a whole one).
+// Bf16, 16383 rows of 4096 with a residual: forward 94 us for 570 MB (6.1 TB/s; a copy reaches 5.1), back 120 us for 570 MB (4.8) and 5 for the sum of the partial
+// sums, of which the four bits are 6 and 8; 4096 rows of 768 8.1, 9.4 and 3.7.  What carried it: every load of a row ahead of its first sum, the weights' among them (forward 99 -> 93, eight rows of 8192 6.4 -> 4.5), and the
 // next row's loads under this one's sums (back 180 -> 112).
 #include "sk_block_launch.h"
 #include "sk_rows.h"
@@ -16,6 +17,28 @@ namespace sk {
 namespace {
 
 constexpr int PIECE = 8;   // values
+
+// What a piece's rounding to bf16 left off, in 16ths of a step, four bits a value (the far half of a step is 8 of them: one less).  On the numbers' bits: a step
+// of the magnitude is one of the bits, across powers of two too, so that the fp32 bits less the rounded ones are what was left, and adding them gives it back.
+__device__ __forceinline__ unsigned rest_of(const float (&v)[PIECE]) {
+  unsigned rest = 0;
+#pragma unroll
+  for (int i = 0; i < PIECE; i += 2) {
+    const unsigned rounded = pack_bf16x2(v[i], v[i + 1]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int left = (int)(__builtin_bit_cast(unsigned, v[i + h]) - (h ? rounded & 0xffff0000u : rounded << 16));
+      const int q = (left + 0x800) >> 12;
+      rest |= (unsigned)((q < -8 ? -8 : q > 7 ? 7 : q) & 15) << (4 * (i + h));
+    }
+  }
+  return rest;
+}
+__device__ __forceinline__ void add_rest(float (&v)[PIECE], unsigned rest) {
+#pragma unroll
+  for (int i = 0; i < PIECE; ++i)
+    v[i] = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, v[i]) + ((unsigned)((int)(rest << (28 - 4 * i)) >> 28) << 12));
+}
 
 // The sum of a row's lanes, L of a wave or all of a work-group's (`shared`: a float a wave, another place for each sum).  Every lane gets it.
 template <int L>
@@ -110,6 +133,8 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_fwd_kernel(const
     const int at = (n * L + lane) * PIECE;
     if (at >= p.width) continue;
     if (p.s) store_values<T, PIECE>(static_cast<T*>(p.s) + row * p.width + at, v[n]);
+    if constexpr (sizeof(T) == 2)
+      if (p.rest) p.rest[(row * p.width + at) / PIECE] = rest_of(v[n]);
     float w[PIECE], b[PIECE], y[PIECE];
 #pragma unroll
     for (int i = 0; i < PIECE; ++i) { w[i] = 1.f; b[i] = 0.f; }
@@ -122,28 +147,35 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_fwd_kernel(const
 }
 
 // Gradients: work-groups walk over the rows with their lanes' terms of dw and db in registers, and leave one row of each, [group][dw, db][width].
-// What the next row needs is on its way while this one's sums are formed.
-template <typename T, int L, int N, bool SUM>
+// What the next row needs is on its way while this one's sums are formed.  Where a row takes 1024 lanes, there are 128 registers a lane, and the terms' sums do not fit beside the row: those
+// rows are a work-group each, and the weights' gradients have a launch that reads s and dy again (with all of it in one, spilled, 4096 rows of 16384 302 us for 119 + 72,
+// 2048 of 32768 814 for 132 + 71).
+template <typename T, int L, int N, bool SUM, bool REST>
 __global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_bwd_kernel(const LayerNormArgs p) {
   constexpr int THREADS = L > 256 ? L : 256, ROWS = THREADS / L, WAVES = L > 64 ? L / 64 : 1;
+  constexpr bool WIDE = L > 256;
   __shared__ float shared[2][2 * WAVES];
   __shared__ float rows[ROWS > 1 ? THREADS * N * PIECE : 1];
   const int lane = threadIdx.x % L, sub = threadIdx.x / L;
-  float dw[N][PIECE], db[N][PIECE];
+  float dw[WIDE ? 1 : N][PIECE], db[WIDE ? 1 : N][PIECE];
   Raw<T, N> weight;
   if (p.weight) weight.template load<L>(static_cast<const T*>(p.weight), lane, p.width);
 #pragma unroll
-  for (int n = 0; n < N; ++n)
+  for (int n = 0; n < (WIDE ? 1 : N); ++n)
 #pragma unroll
     for (int i = 0; i < PIECE; ++i) dw[n][i] = db[n][i] = 0.f;
   struct Row {
     Raw<T, N> s, dy, ds;
+    unsigned rest[N];
     float2 stat;
   };
   auto fetch = [&](Row& r, int64_t row) {   // (past the last row: it again, for nothing)
     const int64_t at = row < p.rows ? row : p.rows - 1;
     r.stat = *reinterpret_cast<const float2*>(p.stats + at * 2);
     r.s.template load<L>(static_cast<const T*>(p.x) + at * p.x_stride, lane, p.width);
+    if constexpr (REST)
+#pragma unroll
+      for (int n = 0; n < N; ++n) r.rest[n] = (n * L + lane) * PIECE < p.width ? p.rest[at * (p.width / PIECE) + n * L + lane] : 0u;
     r.dy.template load<L>(static_cast<const T*>(p.dy) + at * p.width, lane, p.width);
     if constexpr (SUM) r.ds.template load<L>(static_cast<const T*>(p.ds) + at * p.width, lane, p.width);
   };
@@ -159,13 +191,16 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_bwd_kernel(const
       for (int i = 0; i < PIECE; ++i) w[i] = 1.f;
       if (p.weight) weight.values(w, n);
       r.s.values(u[n], n);
+      if constexpr (REST) add_rest(u[n], r.rest[n]);
       r.dy.values(g[n], n);
 #pragma unroll
       for (int i = 0; i < PIECE; ++i) {
         u[n][i] = in ? (u[n][i] - r.stat.x) * r.stat.y : 0.f;
         const float d = in ? g[n][i] : 0.f;
-        dw[n][i] += d * u[n][i];
-        db[n][i] += d;
+        if constexpr (!WIDE) {
+          dw[n][i] += d * u[n][i];
+          db[n][i] += d;
+        }
         g[n][i] = d * w[i];
         sums[0] += g[n][i];
         sums[1] += g[n][i] * u[n][i];
@@ -205,42 +240,98 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_bwd_kernel(const
     }
   };
   const int64_t step = (int64_t)gridDim.x * ROWS;
-  Row here, next;
   int64_t row = (int64_t)blockIdx.x * ROWS + sub;
-  fetch(here, row);
-  for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < p.rows; row0 += 2 * step) {
-    fetch(next, row + step);
+  Row here;
+  if constexpr (WIDE) {   // a row to a work-group
+    fetch(here, row);
     one(here, row);
-    if (row0 + step >= p.rows) break;
-    fetch(here, row + 2 * step);
-    one(next, row + step);
-    row += 2 * step;
+    return;
+  } else {
+    Row next;
+    fetch(here, row);
+    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < p.rows; row0 += 2 * step) {
+      fetch(next, row + step);
+      one(here, row);
+      if (row0 + step >= p.rows) break;
+      fetch(here, row + 2 * step);
+      one(next, row + step);
+      row += 2 * step;
+    }
   }
-  if (!p.partial) return;
-  float* const out = p.partial + (int64_t)blockIdx.x * 2 * p.width;
+  if constexpr (!WIDE) {
+    if (!p.partial) return;
+    float* const out = p.partial + (int64_t)blockIdx.x * 2 * p.width;
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    float (&d)[N][PIECE] = which ? db : dw;
-    if constexpr (ROWS > 1) {   // the rows side by side, added in their order
-      __syncthreads();
+    for (int which = 0; which < 2; ++which) {
+      float (&d)[N][PIECE] = which ? db : dw;
+      if constexpr (ROWS > 1) {   // the rows side by side, added in their order
+        __syncthreads();
 #pragma unroll
-      for (int n = 0; n < N; ++n)
+        for (int n = 0; n < N; ++n)
 #pragma unroll
-        for (int i = 0; i < PIECE; ++i) rows[sub * (L * N * PIECE) + (n * L + lane) * PIECE + i] = d[n][i];
-      __syncthreads();
-      for (int c = threadIdx.x; c < p.width; c += THREADS) {
-        float t = 0.f;
+          for (int i = 0; i < PIECE; ++i) rows[sub * (L * N * PIECE) + (n * L + lane) * PIECE + i] = d[n][i];
+        __syncthreads();
+        for (int c = threadIdx.x; c < p.width; c += THREADS) {
+          float t = 0.f;
 #pragma unroll
-        for (int q = 0; q < ROWS; ++q) t += rows[q * (L * N * PIECE) + c];
-        out[which * p.width + c] = t;
-      }
-    } else {
+          for (int q = 0; q < ROWS; ++q) t += rows[q * (L * N * PIECE) + c];
+          out[which * p.width + c] = t;
+        }
+      } else {
 #pragma unroll
-      for (int n = 0; n < N; ++n) {
-        const int at = (n * L + lane) * PIECE;
-        if (at < p.width) store_values<float, PIECE>(out + which * p.width + at, d[n]);
+        for (int n = 0; n < N; ++n) {
+          const int at = (n * L + lane) * PIECE;
+          if (at < p.width) store_values<float, PIECE>(out + which * p.width + at, d[n]);
+        }
       }
     }
+  }
+}
+
+// The weights' gradients of wide rows: a work-group has 512 columns (eight a lane) of a run of rows, its four waves every fourth row each, their sums joined in the waves' order.
+template <typename T, bool REST>
+__global__ __launch_bounds__(256) void layer_norm_columns_kernel(const LayerNormArgs p, int rows_per_run) {
+  constexpr int AHEAD = 4;
+  __shared__ float part[2][4][512];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = blockIdx.x * 512 + lane * PIECE;
+  const int64_t begin = (int64_t)blockIdx.y * rows_per_run, end = begin + rows_per_run < p.rows ? begin + rows_per_run : p.rows;
+  float dw[PIECE], db[PIECE];
+#pragma unroll
+  for (int i = 0; i < PIECE; ++i) dw[i] = db[i] = 0.f;
+  if (at < p.width)
+    for (int64_t row = begin + wave; row < end; row += 4 * AHEAD) {
+      float s[AHEAD][PIECE], d[AHEAD][PIECE];
+      float2 stat[AHEAD];
+      unsigned rest[AHEAD];
+#pragma unroll
+      for (int a = 0; a < AHEAD; ++a) {   // (past the run: its last row again, for nothing)
+        const int64_t r = row + 4 * a < end ? row + 4 * a : end - 1;
+        load_values<T, PIECE>(s[a], static_cast<const T*>(p.x) + r * p.x_stride + at);
+        load_values<T, PIECE>(d[a], static_cast<const T*>(p.dy) + r * p.width + at);
+        stat[a] = *reinterpret_cast<const float2*>(p.stats + r * 2);
+        if constexpr (REST) rest[a] = p.rest[(r * p.width + at) / PIECE];
+      }
+#pragma unroll
+      for (int a = 0; a < AHEAD; ++a) {
+        if (row + 4 * a >= end) break;
+        if constexpr (REST) add_rest(s[a], rest[a]);
+#pragma unroll
+        for (int i = 0; i < PIECE; ++i) {
+          dw[i] += d[a][i] * ((s[a][i] - stat[a].x) * stat[a].y);
+          db[i] += d[a][i];
+        }
+      }
+    }
+#pragma unroll
+  for (int i = 0; i < PIECE; ++i) {
+    part[0][wave][lane * PIECE + i] = dw[i];
+    part[1][wave][lane * PIECE + i] = db[i];
+  }
+  __syncthreads();
+  for (int c = threadIdx.x; c < 1024; c += 256) {
+    const int which = c >> 9, column = blockIdx.x * 512 + (c & 511);
+    const float(&of)[4][512] = part[which];
+    if (column < p.width) p.partial[((int64_t)blockIdx.y * 2 + which) * p.width + column] = ((of[0][c & 511] + of[1][c & 511]) + of[2][c & 511]) + of[3][c & 511];
   }
 }
 
@@ -278,6 +369,7 @@ hipError_t fwd(const LayerNormArgs& a, hipStream_t s) {
   note_matrix(a.bias, 1, a.width, a.width, sizeof(T), false);
   note_matrix(a.y, a.rows, a.width, a.width, sizeof(T), true);
   note_matrix(a.s, a.rows, a.width, a.width, sizeof(T), true);
+  note_matrix(a.rest, a.rows, a.width / PIECE, a.width / PIECE, 4, true);
   note_matrix(a.stats, a.rows, 2, 2, 4, true);
   const int tensors = 2 + (a.residual != nullptr) + (a.s != nullptr);
   return launch_kernel("layer_norm_fwd_kernel", Work{8 * values_of(a), tensors * values_of(a) * sizeof(T)}, layer_norm_fwd_kernel<T, L, N>,
@@ -289,15 +381,32 @@ hipError_t bwd(const LayerNormArgs& a, hipStream_t s) {
   constexpr int THREADS = L > 256 ? L : 256;
   const int groups = layer_norm_groups(a.rows, a.width);
   note_matrix(a.x, a.rows, a.width, a.x_stride, sizeof(T), false);
+  note_matrix(a.rest, a.rows, a.width / PIECE, a.width / PIECE, 4, false);
   note_matrix(a.weight, 1, a.width, a.width, sizeof(T), false);
   note_matrix(a.stats, a.rows, 2, 2, 4, false);
   note_matrix(a.dy, a.rows, a.width, a.width, sizeof(T), false);
   note_matrix(a.ds, a.rows, a.width, a.width, sizeof(T), false);
   note_matrix(a.dx, a.rows, a.width, a.width, sizeof(T), true);
-  note_matrix(a.partial, groups, 2 * a.width, 2 * a.width, 4, true);
-  const hipError_t e = launch_kernel("layer_norm_bwd_kernel", Work{14 * values_of(a), (a.ds ? 4 : 3) * values_of(a) * sizeof(T)},
-                                     a.ds ? layer_norm_bwd_kernel<T, L, N, true> : layer_norm_bwd_kernel<T, L, N, false>, dim3(groups), dim3(THREADS), s, a);
+  if (L <= 256) note_matrix(a.partial, groups, 2 * a.width, 2 * a.width, 4, true);
+  auto kernel = a.ds ? layer_norm_bwd_kernel<T, L, N, true, false> : layer_norm_bwd_kernel<T, L, N, false, false>;
+  if constexpr (sizeof(T) == 2)
+    if (a.rest) kernel = a.ds ? layer_norm_bwd_kernel<T, L, N, true, true> : layer_norm_bwd_kernel<T, L, N, false, true>;
+  hipError_t e = launch_kernel("layer_norm_bwd_kernel", Work{14 * values_of(a), ((a.ds ? 4 : 3) * sizeof(T) + (a.rest ? 0.5 : 0.0)) * values_of(a)},
+                               kernel, dim3(L > 256 ? (unsigned)a.rows : groups), dim3(THREADS), s, a);
   if (e != hipSuccess || !a.partial) return e;
+  if constexpr (L > 256) {
+    const ColumnRuns r(a.rows, a.width);
+    note_matrix(a.x, a.rows, a.width, a.x_stride, sizeof(T), false);
+    note_matrix(a.rest, a.rows, a.width / PIECE, a.width / PIECE, 4, false);
+    note_matrix(a.dy, a.rows, a.width, a.width, sizeof(T), false);
+    note_matrix(a.stats, a.rows, 2, 2, 4, false);
+    note_matrix(a.partial, groups, 2 * a.width, 2 * a.width, 4, true);
+    auto columns = layer_norm_columns_kernel<T, false>;
+    if constexpr (sizeof(T) == 2)
+      if (a.rest) columns = layer_norm_columns_kernel<T, true>;
+    e = launch_kernel("layer_norm_columns_kernel", Work{5 * values_of(a), (2 * sizeof(T) + (a.rest ? 0.5 : 0.0)) * values_of(a)}, columns, dim3((unsigned)r.groups, (unsigned)r.runs), dim3(256), s, a, r.rows);
+    if (e != hipSuccess) return e;
+  }
   note_matrix(a.partial, groups, 2 * a.width, 2 * a.width, 4, false);
   note_matrix(a.dweight, 1, a.width, a.width, sizeof(T), true);
   note_matrix(a.dbias, 1, a.width, a.width, sizeof(T), true);

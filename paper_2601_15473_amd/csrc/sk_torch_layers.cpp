@@ -57,12 +57,13 @@ sk_layer_norm_shape norm_shape(const Tensor& x, const Tensor& residual, double e
   return s;
 }
 
-variable_list norm_forward(const Tensor& x, const Tensor& weight, const Tensor& bias, const Tensor& residual, const sk_layer_norm_shape& s, Tensor* stats) {
+variable_list norm_forward(const Tensor& x, const Tensor& weight, const Tensor& bias, const Tensor& residual, const sk_layer_norm_shape& s, Tensor* stats, Tensor* rest) {
   const c10::DeviceGuard guard(x.device());
   Tensor y = at::empty(x.sizes(), x.options()), sum;
   if (residual.defined()) sum = at::empty(x.sizes(), x.options());
   if (stats) *stats = at::empty({s.rows, 2}, x.options().dtype(at::kFloat));
-  check(sk_layer_norm_fwd(&s, x.data_ptr(), data(residual), data(weight), data(bias), y.data_ptr(), data(sum), stats ? stats->data_ptr<float>() : nullptr, stream_of(x.device())));
+  if (rest && s.dtype == SK_BF16) *rest = at::empty({s.rows, s.width / 8}, x.options().dtype(at::kInt));
+  check(sk_layer_norm_fwd(&s, x.data_ptr(), data(residual), data(weight), data(bias), y.data_ptr(), data(sum), rest ? data(*rest) : nullptr, stats ? stats->data_ptr<float>() : nullptr, stream_of(x.device())));
   return residual.defined() ? variable_list{y, sum} : variable_list{y};
 }
 
@@ -70,9 +71,9 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
   static variable_list forward(AutogradContext* ctx, const Tensor& x, const std::optional<Tensor>& weight, const std::optional<Tensor>& bias, const std::optional<Tensor>& residual,
                                double eps) {
     const Tensor w = weight.value_or(Tensor()), r = residual.value_or(Tensor());
-    Tensor stats;
-    const variable_list out = norm_forward(x, w, bias.value_or(Tensor()), r, norm_shape(x, r, eps), &stats);
-    ctx->save_for_backward({r.defined() ? out[1] : x, w, stats});
+    Tensor stats, rest;
+    const variable_list out = norm_forward(x, w, bias.value_or(Tensor()), r, norm_shape(x, r, eps), &stats, r.defined() && wants(weight) ? &rest : nullptr);
+    ctx->save_for_backward({r.defined() ? out[1] : x, w, stats, rest});
     ctx->saved_data["wanted"] = wanted(x, weight, bias, residual);
     ctx->saved_data["bias"] = bias.has_value();
     ctx->saved_data["residual"] = r.defined();
@@ -91,7 +92,7 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
   static variable_list gradients(AutogradContext* ctx, const variable_list& grads, bool all) {
     const variable_list saved = ctx->get_saved_variables();
     const c10::DeviceGuard guard(saved[0].device());
-    const Tensor x = saved_rows(saved[0], 0, (int64_t)1 << 40), w = saved_dense(saved[1]), stats = saved_dense(saved[2]);
+    const Tensor x = saved_rows(saved[0], 0, (int64_t)1 << 40), w = saved_dense(saved[1]), stats = saved_dense(saved[2]), rest = saved_dense(saved[3]);
     const Tensor dy = grads[0].defined() ? made_dense(grads[0]) : at::zeros(x.sizes(), x.options());
     const Tensor ds = grads.size() > 1 && grads[1].defined() ? made_dense(grads[1]) : Tensor();
     const sk_layer_norm_shape s = norm_shape(x, Tensor(), 0.0);
@@ -101,7 +102,7 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
     const Tensor dw = w.defined() && (all || (want & WANT_WEIGHT)) ? at::empty({s.width}, x.options()) : none;
     const Tensor db = ctx->saved_data["bias"].toBool() && (all || (want & WANT_BIAS)) ? at::empty({s.width}, x.options()) : none;
     with_workspace(x, sk_layer_norm_workspace_bytes(&s), [&](void* ws, size_t n, void* stream) {
-      return sk_layer_norm_bwd(&s, x.data_ptr(), data(w), stats.data_ptr<float>(), dy.data_ptr(), data(ds), dx.data_ptr(), data(dw), data(db), ws, n, stream);
+      return sk_layer_norm_bwd(&s, x.data_ptr(), data(rest), data(w), stats.data_ptr<float>(), dy.data_ptr(), data(ds), dx.data_ptr(), data(dw), data(db), ws, n, stream);
     });
     return {dx, dw, db};
   }
@@ -253,7 +254,7 @@ PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (at::GradMode::is_enabled() && (x->requires_grad() || wants(given(weight)) || wants(given(bias)) || wants(given(residual))))
       out = LayerNorm::apply(*x, given(weight), given(bias), given(residual), eps);
     else
-      out = norm_forward(*x, weight, bias, residual, s, nullptr);
+      out = norm_forward(*x, weight, bias, residual, s, nullptr, nullptr);
   }
   return wrapped(std::move(out));
   END_HANDLE_TH_ERRORS

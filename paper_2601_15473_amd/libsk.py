@@ -123,9 +123,9 @@ for _name, _restype, _argtypes in (
         ("sk_embedding_workspace_bytes", _sz, [_i64, _i64, _i64, ctypes.c_int]),
         ("sk_embedding_bwd", ctypes.c_int, [_vp, _i32, _vp, _vp, _i64, _i64, _i64, _f32, ctypes.c_int, _vp, _sz, _vp]),
         ("sk_dropout", ctypes.c_int, [_vp, _vp, _vp, _i64, _f32, _u64, _u64, ctypes.c_int, _vp]),
-        ("sk_layer_norm_fwd", ctypes.c_int, [_layer_norm_shape] + [_vp] * 8),
+        ("sk_layer_norm_fwd", ctypes.c_int, [_layer_norm_shape] + [_vp] * 9),
         ("sk_layer_norm_workspace_bytes", _sz, [_layer_norm_shape]),
-        ("sk_layer_norm_bwd", ctypes.c_int, [_layer_norm_shape] + [_vp] * 9 + [_sz, _vp]),
+        ("sk_layer_norm_bwd", ctypes.c_int, [_layer_norm_shape] + [_vp] * 10 + [_sz, _vp]),
         ("sk_dense_workspace_bytes", _sz, [_dense_shape, _i32]),
         ("sk_dense_fwd", ctypes.c_int, [_dense_shape] + [_vp] * 7 + [_sz, _vp]),
         ("sk_dense_bwd", ctypes.c_int, [_dense_shape] + [_vp] * 8 + [_sz, _vp]),
@@ -309,16 +309,16 @@ def sk_dropout(x, residual, y, n, p, seed, offset, dtype, stream=None):
     return _lib.sk_dropout(_ptr(x), _ptr(residual), _ptr(y), n, p, seed, offset, dtype, _stream(stream))
 
 
-def sk_layer_norm_fwd(shape, x, residual, weight, bias, y, sum, stats, stream=None):
-    return _lib.sk_layer_norm_fwd(shape, _ptr(x), _ptr(residual), _ptr(weight), _ptr(bias), _ptr(y), _ptr(sum), _ptr(stats), _stream(stream))
+def sk_layer_norm_fwd(shape, x, residual, weight, bias, y, sum, stats, stream=None, sum_rest=None):
+    return _lib.sk_layer_norm_fwd(shape, _ptr(x), _ptr(residual), _ptr(weight), _ptr(bias), _ptr(y), _ptr(sum), _ptr(sum_rest), _ptr(stats), _stream(stream))
 
 
 def sk_layer_norm_workspace_bytes(shape):
     return _lib.sk_layer_norm_workspace_bytes(shape)
 
 
-def sk_layer_norm_bwd(shape, x, weight, stats, dy, d_sum, dx, dweight, dbias, workspace, workspace_bytes, stream=None):
-    return _lib.sk_layer_norm_bwd(shape, _ptr(x), _ptr(weight), _ptr(stats), _ptr(dy), _ptr(d_sum), _ptr(dx), _ptr(dweight), _ptr(dbias),
+def sk_layer_norm_bwd(shape, x, weight, stats, dy, d_sum, dx, dweight, dbias, workspace, workspace_bytes, stream=None, sum_rest=None):
+    return _lib.sk_layer_norm_bwd(shape, _ptr(x), _ptr(sum_rest), _ptr(weight), _ptr(stats), _ptr(dy), _ptr(d_sum), _ptr(dx), _ptr(dweight), _ptr(dbias),
                                   _ptr(workspace), workspace_bytes, _stream(stream))
 
 

@@ -57,6 +57,11 @@ def test_layer_norm_pointers_and_workspace():
         assert i not in (0, 2, 3, 5) or sk.sk_layer_norm_bwd(s, *args, P, BIG) == sk.SK_ERR_INVALID_ARG, i
     assert sk.sk_layer_norm_bwd(s, *(P,) * 8, P, need - 1) == sk.sk_layer_norm_bwd(s, *(P,) * 8, None, 0) == sk.SK_ERR_WORKSPACE
     assert sk.sk_layer_norm_fwd(None, *(P,) * 7) == sk.SK_ERR_INVALID_ARG
+    # what a sum's rounding left off: of a sum, in bf16, from a boundary on
+    assert sk.sk_layer_norm_fwd(s, *(P,) * 5, None, P, sum_rest=P) == sk.SK_ERR_INVALID_ARG
+    assert sk.sk_layer_norm_fwd(s, *(P,) * 7, sum_rest=P + 4) == sk.sk_layer_norm_bwd(s, *(P,) * 8, P, BIG, sum_rest=P + 4) == sk.SK_ERR_INVALID_ARG
+    f32 = norm_shape(dtype=sk.SK_F32)
+    assert sk.sk_layer_norm_fwd(f32, *(P,) * 7, sum_rest=P) == sk.sk_layer_norm_bwd(f32, *(P,) * 8, P, BIG, sum_rest=P) == sk.SK_ERR_INVALID_ARG
 
 
 @pytest.mark.parametrize("change, want", [
@@ -134,13 +139,15 @@ def test_layer_norm_accesses(rows, width, dtype, e):
         w, b, y, stats = buf.new(width * e), buf.new(width * e), buf.new(rows * width * e, both=True), buf.new(rows * 8, both=True)
         total = buf.new(rows * width * e, both=True) if residual else None
         buf.check(traced(lambda: sk.sk_layer_norm_fwd(s, x, r, w, b, y, total, stats))[0])
+        rest = buf.new(rows * width // 2, both=True) if residual and dtype == sk.SK_BF16 else None
+        buf.check(traced(lambda: sk.sk_layer_norm_fwd(s, x, r, w, b, y, total, stats, sum_rest=rest))[0])
         need = sk.sk_layer_norm_workspace_bytes(s)
         dy, ds = buf.new(rows * width * e), buf.new(rows * width * e) if residual else None
         out = buf.new(rows * width * e, write=True), buf.new(width * e, write=True), buf.new(width * e, write=True)
         ws = buf.new(need, both=True)
-        accesses, launches = traced(lambda: sk.sk_layer_norm_bwd(s, x, w, stats, dy, ds, *out, ws, need))
+        accesses, launches = traced(lambda: sk.sk_layer_norm_bwd(s, x, w, stats, dy, ds, *out, ws, need, sum_rest=rest))
         buf.check(accesses)
-        assert launches == 2 and traced(lambda: sk.sk_layer_norm_bwd(s, x, w, stats, dy, ds, out[0], None, None, None, 0))[1] == 1
+        assert launches == (2 if width <= 8192 else 3) and traced(lambda: sk.sk_layer_norm_bwd(s, x, w, stats, dy, ds, out[0], None, None, None, 0))[1] == 1
 
 
 def _dense_accesses(tokens, d_in, d_out, dtype, e, act, x_stride):
