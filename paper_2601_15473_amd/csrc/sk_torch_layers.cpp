@@ -8,10 +8,11 @@ namespace sk_torch {
 namespace {
 
 // Which inputs' gradients a backward pass forms: those that had one at the forward pass; where a graph of it is made, every one (a function's results are all there).
-enum Wanted : int64_t { WANT_X = 1, WANT_WEIGHT = 2, WANT_BIAS = 4, WANT_RESIDUAL = 8 };
+// (With them, in one number: what else there was, and a dense layer's activation.)
+enum Wanted : int64_t { WANT_X = 1, WANT_WEIGHT = 2, WANT_BIAS = 4, WANT_RESIDUAL = 8, HAS_BIAS = 16, HAS_REST = 32, ACTIVATION = 256 };
 bool wants(const std::optional<Tensor>& t) { return t.has_value() && t->requires_grad(); }
 int64_t wanted(const Tensor& x, const std::optional<Tensor>& weight, const std::optional<Tensor>& bias, const std::optional<Tensor>& residual) {
-  return (x.requires_grad() ? WANT_X : 0) | (wants(weight) ? WANT_WEIGHT : 0) | (wants(bias) ? WANT_BIAS : 0) | (wants(residual) ? WANT_RESIDUAL : 0);
+  return (x.requires_grad() ? WANT_X : 0) | (wants(weight) ? WANT_WEIGHT : 0) | (wants(bias) ? WANT_BIAS : 0) | (wants(residual) ? WANT_RESIDUAL : 0) | (bias.has_value() ? HAS_BIAS : 0);
 }
 
 // Rows that the library takes in place: of a dense tensor, or of a matrix with a stride between them.
@@ -57,13 +58,16 @@ sk_layer_norm_shape norm_shape(const Tensor& x, const Tensor& residual, double e
   return s;
 }
 
-variable_list norm_forward(const Tensor& x, const Tensor& weight, const Tensor& bias, const Tensor& residual, const sk_layer_norm_shape& s, Tensor* stats, Tensor* rest) {
+// What a sum's rounding left off stands behind the rows' statistics, from a boundary on: the values ahead of it.
+int64_t rest_at(const sk_layer_norm_shape& s) { return (s.rows + 1) / 2 * 4; }
+
+variable_list norm_forward(const Tensor& x, const Tensor& weight, const Tensor& bias, const Tensor& residual, const sk_layer_norm_shape& s, Tensor* stats, bool rest) {
   const c10::DeviceGuard guard(x.device());
   Tensor y = at::empty(x.sizes(), x.options()), sum;
   if (residual.defined()) sum = at::empty(x.sizes(), x.options());
-  if (stats) *stats = at::empty({s.rows, 2}, x.options().dtype(at::kFloat));
-  if (rest && s.dtype == SK_BF16) *rest = at::empty({s.rows, s.width / 8}, x.options().dtype(at::kInt));
-  check(sk_layer_norm_fwd(&s, x.data_ptr(), data(residual), data(weight), data(bias), y.data_ptr(), data(sum), rest ? data(*rest) : nullptr, stats ? stats->data_ptr<float>() : nullptr, stream_of(x.device())));
+  if (stats) *stats = at::empty({rest ? rest_at(s) + s.rows * (s.width / 8) : s.rows * 2}, x.options().dtype(at::kFloat));
+  float* const kept = stats ? stats->data_ptr<float>() : nullptr;
+  check(sk_layer_norm_fwd(&s, x.data_ptr(), data(residual), data(weight), data(bias), y.data_ptr(), data(sum), rest ? kept + rest_at(s) : nullptr, kept, stream_of(x.device())));
   return residual.defined() ? variable_list{y, sum} : variable_list{y};
 }
 
@@ -71,38 +75,36 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
   static variable_list forward(AutogradContext* ctx, const Tensor& x, const std::optional<Tensor>& weight, const std::optional<Tensor>& bias, const std::optional<Tensor>& residual,
                                double eps) {
     const Tensor w = weight.value_or(Tensor()), r = residual.value_or(Tensor());
-    Tensor stats, rest;
-    const variable_list out = norm_forward(x, w, bias.value_or(Tensor()), r, norm_shape(x, r, eps), &stats, r.defined() && wants(weight) ? &rest : nullptr);
-    ctx->save_for_backward({r.defined() ? out[1] : x, w, stats, rest});
-    ctx->saved_data["wanted"] = wanted(x, weight, bias, residual);
-    ctx->saved_data["bias"] = bias.has_value();
-    ctx->saved_data["residual"] = r.defined();
+    Tensor stats;
+    const bool rest = r.defined() && wants(weight) && x.scalar_type() == at::kBFloat16;
+    const variable_list out = norm_forward(x, w, bias.value_or(Tensor()), r, norm_shape(x, r, eps), &stats, rest);
+    ctx->save_for_backward({r.defined() ? out[1] : x, w, stats});
+    ctx->saved_data["wanted"] = wanted(x, weight, bias, residual) | (rest ? HAS_REST : 0);
     ctx->set_materialize_grads(false);
     return out;
   }
 
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
     const bool all = at::GradMode::is_enabled();   // (off inside)
-    const variable_list out = once([&] { return gradients(ctx, grads, all); });
     const int64_t want = ctx->saved_data["wanted"].toInt();
-    const bool residual = ctx->saved_data["residual"].toBool();
-    return {want & WANT_X ? out[0] : Tensor(), want & WANT_WEIGHT ? out[1] : Tensor(), want & WANT_BIAS ? out[2] : Tensor(), residual && (want & WANT_RESIDUAL) ? out[0] : Tensor(), Tensor()};
+    const variable_list out = once([&] { return gradients(ctx, grads, want, all); });
+    return {want & WANT_X ? out[0] : Tensor(), want & WANT_WEIGHT ? out[1] : Tensor(), want & WANT_BIAS ? out[2] : Tensor(), want & WANT_RESIDUAL ? out[0] : Tensor(), Tensor()};
   }
 
-  static variable_list gradients(AutogradContext* ctx, const variable_list& grads, bool all) {
+  static variable_list gradients(AutogradContext* ctx, const variable_list& grads, int64_t want, bool all) {
     const variable_list saved = ctx->get_saved_variables();
     const c10::DeviceGuard guard(saved[0].device());
-    const Tensor x = saved_rows(saved[0], 0, (int64_t)1 << 40), w = saved_dense(saved[1]), stats = saved_dense(saved[2]), rest = saved_dense(saved[3]);
+    const Tensor x = saved_rows(saved[0], 0, (int64_t)1 << 40), w = saved_dense(saved[1]), stats = saved_dense(saved[2]);
     const Tensor dy = grads[0].defined() ? made_dense(grads[0]) : at::zeros(x.sizes(), x.options());
     const Tensor ds = grads.size() > 1 && grads[1].defined() ? made_dense(grads[1]) : Tensor();
     const sk_layer_norm_shape s = norm_shape(x, Tensor(), 0.0);
-    const int64_t want = ctx->saved_data["wanted"].toInt();
+    float* const kept = stats.data_ptr<float>();
     const Tensor none = all ? at::zeros({0}, x.options()) : Tensor();
     const Tensor dx = at::empty(x.sizes(), x.options());
     const Tensor dw = w.defined() && (all || (want & WANT_WEIGHT)) ? at::empty({s.width}, x.options()) : none;
-    const Tensor db = ctx->saved_data["bias"].toBool() && (all || (want & WANT_BIAS)) ? at::empty({s.width}, x.options()) : none;
+    const Tensor db = (want & HAS_BIAS) && (all || (want & WANT_BIAS)) ? at::empty({s.width}, x.options()) : none;
     with_workspace(x, sk_layer_norm_workspace_bytes(&s), [&](void* ws, size_t n, void* stream) {
-      return sk_layer_norm_bwd(&s, x.data_ptr(), data(rest), data(w), stats.data_ptr<float>(), dy.data_ptr(), data(ds), dx.data_ptr(), data(dw), data(db), ws, n, stream);
+      return sk_layer_norm_bwd(&s, x.data_ptr(), want & HAS_REST ? kept + rest_at(s) : nullptr, data(w), kept, dy.data_ptr(), data(ds), dx.data_ptr(), data(dw), data(db), ws, n, stream);
     });
     return {dx, dw, db};
   }
@@ -136,9 +138,7 @@ struct Dense : torch::autograd::Function<Dense> {
     Tensor z;
     const Tensor y = layer_forward(x, weight, bias.value_or(Tensor()), r, layer_shape(x, weight, r, activation), &z);
     ctx->save_for_backward({x, weight, z});
-    ctx->saved_data["wanted"] = wanted(x, weight, bias, residual);
-    ctx->saved_data["bias"] = bias.has_value();
-    ctx->saved_data["activation"] = activation;
+    ctx->saved_data["wanted"] = wanted(x, weight, bias, residual) | activation * ACTIVATION;
     return y;
   }
 
@@ -146,21 +146,20 @@ struct Dense : torch::autograd::Function<Dense> {
     const int64_t want = ctx->saved_data["wanted"].toInt();
     variable_list out{Tensor(), Tensor(), Tensor()};
     const bool all = at::GradMode::is_enabled();   // (off inside)
-    if (want & ~WANT_RESIDUAL) out = once([&] { return gradients(ctx, grads, all); });
+    if (want & (WANT_X | WANT_WEIGHT | WANT_BIAS)) out = once([&] { return gradients(ctx, grads, want, all); });
     return {want & WANT_X ? out[0] : Tensor(), want & WANT_WEIGHT ? out[1] : Tensor(), want & WANT_BIAS ? out[2] : Tensor(), want & WANT_RESIDUAL ? grads[0] : Tensor(), Tensor()};
   }
 
-  static variable_list gradients(AutogradContext* ctx, const variable_list& grads, bool all) {
+  static variable_list gradients(AutogradContext* ctx, const variable_list& grads, int64_t want, bool all) {
     const variable_list saved = ctx->get_saved_variables();
     const c10::DeviceGuard guard(saved[0].device());
     const Tensor x = saved_rows(saved[0], saved[0].size(-1), 1 << 20), w = saved_dense(saved[1]), z = saved_dense(saved[2]);
     const Tensor dy = made_dense(grads[0]);
-    const sk_dense_shape s = layer_shape(x, w, Tensor(), ctx->saved_data["activation"].toInt());
-    const int64_t want = ctx->saved_data["wanted"].toInt();
+    const sk_dense_shape s = layer_shape(x, w, Tensor(), want / ACTIVATION);
     const Tensor none = all ? at::zeros({0}, x.options()) : Tensor();
     const Tensor dx = all || (want & WANT_X) ? at::empty(x.sizes(), x.options()) : none;
     const Tensor dw = all || (want & WANT_WEIGHT) ? at::empty(w.sizes(), x.options()) : none;
-    const Tensor db = ctx->saved_data["bias"].toBool() && (all || (want & WANT_BIAS)) ? at::empty({s.out}, x.options()) : none;
+    const Tensor db = (want & HAS_BIAS) && (all || (want & WANT_BIAS)) ? at::empty({s.out}, x.options()) : none;
     with_workspace(x, sk_dense_workspace_bytes(&s, 1), [&](void* ws, size_t n, void* stream) {
       return sk_dense_bwd(&s, x.data_ptr(), w.data_ptr(), data(z), dy.data_ptr(), data(dx), data(dw), data(db), ws, n, stream);
     });
@@ -254,7 +253,7 @@ PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (at::GradMode::is_enabled() && (x->requires_grad() || wants(given(weight)) || wants(given(bias)) || wants(given(residual))))
       out = LayerNorm::apply(*x, given(weight), given(bias), given(residual), eps);
     else
-      out = norm_forward(*x, weight, bias, residual, s, nullptr, nullptr);
+      out = norm_forward(*x, weight, bias, residual, s, nullptr, false);
   }
   return wrapped(std::move(out));
   END_HANDLE_TH_ERRORS
