@@ -192,6 +192,15 @@ int choose_expansion_tile(GemmKind kind, int64_t M, int64_t N, int64_t K) {
   return us < (t == TILE_256x256 ? big_tiles_us(M, N, (double)K, 1) : small_tiles_us(small, (double)K)) ? TILE_256x128 : t;
 }
 
+// ... of a dense layer's product: where 64 x 64 tiles make more than one round and at most two, those, on a ring with two work-groups to a CU.  Us, the
+// product's own choice : these: forward, 512 tokens, 4096 -> 4096 33 : 29, 1024 -> 4096 13.1 : 10.5; dx, 512 tokens, 4096 <- 1024 10.3 : 8.5, 2000, 1024 <- 2048 16.1 : 14.3,
+// but past 2048 values of a row of dz 768, 2048 <- 4096 24 : 29; dW, 2048 tokens, 2048 -> 1024 20.5 : 14.7, 1000, 1024 -> 2048 12.1 : 8.7.  (At 64 to 512 values of a contraction 3 to 20 % too.)
+int dense_tile(GemmKind kind, int64_t M, int64_t N, int64_t K) {
+  const int64_t groups = ((M + 63) / 64) * ((N + 63) / 64);
+  if (tune(SK_TUNE_TILE) < 0 && groups > NUM_CUS && groups <= 2 * NUM_CUS && (kind != GEMM_NN || K <= 2048)) return TILE_64x64;
+  return choose_expansion_tile(kind, M, N, K);
+}
+
 // fp32 contraction [M, N] over K: tile and split of the contraction (fp32 slabs, summed by one
 // more launch), the pair with the least modelled time.  Measured rates of one CU: a lone 64 x 64
 // work-group 0.39 TFLOP/s, two or more 0.52; 128 x 128 tiles 0.50 and 0.53, at 2 us more before
@@ -863,14 +872,14 @@ hipError_t launch_product(GemmKind kind, GemmArgs a, bool f32, void* slabs, hipS
   a.k_per_split = (a.K + 63) / 64 * 64;
   if (kind != GEMM_TN) {
     const GemmKind in_slabs = kind == GEMM_NT ? GEMM_NT_F32 : GEMM_NN_F32;
-    if (a.bias != nullptr || product_bytes(kind, a.M, a.N, a.K, f32) == 0) return gemm(s, kind, a, st);
+    if (a.bias != nullptr || product_bytes(kind, a.M, a.N, a.K, f32) == 0) return f32 ? gemm(s, kind, a, st) : launch_gemm_bf16(kind, dense_tile(kind, a.M, a.N, a.K), a, st);
     return first_gemm(s, kind, in_slabs, a, slabs, st);
   }
   const TokenPlan t = plan_tokens(a.M, a.N, a.K, s.dtype, false, 0);
   void* const out = a.C;
   a.splits = t.splits;
   a.k_per_split = t.k_per_split;
-  if (t.splits == 1) return f32 ? launch_gemm_f32(GEMM_TN_F32, t.tile, a, st) : launch_gemm_bf16(GEMM_TN, choose_expansion_tile(GEMM_TN, a.M, a.N, a.K), a, st);
+  if (t.splits == 1) return f32 ? launch_gemm_f32(GEMM_TN_F32, t.tile, a, st) : launch_gemm_bf16(GEMM_TN, dense_tile(GEMM_TN, a.M, a.N, a.K), a, st);
   a.C = slabs;
   const hipError_t e = f32 ? launch_gemm_f32(GEMM_TN_F32, t.tile, a, st) : launch_gemm_bf16(GEMM_TN_F32_PLAIN, t.tile, a, st);
   if (e != hipSuccess) return e;
@@ -895,7 +904,7 @@ DensePlan plan_dense(int64_t M, int64_t N, int64_t K, bool f32) {
   d.splits = f.splits;
   d.fused = f.splits == 1;
   d.few = f.few;
-  d.tile = f.few ? f.tile : choose_expansion_tile(GEMM_NT, M, N, K);
+  d.tile = f.few ? f.tile : dense_tile(GEMM_NT, M, N, K);
   return d;
 }
 

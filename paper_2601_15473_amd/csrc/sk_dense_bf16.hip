@@ -1,6 +1,6 @@
 // A dense layer's product in bf16 with all that follows it in its epilogue (sk_bf16_finish.h): the GEMM's tiles, one kernel an activation.
-// The tile is the one that the product would take by itself (choose_expansion_tile): of 26 layers of 512 to 16384 tokens, 256 to 4096 wide, with gelu and z or with a residual, 23 were on the best of the
-// five or within 5 % of it (the others 3000 tokens of 1536 -> 1536 with gelu, 31 : 28 us, and 512 of 4096 -> 4096, 31 : 27, on 64 x 64).
+// The tile is dense_tile's: of 26 layers of 512 to 16384 tokens, 256 to 4096 wide, with gelu and z or with a residual, all but one were on the best of the five or within 5 % of it
+// (3000 tokens of 1536 -> 1536 with gelu, 31 : 28 us).
 #include "sk_bf16_ring.h"
 #include "sk_bf16_staged.h"
 #include "sk_dense_launch.h"
