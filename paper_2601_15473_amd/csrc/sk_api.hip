@@ -855,9 +855,23 @@ hipError_t first_gemm(const Shape& s, GemmKind kind, GemmKind kind_slabs, GemmAr
 
 namespace sk {
 
+// The ranges of tokens of a dense layer's dW [M, N] in bf16: none while 64 x 64 tiles make no more than a round and the tokens are few beside them, and where 128 x 128 tiles fill
+// more than half of one.  Us, in plan_tokens' ranges with the launch that sums them : in one, 256 x 256 of 1024 tokens 7.4 : 5.9 and of 2048 8.0 : 8.7, 512 x 512 of 2048 9.8 : 9.0 and of 3000
+// 10.9 : 11.7, 1024 x 512 of 2048 12.7 : 9.1 and of 4096 15.0 : 15.6, 1024 x 1024 of 2048 14.4 : 9.4, of 3000 20.5 : 12.4 and of 8192 25.6 : 28.7; 1536 x 1536 of 8192 58.6 : 51.0, of 32768 188 : 195.
+static TokenPlan plan_dense_tokens(int64_t M, int64_t N, int64_t tokens, sk_dtype dtype) {
+  TokenPlan t = plan_tokens(M, N, tokens, dtype, false, 0);
+  if (dtype != SK_BF16 || t.splits == 1) return t;
+  const int64_t small = ((M + 63) / 64) * ((N + 63) / 64), mid = small_tiles(M, N);
+  if ((small <= NUM_CUS && tokens <= 1280 + 20 * small) || (mid > NUM_CUS / 2 && mid <= NUM_CUS)) {
+    t.splits = 1;
+    t.k_per_split = (int)((tokens + 63) / 64 * 64);
+  }
+  return t;
+}
+
 size_t product_bytes(GemmKind kind, int64_t M, int64_t N, int64_t K, bool f32) {
   if (kind == GEMM_TN) {
-    const TokenPlan t = plan_tokens(M, N, K, f32 ? SK_F32 : SK_BF16, false, 0);
+    const TokenPlan t = plan_dense_tokens(M, N, K, f32 ? SK_F32 : SK_BF16);
     return t.splits == 1 ? 0 : align_up((size_t)t.splits * M * N * 4);
   }
   if (f32) return plan_f32_first(M, N, K).slab_bytes;
@@ -875,7 +889,7 @@ hipError_t launch_product(GemmKind kind, GemmArgs a, bool f32, void* slabs, hipS
     if (a.bias != nullptr || product_bytes(kind, a.M, a.N, a.K, f32) == 0) return f32 ? gemm(s, kind, a, st) : launch_gemm_bf16(kind, dense_tile(kind, a.M, a.N, a.K), a, st);
     return first_gemm(s, kind, in_slabs, a, slabs, st);
   }
-  const TokenPlan t = plan_tokens(a.M, a.N, a.K, s.dtype, false, 0);
+  const TokenPlan t = plan_dense_tokens(a.M, a.N, a.K, s.dtype);
   void* const out = a.C;
   a.splits = t.splits;
   a.k_per_split = t.k_per_split;
