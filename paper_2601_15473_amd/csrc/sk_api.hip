@@ -885,9 +885,8 @@ hipError_t launch_product(GemmKind kind, GemmArgs a, bool f32, void* slabs, hipS
   a.splits = 1;
   a.k_per_split = (a.K + 63) / 64 * 64;
   if (kind != GEMM_TN) {
-    const GemmKind in_slabs = kind == GEMM_NT ? GEMM_NT_F32 : GEMM_NN_F32;
-    if (a.bias != nullptr || product_bytes(kind, a.M, a.N, a.K, f32) == 0) return f32 ? gemm(s, kind, a, st) : launch_gemm_bf16(kind, dense_tile(kind, a.M, a.N, a.K), a, st);
-    return first_gemm(s, kind, in_slabs, a, slabs, st);
+    if (product_bytes(kind, a.M, a.N, a.K, f32) == 0) return f32 ? gemm(s, kind, a, st) : launch_gemm_bf16(kind, dense_tile(kind, a.M, a.N, a.K), a, st);
+    return first_gemm(s, kind, GEMM_NN_F32, a, slabs, st);
   }
   const TokenPlan t = plan_dense_tokens(a.M, a.N, a.K, s.dtype);
   void* const out = a.C;

@@ -173,8 +173,8 @@ hipError_t launch_gemm_f32(GemmKind kind, int tile, const GemmArgs& a, hipStream
 hipError_t launch_dual_gemm_f32(GemmKind kind_a, const GemmArgs& a, GemmKind kind_b, const GemmArgs& b, int tile, hipStream_t s);
 constexpr int F32_BK = 32;
 
-// Products of the dense layers, planned much as the sketched layers' are (sk_api.hip), the result in the storage type: C [M, N] = A . B (+ bias) of A [M, K] and B [K, N]
-// (GEMM_NN) or [N, K] (GEMM_NT); of A [K, M] and B [K, N] (GEMM_TN), a contraction over rows.  `slabs`: product_bytes of room (none with a bias).
+// Products of the dense layers' gradients, planned much as the sketched layers' are (sk_api.hip), the result in the storage type: C [M, N] = A . B of A [M, K] and B [K, N]
+// (GEMM_NN), or of A [K, M] and B [K, N] (GEMM_TN), a contraction over rows.  `slabs`: product_bytes of room.
 size_t product_bytes(GemmKind kind, int64_t M, int64_t N, int64_t K, bool f32);
 hipError_t launch_product(GemmKind kind, GemmArgs a, bool f32, void* slabs, hipStream_t s);
 // A dense layer's forward product, planned: with all that follows it in its epilogue (`few`: the few-rows kernel, else on `tile`), or in fp32 slabs [splits][M, N]
