@@ -59,7 +59,7 @@ def test_bias_and_residual(block, act, dtype):
 
 
 @pytest.mark.parametrize("act", [None, "gelu", "silu"], ids=str)
-@pytest.mark.parametrize("T, I, O", [(2049, 512, 1536), (4097, 256, 2048), (1030, 2056, 1032), (8200, 136, 264), (700, 1032, 4104)])
+@pytest.mark.parametrize("T, I, O", [(2049, 512, 1536), (4097, 256, 2048), (1030, 2056, 1032), (8200, 136, 264), (700, 1032, 4104), (900, 1032, 1096), (2300, 1096, 1032), (6100, 1536, 1544), (9000, 200, 520)])
 def test_large_tiles(block, T, I, O, act):
     """Sizes on the tiles of whole rounds, by every way through the plans."""
     _check(block, *_case(T, I, O, torch.bfloat16), act)
