@@ -885,8 +885,13 @@ hipError_t launch_product(GemmKind kind, GemmArgs a, bool f32, void* slabs, hipS
   a.splits = 1;
   a.k_per_split = (a.K + 63) / 64 * 64;
   if (kind != GEMM_TN) {
-    if (product_bytes(kind, a.M, a.N, a.K, f32) == 0) return f32 ? gemm(s, kind, a, st) : launch_gemm_bf16(kind, dense_tile(kind, a.M, a.N, a.K), a, st);
-    return first_gemm(s, kind, GEMM_NN_F32, a, slabs, st);
+    if (product_bytes(kind, a.M, a.N, a.K, f32) > 0) return first_gemm(s, kind, GEMM_NN_F32, a, slabs, st);
+    // dx of few tokens on the few-rows kernel, as gemm() has it, while its work-groups of 32 columns make no more than a round.  Us, the weight in the Infinity Cache / in memory, 64 x 64
+    // tiles : these: 8 tokens, 1024 <- 1024 5.9 / 6.1 : 3.4 / 5.1, 768 <- 2304 9.7 / 10.0 : 4.7 / 7.2; 64 tokens 5.9 / 6.2 : 4.7 / 6.1, 9.8 / 10.0 : 6.9 / 8.9; 200, 1024 <- 512 4.5 / 4.7 : 3.8 / 4.6.
+    // Past a round the tiles: 64 tokens, 11008 <- 2048 10.1 / 14.6 : 11.4 / 15.8, 16 tokens, 16384 <- 1024 6.3 / 8.7 : 5.7 / 9.9, 8 tokens, 11008 <- 2048 9.7 / 12.1 : 9.3 / 12.0.
+    const bool few = !f32 && few_rows_splits(a.M, a.N, a.K, false) > 0 && (int64_t)((a.M + 63) / 64) * ((a.N + 31) / 32) <= NUM_CUS;
+    if (f32 || few) return gemm(s, kind, a, st);
+    return launch_gemm_bf16(kind, dense_tile(kind, a.M, a.N, a.K), a, st);
   }
   const TokenPlan t = plan_dense_tokens(a.M, a.N, a.K, s.dtype);
   void* const out = a.C;

@@ -1,0 +1,42 @@
+"""Which kernels the dense layers' products run on (host trace, no GPU)."""
+import pytest
+
+from paper_2601_15473_amd import libsk as sk
+
+BASE = 1 << 44      # made-up device addresses, far apart; never dereferenced
+
+
+def kernels(tokens, d_in, d_out, which, activation=sk.SK_ACT_NONE, dtype=sk.SK_BF16, residual=False, z=False):
+    """Names and work-groups of a layer's launches: "fwd", "dx" or "dw"."""
+    P = [i * BASE for i in range(1, 9)]
+    s = sk.DenseShape(tokens, d_in, d_out, activation, dtype, d_in, d_out)
+    n = sk.sk_dense_workspace_bytes(s, 0 if which == "fwd" else 1)
+    sk.sk_trace_begin()
+    try:
+        if which == "fwd":
+            sk.check(sk.sk_dense_fwd(s, *P[:3], P[3] if residual else None, P[4], P[5] if z else None, P[6], n))
+        else:
+            sk.check(sk.sk_dense_bwd(s, P[0], P[1], P[2], P[3], P[4] if which == "dx" else None, P[5] if which == "dw" else None, None, P[7], n))
+        return sk.sk_trace_kernels()
+    finally:
+        sk.sk_trace_end()
+
+
+@pytest.mark.parametrize("tokens, d_in, d_out, want", [
+    (1, 64, 64, "<1, 1, false>"), (8, 1024, 1024, "<1, 1, false>"), (8, 8192, 1024, "<1, 1, false>"), (16, 768, 768, "<2, 1, false>"), (32, 768, 1536, "<4, 1, false>"),
+    (64, 512, 1024, "<8, 1, false>"), (64, 768, 2048, "<8, 1, false>"), (100, 768, 768, "<8, 1, false>"), (128, 384, 768, "<8, 1, false>"), (200, 1024, 512, "<8, 1, false>"),
+    (256, 512, 512, "<8, 1, false>"),
+])
+def test_input_gradients_of_few_tokens(tokens, d_in, d_out, want):
+    got = kernels(tokens, d_in, d_out, "dx")
+    assert [n for n, _ in got] == ["gemm_bf16_few_rows_kernel" + want], got
+
+
+@pytest.mark.parametrize("tokens, d_in, d_out", [(257, 512, 512), (256, 2048, 2048), (512, 1024, 4096), (8, 8224, 1024), (17, 32768, 1024), (64, 11008, 2048), (200, 2080, 512)])
+def test_input_gradients_of_more_tokens(tokens, d_in, d_out):
+    """... on the tiles, and so are those whose columns make more than a round of 32-column work-groups."""
+    assert all("few_rows" not in n for n, _ in kernels(tokens, d_in, d_out, "dx"))
+
+
+def test_input_gradients_over_many_features_in_ranges():
+    assert [n.split("<")[0] for n, _ in kernels(8, 1024, 4096, "dx")] == ["gemm_bf16_few_rows_kernel", "reduce_to_bf16_kernel"]
