@@ -855,14 +855,16 @@ hipError_t first_gemm(const Shape& s, GemmKind kind, GemmKind kind_slabs, GemmAr
 
 namespace sk {
 
-// The ranges of tokens of a dense layer's dW [M, N] in bf16: none while 64 x 64 tiles make no more than a round and the tokens are few beside them, and where 128 x 128 tiles fill
-// more than half of one.  Us, in plan_tokens' ranges with the launch that sums them : in one, 256 x 256 of 1024 tokens 7.4 : 5.9 and of 2048 8.0 : 8.7, 512 x 512 of 2048 9.8 : 9.0 and of 3000
-// 10.9 : 11.7, 1024 x 512 of 2048 12.7 : 9.1 and of 4096 15.0 : 15.6, 1024 x 1024 of 2048 14.4 : 9.4, of 3000 20.5 : 12.4 and of 8192 25.6 : 28.7; 1536 x 1536 of 8192 58.6 : 51.0, of 32768 188 : 195.
+// The ranges of tokens of a dense layer's dW [M, N] in bf16: none while 64 x 64 tiles make no more than a round and the tokens are few beside them.  Us, in plan_tokens' ranges with the
+// launch that sums them : in one, x and dy in the Infinity Cache / from memory: 256 x 256 of 1024 tokens 7.4 / 7.0 : 6.4 / 5.9, 512 x 512 of 1536 9.6 / 9.2 : 8.0 / 8.6 and of 2048 10.4 / 10.5 :
+// 9.4 / 11.1, 1024 x 512 of 2048 13.2 / 14.0 : 9.6 / 12.7 and of 3000 13.9 / 15.2 : 12.3 / 17.3, 1024 x 1024 of 2048 16.0 / 17.4 : 10.4 / 12.8, of 4096 22.1 / 22.8 : 17.1 / 22.6 and of 6144
+// 25.1 / 26.2 : 23.7 / 32.5.  (128 x 128 tiles of more than half a round in one range, 1536 x 1536 of 8192 tokens: 59 / 65 : 53 / 77, and 59 / 62 : 53 / 74 with x alone from memory, as
+// in training; of 65536 387 : 584 either way.  Those go by plan_tokens.)
 static TokenPlan plan_dense_tokens(int64_t M, int64_t N, int64_t tokens, sk_dtype dtype) {
   TokenPlan t = plan_tokens(M, N, tokens, dtype, false, 0);
   if (dtype != SK_BF16 || t.splits == 1) return t;
-  const int64_t small = ((M + 63) / 64) * ((N + 63) / 64), mid = small_tiles(M, N);
-  if ((small <= NUM_CUS && tokens <= 1280 + 20 * small) || (mid > NUM_CUS / 2 && mid <= NUM_CUS)) {
+  const int64_t small = ((M + 63) / 64) * ((N + 63) / 64);
+  if (small <= NUM_CUS && tokens <= 1280 + 11 * small) {
     t.splits = 1;
     t.k_per_split = (int)((tokens + 63) / 64 * 64);
   }

@@ -40,3 +40,16 @@ def test_input_gradients_of_more_tokens(tokens, d_in, d_out):
 
 def test_input_gradients_over_many_features_in_ranges():
     assert [n.split("<")[0] for n, _ in kernels(8, 1024, 4096, "dx")] == ["gemm_bf16_few_rows_kernel", "reduce_to_bf16_kernel"]
+
+
+@pytest.mark.parametrize("tokens, d_in, d_out", [(6144, 1536, 1536), (8192, 1408, 1536), (65536, 1536, 1536), (65536, 2048, 1280), (1 << 20, 1536, 1536), (49152, 2048, 1536), (6144, 1024, 1024),
+                                                 (3000, 512, 1024)])
+def test_weight_gradients_of_many_tokens_in_ranges(tokens, d_in, d_out):
+    """... so that they have the chip, and no sum is one chain over all of them."""
+    got = kernels(tokens, d_in, d_out, "dw")
+    assert len(got) == 2 and got[1][0] == "reduce_to_bf16_kernel" and got[0][1] > 160, got
+
+
+@pytest.mark.parametrize("tokens, d_in, d_out", [(1400, 256, 256), (2500, 512, 1024), (4096, 1024, 1024), (2048, 768, 768), (4096, 1536, 1536)])
+def test_weight_gradients_of_few_tokens_in_one_range(tokens, d_in, d_out):
+    assert [n.split("<")[0] for n, _ in kernels(tokens, d_in, d_out, "dw")] == ["gemm_bf16_kernel"]
