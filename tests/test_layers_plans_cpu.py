@@ -1,6 +1,10 @@
 """Which kernels the dense layers' products run on (host trace, no GPU)."""
+import math
+import random
+
 import pytest
 
+import test_gpu_linear_variants as variants
 from paper_2601_15473_amd import libsk as sk
 
 BASE = 1 << 44      # made-up device addresses, far apart; never dereferenced
@@ -53,3 +57,31 @@ def test_weight_gradients_of_many_tokens_in_ranges(tokens, d_in, d_out):
 @pytest.mark.parametrize("tokens, d_in, d_out", [(1400, 256, 256), (2500, 512, 1024), (4096, 1024, 1024), (2048, 768, 768), (4096, 1536, 1536)])
 def test_weight_gradients_of_few_tokens_in_one_range(tokens, d_in, d_out):
     assert [n.split("<")[0] for n, _ in kernels(tokens, d_in, d_out, "dw")] == ["gemm_bf16_kernel"]
+
+
+def _variants(sizes, dtype):
+    """The kernels of these layers' forward and backward products; apart those whose work-groups walk on to another tile, which have more to wait for."""
+    seen = set()
+    for T, I, O in sizes:
+        for which, tiles in (("fwd", (T, O)), ("dx", (T, I)), ("dw", (O, I))):
+            for name, _ in kernels(T, I, O, which, sk.SK_ACT_RELU if which == "fwd" else sk.SK_ACT_NONE, dtype, residual=True, z=True):
+                walks = "256, 256" in name or "crew" in name or "far" in name
+                seen.add((name, walks and -(-tiles[0] // 256) * -(-tiles[1] // 256) > 256))
+    return seen
+
+
+@pytest.mark.parametrize("dtype", [sk.SK_BF16, sk.SK_F32], ids=["bf16", "f32"])
+def test_every_kernel_that_is_taken_has_a_tested_size(dtype):
+    rng = random.Random(1)
+
+    def size(lo, hi):
+        return int(math.exp(rng.uniform(math.log(lo), math.log(hi))))
+
+    drawn = [(size(1, 1 << 16), 8 * size(1, 2048), 8 * size(1, 2048)) for _ in range(4000)]
+    tested = _variants(variants.SIZES if dtype == sk.SK_BF16 else variants.SIZES_F32, dtype)
+    assert _variants(drawn, dtype) <= tested
+
+
+def test_operands_past_two_gigabytes_have_a_tested_size():
+    names = [kernels(*s, "dw")[0][0] for s in variants.SIZES_FAR]
+    assert names == ["gemm_bf16_far_kernel<false, false, bf16>"] * 2 + ["gemm_bf16_far_kernel<false, false, float>"], names
