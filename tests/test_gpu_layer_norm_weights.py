@@ -79,3 +79,29 @@ def test_sums_that_are_not_finite(block):
     alone, = torch.autograd.grad(y2, w2, dy[rows])
     assert ((alone.double() - u.sum(0)).abs() <= u.sum(0).abs() * 2.0 ** -7 + u.abs().sum(0) * 2.0 ** -11).all()
     assert got.isnan().any()
+
+
+@pytest.mark.parametrize("native", [True, False], ids=["native", "python"])
+@pytest.mark.parametrize("width", [64, 2056, 8200])
+def test_a_rest_of_what_is_not_finite(block, monkeypatch, width, native):
+    """Rows that hold a NaN, an infinity or a sum past the largest number are NaN in their dx and in the sums over rows, as u is; every other row has the bits that it has without them."""
+    if not native:
+        monkeypatch.setattr(block, "_natively", lambda: False)
+    x, r, w, dy = _normal(1, (9, width), 0.5), _normal(2, (9, width)), _normal(3, (width,), 0.2, 1.0), _normal(4, (9, width))
+    x[7], r[7] = 1e15 * x[7], 1e15 * r[7]
+
+    def call(x, r):
+        w_, r_ = w.clone().requires_grad_(), r.clone().requires_grad_()
+        y, s = block.layer_norm(x, w_, None, r_)
+        return y.detach(), s.detach(), *torch.autograd.grad(y, [r_, w_], dy)
+
+    y, s, dr, dw = call(x, r)
+    assert y.isfinite().all() and dr.isfinite().all() and dw.isfinite().all()
+    x2, r2 = x.clone(), r.clone()
+    x2[0, 3], x2[4, 5], x2[5, 7], r2[5, 7] = float("inf"), float("nan"), 3.3e38, 3.3e38
+    y2, s2, dr2, dw2 = call(x2, r2)
+    bad = torch.tensor([0, 4, 5], device="cuda")
+    good = torch.tensor([1, 2, 3, 6, 7, 8], device="cuda")
+    assert y2[bad].isnan().all() and dr2[bad].isnan().all() and dw2.isnan().all()
+    assert torch.equal(y2[good], y[good]) and torch.equal(s2[good], s[good]) and torch.equal(dr2[good], dr[good])
+    assert s2[0, 3] == float("inf") and s2[4, 5].isnan() and s2[5, 7] == float("inf")

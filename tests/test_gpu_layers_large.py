@@ -133,3 +133,68 @@ def test_gradients_do_not_share_memory(block):
     out = block.linear(x.detach().requires_grad_(), W, None, res, activation="silu")
     (out * out).sum().backward()
     assert torch.equal(res.grad, 2 * out.detach())
+
+
+def _signs(seed, n):
+    return (torch.randint(0, 2, (n,), generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda") * 2 - 1).bfloat16()
+
+
+@pytest.mark.parametrize("with_residual", [False, True], ids=["alone", "residual"])
+@pytest.mark.parametrize("width", [136, 2056, 16400])
+def test_layer_norm_past_32_bits_exactly(block, width, with_residual):
+    """Rows of two values, a power of two apart from zero: normed they are 1 and -1 (without eps), so that every result of every row and the sums over all rows have one right value."""
+    rows = (1 << 31) // width + 70
+    # (as many of one sign as of the other)
+    c = (torch.randperm(width, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda") % 2 * 2 - 1).bfloat16()
+    q = _signs(3, rows) * 2.0 ** (torch.arange(rows, device="cuda") % 3).bfloat16()
+    x = q[:, None] * c
+    dy = torch.randint(-2, 3, (rows, width), generator=torch.Generator(device="cuda").manual_seed(4), device="cuda", dtype=torch.int8).bfloat16()
+    w, b = 2.0 ** (torch.arange(width, device="cuda") % 3).bfloat16(), (torch.arange(width, device="cuda") % 5).bfloat16()
+    leaves = [t.requires_grad_() for t in (x, w, b)]
+    if with_residual:
+        out, total = block.layer_norm(*leaves, residual=x.detach(), eps=0.0)
+    else:
+        out = block.layer_norm(*leaves, eps=0.0)
+    dw, db = torch.autograd.grad(out, leaves[1:], dy)
+    want_w, want_b = torch.zeros(width, dtype=torch.float64, device="cuda"), torch.zeros(width, dtype=torch.float64, device="cuda")
+    with torch.no_grad():
+        for i in range(0, rows, max(1, (1 << 27) // width)):
+            at = slice(i, i + max(1, (1 << 27) // width))
+            u = torch.sign(q[at, None]) * c
+            assert torch.equal(out[at], u * w + b)
+            if with_residual:
+                assert torch.equal(total[at], 2 * x[at])
+            want_w += (dy[at] * u).sum(0, dtype=torch.float64)
+            want_b += dy[at].sum(0, dtype=torch.float64)
+    assert torch.equal(dw, want_w.bfloat16()) and torch.equal(db, want_b.bfloat16())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows, V, K", [(2100, 600, 70), (2100, 3001, 5), (5000, 40, 10), (2050, 12300, 3), (300, 70001, 300)])
+def test_distillation_of_each_row_by_itself(block, rows, V, K, dtype):
+    """The same bits whatever the other rows hold, NaN and lists that are empty among it; and by itself, where other lanes may sum it, within twice what a correct result may be off by."""
+    g = torch.Generator().manual_seed(1)
+    z = (torch.randn((rows, V), generator=g) * 2).to(dtype).cuda()
+    ids = torch.randint(-1, V, (rows, K), generator=g).cuda()
+    t, labels = torch.randn((rows, K), generator=g).to(dtype).cuda(), torch.randint(-1, V, (rows,), generator=g).cuda()
+    up = torch.randn((rows,), generator=g).cuda()
+
+    def call(z, t, ids, labels, up):
+        leaf = z.detach().requires_grad_()
+        loss = block.distillation_loss(leaf, t, ids, labels, temperature=3.0, label_weight=0.4)
+        return loss.detach(), torch.autograd.grad(loss, leaf, up)[0]
+
+    loss, dz = call(z, t, ids, labels, up)
+    keep = torch.arange(rows, device="cuda") % 3 == 1
+    other = [v.clone() for v in (z, t, ids, labels, up)]
+    other[0][~keep], other[1][~keep], other[2][~keep], other[3][~keep], other[4][~keep] = float("nan"), float("inf"), -5, 0, 7.0
+    other[0][2::6], other[2][2::6] = float("inf"), 1
+    loss2, dz2 = call(*other)
+    assert torch.equal(loss2[keep], loss[keep]) and torch.equal(dz2[keep], dz[keep])
+    for i in (0, 5, rows - 1):
+        row = slice(i, i + 1)
+        want = layers_oracle.distill(z[row], t[row], ids[row], labels[row], 3.0, 0.4, up[row])
+        alone = call(z[row], t[row], ids[row], labels[row], up[row])
+        for got, batch, name in zip(alone, (loss, dz), ("loss", "dlogits")):
+            assert_within(got, *want[name], name)
+            assert ((got - batch[row]).double().cpu().abs() <= 2 * want[name][1]).all(), name
