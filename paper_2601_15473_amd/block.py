@@ -500,7 +500,8 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
     """Layer norm over the last dimension of ``x [..., width]``, times ``weight`` and plus ``bias [width]`` where they are given.
 
     With a ``residual`` (as x) the norm is of ``x + residual``, and the sum comes back too: ``(y, sum)``, the stream that a block goes on with.  What is
-    normed is the sum before it is rounded.  Rows of a strided matrix are read in place.  width: a multiple of 8 up to 32768.
+    normed is the sum before it is rounded.  (In bf16 its gradients are too, to four bits behind the rounding, where ``weight`` wants one; with a frozen weight they are
+    those at the rounded sum.)  Rows of a strided matrix are read in place.  width: a multiple of 8 up to 32768.
     """
     if _natively():
         out = _native.layer_norm(x, weight, bias, residual, eps)
@@ -584,7 +585,7 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = No
     ``torch.nn.Linear`` has them, ``residual [..., out]``.
 
     ``activation``: None, "relu", "gelu" (z Phi(z)), "gelu_tanh" (its approximation by tanh) or "silu".  A backward pass has what goes into
-    it, in the tensors' type.  Rows of strided matrices x and residual are read in place.  in and out: multiples of 8.
+    it, in the tensors' type.  Rows of strided matrices x and residual are read in place, of other layouts that are not dense from a copy.  in and out: multiples of 8.
     """
     if activation not in _ACTIVATIONS:
         raise ValueError(f"linear: no activation {activation!r}; there are {', '.join(map(repr, _ACTIVATIONS))}")
@@ -654,7 +655,8 @@ def distillation_loss(logits: torch.Tensor, teacher_logits: torch.Tensor, teache
     with p the softmax of the teacher's entries over the temperature and q that of all of a row's logits.  An entry whose id is outside the vocabulary or
     whose logit is -infinity is not there (a list that ends early), an id that is named twice has both entries; a row without an entry has no first
     term, one whose label is outside the vocabulary no second.  The logits alone get a gradient.  Ids and labels are int32 or int64.  Any size of
-    vocabulary; rows of a strided matrix are read in place.
+    vocabulary.  Dense logits and the rows of a strided matrix are read in place; others (a part of the positions of each of many sequences, ``logits[:, a:b]``)
+    are copied first, and the copy is kept for the backward pass.
     """
     if _natively():
         loss = _native.distillation_loss(logits, teacher_logits, teacher_ids, labels, temperature, label_weight)

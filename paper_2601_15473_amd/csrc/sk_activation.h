@@ -7,9 +7,9 @@ namespace sk {
 enum Activation : int { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_GELU_TANH = 3, ACT_SILU = 4, ACT_COUNT = 5 };
 
 // The normal distribution's Phi(-a) for a >= 0 and exp(-a^2 / 2): their quotient, erfcx(a / sqrt 2) / 2, is smooth and falls like 1 / a, here a polynomial
-// in t = 1 / (1 + p a) without a constant, fitted to it over 0 .. 14 for the least relative error: 4.6e-6 at degree 6, far below a
-// rounding to bf16, 1.5e-7 at degree 8 (4e-7 as evaluated).  Either keeps its relative precision where Phi is small, and makes one exponential serve
-// value and derivative.
+// in t = 1 / (1 + p a) without a constant, fitted to it over 0 .. 14 for the least relative error: 4.6e-6 at degree 6 (4.9e-6 as evaluated), far below a
+// rounding to bf16, 1.5e-7 at degree 8 (4.3e-7).  Phi has that and the exponential's, whose argument is rounded: with degree 8 1.5e-6 of itself up to a = 5, 8e-6 at 12, where Phi is 1e-33.
+// One exponential serves value and derivative.
 template <bool PRECISE>
 __device__ __forceinline__ float phi_below(float a, float& bell) {
   bell = __builtin_amdgcn_exp2f(a * a * -0.72134752044f);

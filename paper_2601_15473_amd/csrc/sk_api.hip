@@ -195,6 +195,7 @@ int choose_expansion_tile(GemmKind kind, int64_t M, int64_t N, int64_t K) {
 // ... of a dense layer's product: where 64 x 64 tiles make more than one round and at most two, those, on a ring with two work-groups to a CU.  Us, the
 // product's own choice : these: forward, 512 tokens, 4096 -> 4096 33 : 29, 1024 -> 4096 13.1 : 10.5; dx, 512 tokens, 4096 <- 1024 10.3 : 8.5, 2000, 1024 <- 2048 16.1 : 14.3,
 // but past 2048 values of a row of dz 768, 2048 <- 4096 24 : 29; dW, 2048 tokens, 2048 -> 1024 20.5 : 14.7, 1000, 1024 -> 2048 12.1 : 8.7.  (At 64 to 512 values of a contraction 3 to 20 % too.)
+// With the weight (dW: x) from memory instead of the Infinity Cache: 36.4 : 35.9, 11.9 : 11.8; dx, 512 tokens, 4096 <- 1024 11.5 : 12.4, 1024, 2048 <- 2048 22.1 : 20.0; dW 20.3 : 15.9, 12.0 : 9.6.
 int dense_tile(GemmKind kind, int64_t M, int64_t N, int64_t K) {
   const int64_t groups = ((M + 63) / 64) * ((N + 63) / 64);
   if (tune(SK_TUNE_TILE) < 0 && groups > NUM_CUS && groups <= 2 * NUM_CUS && (kind != GEMM_NN || K <= 2048)) return TILE_64x64;

@@ -7,10 +7,11 @@
 // Bound by memory: forward z is read once, with the largest value so far and the sums of exponentials below it carried along (rescaled once in
 // some values), back it is read again and dz written (what the gradient is scaled by is known then only).  The entries are few: one thread each.
 // Bf16, 8192 rows of 65536: forward 179 us with one exponential a value (1.07 GB, 6.0 TB/s), 265 with two, back 398 with lists of 128 (2.15 GB, 5.4; a copy reaches 5.1).  Behind a backward pass
-// the forward one takes 215 and 267: it shares the memory with what that pass left to be written back.
+// the forward one takes 215 and 267: it shares the memory with what that pass left to be written back.  Fp32, 8192 rows of 32000: 177 forward (5.9 TB/s), 725 with the gradient.
 //
 // A row begins wherever the vocabulary's size puts it: its values are taken 16 bytes at a time at the places where memory has them, and one by one
-// in the pieces that it shares with its neighbours.
+// in the pieces that it shares with its neighbours.  dz's rows are dense.  Where one of them lies otherwise to a 16-byte boundary than its row of logits (an odd vocabulary as a part of
+// a padded head's columns), its values are stored one by one: no slower, 4001 rows of 32001 bf16 176 us forward and back from dense rows, 175 from rows 32008 apart, in fp32 405 and 408.
 #include "sk_block_launch.h"
 #include "sk_rows.h"
 

@@ -149,7 +149,8 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_fwd_kernel(const
 // Gradients: work-groups walk over the rows with their lanes' terms of dw and db in registers, and leave one row of each, [group][dw, db][width].
 // What the next row needs is on its way while this one's sums are formed.  Where a row takes 1024 lanes, there are 128 registers a lane, and the terms' sums do not fit beside the row: those
 // rows are a work-group each, and the weights' gradients have a launch that reads s and dy again (with all of it in one, spilled, 4096 rows of 16384 302 us for 119 + 72,
-// 2048 of 32768 814 for 132 + 71).
+// 2048 of 32768 814 for 132 + 71).  Rows past 16384 still do not fit in some forms: spilled are 3 registers of a lane in bf16 with ds and the four bits, in fp32 39 forward, 76 back with ds and
+// 2 without (2048 of 32768 with a residual in fp32: forward 293 us, 3.7 TB/s; rows of 16384, which fit, 220 for 4096 of them, 4.9).
 template <typename T, int L, int N, bool SUM, bool REST>
 __global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_bwd_kernel(const LayerNormArgs p) {
   constexpr int THREADS = L > 256 ? L : 256, ROWS = THREADS / L, WAVES = L > 64 ? L / 64 : 1;
