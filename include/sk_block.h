@@ -221,6 +221,7 @@ sk_status sk_dense_bwd(const sk_dense_shape* shape, const void* x, const void* w
  *   logits on any boundary of a value, with a row stride of any number of elements, teacher_logits [rows, top] in `dtype`, teacher_ids [rows, top], labels [rows], loss [rows] fp32.
  * stats [rows, 8] fp32 for a backward pass, or NULL.  (A row whose logits are all -infinity has no softmax: NaN.)
  *   rows below 2^23, vocabulary up to 2^24, top up to 2^16 (0: no teacher; its pointers may be NULL), temperature from 10^-3 to 10^3.
+ * Made for lists of some hundred entries: past about a thousand the gradient's time grows with the square of their length.
  */
 typedef struct {
   int64_t rows, vocabulary, logits_stride;

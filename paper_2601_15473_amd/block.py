@@ -656,7 +656,8 @@ def distillation_loss(logits: torch.Tensor, teacher_logits: torch.Tensor, teache
     whose logit is -infinity is not there (a list that ends early), an id that is named twice has both entries; a row without an entry has no first
     term, one whose label is outside the vocabulary no second.  The logits alone get a gradient.  Ids and labels are int32 or int64.  Any size of
     vocabulary.  Dense logits and the rows of a strided matrix are read in place; others (a part of the positions of each of many sequences, ``logits[:, a:b]``)
-    are copied first, and the copy is kept for the backward pass.
+    are copied first, and the copy is kept for the backward pass.  Made for lists of up to some hundred entries: past about a thousand the gradient's time
+    grows with the square of ``top``.
     """
     if _natively():
         loss = _native.distillation_loss(logits, teacher_logits, teacher_ids, labels, temperature, label_weight)

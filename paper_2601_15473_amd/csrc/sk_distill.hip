@@ -255,7 +255,8 @@ struct alignas(16) Places {
 
 // dz by pieces; what is subtracted at a place is by the thread that has its piece, before it goes.  (As a pass over the entries behind the row, whose lines had left
 // the L2, 128 of them cost 8192 rows of 65536 90 us of 484.)  Lists that do not fit LDS are taken that way, a stretch at a time, behind a wait for the
-// work-group's stores.
+// work-group's stores; every entry looks through the whole list for its place, so that long ones cost their square: 1024 rows of 32000, bf16, forward and back, lists of 128 61 us,
+// 512 94, 1024 197, 2048 553, 4096 1900, 8192 7070, of which the forward pass is 20 to 93.
 template <typename T, int THREADS, bool HARD>
 __global__ __launch_bounds__(THREADS) void distill_bwd_kernel(const DistillArgs p) {
   constexpr int E = RowPieces<T>::E, AHEAD = 2, NONE = 0x7fffffff;

@@ -187,3 +187,15 @@ def test_refusals(block):
     e = z[:0].clone().requires_grad_()
     loss = block.distillation_loss(e, t[:0], ids[:0])
     assert loss.shape == (0,) and torch.autograd.grad(loss.sum(), e)[0].shape == (0, 50)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("V, K", [(4099, 4099), (1000, 5000), (257, 256), (600, 255), (17, 1025)])
+def test_long_lists(block, V, K, dtype):
+    """Of a whole vocabulary, and longer than it: places many times over."""
+    g = torch.Generator().manual_seed(3)
+    z = (torch.randn((3, V), generator=g) * 2.5).to(dtype).cuda()
+    ids = (torch.stack([torch.randperm(V, generator=g) for _ in range(3)]) if K == V else torch.randint(-3, V + 3, (3, K), generator=g)).cuda()
+    t, labels = (torch.randn((3, K), generator=g) * 2).to(dtype).cuda(), torch.tensor([0, V - 1, -1]).cuda()
+    for tau, w in ((1.0, 0.0), (2.0, 0.3)):
+        _check(block, z, t, ids, labels, tau, w, (tau, w))
